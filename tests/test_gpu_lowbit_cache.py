@@ -1,0 +1,422 @@
+"""The paged 8-bit cache and its attention on the GPU against plain forms in 64 bits."""
+import numpy as np
+import pytest
+
+import lowbit_plain as plain
+
+pytestmark = pytest.mark.gpu
+
+torch = pytest.importorskip("torch")
+HALF = [torch.bfloat16, torch.float16]
+
+
+@pytest.fixture(scope="module")
+def lowbit():
+    assert torch.cuda.is_available(), "needs the MI355X"
+    from paper_2604_03298_amd import lowbit as module
+    module.lib()
+    return module
+
+
+def ints(v):
+    return torch.tensor(v, dtype=torch.int32, device="cuda")
+
+
+def starts_of(counts):
+    return [0] + list(np.cumsum(counts))
+
+
+class Both:
+    """The same cache on the GPU and in its plain form, with pages in random order and rubbish in every byte that nothing was written to."""
+
+    def __init__(self, lowbit, lengths, page, heads, dim, seed=0):
+        self.lowbit, self.rng = lowbit, np.random.default_rng(seed)
+        self.most = max(1, max(-(-n // page) for n in lengths))
+        pages = sum(-(-n // page) for n in lengths) + 2
+        order = self.rng.permutation(pages)
+        self.table = np.full((len(lengths), self.most), -7, dtype=np.int32)
+        at = 0
+        for b, n in enumerate(lengths):
+            need = -(-n // page)
+            self.table[b, :need] = order[at:at + need]
+            at += need
+        self.cache = lowbit.Cache.empty(pages, heads, dim, page)
+        for t in self.cache.tensors:
+            t.copy_(torch.from_numpy(self.rng.integers(0, 256, tuple(t.shape), dtype=np.uint8)))
+        self.k, self.v = plain.PlainCache(page, heads, dim), plain.PlainCache(page, heads, dim)
+        self.heads, self.dim = heads, dim
+        self.gpu_table = torch.from_numpy(self.table).cuda()
+
+    def values(self, tokens, dtype, scale=1.0, layout=0):
+        """Random keys or values: plain, as a slice of a wider tensor at an odd place, or with heads outermost."""
+        x = torch.from_numpy(self.rng.standard_normal((tokens, self.heads, self.dim)).astype(np.float32) * scale).to(dtype)
+        return x, self.laid_out(x, layout)
+
+    def laid_out(self, x, layout):
+        tokens, heads, dim = x.shape
+        if layout == 1:
+            buf = torch.full((tokens, heads + 1, dim + 3), float("nan"), dtype=x.dtype, device="cuda")
+            out = buf[:, 1:, 1:dim + 1]
+        elif layout == 2:
+            out = torch.empty(heads, tokens, dim, dtype=x.dtype, device="cuda").transpose(0, 1)
+        else:
+            out = torch.empty(tokens, heads, dim, dtype=x.dtype, device="cuda")
+        out.copy_(x)
+        return out
+
+    def write(self, counts, lengths, k, v, status=None):
+        """k, v: pairs of (values, values on the GPU)."""
+        starts = starts_of(counts)
+        assert self.lowbit.cache_write(self.cache, k[1], v[1], self.gpu_table, ints(starts), ints(lengths), status) == self.lowbit.OK
+        self.k.write(k[0].double().numpy(), self.table, starts, lengths)
+        self.v.write(v[0].double().numpy(), self.table, starts, lengths)
+
+    def fill(self, lengths, dtype, layout=0):
+        n = sum(lengths)
+        self.write(lengths, lengths, self.values(n, dtype, 2.0, layout), self.values(n, dtype, 1.0, layout))
+
+    def check(self, lengths, dtype=torch.float32, layout=0):
+        """Everything that is cached, read back."""
+        n, starts = sum(lengths), starts_of(lengths)
+        out = [self.laid_out(torch.full((n, self.heads, self.dim), 9.0, dtype=dtype), layout) for _ in range(2)]
+        assert self.lowbit.cache_read(self.cache, *out, self.gpu_table, ints(starts), ints(lengths)) == self.lowbit.OK
+        for got, form in zip(out, (self.k, self.v)):
+            want = np.concatenate([form.read(self.table[b], n) for b, n in enumerate(lengths)])
+            want = plain.rounded(want, dtype)
+            assert torch.equal(torch.isnan(got).cpu(), torch.isnan(want))
+            assert torch.equal(torch.nan_to_num(got).cpu(), torch.nan_to_num(want))
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("page,dim,heads", [(16, 64, 3), (32, 128, 2), (64, 64, 1), (64, 128, 2), (128, 128, 1), (256, 64, 1), (16, 256, 2), (256, 256, 1)])
+def test_prompts_then_single_tokens_then_a_few(lowbit, dtype, page, dim, heads):
+    """Appending to pages that hold tokens: the scale grows (each step's values are larger), keeps, or the page is new."""
+    first = [2 * page + 5, 1, page, 0, page - 1]
+    last = [n + 1 + 3 + 2 + (page + 1) for n in first]
+    c = Both(lowbit, last, page, heads, dim, seed=page + dim)
+    lengths = list(first)
+    c.write(first, lengths, c.values(sum(first), dtype, 1.0), c.values(sum(first), dtype, 0.5))
+    c.check(lengths)
+    for counts, scale, layout in (([1] * 5, 40.0, 1), ([3] * 5, 0.01, 2), ([2, 2, 2, 2, 2], 700.0, 1), ([page + 1] * 5, 1.0, 0)):
+        lengths = [n + m for n, m in zip(lengths, counts)]
+        c.write(counts, lengths, c.values(sum(counts), dtype, scale, layout), c.values(sum(counts), dtype, scale / 3, layout))
+        c.check(lengths)
+    for out, layout in ((torch.bfloat16, 1), (torch.float16, 2), (torch.float32, 1)):
+        c.check(lengths, out, layout)
+
+
+@pytest.mark.parametrize("dtype", HALF)
+def test_values_at_the_formats_ends(lowbit, dtype):
+    page, heads, dim = 32, 6, 64
+    c = Both(lowbit, [40], page, heads, dim, 5)
+    x = torch.randn(40, heads, dim, generator=torch.Generator().manual_seed(1))
+    top = torch.finfo(dtype)
+    x[:, 0] = 0                                           # zeros
+    x[3, 1, 5], x[7, 1, 9], x[9, 1, 63] = float("inf"), float("-inf"), float("nan")
+    x[:, 2] *= top.tiny * top.eps * 4                     # subnormal
+    x[:, 3] = top.max * torch.sign(x[:, 3])               # the largest
+    x[:, 4] = 448.0 * torch.sign(x[:, 4])                 # exactly the largest code ...
+    x[20, 4, 1] = 448.0 * 2 if dtype == torch.bfloat16 else 449.0  # ... and one page needs more
+    x[:, 5] = float("nan")
+    x = x.to(dtype)
+    c.write([40], [40], (x, x.cuda()), (x, x.cuda()))
+    c.check([40])
+    # the next token of the second page of head 0 is far larger than its zeros; the NaN of head 5 meet numbers
+    y = torch.full((1, heads, dim), 100.0).to(dtype)
+    c2 = Both(lowbit, [41], page, heads, dim, 6)
+    c2.write([40], [40], (x, x.cuda()), (x, x.cuda()))
+    c2.write([1], [41], (y, y.cuda()), (y, y.cuda()))
+    c2.check([41])
+
+
+def test_idle_slots_and_tokens_before_a_sequence(lowbit):
+    page, heads, dim = 16, 2, 64
+    lengths, counts = [5, 0, 2, 17, 0], [1, 1, 4, 1, 0]   # the second sequence is an idle slot, the third has two tokens at negative positions
+    c = Both(lowbit, [20, 0, 20, 20, 0], page, heads, dim, 7)
+    prior = [4, 0, 0, 16, 0]
+    c.write(prior, prior, c.values(20, torch.bfloat16), c.values(20, torch.bfloat16))
+    k, v = c.values(7, torch.bfloat16), c.values(7, torch.bfloat16)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    before = [t.clone() for t in c.cache.tensors]
+    assert lowbit.cache_write(c.cache, k[1], v[1], c.gpu_table, ints(starts_of(counts)), ints(lengths), status) == lowbit.OK
+    starts = starts_of(counts)
+    kk, vv = k[0].double().numpy(), v[0].double().numpy()
+    # the same without the tokens that have no place
+    keep = [0, 4, 5, 6]
+    for form, x in ((c.k, kk), (c.v, vv)):
+        form.write(x[keep], c.table, starts_of([1, 0, 2, 1, 0]), lengths)
+    c.check(lengths)
+    assert status.item() == 0
+    used = {int(c.table[b, (lengths[b] - 1) // page]) for b in (0, 2, 3)}
+    for t, old in zip(c.cache.tensors, before):
+        for p in range(t.shape[0]):
+            if p not in used:
+                assert torch.equal(t[p], old[p])
+    out = [torch.full((7, heads, dim), 3.0, device="cuda") for _ in range(2)]
+    assert lowbit.cache_read(c.cache, *out, c.gpu_table, ints(starts), ints(lengths), status) == lowbit.OK
+    for t, form in zip(out, (c.k, c.v)):
+        assert not t[[1, 2, 3]].any()
+        assert np.array_equal(t[[0]].cpu().double().numpy(), form.read(c.table[0], 5)[4:])
+        assert np.array_equal(t[[4, 5]].cpu().double().numpy(), form.read(c.table[2], 2))
+    assert status.item() == 0
+
+
+def test_what_only_the_device_can_see_is_left_out_and_told(lowbit):
+    page, heads, dim = 16, 2, 64
+    c = Both(lowbit, [30, 30, 30], page, heads, dim, 8)
+    c.fill([30, 30, 30], torch.bfloat16)
+    x = torch.randn(90, heads, dim, device="cuda").to(torch.bfloat16)
+    q = torch.randn(3, 4, dim, device="cuda").to(torch.bfloat16)
+    good = c.gpu_table.clone()
+    pages = c.cache.n_pages
+
+    def attend(table, starts, lengths, max_new=1, max_length=32):
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        out = torch.full_like(q, 5.0)
+        ws = torch.empty(max(16, lowbit.cache_attention_workspace(c.cache, 3, 3, 4, max_new, max_length)), dtype=torch.uint8, device="cuda")
+        assert lowbit.cache_attention(c.cache, q, out, table, ints(starts), ints(lengths), max_new, max_length, ws, status=status) == lowbit.OK
+        return out, status.item()
+
+    want, told = attend(good, [0, 1, 2, 3], [30, 30, 30])
+    assert told == 0
+    # a length beyond the table, or beyond max_length
+    for lengths, most in (([30, 33, 30], 40), ([30, 30, 30], 29), ([30, -1, 30], 32)):
+        out, told = attend(good, [0, 1, 2, 3], lengths, max_length=most)
+        assert told == lowbit.E_ARG
+        for b in range(3):
+            assert torch.equal(out[b], want[b]) if 0 <= lengths[b] <= min(32, most) else bool((out[b] == 5).all())
+    # starts out of order, or beyond the tokens
+    for starts in ([0, 2, 1, 3], [0, 1, 2, 4], [-1, 1, 2, 3]):
+        assert attend(good, starts, [30, 30, 30])[1] == lowbit.E_ARG
+    # more tokens than max_new
+    out, told = attend(good, [0, 2, 2, 3], [30, 30, 30])
+    assert told == lowbit.E_ARG and bool((out[:2] == 5).all()) and torch.equal(out[2], want[2])
+    # page numbers outside the cache: their tokens are not seen
+    for bad in (-1, pages, 0x7FFFFFFF):
+        table = good.clone()
+        table[1, 1] = bad
+        out, told = attend(table, [0, 1, 2, 3], [30, 30, 30])
+        assert told == lowbit.E_ARG and torch.equal(out[0], want[0]) and torch.equal(out[2], want[2])
+        short, _ = attend(good, [0, 1, 2, 3], [30, 16, 30])
+        assert torch.allclose(out[1].float(), short[1].float(), rtol=0.02, atol=0.02)
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        before = [t.clone() for t in c.cache.tensors]
+        back = [torch.full((90, heads, dim), 9.0, device="cuda") for _ in range(2)]
+        assert lowbit.cache_read(c.cache, *back, table, ints([0, 30, 60, 90]), ints([30, 30, 30]), status) == lowbit.OK
+        assert status.item() == lowbit.E_ARG
+        for t, form in zip(back, (c.k, c.v)):
+            full = np.concatenate([form.read(c.table[b], 30) for b in range(3)])
+            full[46:60] = 0
+            assert np.array_equal(t.cpu().double().numpy(), full)
+        status.zero_()
+        assert lowbit.cache_write(c.cache, x[:3], x[3:6], table, ints([0, 1, 2, 3]), ints([30, 30, 30]), status) == lowbit.OK
+        assert status.item() == lowbit.E_ARG
+        page = int(good[1, 1])
+        for t, old in zip(c.cache.tensors, before):
+            assert torch.equal(t[page], old[page])
+            t.copy_(old)
+    status = torch.zeros(1, dtype=torch.int32).pin_memory()          # a word in host memory is told too
+    before = [t.clone() for t in c.cache.tensors]
+    assert lowbit.cache_write(c.cache, x, x, good, ints([0, 30, 60, 90]), ints([33, 33, 33]), status) == lowbit.OK
+    torch.cuda.synchronize()
+    assert status.item() == lowbit.E_ARG
+    for t, old in zip(c.cache.tensors, before):
+        assert torch.equal(t, old)
+
+
+# ---- attention ----------------------------------------------------------------------
+
+def attend(c, q, counts, lengths, scale=None, layout=0, max_new=None, max_length=None):
+    lowbit = c.lowbit
+    src = c.laid_out(q, layout)
+    out = c.laid_out(torch.full(q.shape, 77.0, dtype=q.dtype), layout)
+    new, most = max_new or max(counts), max_length or max(1, max(lengths))
+    need = lowbit.cache_attention_workspace(c.cache, len(counts), q.shape[0], q.shape[1], new, most)
+    ws = torch.full((max(16, need),), 0xFF, dtype=torch.uint8, device="cuda")       # NaN, were it read unwritten
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert lowbit.cache_attention(c.cache, src, out, c.gpu_table, ints(starts_of(counts)), ints(lengths), new, most, ws, scale, status) == lowbit.OK
+    assert status.item() == 0
+    return out
+
+
+def check_attention(c, out, q, counts, lengths, scale=None):
+    scale = c.dim ** -0.5 if scale is None else scale
+    starts = starts_of(counts)
+    for b, n in enumerate(lengths):
+        k, v = c.k.read(c.table[b], n), c.v.read(c.table[b], n)
+        rows = slice(starts[b], starts[b + 1])
+        want, bound = plain.attention(q[rows].double().numpy(), k, v, scale, q.dtype)
+        got = out[rows].double().cpu().numpy()
+        assert np.isfinite(got).all(), (b, n)
+        off = np.abs(got - want) - bound
+        assert off.size == 0 or off.max() <= 0, (b, n, off.max(), np.unravel_index(off.argmax(), off.shape))
+
+
+CALLS = [
+    # page, head_dim, heads, group, new tokens, lengths
+    (64, 128, 2, 4, [1, 1, 1, 1], [1, 64, 65, 300]),
+    (16, 64, 1, 1, [1] * 5, [15, 16, 17, 0, 1]),
+    (32, 128, 2, 8, [1, 1], [33, 700]),
+    (64, 256, 1, 5, [1, 1, 1], [2, 129, 640]),
+    (128, 64, 2, 3, [1], [1700]),
+    (16, 128, 1, 16, [1, 1], [5, 1100]),
+    (64, 128, 1, 40, [1, 1], [63, 500]),                  # more rows than one tile
+    (64, 128, 2, 4, [3, 1, 0, 5], [3, 100, 50, 260]),     # a few tokens each, none
+    (32, 64, 2, 2, [7, 40], [7, 333]),
+    (64, 128, 2, 1, [130, 64, 1], [130, 200, 64]),        # prompts, one behind a cached beginning
+    (16, 128, 1, 5, [77, 33], [77, 190]),
+    (64, 64, 1, 8, [150], [150]),
+    (16, 256, 1, 2, [70, 10], [101, 10]),
+    (256, 128, 1, 3, [65], [400]),
+    (64, 128, 1, 4, [4, 6], [2, 6]),                      # more tokens than the sequence has
+]
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("call", range(len(CALLS)))
+def test_attention_is_that_of_the_definition(lowbit, call, dtype):
+    page, dim, heads, group, counts, lengths = CALLS[call]
+    c = Both(lowbit, lengths, page, heads, dim, seed=call)
+    c.fill(lengths, dtype)
+    q = torch.from_numpy(c.rng.standard_normal((sum(counts), heads * group, dim)).astype(np.float32) * 1.5).to(dtype)
+    check_attention(c, attend(c, q, counts, lengths), q, counts, lengths)
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("layout", [1, 2])
+def test_strides_scale_and_generous_bounds(lowbit, layout, dtype):
+    counts, lengths = [1, 9, 100], [500, 9, 164]
+    c = Both(lowbit, lengths, 32, 2, 64, seed=layout)
+    c.fill(lengths, dtype, layout)
+    q = torch.from_numpy(c.rng.standard_normal((110, 6, 64)).astype(np.float32)).to(dtype)
+    for new, most in ((None, None), (120, 512), (100, 100000)):
+        check_attention(c, attend(c, q, counts, lengths, 0.3, layout, new, most), q, counts, lengths, 0.3)
+
+
+@pytest.mark.parametrize("dtype", HALF)
+def test_pages_of_very_different_scales(lowbit, dtype):
+    """Zeros, small and large pages side by side: no weight is lost to another page's scale."""
+    page, heads, dim, n = 16, 1, 64, 16 * 12
+    c = Both(lowbit, [n], page, heads, dim, 12)
+    k, v = c.values(n, dtype), c.values(n, dtype)
+    for i in range(12):
+        f = (0.0, 2.0 ** -12, 1.0, 2.0 ** 8)[i % 4]
+        v[0][16 * i:16 * i + 16] *= f
+        k[0][16 * i:16 * i + 16] *= (0.0, 1.0, 2.0 ** -10)[i % 3]
+    k, v = (k[0], k[0].cuda()), (v[0], v[0].cuda())
+    c.write([n], [n], k, v)
+    for counts in ([1], [30], [n]):
+        q = torch.randn(counts[0], 2, dim, generator=torch.Generator().manual_seed(3)).to(dtype)
+        check_attention(c, attend(c, q, counts, [n]), q, counts, [n])
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("counts", [[1], [20], [90]])
+def test_large_scores_and_one_certain_key(lowbit, counts, dtype):
+    c = Both(lowbit, [300], 64, 1, 128, 13)
+    k, v = c.values(300, dtype), c.values(300, dtype)
+    c.write([300], [300], k, v)
+    q = (torch.randn(counts[0], 2, 128, generator=torch.Generator().manual_seed(4)) * 40).to(dtype)
+    check_attention(c, attend(c, q, counts, [300]), q, counts, [300])
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("new", [6, 90])
+def test_what_a_row_does_not_see_cannot_reach_it(lowbit, new, dtype):
+    """NaN in a late token's key or value: rows before it are as without it, rows from it on are NaN where they have to be."""
+    n, heads, dim = 200, 1, 128
+    at = n - new // 2                                     # a token that the first half of the rows does not see
+    for what in ("k", "v"):
+        c = Both(lowbit, [n], 64, heads, dim, 14)
+        k, v = c.values(n, dtype), c.values(n, dtype)
+        q = torch.randn(new, 3, dim, generator=torch.Generator().manual_seed(5)).to(dtype)
+        c.write([n], [n], k, v)
+        clean = attend(c, q, [new], [n])
+        x = k if what == "k" else v
+        x[0][at, 0, 17] = float("nan")
+        c.write([n], [n], (k[0], k[0].cuda()), (v[0], v[0].cuda()))
+        out = attend(c, q, [new], [n])
+        first = new - (n - at)
+        assert torch.equal(out[:first], clean[:first])
+        nan = torch.isnan(out[first:])
+        assert nan.all() if what == "k" else (nan[:, :, 17].all() and int(nan.sum()) == nan[:, :, 17].numel())
+
+
+def test_the_same_call_gives_the_same_bits(lowbit):
+    lengths = [2000, 700]
+    c = Both(lowbit, lengths, 64, 2, 128, 15)
+    c.fill(lengths, torch.bfloat16)
+    for counts in ([1, 1], [100, 3]):
+        q = torch.randn(sum(counts), 8, 128, generator=torch.Generator().manual_seed(6)).to(torch.bfloat16)
+        outs = [attend(c, q, counts, lengths) for _ in range(4)]
+        assert all(torch.equal(outs[0], o) for o in outs)
+
+
+@pytest.mark.parametrize("new", [1, 70])
+def test_a_cache_of_more_than_4_gib(lowbit, new):
+    """Page numbers whose codes lie behind 2^32 bytes, for keys and for values."""
+    pages, page, heads, dim, n = 70000, 64, 8, 128, 150
+    cache = lowbit.Cache.empty(pages, heads, dim, page)
+    table = ints([[69999, 3, 69998]])
+    k, v = (torch.randn(n, heads, dim, generator=torch.Generator().manual_seed(s)).to(torch.bfloat16) for s in (1, 2))
+    assert lowbit.cache_write(cache, k.cuda(), v.cuda(), table, ints([0, n]), ints([n])) == lowbit.OK
+    small = Both(lowbit, [n], page, heads, dim, 16)
+    small.write([n], [n], (k, k.cuda()), (v, v.cuda()))
+    out = [torch.empty(n, heads, dim, device="cuda") for _ in range(2)]
+    assert lowbit.cache_read(cache, *out, table, ints([0, n]), ints([n])) == lowbit.OK
+    assert np.array_equal(out[0].cpu().double().numpy(), small.k.read(small.table[0], n))
+    assert np.array_equal(out[1].cpu().double().numpy(), small.v.read(small.table[0], n))
+    q = torch.randn(new, 16, dim, generator=torch.Generator().manual_seed(3)).to(torch.bfloat16)
+    want = attend(small, q, [new], [n])
+    small.cache, small.gpu_table = cache, table
+    assert torch.equal(attend(small, q, [new], [n]), want)
+
+
+@pytest.mark.parametrize("counts,lengths", [([1, 1, 1], [1000, 3, 0]), ([60, 1, 17], [60, 900, 200])])
+def test_another_stream_and_a_graph_give_the_same(lowbit, counts, lengths):
+    c = Both(lowbit, lengths, 64, 2, 128, 17)
+    g = torch.Generator().manual_seed(7)
+    n = sum(counts)
+    inputs = [[torch.randn(n, h, 128, generator=g).to(torch.bfloat16).cuda() for h in (2, 2, 8)] for _ in range(3)]
+    k, v, q = (torch.empty_like(t) for t in inputs[0])
+    prior = [max(0, a - b) for a, b in zip(lengths, counts)]
+    old = [torch.randn(sum(prior), 2, 128, generator=g).to(torch.bfloat16).cuda() for _ in range(2)]
+    table, starts, total = c.gpu_table, ints(starts_of(counts)), ints(lengths)
+    assert lowbit.cache_write(c.cache, *old, table, ints(starts_of(prior)), ints(prior)) == lowbit.OK
+    held = [t.clone() for t in c.cache.tensors]
+    out, back = torch.empty_like(q), [torch.empty_like(k), torch.empty_like(v)]
+    new, most = max(counts), max(lengths)
+    ws = torch.empty(max(16, lowbit.cache_attention_workspace(c.cache, 3, n, 8, new, most)), dtype=torch.uint8, device="cuda")
+
+    def step(stream=None):
+        assert lowbit.cache_write(c.cache, k, v, table, starts, total, stream=stream) == lowbit.OK
+        assert lowbit.cache_attention(c.cache, q, out, table, starts, total, new, most, ws, stream=stream) == lowbit.OK
+        assert lowbit.cache_read(c.cache, *back, table, starts, total, stream=stream) == lowbit.OK
+
+    def begin(i):
+        for t, old_ in zip(c.cache.tensors, held):
+            t.copy_(old_)
+        for t, x in zip((k, v, q), inputs[i]):
+            t.copy_(x)
+        for t in (out, *back):
+            t.zero_()
+
+    want = []
+    for i in range(3):
+        begin(i)
+        step()
+        want.append([t.clone() for t in (out, *back)])
+    side = torch.cuda.Stream()
+    begin(1)
+    side.wait_stream(torch.cuda.current_stream())
+    step(side)
+    torch.cuda.current_stream().wait_stream(side)
+    assert all(torch.equal(a, b) for a, b in zip((out, *back), want[1]))
+    graph = torch.cuda.CUDAGraph()
+    with torch.cuda.graph(graph):
+        step()
+    for i in (2, 0, 1, 2):
+        begin(i)
+        graph.replay()
+        torch.cuda.synchronize()
+        assert all(torch.equal(a, b) for a, b in zip((out, *back), want[i]))

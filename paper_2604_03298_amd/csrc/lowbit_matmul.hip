@@ -2,6 +2,8 @@
 #include "enec_lowbit.h"
 #include "lowbit.hpp"
 
+#include <type_traits>
+
 namespace enec {
 namespace lowbit {
 
@@ -176,38 +178,53 @@ __global__ void __launch_bounds__(64 * W) product_few_kernel(Product a)
 
 // ---- many tokens -------------------------------------------------------------------------------------------------------
 
-// LDS rows of 256 bytes a token, sixteen chunks of 16 bytes; chunk i of token t lies at place i ^ (t mod 16), so that sixteen tokens'
-// chunks of one number are in sixteen places and a wave's reads meet no bank twice.
-constexpr int STAGE_ROW = 256;
-
-// Memory through a descriptor, whose range the memory unit checks: what lies outside reads as zeros, so that neither the last rows nor the last
-// columns need a branch.  Offsets are 32 bits wide, from a tile's first row; an offset of NOWHERE plus any inside a tile lies outside.
+// Memory through a descriptor, whose range the memory unit checks: rows behind a matrix's last one need no branch.  Offsets are 32 bits wide,
+// from a tile's first row.
 using Range = __amdgpu_buffer_rsrc_t;
-constexpr uint32_t NOWHERE = 0x80000000u;
 __device__ __forceinline__ Range range_of(const void *p, uint32_t bytes)
 {
     return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
 }
-__device__ __forceinline__ u32x4 read16(Range r, uint32_t at) { return __builtin_bit_cast(u32x4, __builtin_amdgcn_raw_buffer_load_b128(r, (int)at, 0, 0)); }
-__device__ __forceinline__ uint32_t read4(Range r, uint32_t at) { return (uint32_t)__builtin_amdgcn_raw_buffer_load_b32(r, (int)at, 0, 0); }
-__device__ __forceinline__ uint32_t read2(Range r, uint32_t at) { return (uint32_t)(uint16_t)__builtin_amdgcn_raw_buffer_load_b16(r, (int)at, 0, 0); }
-// 16 bytes a lane into LDS, the lanes' side by side
-__device__ __forceinline__ void copy_to_lds(Range r, uint32_t at, uint8_t *to)
+// 16 or 4 bytes a lane into LDS, the lanes' side by side
+template <int BYTES> __device__ __forceinline__ void copy_to_lds(Range r, uint32_t at, uint8_t *to)
 {
-    __builtin_amdgcn_raw_ptr_buffer_load_lds(r, (__attribute__((address_space(3))) void *)to, 16, (int)at, 0, 0, 0);
+    const auto lds = (__attribute__((address_space(3))) void *)to;
+    if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds, 16, (int)at, 0, 0, 0);
+    else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds, 4, (int)at, 0, 0, 0);
 }
 
-// A workgroup has 16 RT WN rows of weights and 16 MT WM tokens; a wave 16 RT rows and 16 MT tokens of them.  Activations of a stage go into LDS by the
-// memory unit, two stages in turn, for all waves; weights go from memory into the registers of the waves that multiply with them, a stage ahead: at 4 bits
-// they are a quarter of the bytes, and WM = 1 brings each of them to one wave only, which makes 16-bit values of it once.
-// A stage is 256 bytes of a token.  16-bit activations: 128 columns, the halves of the four double blocks of 256 columns (a lane takes
-// 32 bytes of codes in a row from a double block: whole lines of memory); 4-bit ones: 512 columns, as in the kernel above.
-template <int ACT, int RT, int MT, int WN, int WM>
-__global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(Product a)
+// How a stage lies in LDS.  A row (of weights, or a token's) is a run of chunks of 16 bytes, chunk i at place i ^ turn(row).  A wave reads 16 bytes a lane
+// in four goes of sixteen lanes, lanes {0-3, 12-15, 20-27} the first: rows {0-3, 12-15} of one lane group and rows {4-11} of its neighbour.  Each
+// turn puts such sixteen chunks into the sixteen different places of 256 bytes, so that no bank is asked twice:
+//   256 bytes a row, the groups' chunks four apart (16-bit activations); 128 bytes, one apart (4-bit ones, and their weights); 64 bytes, one apart
+template <int ROW> __device__ __forceinline__ uint32_t turn(uint32_t r)
 {
-    constexpr int THREADS = 64 * WN * WM, TOKENS = 16 * MT * WM, ROWS = 16 * RT * WN, COPIES = TOKENS * STAGE_ROW / (16 * THREADS), U = MT == 4 ? 4 : 2;
-    constexpr int UNITS = 4 * (MT / U), PLANES = ACT == FP16 ? 2 : 1;
-    __shared__ __attribute__((aligned(16))) uint8_t stage[2][TOKENS * STAGE_ROW];
+    if constexpr (ROW == 256) return (r & 3) + 12 * (r >> 3 & 1);
+    if constexpr (ROW == 128) return (r & 2) + 4 * (r >> 3 & 1);
+    return 2 * (r >> 3 & 1);
+}
+
+// A workgroup has 16 RT WN rows of weights and 16 MT WM tokens; a wave 16 RT rows and 16 MT tokens of them.  A stage is 128 columns (4-bit activations: 256),
+// whose codes, scales and activations the memory unit brings into LDS, BUFFERS stages in turn.  Loads straight into registers were slower: a lane has
+// a row of its own there, so that each lane's 16 bytes are an access by themselves to the vector cache, where four neighbouring lanes of a copy make one
+// (2048 tokens x 4096 x 16384: 125 million accesses and 272 us then; the cache takes about one in a cycle).
+// As left operand a lane has row lane mod 16, and of a stage's blocks of 32 columns block lane / 16 (or 4 s + lane / 16 at step s).
+template <int ACT, int RT, int MT, int WN, int WM, int BUFFERS>
+__global__ void __launch_bounds__(64 * WN * WM, RT * MT > 32 ? 1 : 2) product_tile_kernel(Product a)
+{
+    constexpr int THREADS = 64 * WN * WM, TOKENS = 16 * MT * WM, ROWS = 16 * RT * WN, PLANES = ACT == FP16 ? 2 : 1;
+    constexpr int X_ROW = ACT == MX4 ? 128 : 256, W_ROW = ACT == MX4 ? 128 : 64, X_CHUNKS = X_ROW / 16, W_CHUNKS = W_ROW / 16;
+    constexpr int X_SIZE = TOKENS * X_ROW, W_SIZE = ROWS * W_ROW, S_SIZE = ROWS * 16, XS_SIZE = ACT == MX4 ? TOKENS * 16 : 0;
+    constexpr uint32_t S_STAGES = ACT == MX4 ? 2 : 4;                    // that sixteen bytes of scales are for
+    constexpr int X_COPIES = X_SIZE / 16 / THREADS, W_COPIES = W_SIZE / 16 / THREADS;
+    static_assert(X_SIZE % (16 * THREADS) == 0 && W_SIZE % (16 * THREADS) == 0 && S_SIZE % 256 == 0 && XS_SIZE % 256 == 0, "whole copies of a wave");
+    constexpr int U = MT < 4 ? MT : 4, STEPS = ACT == MX4 ? 2 : 4, UNITS = STEPS * (MT / U);
+    struct Stage {
+        uint8_t x[X_SIZE], w[W_SIZE];
+    };
+    extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
+    Stage *stage = reinterpret_cast<Stage *>(shared);
+    uint8_t *scale_bytes = shared + BUFFERS * sizeof(Stage);             // two of S_SIZE + XS_SIZE, in turn
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
     const uint32_t wn = wave % WN, wm = wave / WN;
     // Workgroups are dealt out to the eight dies one by one.  Each die takes a run of tiles, tokens first, so that it reads few rows of weights.
@@ -215,148 +232,147 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(Product a
     if (tile >= tiles) return;
     const uint32_t n0 = tile / a.m_tiles * ROWS, m0 = tile % a.m_tiles * TOKENS;
     const uint32_t rows = a.n - n0 < ROWS ? a.n - n0 : ROWS, tokens = a.m - m0 < TOKENS ? a.m - m0 : TOKENS;
-    const uint32_t pitch = a.groups * 64;
-    const Range codes = range_of(a.codes + (size_t)n0 * pitch, rows * pitch), scales = range_of(a.scales + (size_t)n0 * (a.groups * 4), rows * a.groups * 4);
-    const Range x = range_of(static_cast<const uint8_t *>(a.x) + (size_t)m0 * a.x_row, (tokens - 1) * (uint32_t)a.x_row + a.x_bytes);
+    const uint32_t w_pitch = a.groups * 64, s_pitch = a.groups * 4, x_pitch = (uint32_t)a.x_row;
+    const Range codes = range_of(a.codes + (size_t)n0 * w_pitch, rows * w_pitch), scales = range_of(a.scales + (size_t)n0 * s_pitch, rows * s_pitch);
+    const Range x = range_of(static_cast<const uint8_t *>(a.x) + (size_t)m0 * a.x_row, (tokens - 1) * x_pitch + a.x_bytes);
+    const Range x_scales = range_of(ACT == MX4 ? a.x_scales + (size_t)m0 * s_pitch : a.scales, ACT == MX4 ? tokens * s_pitch : 0);
 
-    const uint32_t stages = ACT == MX4 ? (a.groups + 3) / 4 : (a.groups + 1) / 2 * 2;      // (of one plane)
-    const uint32_t first = blockIdx.y * a.split_stages, end = first + a.split_stages < stages ? first + a.split_stages : stages;
+    const uint32_t first = blockIdx.y * a.split_stages, stages = ACT == MX4 ? (a.groups + 1) / 2 : a.groups;
+    const uint32_t end = first + a.split_stages < stages ? first + a.split_stages : stages;
 
-    uint32_t from[COPIES];
-    const uint32_t chunk = (threadIdx.x & 15) ^ (threadIdx.x >> 4 & 15);
+    // (the places of a thread's copies are whole multiples of sixteen rows apart, so its chunk is the same in all of them)
+    const uint32_t x_token = threadIdx.x / X_CHUNKS, w_row = threadIdx.x / W_CHUNKS;
+    const uint32_t x_from = x_token * x_pitch + 16 * ((threadIdx.x % X_CHUNKS) ^ turn<X_ROW>(x_token & 15));
+    const uint32_t w_from = w_row * w_pitch + 16 * ((threadIdx.x % W_CHUNKS) ^ turn<W_ROW>(w_row & 15));
+    const uint32_t s_from = threadIdx.x / 4 * s_pitch + 4 * (threadIdx.x % 4);
+    auto copy = [&](uint32_t unit) {                        // unit: a stage, or one plane of it
+        const uint32_t i = unit / PLANES, p = unit % PLANES;
+        Stage *to = stage + unit % BUFFERS;
 #pragma unroll
-    for (int r = 0; r < COPIES; ++r) {
-        const uint32_t token = r * (THREADS / 16) + (threadIdx.x >> 4);
-        from[r] = (token < tokens ? token : tokens - 1) * (uint32_t)a.x_row + (ACT == MX4 ? 16 * chunk : 128 * (chunk >> 2) + 16 * (chunk & 3));
-    }
-    auto copy = [&](uint32_t i, uint32_t plane) {
-        const uint32_t at = ACT == MX4 ? (4 * i + (chunk >> 2) < a.groups ? 256 * i : NOWHERE) : 256 * (i & ~1u) + 64 * (i & 1) + plane * a.x_plane;
-        uint8_t *to = stage[(i * PLANES + plane) & 1] + wave * 1024;
+        for (int r = 0; r < X_COPIES; ++r)
+            copy_to_lds<16>(x, x_from + r * (THREADS / X_CHUNKS) * x_pitch + i * X_ROW + p * a.x_plane, to->x + (r * THREADS + wave * 64) * 16);
 #pragma unroll
-        for (int r = 0; r < COPIES; ++r) copy_to_lds(x, at + from[r], to + r * (THREADS * 16));
+        for (int r = 0; r < W_COPIES; ++r)
+            copy_to_lds<16>(codes, w_from + r * (THREADS / W_CHUNKS) * w_pitch + i * W_ROW, to->w + (r * THREADS + wave * 64) * 16);
     };
-    // where this lane's chunks of its tokens lie: chunk 4 g + j of tokens c, 16 + c, ...
-    uint32_t read[4];
+    // Scales come for several stages at once, sixteen bytes of each row: four lanes' words are one access.
+    auto copy_scales = [&](uint32_t block) {
+        uint8_t *to = scale_bytes + (block & 1) * (S_SIZE + XS_SIZE);
 #pragma unroll
-    for (int j = 0; j < 4; ++j) read[j] = (wm * (16 * MT) + c) * STAGE_ROW + (((4 * g + j) ^ c) << 4);
-    auto chunk_at = [&](const uint8_t *s, int j, int u) { return *reinterpret_cast<const u32x4 *>(s + read[j] + u * (16 * STAGE_ROW)); };
+        for (int r = 0; r * THREADS * 4 < S_SIZE; ++r)
+            if ((r * THREADS + wave * 64) * 4 < S_SIZE) copy_to_lds<4>(scales, s_from + r * (THREADS / 4) * s_pitch + block * 16, to + (r * THREADS + wave * 64) * 4);
+#pragma unroll
+        for (int r = 0; r * THREADS * 4 < XS_SIZE; ++r)
+            if ((r * THREADS + wave * 64) * 4 < XS_SIZE)
+                copy_to_lds<4>(x_scales, s_from + r * (THREADS / 4) * s_pitch + block * 16, to + S_SIZE + (r * THREADS + wave * 64) * 4);
+    };
+    // A wave's copies are counted, and done in the order in which they were issued: with at most AHEAD left, those before them are in LDS.  Then
+    // all waves' are, and nobody reads the stage before any more.
+    constexpr int AHEAD = (BUFFERS - 2) * (X_COPIES + W_COPIES);         // (scales' copies make it more)
+    auto landed = [&](bool last) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (AHEAD == 0 || last) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        else asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(AHEAD) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+    };
 
-    uint32_t row[RT];
+    // where this lane's chunks lie: of tokens c, 16 + c, ..., and of rows c, 16 + c, ...
+    uint32_t x_at[STEPS], w_at[2];
 #pragma unroll
-    for (int t = 0; t < RT; ++t) row[t] = (16 * (wn * RT + t) + c) * a.groups;
+    for (int j = 0; j < STEPS; ++j) x_at[j] = (wm * (16 * MT) + c) * X_ROW + (((ACT == MX4 ? 4 * j + g : 4 * g + j) ^ turn<X_ROW>(c)) << 4);
+#pragma unroll
+    for (int j = 0; j < 2; ++j) w_at[j] = (wn * (16 * RT) + c) * W_ROW + (((ACT == MX4 ? 4 * j + g : g) ^ turn<W_ROW>(c)) << 4);
+    auto x_chunk = [&](const Stage *t, int j, int u) { return *reinterpret_cast<const u32x4 *>(t->x + x_at[j] + u * (16 * X_ROW)); };
+    auto w_chunk = [&](const Stage *t, int j, int r) { return *reinterpret_cast<const u32x4 *>(t->w + w_at[j] + r * (16 * W_ROW)); };
+
     f32x4 acc[RT][MT] = {};
-    uint32_t ws[RT], next_ws[RT];
-    auto landed = [&]() {                                   // this wave's copies and loads are there, and then all waves' copies are
-        asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        __syncthreads();
-    };
-
-    // In units of U tokens' tiles: the next unit's chunks are asked for before this one's are multiplied, and no earlier.
-    if constexpr (ACT == MX4) {
-        const Range x_scales = range_of(a.x_scales + (size_t)m0 * (a.groups * 4), tokens * a.groups * 4);
-        u32x4 w[RT][4];
-        uint32_t xs[MT], next_xs[MT];
-        auto fetch = [&](uint32_t i, int s) {
-            const uint32_t at = 4 * i + g < a.groups ? 256 * i + 64 * g + 16 * s : NOWHERE;
+    const uint32_t begin = first * PLANES, finish = end * PLANES;
+    copy_scales(first / S_STAGES);                          // (a split begins with such a block)
+    copy(begin);
+    if (BUFFERS == 3 && begin + 1 < finish) copy(begin + 1);
+    for (uint32_t unit = begin; unit < finish; ++unit) {
+        landed(unit + 1 >= finish);
+        const uint32_t i = unit / PLANES;
+        if (unit % (PLANES * S_STAGES) == 0 && i + S_STAGES < end) copy_scales(i / S_STAGES + 1);
+        if (unit + BUFFERS - 1 < finish) copy(unit + BUFFERS - 1);
+        const Stage *now = stage + unit % BUFFERS;
+        const uint8_t *ws_now = scale_bytes + (i / S_STAGES & 1) * (S_SIZE + XS_SIZE) + (16 / S_STAGES) * (i % S_STAGES);
+        // tokens' tiles are taken U at a time; the next ones' chunks are asked for before these are multiplied, and no earlier
+        u32x4 xv[2][U];
+        if constexpr (ACT == MX4) {
+            u32x4 w[2][RT];
+            uint32_t ws[RT], xs[MT];
+            const uint32_t pick = 0x0c0c0400u + 0x101u * g;              // of a row's eight bytes this lane's block's two
 #pragma unroll
-            for (int t = 0; t < RT; ++t) w[t][s] = read16(codes, row[t] * 64 + at);
-        };
-        auto fetch_scales = [&](uint32_t i) {
-            const uint32_t at = 4 * i + g < a.groups ? 16 * i + 4 * g : NOWHERE;
+            for (int t = 0; t < RT; ++t) w[0][t] = w_chunk(now, 0, t);
 #pragma unroll
-            for (int t = 0; t < RT; ++t) next_ws[t] = read4(scales, row[t] * 4 + at);
+            for (int t = 0; t < RT; ++t) {
+                const u32x2 v = *reinterpret_cast<const u32x2 *>(ws_now + (wn * (16 * RT) + 16 * t + c) * 16);
+                ws[t] = __builtin_amdgcn_perm(v[1], v[0], pick);
+            }
 #pragma unroll
-            for (int u = 0; u < MT; ++u) next_xs[u] = read4(x_scales, (wm * (16 * MT) + 16 * u + c) * (a.groups * 4) + at);
-        };
-        copy(first, 0);
-        fetch_scales(first);
+            for (int u = 0; u < MT; ++u) {
+                const u32x2 v = *reinterpret_cast<const u32x2 *>(ws_now + S_SIZE + (wm * (16 * MT) + 16 * u + c) * 16);
+                xs[u] = __builtin_amdgcn_perm(v[1], v[0], pick);
+            }
+            if (unit == a.groups / 2) {                                  // one group only: the other's bytes are not this row's
 #pragma unroll
-        for (int s = 0; s < 4; ++s) fetch(first, s);
-        for (uint32_t i = first; i < end; ++i) {
-            landed();
+                for (int t = 0; t < RT; ++t) ws[t] &= 255;
 #pragma unroll
-            for (int t = 0; t < RT; ++t) ws[t] = next_ws[t];
+                for (int u = 0; u < MT; ++u) xs[u] &= 255;
+            }
 #pragma unroll
-            for (int u = 0; u < MT; ++u) xs[u] = next_xs[u];
-            if (i + 1 < end) copy(i + 1, 0);
-            fetch_scales(i + 1);
-            const uint8_t *now = stage[i & 1];
-            u32x4 xv[2][U];
+            for (int u = 0; u < U; ++u) xv[0][u] = x_chunk(now, 0, u);
 #pragma unroll
-            for (int u = 0; u < U; ++u) xv[0][u] = chunk_at(now, 0, u);
-#pragma unroll
-            for (int unit = 0; unit < UNITS; ++unit) {
-                const int s = unit / (MT / U), b = unit % (MT / U), next = unit + 1;
+            for (int k = 0; k < UNITS; ++k) {
+                const int s = k / (MT / U), b = k % (MT / U), next = k + 1;
                 __builtin_amdgcn_sched_barrier(0);
                 if (next < UNITS) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) xv[next & 1][u] = chunk_at(now, next / (MT / U), next % (MT / U) * U + u);
+                    for (int u = 0; u < U; ++u) xv[next & 1][u] = x_chunk(now, next / (MT / U), next % (MT / U) * U + u);
+                }
+                if (k == 0) {
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) w[1][t] = w_chunk(now, 1, t);
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u)
 #pragma unroll
-                    for (int t = 0; t < RT; ++t) acc[t][b * U + u] = mfma_mx4(s, w[t][s], xv[unit & 1][u], acc[t][b * U + u], (int)ws[t], (int)xs[b * U + u]);
-                if (b == MT / U - 1) fetch(i + 1, s);
+                    for (int t = 0; t < RT; ++t) acc[t][b * U + u] = mfma_mx4(s, w[s][t], xv[k & 1][u], acc[t][b * U + u], (int)ws[t], (int)xs[b * U + u]);
             }
-            __builtin_amdgcn_sched_barrier(0);
-        }
-    } else {
-        u32x4 w[RT][2];
-        auto fetch = [&](uint32_t i, int h) {                // the codes of stage i + h, i even
-            const uint32_t at = 2 * i + g < 2 * a.groups ? 64 * i + 32 * g + 16 * h : NOWHERE;
+        } else {
+            u32x4 w[RT];
+            uint32_t ws[RT];
+            bf16x8 wv[2][RT];
 #pragma unroll
-            for (int t = 0; t < RT; ++t) w[t][h] = read16(codes, row[t] * 64 + at);
-        };
-        auto fetch_scales = [&](uint32_t i) {                // of stages i and i + 1
-            const uint32_t at = 2 * i + g < 2 * a.groups ? 4 * i + 2 * g : NOWHERE;
+            for (int t = 0; t < RT; ++t) {
+                w[t] = w_chunk(now, 0, t);
+                ws[t] = ws_now[(wn * (16 * RT) + 16 * t + c) * 16 + g];
+            }
 #pragma unroll
-            for (int t = 0; t < RT; ++t) next_ws[t] = read2(scales, row[t] * 4 + at);
-        };
-        copy(first, 0);
-        fetch_scales(first);
-        fetch(first, 0);
-        fetch(first, 1);
-        for (uint32_t i = first; i < end; i += 2) {          // (first and end are even)
+            for (int u = 0; u < U; ++u) xv[0][u] = x_chunk(now, 0, u);
 #pragma unroll
-            for (int h = 0; h < 2; ++h) {
+            for (int t = 0; t < RT; ++t) wv[0][t] = values_of(w[t][0], f32_of_bits(ws[t] << 23));
 #pragma unroll
-                for (int p = 0; p < PLANES; ++p) {
-                    landed();
-                    if (h == 0 && p == 0) {
+            for (int k = 0; k < UNITS; ++k) {
+                const int j = k / (MT / U), b = k % (MT / U), next = k + 1;
+                __builtin_amdgcn_sched_barrier(0);
+                if (next < UNITS) {
 #pragma unroll
-                        for (int t = 0; t < RT; ++t) ws[t] = next_ws[t];
-                        fetch_scales(i + 2);
-                    }
-                    if (p + 1 < PLANES) copy(i + h, p + 1);
-                    else if (i + h + 1 < end) copy(i + h + 1, 0);
-                    const uint8_t *now = stage[(h * PLANES + p) & 1];
-                    u32x4 xv[2][U];
-                    bf16x8 wv[RT];
-#pragma unroll
-                    for (int u = 0; u < U; ++u) xv[0][u] = chunk_at(now, 0, u);
-#pragma unroll
-                    for (int unit = 0; unit < UNITS; ++unit) {
-                        const int j = unit / (MT / U), b = unit % (MT / U), next = unit + 1;
-                        __builtin_amdgcn_sched_barrier(0);
-                        if (b == 0) {
-#pragma unroll
-                            for (int t = 0; t < RT; ++t) wv[t] = values_of(w[t][h][j], f32_of_bits((ws[t] >> (8 * h) & 255) << 23));
-                        }
-                        if (next < UNITS) {
-#pragma unroll
-                            for (int u = 0; u < U; ++u) xv[next & 1][u] = chunk_at(now, next / (MT / U), next % (MT / U) * U + u);
-                        }
-#pragma unroll
-                        for (int u = 0; u < U; ++u)
-#pragma unroll
-                            for (int t = 0; t < RT; ++t)
-                                acc[t][b * U + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[t], __builtin_bit_cast(bf16x8, xv[unit & 1][u]), acc[t][b * U + u], 0, 0, 0);
-                    }
-                    __builtin_amdgcn_sched_barrier(0);
+                    for (int u = 0; u < U; ++u) xv[next & 1][u] = x_chunk(now, next / (MT / U), next % (MT / U) * U + u);
                 }
-                fetch(i + 2, h);
+                if (b == MT / U - 1 && j < 3) {
+#pragma unroll
+                    for (int t = 0; t < RT; ++t) wv[(j + 1) & 1][t] = values_of(w[t][j + 1], f32_of_bits(ws[t] << 23));
+                }
+#pragma unroll
+                for (int u = 0; u < U; ++u)
+#pragma unroll
+                    for (int t = 0; t < RT; ++t)
+                        acc[t][b * U + u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[j & 1][t], __builtin_bit_cast(bf16x8, xv[k & 1][u]), acc[t][b * U + u], 0, 0, 0);
             }
         }
+        __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
     for (int u = 0; u < MT; ++u) {
@@ -372,7 +388,7 @@ __global__ void __launch_bounds__(64 * WN * WM, 2) product_tile_kernel(Product a
     }
 }
 
-// Activations as the kernel above copies them: bf16, rows of a multiple of 256 columns, zeros behind the last one; of fp16 two
+// Activations as the kernel above copies them: bf16, rows of a multiple of 128 columns, zeros behind the last one; of fp16 two
 // such rows one behind the other, the values' parts.
 template <int DT>
 __global__ void __launch_bounds__(256) lay_out_kernel(const uint16_t *__restrict__ x, size_t x_stride, uint32_t k, Divide per_row, uint32_t n_vec,
@@ -434,11 +450,12 @@ inline size_t part_row(uint32_t n) { return ((size_t)n + 15) / 16 * 16; }
 
 Plan plan_of(uint32_t m, uint32_t n, uint32_t k, bool mx4)
 {
-    static const uint32_t shapes[][2] = {{256, 128}, {128, 128}, {256, 64}, {128, 64}, {128, 32}};
+    const uint32_t shapes[][2] = {{256, mx4 ? 256u : 128u}, {mx4 ? 128u : 256u, mx4 ? 128u : 64u}, {128, 64}, {128, 32}, {64, 32}};
     Plan p{};
     // (the counts of vectors that are laid out, and of tiles, have 31 bits)
-    if (m <= 16 || k > MOST_COLUMNS || k == 0 || (uint64_t)m * up(k, 256) >= 1u << 26 || (uint64_t)up(n, 128) * up(m, 32) >= 1u << 27) return p;
-    const uint32_t groups = up(k, 128), unit = mx4 ? 1 : 2, stages = mx4 ? up(groups, 4) : up(groups, 2) * 2;
+    if (m <= 16 || k > MOST_COLUMNS || k == 0 || (uint64_t)m * up(k, 128) >= 1u << 27 || (uint64_t)up(n, 128) * up(m, 32) >= 1u << 27) return p;
+    const uint32_t groups = up(k, 128), unit = mx4 ? 2 : 4, stages = mx4 ? up(groups, 2) : groups;      // a split is whole blocks of scales
+
     double best = 1e300;
     for (int kind = 1; kind <= 5; ++kind) {
         const uint32_t rows = shapes[kind - 1][0], tokens = shapes[kind - 1][1];
@@ -453,14 +470,20 @@ Plan plan_of(uint32_t m, uint32_t n, uint32_t k, bool mx4)
             if (cost < best) best = cost, p = {kind, rows, tokens, up(stages, each), each, 0, 0};
         }
     }
-    if (!mx4) p.laid_out = 4 * (size_t)m * (up(k, 256) * 256);
+    if (!mx4) p.laid_out = 4 * (size_t)m * (up(k, 128) * 128);
     if (p.splits > 1) p.parts = p.splits * (size_t)m * part_row(n) * sizeof(float);
     return p;
 }
 
-template <int ACT, int RT, int MT, int WN, int WM> void launch_tile(const Product &a, uint32_t splits, hipStream_t s)
+template <int ACT, int RT, int MT, int WN, int WM, int BUFFERS> bool launch_tile(const Product &a, uint32_t splits, hipStream_t s)
 {
-    product_tile_kernel<ACT, RT, MT, WN, WM><<<dim3(up(a.n_tiles * a.m_tiles, 8) * 8, splits), 64 * WN * WM, 0, s>>>(a);
+    constexpr size_t TOKENS = 16 * MT * WM, ROWS = 16 * RT * WN;
+    constexpr size_t LDS = BUFFERS * (ACT == MX4 ? (TOKENS + ROWS) * 128 : TOKENS * 256 + ROWS * 64) + 2 * 16 * (ACT == MX4 ? TOKENS + ROWS : ROWS);
+    static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
+    const auto kernel = product_tile_kernel<ACT, RT, MT, WN, WM, BUFFERS>;
+    if (LDS > 65536 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS) != hipSuccess) return false;
+    kernel<<<dim3(up(a.n_tiles * a.m_tiles, 8) * 8, splits), 64 * WN * WM, LDS, s>>>(a);
+    return true;
 }
 
 template <int ACT> int launch(Product a, void *workspace, hipStream_t s)
@@ -474,10 +497,10 @@ template <int ACT> int launch(Product a, void *workspace, hipStream_t s)
     }
     if constexpr (ACT == MX4) {
         a.x_row = a.x_bytes = a.groups * 64;
-    } else if (ACT == BF16 && a.k % 256 == 0 && a.x_stride % 8 == 0 && a.x_stride <= MOST_COLUMNS && aligned(a.x, 16)) {
+    } else if (ACT == BF16 && a.k % 128 == 0 && a.x_stride % 8 == 0 && a.x_stride <= MOST_COLUMNS && aligned(a.x, 16)) {
         a.x_row = a.x_stride * 2, a.x_bytes = a.k * 2;
     } else {
-        const uint32_t cols = up(a.k, 256) * 256, n_vec = a.m * (cols / 8);
+        const uint32_t cols = up(a.k, 128) * 128, n_vec = a.m * (cols / 8);
         lay_out_kernel<ACT><<<up(n_vec, 256), 256, 0, s>>>(static_cast<const uint16_t *>(a.x), a.x_stride, a.k, divide_by(cols / 8), n_vec,
                                                            static_cast<u32x4 *>(workspace));
         a.x = workspace;
@@ -486,13 +509,15 @@ template <int ACT> int launch(Product a, void *workspace, hipStream_t s)
     }
     a.n_tiles = up(a.n, p.rows), a.m_tiles = up(a.m, p.tokens), a.split_stages = p.split_stages;
     if (p.splits > 1) a.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.laid_out), a.part_row = part_row(a.n);
+    bool ok;
     switch (p.kind) {
-    case 1: launch_tile<ACT, 4, 8, 4, 1>(a, p.splits, s); break;
-    case 2: launch_tile<ACT, 4, 4, 2, 2>(a, p.splits, s); break;
-    case 3: launch_tile<ACT, 4, 4, 4, 1>(a, p.splits, s); break;
-    case 4: launch_tile<ACT, 2, 4, 4, 1>(a, p.splits, s); break;
-    default: launch_tile<ACT, 2, 2, 4, 1>(a, p.splits, s); break;
+    case 1: ok = ACT == MX4 ? launch_tile<ACT, 4, ACT == MX4 ? 8 : 4, 4, 2, 2>(a, p.splits, s) : launch_tile<ACT, 4, 4, 4, 2, 2>(a, p.splits, s); break;
+    case 2: ok = ACT == MX4 ? launch_tile<ACT, 4, 4, 2, 2, 2>(a, p.splits, s) : launch_tile<ACT, 4, 4, 4, 1, 2>(a, p.splits, s); break;
+    case 3: ok = launch_tile<ACT, 2, 4, 4, 1, 2>(a, p.splits, s); break;
+    case 4: ok = launch_tile<ACT, 2, 2, 4, 1, 3>(a, p.splits, s); break;
+    default: ok = launch_tile<ACT, 1, 2, 4, 1, 3>(a, p.splits, s); break;
     }
+    if (!ok) return ENEC_E_HIP;
     if (p.splits > 1) {
         const uint32_t per_row = up(a.n, 4);
         join_kernel<<<up(a.m * per_row, 256), 256, 0, s>>>(a.parts, p.splits, a.m, a.n, a.part_row, divide_by(per_row), a.y, a.y_stride, a.y_dtype);

@@ -276,6 +276,281 @@ __global__ void __launch_bounds__(256) attend_kernel(Attend a)
     }
 }
 
+// ---- many rows ---------------------------------------------------------------------------------------------------------
+
+// Keys and values of a tile of 64 tokens in LDS, two tiles in turn, as codes: a token's keys are a row of D / 16 chunks of 16 bytes, a
+// dimension's values a row of four.  Chunk i of a row lies at place i ^ turn: the sixteen lanes whose 16 bytes are read in one go (rows {0-3, 12-15} of a
+// lane group and rows {4-11} of its neighbour) find theirs in sixteen different places of 256 bytes.
+template <int D> __device__ __forceinline__ uint32_t key_turn(uint32_t token)
+{
+    const uint32_t half = token >> 5 & 1;
+    if constexpr (D == 64) return 2 * half;
+    if constexpr (D == 128) return (token & 2) + 4 * half;
+    return 2 * (token & 3) + 8 * half;
+}
+__device__ __forceinline__ uint32_t value_turn(uint32_t dim) { return 2 * (dim >> 3 & 1); }
+
+// The same arrangement as above, with 16 NT query rows to each of the four waves, which share the tiles: a wave has all of them, so nothing is
+// joined in the end.  The memory unit copies the codes of a tile into LDS while the one before is worked on.  Every wave makes
+// 16-bit values of the codes by itself: a conversion makes two of them in the time of any vector instruction, and NT tiles of rows use each.
+template <int DT, int D, int NT>
+__global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
+{
+    constexpr int KC = D / 64, VT = D / 16, COPIES = D / 64, ROWS = 64 * NT;
+    __shared__ __attribute__((aligned(16))) uint8_t keys[2][64 * D], values[2][64 * D];
+    const Pages &c = a.c;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
+    // Workgroups are dealt out to the eight dies one by one.  Each die takes a run of (sequence, head)s, whose keys and values stay in its cache,
+    // and of their rows the last ones first: they see most.
+    const uint32_t groups = c.batch * c.heads, each = a.row_tiles * a.splits, total_tiles = groups * each, per_die = (total_tiles + 7) / 8;
+    const uint32_t tile = blockIdx.x % 8 * per_die + blockIdx.x / 8;
+    if (blockIdx.x / 8 >= per_die || tile >= total_tiles) return;
+    const uint32_t group = tile / each, within = tile % each, b = group / c.heads, head = group % c.heads;
+    const uint32_t split = within % a.splits, row_tile = a.row_tiles - 1 - within / a.splits;
+    const Sequence s = sequence_of(a, b);
+    if (!s.good) {
+        complain(c);
+        return;
+    }
+    const uint32_t rows = s.count * a.group.by, first_row = row_tile * ROWS;
+    if (first_row >= rows) return;
+    const int32_t begin = s.length - (int32_t)s.count;
+    const uint32_t last_row = first_row + ROWS < rows ? first_row + ROWS - 1 : rows - 1;
+    const int32_t end = begin + (int32_t)quotient(last_row, a.group) + 1;     // no row here sees a position from here on
+    const int32_t from = (int32_t)(split * a.chunk), to = end - from < (int32_t)a.chunk ? end : from + (int32_t)a.chunk;
+    if (split > 0 && from >= to) return;
+
+    const uint32_t row0 = first_row + wave * (16 * NT);
+    uint32_t token[NT], q_head[NT];
+    int32_t limit[NT];                                                        // the last position that the row sees
+    u32x4 q[NT][KC][2] = {};
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const uint32_t row = row0 + 16 * n + col;
+        token[n] = quotient(row, a.group), q_head[n] = head * a.group.by + (row - token[n] * a.group.by);
+        limit[n] = row < rows ? begin + (int32_t)token[n] : -1;
+        if (row < rows) {
+            const uint16_t *p = static_cast<const uint16_t *>(a.q) + (size_t)(s.start + token[n]) * a.q_token + (size_t)q_head[n] * a.q_head;
+#pragma unroll
+            for (int i = 0; i < KC; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) q[n][i][h] = *reinterpret_cast<const u32x4_a2 *>(p + 64 * i + 16 * g + 8 * h);
+        }
+    }
+    // of this wave's rows: what the first sees, and where the last one's view ends (none: nothing)
+    const int32_t least = row0 < rows ? begin + (int32_t)quotient(row0, a.group) : 0;
+    const uint32_t my_last = row0 + 16 * NT - 1 < last_row ? row0 + 16 * NT - 1 : last_row;
+    const int32_t my_end = row0 < rows ? begin + (int32_t)quotient(my_last, a.group) + 1 : 0;
+
+    f32x4 o[NT][VT] = {};
+    float most[NT], total[NT];
+#pragma unroll
+    for (int n = 0; n < NT; ++n) most[n] = -__builtin_inff(), total[n] = 0;
+    const uint32_t page_mask = (1u << c.log_page) - 1;
+    const size_t head_values = (size_t)D << c.log_page;
+    const int32_t *table = c.table + (size_t)b * c.table_stride;
+
+    // The page of 16 tokens from position t on, -1 where there is none.  Copies from no page take page 0, which exists, and are not looked at.
+    auto page_at = [&](int32_t t) {
+        const int32_t p = t < s.length ? table[t >> c.log_page] : -1;
+        if ((uint32_t)p < c.n_pages) return p;
+        if (t < s.length) complain(c);
+        return -1;
+    };
+    // wave w copies the keys of 16 tokens and a quarter of the dimensions' values
+    const uint32_t value_group = (lane & 3) ^ value_turn(lane >> 2);
+    auto copy = [&](int32_t t0, int buffer, int32_t key_page, int32_t value_page) {
+        using from_t = const __attribute__((address_space(1))) void *;
+        using to_t = __attribute__((address_space(3))) void *;
+        const uint8_t *k = c.k_codes + ((size_t)(uint32_t)(key_page < 0 ? 0 : key_page) * c.heads + head) * head_values + (size_t)((t0 + 16 * wave) & page_mask) * D;
+        const uint8_t *v = c.v_codes + ((size_t)(uint32_t)(value_page < 0 ? 0 : value_page) * c.heads + head) * head_values + ((t0 + 16 * value_group) & page_mask);
+#pragma unroll
+        for (int r = 0; r < COPIES; ++r) {
+            const uint32_t place = r * 64 + lane, row = place / (D / 16), chunk = place % (D / 16) ^ key_turn<D>(16 * wave + row);
+            __builtin_amdgcn_global_load_lds((from_t)(k + row * D + 16 * chunk), (to_t)(keys[buffer] + 16 * wave * D + r * 1024), 16, 0, 0);
+        }
+#pragma unroll
+        for (int r = 0; r < COPIES; ++r) {
+            const uint32_t dim = (wave * COPIES + r) * 16 + (lane >> 2);
+            __builtin_amdgcn_global_load_lds((from_t)(v + ((size_t)dim << c.log_page)), (to_t)(values[buffer] + (wave * COPIES + r) * 1024), 16, 0, 0);
+        }
+    };
+    uint32_t key_at[4], value_at = col * 64 + ((g ^ value_turn(col)) << 4);
+#pragma unroll
+    for (int i = 0; i < KC; ++i) {
+        const uint32_t t = 16 * (col >> 2) + (col & 3);                       // (+ 4 j, which does not turn)
+        key_at[i] = t * D + (((4 * i + g) ^ key_turn<D>(t)) << 4);
+    }
+
+    int32_t page = page_at(from + 16 * (int32_t)g), next_page = -1;           // of the tokens that this lane has weights of
+    {
+        const int32_t kp = page_at(from + 16 * (int32_t)wave), vp = page_at(from + 16 * (int32_t)value_group);
+        if (from < to) copy(from, 0, kp, vp);
+    }
+    auto scales_of = [&](int32_t p, float &k, float &v) {
+        const size_t at = (size_t)(uint32_t)(p < 0 ? 0 : p) * c.heads + head;
+        k = power_of(c.k_scales[at]), v = power_of(c.v_scales[at]);
+    };
+    float ks, vs, next_ks = 0, next_vs = 0;
+    scales_of(page, ks, vs);
+    int32_t next_kp = page_at(from + 64 + 16 * (int32_t)wave), next_vp = page_at(from + 64 + 16 * (int32_t)value_group);
+    next_page = page_at(from + 64 + 16 * (int32_t)g);
+
+    int buffer = 0;
+    for (int32_t t0 = from; t0 < to; t0 += 64, buffer ^= 1) {
+        __builtin_amdgcn_sched_barrier(0);
+        // this wave's copies are in LDS, then all waves' are, and nobody reads the tile before any more
+        asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        int32_t far_page = -1, far_kp = -1, far_vp = -1;
+        if (t0 + 64 < to) {
+            copy(t0 + 64, buffer ^ 1, next_kp, next_vp);
+            scales_of(next_page, next_ks, next_vs);
+            far_page = page_at(t0 + 128 + 16 * (int32_t)g);
+            far_kp = page_at(t0 + 128 + 16 * (int32_t)wave);
+            far_vp = page_at(t0 + 128 + 16 * (int32_t)value_group);
+        }
+        if (t0 < my_end) {
+            const int32_t tv = t0 + 16 * (int32_t)g;
+            const bool partial = t0 + 63 > least || t0 + 64 > s.length || __any(page < 0);
+            f32x4 x[NT][4] = {};
+#pragma unroll
+            for (int i = 0; i < KC; ++i) {
+                u32x4 k[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const u32x4 *>(keys[buffer] + key_at[i] + 4 * j * D);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const u32x4 v = values8<DT>(k[j][2 * h], k[j][2 * h + 1], 1.0f);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) x[n][j] = mfma16<DT>(v, q[n][i][h], x[n][j]);
+                    }
+            }
+            const float by = ks * a.scale;
+            u32x4 p[NT][2], rest_of[NT][2];
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                if (partial) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j)
+#pragma unroll
+                        for (int i = 0; i < 4; ++i) x[n][j][i] = page >= 0 && tv + 4 * j + i <= limit[n] ? x[n][j][i] * by : -__builtin_inff();
+                } else {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[n][j] *= by;
+                }
+                float high = -__builtin_inff();
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) high = fmaxf(high, x[n][j][i]);
+                high = over_groups_max(high);
+                // Weights are taken relative to a maximum that may lag behind by up to 2^8, which costs nothing in 32 bits: most tiles need no
+                // change of what is summed already.
+                if (__any(high > most[n] + 8.0f)) {
+                    const float now = fmaxf(most[n], high), fade = now == -__builtin_inff() ? 1.0f : exp2_of(most[n] - now);
+                    most[n] = now;
+                    total[n] *= fade;
+#pragma unroll
+                    for (int i = 0; i < VT; ++i) o[n][i] *= fade;
+                }
+                const float base = most[n] == -__builtin_inff() ? 0.0f : most[n];
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const float lo = exp2_of(x[n][2 * h + j / 2][2 * (j & 1)] - base), hi = exp2_of(x[n][2 * h + j / 2][2 * (j & 1) + 1] - base);
+                        total[n] += lo;
+                        total[n] += hi;
+                        p[n][h][j] = pack2<BF16>(lo, hi);
+                        if constexpr (DT == FP16) {
+                            const f32x2 r = unpack2<BF16>(p[n][h][j]);
+                            rest_of[n][h][j] = pack2<BF16>(lo - r[0], hi - r[1]);
+                        }
+                    }
+            }
+            // in a tile that not every row sees whole: bytes behind the sequence's end and of no page are anyone's, and a NaN is
+            // told to the rows that see it, as above
+            uint32_t mask[4] = {~0u, ~0u, ~0u, ~0u};
+            bool careful = false;
+            if (partial) {
+                uint32_t any = 0;
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const int32_t here = s.length - tv - 4 * j;
+                    mask[j] = page < 0 || here <= 0 ? 0 : here >= 4 ? ~0u : (1u << (8 * here)) - 1;
+                }
+                for (int i = 0; i < VT; ++i) {
+                    const u32x4 v = *reinterpret_cast<const u32x4 *>(values[buffer] + value_at + i * 1024);
+                    for (int j = 0; j < 4; ++j) any |= nan_bytes(v[j] & mask[j]);
+                }
+                careful = __any(any);
+            }
+#pragma unroll
+            for (int i = 0; i < VT; ++i) {
+                u32x4 v = *reinterpret_cast<const u32x4 *>(values[buffer] + value_at + i * 1024);
+                if (partial) {
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) v[j] &= mask[j];
+                    if (careful) {
+                        u32x4 bad;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) {
+                            const uint32_t nan = nan_bytes(v[j]);
+                            v[j] &= ~nan;
+                            bad[j] = nan & 0x38383838u;              // 1.0 as E4M3
+                        }
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) {
+                            f32x4 seen = {};
+#pragma unroll
+                            for (int h = 0; h < 2; ++h) {
+                                u32x4 sees;
+#pragma unroll
+                                for (int j = 0; j < 4; ++j) {
+                                    const int32_t at = tv + 8 * h + 2 * j;
+                                    sees[j] = (at <= limit[n] ? 0x3F80u : 0) | (at + 1 <= limit[n] ? 0x3F800000u : 0);
+                                }
+                                seen = mfma16<BF16>(values8<BF16>(bad[2 * h], bad[2 * h + 1], 1.0f), sees, seen);
+                            }
+#pragma unroll
+                            for (int e = 0; e < 4; ++e) o[n][i][e] = seen[e] > 0 ? __builtin_nanf("") : o[n][i][e];
+                        }
+                    }
+                }
+#pragma unroll
+                for (int h = 0; h < 2; ++h) {
+                    const u32x4 vv = values8<BF16>(v[2 * h], v[2 * h + 1], vs);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        o[n][i] = mfma16<BF16>(vv, p[n][h], o[n][i]);
+                        if constexpr (DT == FP16) o[n][i] = mfma16<BF16>(vv, rest_of[n][h], o[n][i]);
+                    }
+                }
+            }
+        }
+        page = next_page, ks = next_ks, vs = next_vs;
+        next_page = far_page, next_kp = far_kp, next_vp = far_vp;
+    }
+#pragma unroll
+    for (int n = 0; n < NT; ++n) {
+        const float sum = over_groups_sum(total[n]);
+        if (row0 + 16 * n + col >= rows) continue;
+        const float by = sum == 0 ? 0.0f : 1.0f / sum;
+        const size_t at = ((size_t)split * c.n_tokens + s.start + token[n]) * a.q_heads + q_head[n];
+        uint16_t *out = static_cast<uint16_t *>(a.out) + (size_t)(s.start + token[n]) * a.out_token + (size_t)q_head[n] * a.out_head;
+#pragma unroll
+        for (int i = 0; i < VT; ++i) {
+            const uint32_t d = 16 * i + 4 * g;
+            if (a.splits == 1) *reinterpret_cast<u32x2_a2 *>(out + d) = u32x2{pack2<DT>(o[n][i][0] * by, o[n][i][1] * by), pack2<DT>(o[n][i][2] * by, o[n][i][3] * by)};
+            else *reinterpret_cast<f32x4 *>(a.part + at * D + d) = o[n][i];
+        }
+        if (a.splits > 1 && g == 0) *reinterpret_cast<f32x2 *>(a.part_stat + 2 * at) = f32x2{most[n], sum};
+    }
+}
+
 // The splits of a row, in their order: one wave a row.
 template <int DT, int D>
 __global__ void __launch_bounds__(64) attend_join_kernel(Attend a)
@@ -312,31 +587,40 @@ namespace {
 using namespace enec::lowbit;
 
 struct Plan {
+    bool many;                          // the kernel for many rows
     uint32_t row_tiles, chunk, splits;
 };
+
+inline uint32_t rows_of_many(uint32_t head_dim) { return head_dim == 256 ? 64 : 128; }
+
 // How a call is cut up.  A sequence's cached tokens are split where rows and heads alone leave the card empty.
-Plan plan_of(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t max_new, uint32_t max_length)
+Plan plan_of(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t head_dim, uint32_t max_new, uint32_t max_length)
 {
     Plan p;
-    p.row_tiles = (uint32_t)(((uint64_t)max_new * group + 15) / 16);
+    const uint64_t rows = (uint64_t)max_new * group;
+    p.many = rows > 32;
+    const uint32_t tile = p.many ? rows_of_many(head_dim) : 16, slots = p.many ? 512 : 1024;
+    p.row_tiles = (uint32_t)((rows + tile - 1) / tile);
     const uint64_t others = (uint64_t)batch * kv_heads * p.row_tiles;
-    const uint64_t want = others >= 1024 ? 1 : (1024 + others - 1) / others;
+    const uint64_t want = others >= slots ? 1 : (slots + others - 1) / others;
     const uint64_t tokens = (max_length + want - 1) / want;
     p.chunk = (uint32_t)(tokens <= 256 ? 256 : (tokens + 255) / 256 * 256);
     p.splits = max_length <= p.chunk ? 1 : (max_length + p.chunk - 1) / p.chunk;
     return p;
 }
 
-template <int DT, int D> void launch(const Attend &a, hipStream_t s)
+template <int DT, int D> void launch(const Attend &a, bool many, hipStream_t s)
 {
-    attend_kernel<DT, D><<<dim3(a.splits * a.c.batch * a.row_tiles, a.c.heads), 256, 0, s>>>(a);
+    const uint32_t tiles = a.splits * a.c.batch * a.row_tiles;
+    if (many) attend_many_kernel<DT, D, D == 256 ? 1 : 2><<<(tiles * a.c.heads + 7) / 8 * 8, 256, 0, s>>>(a);
+    else attend_kernel<DT, D><<<dim3(tiles, a.c.heads), 256, 0, s>>>(a);
     if (a.splits > 1) attend_join_kernel<DT, D><<<dim3(a.c.n_tokens, a.q_heads), 64, 0, s>>>(a);
 }
-template <int DT> void launch(const Attend &a, hipStream_t s)
+template <int DT> void launch(const Attend &a, bool many, hipStream_t s)
 {
-    if (a.c.head_dim == 64) launch<DT, 64>(a, s);
-    else if (a.c.head_dim == 128) launch<DT, 128>(a, s);
-    else launch<DT, 256>(a, s);
+    if (a.c.head_dim == 64) launch<DT, 64>(a, many, s);
+    else if (a.c.head_dim == 128) launch<DT, 128>(a, many, s);
+    else launch<DT, 256>(a, many, s);
 }
 
 // one call's arguments; 0 = none of its kernels can count with these
@@ -354,7 +638,7 @@ extern "C" {
 size_t enec_cache_attention_workspace(const enec_cache *cache, uint32_t batch, uint32_t n_tokens, uint32_t q_heads, uint32_t max_new, uint32_t max_length)
 {
     if (!cache || !shape_ok(cache, batch, n_tokens, q_heads, max_new, max_length) || batch == 0 || n_tokens == 0 || max_new == 0) return 0;
-    const Plan p = plan_of(batch, cache->kv_heads, q_heads / cache->kv_heads, max_new, max_length);
+    const Plan p = plan_of(batch, cache->kv_heads, q_heads / cache->kv_heads, cache->head_dim, max_new, max_length);
     return p.splits == 1 ? 0 : (size_t)p.splits * n_tokens * q_heads * (cache->head_dim + 2) * sizeof(float);
 }
 
@@ -369,8 +653,8 @@ int enec_cache_attention(const enec_cache *cache, const enec_cache_batch *batch,
     if (a.c.batch == 0 || a.c.n_tokens == 0) return ENEC_OK;
     if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 1) || max_new == 0) return ENEC_E_ARG;
     const uint32_t group = q_heads / a.c.heads;
-    const Plan p = plan_of(a.c.batch, a.c.heads, group, max_new, max_length);
-    if ((uint64_t)p.splits * a.c.batch * p.row_tiles > 0x7FFFFFFFu) return ENEC_E_ARG;
+    const Plan p = plan_of(a.c.batch, a.c.heads, group, a.c.head_dim, max_new, max_length);
+    if ((uint64_t)p.splits * a.c.batch * p.row_tiles > 0x3FFFFFFFu / a.c.heads) return ENEC_E_ARG;
     const size_t need = enec_cache_attention_workspace(cache, a.c.batch, a.c.n_tokens, q_heads, max_new, max_length);
     if (workspace_bytes < need || (need && !workspace)) return ENEC_E_CAPACITY;
     if (need && ((uintptr_t)workspace & 15)) return ENEC_E_ARG;
@@ -380,8 +664,8 @@ int enec_cache_attention(const enec_cache *cache, const enec_cache_batch *batch,
     a.max_new = max_new, a.max_length = max_length, a.chunk = p.chunk, a.splits = p.splits, a.row_tiles = p.row_tiles;
     a.part = static_cast<float *>(workspace);
     a.part_stat = a.part + (size_t)p.splits * a.c.n_tokens * q_heads * a.c.head_dim;
-    if (dtype == ENEC_BF16) launch<BF16>(a, (hipStream_t)stream);
-    else launch<FP16>(a, (hipStream_t)stream);
+    if (dtype == ENEC_BF16) launch<BF16>(a, p.many, (hipStream_t)stream);
+    else launch<FP16>(a, p.many, (hipStream_t)stream);
     return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
 }
 

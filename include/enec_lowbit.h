@@ -118,7 +118,7 @@ int enec_cache_read(const enec_cache *cache, const enec_cache_batch *batch, void
  *   q, out  DEVICE, n_tokens x q_heads x head_dim values (bf16 or fp16), token and head strides; must not overlap
  *   q_heads a multiple of kv_heads
  *   max_new, max_length  HOST: no sequence has more tokens in the call, or more in all (they shape the launch)
- *   scale   usually head_dim^-1/2
+ *   scale   above zero, usually head_dim^-1/2
  *   workspace  DEVICE, 16-byte aligned, or NULL if workspace_bytes = enec_cache_attention_workspace(...) is 0
  * Scores, softmax and sums are held in 32 bits; the probabilities are rounded to bf16 for the product with v (to the sum of two
  * bf16 numbers for fp16 tensors). */

@@ -26,15 +26,15 @@ __device__ __forceinline__ Sequence sequence_of(const Attend &a, uint32_t b)
     return s;
 }
 
+// The largest of four lanes sixteen apart.  The exchanges swap rows of lanes of two registers that hold the same; as instructions of their own, since the
+// compiler takes the two results for equal.
 __device__ __forceinline__ float over_groups_max(float v)
 {
-    v = fmaxf(v, __shfl_xor(v, 16));
-    return fmaxf(v, __shfl_xor(v, 32));
-}
-__device__ __forceinline__ float over_groups_sum(float v)
-{
-    v += __shfl_xor(v, 16);
-    return v + __shfl_xor(v, 32);
+    float a = v, b = v;
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+    a = b = fmaxf(a, b);
+    asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
+    return fmaxf(a, b);
 }
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
 
@@ -61,226 +61,26 @@ template <int DT> __device__ __forceinline__ u32x4 values8(uint32_t lo, uint32_t
     return r;
 }
 
-// bytes of a word of codes that are NaN, as 0xFF
+// bytes of a word of codes that are NaN, as 0xFF; whether there are any
 __device__ __forceinline__ uint32_t nan_bytes(uint32_t w)
 {
     uint32_t r = 0;
     for (int k = 0; k < 4; ++k) r |= (w >> (8 * k) & 0x7F) == 0x7F ? 255u << (8 * k) : 0;
     return r;
 }
+__device__ __forceinline__ uint32_t any_nan(uint32_t w) { return ((w & 0x7F7F7F7Fu) + 0x01010101u) & 0x80808080u; }
 
-// Scores are computed transposed: tokens are the rows of the matrix instruction (left operand: keys), query rows its columns.  A lane then
-// holds scores of one query row, and with the tokens of a tile of 64 dealt out as
-//     instruction j, row r: token 16 (r / 4) + 4 j + r mod 4
-// lane group g has tokens 16 g ... 16 g + 15, which is what the product with the values wants of it as right operand: weights
-// go from one product to the next without leaving their lane.  Left operand there are the transposed values, 16 dimensions x
-// 16 consecutive tokens a lane: one run of 16 bytes.  A run of 16 keys' bytes is two steps of the first product, whose order of
-// dimensions is the same for the queries.
-// Query rows are pairs of (token, head of the key head's group), 16 to a workgroup; its four waves take every fourth tile and
-// meet in LDS.
-template <int DT, int D>
-__global__ void __launch_bounds__(256) attend_kernel(Attend a)
+__device__ __forceinline__ void copy_to_lds(const uint8_t *from, uint8_t *to)
 {
-    constexpr int KC = D / 64, VT = D / 16;
-    __shared__ float stat[2][4][16];
-    __shared__ f32x4 sums[4][16][17];
-    const Pages &c = a.c;
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, col = lane & 15;
-    const uint32_t split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits, b = rest / a.row_tiles, head = blockIdx.y;
-    const Sequence s = sequence_of(a, b);
-    if (!s.good) {
-        complain(c);
-        return;
-    }
-    const uint32_t rows = s.count * a.group.by, row0 = rest % a.row_tiles * 16;
-    if (row0 >= rows) return;
-    const int32_t begin = s.length - (int32_t)s.count;
-    const uint32_t row = row0 + col;
-    const uint32_t token = quotient(row, a.group), q_head = head * a.group.by + (row - token * a.group.by);
-    const int32_t limit = row < rows ? begin + (int32_t)token : -1;           // the last position that the row sees
-    const int32_t least = begin + (int32_t)quotient(row0, a.group);           // of all rows here
-    const uint32_t last_row = row0 + 15 < rows ? row0 + 15 : rows - 1;
-    const int32_t end = begin + (int32_t)quotient(last_row, a.group) + 1;     // none sees a position from here on
-    const int32_t from = (int32_t)(split * a.chunk), to = end - from < (int32_t)a.chunk ? end : from + (int32_t)a.chunk;
-    if (split > 0 && from >= to) return;
-
-    u32x4 q[KC][2] = {};
-    if (row < rows) {
-        const uint16_t *p = static_cast<const uint16_t *>(a.q) + (size_t)(s.start + token) * a.q_token + (size_t)q_head * a.q_head;
-#pragma unroll
-        for (int i = 0; i < KC; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) q[i][h] = *reinterpret_cast<const u32x4_a2 *>(p + 64 * i + 16 * g + 8 * h);
-    }
-    f32x4 o[VT] = {};
-    float most = -__builtin_inff(), total = 0;
-    const uint32_t page_mask = (1u << c.log_page) - 1;
-    const size_t head_values = (size_t)D << c.log_page;
-    const int32_t *table = c.table + (size_t)b * c.table_stride;
-
-    for (int32_t t0 = from + 64 * (int32_t)wave; t0 < to; t0 += 256) {
-        // the pages of the 16 tokens that this lane loads keys of, and of those that it loads values of
-        const int32_t tk = t0 + 16 * (int32_t)(col >> 2), tv = t0 + 16 * (int32_t)g;
-        int32_t pk = tk < s.length ? table[tk >> c.log_page] : -1, pv = tv < s.length ? table[tv >> c.log_page] : -1;
-        if ((uint32_t)pk >= c.n_pages) {
-            if (tk < s.length) complain(c);
-            pk = -1;
-        }
-        if ((uint32_t)pv >= c.n_pages) pv = -1;
-        const uint8_t *kp = c.k_codes + ((size_t)(uint32_t)(pk < 0 ? 0 : pk) * c.heads + head) * head_values + (size_t)((tk & page_mask) + (col & 3)) * D + 16 * g;
-        const uint8_t *vp = c.v_codes + ((size_t)(uint32_t)(pv < 0 ? 0 : pv) * c.heads + head) * head_values + ((size_t)col << c.log_page) + (tv & page_mask);
-        u32x4 k[4][KC] = {}, v[VT] = {};
-        float ks = 0, vs = 0;
-        if (pk >= 0) {
-#pragma unroll
-            for (int j = 0; j < 4; ++j)
-#pragma unroll
-                for (int i = 0; i < KC; ++i) k[j][i] = *reinterpret_cast<const u32x4 *>(kp + 4 * j * D + 64 * i);
-        }
-        if (pv >= 0) {
-            ks = power_of(c.k_scales[(size_t)pv * c.heads + head]);
-            vs = power_of(c.v_scales[(size_t)pv * c.heads + head]);
-#pragma unroll
-            for (int i = 0; i < VT; ++i) v[i] = *reinterpret_cast<const u32x4 *>(vp + ((size_t)(16 * i) << c.log_page));
-        }
-        f32x4 x[4] = {};
-#pragma unroll
-        for (int i = 0; i < KC; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) x[j] = mfma16<DT>(values8<DT>(k[j][i][2 * h], k[j][i][2 * h + 1], 1.0f), q[i][h], x[j]);
-        // what a row does not see takes no part, whatever its codes are
-        ks *= a.scale;
-        float high = -__builtin_inff();
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                x[j][i] = pv >= 0 && tv + 4 * j + i <= limit ? x[j][i] * ks : -__builtin_inff();
-                high = fmaxf(high, x[j][i]);
-            }
-        const float now = fmaxf(most, over_groups_max(high)), base = now == -__builtin_inff() ? 0.0f : now;
-        const float fade = exp2_of(most - base);
-        most = now;
-        total *= fade;
-#pragma unroll
-        for (int i = 0; i < VT; ++i) o[i] *= fade;
-        float w[16];
-#pragma unroll
-        for (int j = 0; j < 4; ++j)
-#pragma unroll
-            for (int i = 0; i < 4; ++i) {
-                w[4 * j + i] = exp2_of(x[j][i] - base);
-                total += w[4 * j + i];
-            }
-        // codes behind the sequence's end are anyone's
-        if (t0 + 64 > s.length) {
-            const int32_t n = s.length - tv;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const int32_t here = n - 4 * j;
-                const uint32_t mask = here >= 4 ? 0xFFFFFFFFu : here <= 0 ? 0 : (1u << (8 * here)) - 1;
-#pragma unroll
-                for (int i = 0; i < VT; ++i) v[i][j] &= mask;
-            }
-        }
-        // A value that is NaN has to reach the rows that see it, and no other: 0 * NaN would.  Where some rows do not see the whole tile,
-        // such values are taken out and the rows that see one are told.
-        if (t0 + 63 > least) {
-            uint32_t any = 0;
-#pragma unroll
-            for (int i = 0; i < VT; ++i)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) any |= nan_bytes(v[i][j]);
-            if (__any(any)) {
-                u32x4 sees[2];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const int32_t at = tv + 8 * h + 2 * j;
-                        sees[h][j] = (at <= limit ? 0x3F80u : 0) | (at + 1 <= limit ? 0x3F800000u : 0);
-                    }
-#pragma unroll
-                for (int i = 0; i < VT; ++i) {
-                    f32x4 seen = {};
-                    u32x4 bad;
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const uint32_t n = nan_bytes(v[i][j]);
-                        v[i][j] &= ~n;
-                        bad[j] = n & 0x38383838u;            // 1.0 as E4M3
-                    }
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) seen = mfma16<BF16>(values8<BF16>(bad[2 * h], bad[2 * h + 1], 1.0f), sees[h], seen);
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[i][e] = seen[e] > 0 ? __builtin_nanf("") : o[i][e];
-                }
-            }
-        }
-        u32x4 p[2], rest_of[2];
-#pragma unroll
-        for (int h = 0; h < 2; ++h)
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                const float lo = w[8 * h + 2 * j], hi = w[8 * h + 2 * j + 1];
-                p[h][j] = pack2<BF16>(lo, hi);
-                if constexpr (DT == FP16) {
-                    const f32x2 r = unpack2<BF16>(p[h][j]);
-                    rest_of[h][j] = pack2<BF16>(lo - r[0], hi - r[1]);
-                }
-            }
-#pragma unroll
-        for (int i = 0; i < VT; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h) {
-                const u32x4 values = values8<BF16>(v[i][2 * h], v[i][2 * h + 1], vs);
-                o[i] = mfma16<BF16>(values, p[h], o[i]);
-                if constexpr (DT == FP16) o[i] = mfma16<BF16>(values, rest_of[h], o[i]);
-            }
-    }
-
-    // the waves' sums, in their order
-    total = over_groups_sum(total);
-    if (g == 0) stat[0][wave][col] = most, stat[1][wave][col] = total;
-    __syncthreads();
-    float top = stat[0][0][col];
-    for (int i = 1; i < 4; ++i) top = fmaxf(top, stat[0][i][col]);
-    const float mine = most == -__builtin_inff() ? 0.0f : exp2_of(most - top);
-    // thread: row r of the tile, four dimensions of every 64
-    const uint32_t r = threadIdx.x >> 4, d4 = threadIdx.x & 15;
-    float row_top = stat[0][0][r], row_total = 0;
-    for (int i = 1; i < 4; ++i) row_top = fmaxf(row_top, stat[0][i][r]);
-    for (int i = 0; i < 4; ++i) row_total += stat[0][i][r] == -__builtin_inff() ? 0.0f : stat[1][i][r] * exp2_of(stat[0][i][r] - row_top);
-    const uint32_t out_row = row0 + r, out_token = quotient(out_row, a.group), out_head = head * a.group.by + (out_row - out_token * a.group.by);
-#pragma unroll
-    for (int i = 0; i < KC; ++i) {
-        if (i) __syncthreads();
-#pragma unroll
-        for (int e = 0; e < 4; ++e) sums[wave][col][4 * e + g] = o[4 * i + e] * mine;
-        __syncthreads();
-        f32x4 v = sums[0][r][d4];
-        for (int w = 1; w < 4; ++w) v += sums[w][r][d4];
-        if (out_row >= rows) continue;
-        const uint32_t d = 64 * i + 4 * d4;
-        if (a.splits == 1) {
-            const float by = row_total == 0 ? 0.0f : 1.0f / row_total;
-            uint16_t *p = static_cast<uint16_t *>(a.out) + (size_t)(s.start + out_token) * a.out_token + (size_t)out_head * a.out_head + d;
-            *reinterpret_cast<u32x2_a2 *>(p) = u32x2{pack2<DT>(v[0] * by, v[1] * by), pack2<DT>(v[2] * by, v[3] * by)};
-        } else {
-            const size_t at = ((size_t)split * c.n_tokens + s.start + out_token) * a.q_heads + out_head;
-            *reinterpret_cast<f32x4 *>(a.part + at * D + d) = v;
-            if (i == 0 && d4 == 0) *reinterpret_cast<f32x2 *>(a.part_stat + 2 * at) = f32x2{row_top, row_total};
-        }
-    }
+    using from_t = const __attribute__((address_space(1))) void *;
+    using to_t = __attribute__((address_space(3))) void *;
+    __builtin_amdgcn_global_load_lds((from_t)from, (to_t)to, 16, 0, 0);
 }
 
-// ---- many rows ---------------------------------------------------------------------------------------------------------
-
-// Keys and values of a tile of 64 tokens in LDS, two tiles in turn, as codes: a token's keys are a row of D / 16 chunks of 16 bytes, a
-// dimension's values a row of four.  Chunk i of a row lies at place i ^ turn: the sixteen lanes whose 16 bytes are read in one go (rows {0-3, 12-15} of a
-// lane group and rows {4-11} of its neighbour) find theirs in sixteen different places of 256 bytes.
+// ---- a tile of 64 tokens ----------------------------------------------------------------------------------------------------
+// Keys and values of a tile lie in LDS as codes: a token's keys are a row of D / 16 chunks of 16 bytes, a dimension's values a row of four.
+// Chunk i of a row lies at place i ^ turn: the sixteen lanes whose 16 bytes are read in one go (rows {0-3, 12-15} of a lane group and rows {4-11} of
+// its neighbour) find theirs in sixteen different places of 256 bytes.
 template <int D> __device__ __forceinline__ uint32_t key_turn(uint32_t token)
 {
     const uint32_t half = token >> 5 & 1;
@@ -290,264 +90,465 @@ template <int D> __device__ __forceinline__ uint32_t key_turn(uint32_t token)
 }
 __device__ __forceinline__ uint32_t value_turn(uint32_t dim) { return 2 * (dim >> 3 & 1); }
 
-// The same arrangement as above, with 16 NT query rows to each of the four waves, which share the tiles: a wave has all of them, so nothing is
-// joined in the end.  The memory unit copies the codes of a tile into LDS while the one before is worked on.  Every wave makes
-// 16-bit values of the codes by itself: a conversion makes two of them in the time of any vector instruction, and NT tiles of rows use each.
-template <int DT, int D, int NT>
-__global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
+template <int D> struct Tile {
+    uint8_t keys[64 * D], values[64 * D];
+};
+
+// The pages of a tile's four runs of 16 tokens, the same for all lanes; -1: none.
+struct Runs {
+    int32_t page[4];
+};
+struct Cached {
+    const Pages *c;
+    const __attribute__((address_space(4))) int32_t *table;       // (read through the scalar cache: it does not change under the kernel)
+    int32_t length;
+    uint32_t head;
+    bool bad;                                                      // a page number outside the cache was met
+
+    __device__ __forceinline__ void table_entries(int32_t t0, int32_t (&raw)[4]) const
+    {
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const int32_t t = t0 + 16 * r < length ? t0 + 16 * r : length - 1;        // (a length of zero has no tiles)
+            raw[r] = table[t >> c->log_page];
+        }
+    }
+    __device__ __forceinline__ Runs runs(int32_t t0, const int32_t (&raw)[4])
+    {
+        Runs p;
+#pragma unroll
+        for (int r = 0; r < 4; ++r) {
+            const bool in = (uint32_t)raw[r] < c->n_pages, there = t0 + 16 * r < length;
+            bad |= there && !in;
+            p.page[r] = in && there ? raw[r] : -1;
+        }
+        return p;
+    }
+};
+__device__ __forceinline__ int32_t select4(const Runs &p, uint32_t i)
 {
-    constexpr int KC = D / 64, VT = D / 16, COPIES = D / 64, ROWS = 64 * NT;
-    __shared__ __attribute__((aligned(16))) uint8_t keys[2][64 * D], values[2][64 * D];
+    const int32_t lo = i & 1 ? p.page[1] : p.page[0], hi = i & 1 ? p.page[3] : p.page[2];
+    return i & 2 ? hi : lo;
+}
+
+// Copies part `part` of `parts` of a tile into LDS, 1024 bytes an instruction: PARTS waves share it, or one takes all.  No page: page 0, which exists, and
+// whose codes are not looked at.
+template <int D, int PARTS> __device__ __forceinline__ void copy_tile(const Cached &s, const Runs &p, int32_t t0, Tile<D> &to, uint32_t part)
+{
+    constexpr int COPIES = D / 16 / PARTS, TOKENS = 1024 / D;             // of keys, and as many of values; tokens of one
+    const Pages &c = *s.c;
+    const uint32_t lane = threadIdx.x & 63, mask = (1u << c.log_page) - 1;
+    const size_t head_values = (size_t)D << c.log_page;
+#pragma unroll
+    for (int r = 0; r < COPIES; ++r) {
+        const uint32_t n = part * COPIES + r, first = n * TOKENS;                           // TOKENS divides 16, so it is of one run
+        const int32_t page = PARTS == 1 ? p.page[first / 16 % 4] : select4(p, first / 16);
+        const uint32_t token = first + lane / (D / 16), chunk = lane % (D / 16) ^ key_turn<D>(token);
+        const uint8_t *k = c.k_codes + ((size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + s.head) * head_values + (size_t)((t0 + first) & mask) * D;
+        copy_to_lds(k + (lane / (D / 16) * D + 16 * chunk), to.keys + n * 1024);
+    }
+    const uint32_t run = (lane & 3) ^ value_turn(lane >> 2);
+    const int32_t page = select4(p, run);
+    const uint8_t *v = c.v_codes + ((size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + s.head) * head_values + ((t0 + 16 * run) & mask);
+#pragma unroll
+    for (int r = 0; r < COPIES; ++r) {
+        const uint32_t n = part * COPIES + r;
+        copy_to_lds(v + ((size_t)(n * 16 + (lane >> 2)) << c.log_page), to.values + n * 1024);
+    }
+}
+
+// Scores are computed transposed: tokens are the rows of the matrix instruction (left operand: keys), query rows its columns.  A lane then
+// holds scores of one query row, and with the tokens of a tile dealt out as
+//     instruction j, row r: token 16 (r / 4) + 4 j + r mod 4
+// lane group g has tokens 16 g ... 16 g + 15, which is what the product with the values wants of it as right operand: weights
+// go from one product to the next without leaving their lane.  Left operand there are the transposed values, 16 dimensions x
+// 16 consecutive tokens a lane: one run of 16 bytes.  A run of 16 keys' bytes is two steps of the first product, whose order of
+// dimensions is the same for the queries.
+// Query rows are pairs of (token, head of the key head's group).  A wave has 16 NT of them.
+template <int DT, int D, int NT> struct Rows {
+    static constexpr int KC = D / 64, VT = D / 16;
+    u32x4 q[NT][KC][2];
+    // The weights' sum is a product too, with a row of ones: every register of `total` has it, and it is that of the rounded weights, whose
+    // errors the division takes out again where one weight outdoes the others.
+    f32x4 o[NT][VT], total[NT];
+    float most[NT];
+    int32_t limit[NT];                  // the last position that the row sees; -1: nothing
+    int32_t least;                      // of all of the wave's rows: every tile that ends there is seen whole
+    uint32_t key_at[KC], value_at;
+
+    __device__ __forceinline__ void begin(const Attend &a, const Sequence &s, uint32_t row0, uint32_t rows, uint32_t head)
+    {
+        const uint32_t lane = threadIdx.x & 63, g = lane >> 4, col = lane & 15;
+        const int32_t first = s.length - (int32_t)s.count;
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            const uint32_t row = row0 + 16 * n + col, token = quotient(row, a.group), q_head = head * a.group.by + (row - token * a.group.by);
+            limit[n] = row < rows ? first + (int32_t)token : -1;
+            const uint16_t *p = static_cast<const uint16_t *>(a.q) + (size_t)(s.start + token) * a.q_token + (size_t)q_head * a.q_head;
+#pragma unroll
+            for (int i = 0; i < KC; ++i)
+#pragma unroll
+                for (int h = 0; h < 2; ++h) q[n][i][h] = row < rows ? *reinterpret_cast<const u32x4_a2 *>(p + 64 * i + 16 * g + 8 * h) : u32x4{};
+#pragma unroll
+            for (int i = 0; i < VT; ++i) o[n][i] = f32x4{};
+            total[n] = f32x4{};
+            most[n] = -__builtin_inff();
+        }
+        least = row0 < rows ? first + (int32_t)quotient(row0, a.group) : -1;
+#pragma unroll
+        for (int i = 0; i < KC; ++i) {
+            const uint32_t t = 16 * (col >> 2) + (col & 3);               // (+ 4 j, which does not turn)
+            key_at[i] = t * D + (((4 * i + g) ^ key_turn<D>(t)) << 4);
+        }
+        value_at = col * 64 + ((g ^ value_turn(col)) << 4);
+    }
+
+    // page, ks, vs: of the lane group's run.  by: its keys' scale, the call's and log2 e
+    __device__ __forceinline__ void step(const Tile<D> &tile, int32_t t0, int32_t length, bool whole_pages, int32_t page, float by, float vs)
+    {
+        const uint32_t g = threadIdx.x >> 4 & 3;
+        const int32_t tv = t0 + 16 * (int32_t)g;
+        f32x4 x[NT][4] = {};
+#pragma unroll
+        for (int i = 0; i < KC; ++i) {
+            u32x4 k[4];
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const u32x4 *>(tile.keys + key_at[i] + 4 * j * D);
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const u32x4 v = values8<DT>(k[j][2 * h], k[j][2 * h + 1], 1.0f);
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) x[n][j] = mfma16<DT>(v, q[n][i][h], x[n][j]);
+                }
+        }
+        // what a row does not see takes no part, whatever its codes are
+        const bool partial = t0 + 63 > least || t0 + 64 > length || !whole_pages;
+        if (partial) {
+#pragma unroll
+            for (int n = 0; n < NT; ++n) {
+                const int32_t sees = page >= 0 ? limit[n] - tv : -1;
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int i = 0; i < 4; ++i) x[n][j][i] = 4 * j + i <= sees ? x[n][j][i] * by : -__builtin_inff();
+            }
+            by = 1.0f;
+        }
+        u32x4 p[NT][2], rest_of[NT][2];
+#pragma unroll
+        for (int n = 0; n < NT; ++n) {
+            float high = fmaxf(fmaxf(x[n][0][0], x[n][0][1]), fmaxf(x[n][0][2], x[n][0][3]));
+#pragma unroll
+            for (int j = 1; j < 4; ++j) high = fmaxf(high, fmaxf(fmaxf(x[n][j][0], x[n][j][1]), fmaxf(x[n][j][2], x[n][j][3])));
+            high = over_groups_max(high * by);
+            // Weights are taken relative to a maximum that may lag behind by up to 2^8, which costs nothing in 32 bits: most tiles need no
+            // change of what is summed already.
+            if (__any(high > most[n] + 8.0f)) {
+                const float now = fmaxf(most[n], high), fade = now == -__builtin_inff() ? 1.0f : exp2_of(most[n] - now);
+                most[n] = now;
+                total[n] *= fade;
+#pragma unroll
+                for (int i = 0; i < VT; ++i) o[n][i] *= fade;
+            }
+            const float base = most[n] == -__builtin_inff() ? 0.0f : most[n];
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const float lo = exp2_of(__builtin_fmaf(x[n][2 * h + j / 2][2 * (j & 1)], by, -base));
+                    const float hi = exp2_of(__builtin_fmaf(x[n][2 * h + j / 2][2 * (j & 1) + 1], by, -base));
+                    p[n][h][j] = pack2<BF16>(lo, hi);
+                    if constexpr (DT == FP16) {
+                        const f32x2 r = unpack2<BF16>(p[n][h][j]);
+                        rest_of[n][h][j] = pack2<BF16>(lo - r[0], hi - r[1]);
+                    }
+                }
+        }
+        const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                total[n] = mfma16<BF16>(ones, p[n][h], total[n]);
+                if constexpr (DT == FP16) total[n] = mfma16<BF16>(ones, rest_of[n][h], total[n]);
+            }
+        auto add = [&](int i, const u32x4 &v) {
+#pragma unroll
+            for (int h = 0; h < 2; ++h) {
+                const u32x4 vv = values8<BF16>(v[2 * h], v[2 * h + 1], vs);
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    o[n][i] = mfma16<BF16>(vv, p[n][h], o[n][i]);
+                    if constexpr (DT == FP16) o[n][i] = mfma16<BF16>(vv, rest_of[n][h], o[n][i]);
+                }
+            }
+        };
+        if (!partial) {
+#pragma unroll
+            for (int i = 0; i < VT; ++i) add(i, *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024));
+            return;
+        }
+        // Bytes behind the sequence's end and of no page are anyone's.  A value that is NaN has to reach the rows that see it, and no other: 0 * NaN would.
+        // Such values are taken out, and the rows that see one are told.
+        u32x4 mask;
+#pragma unroll
+        for (int j = 0; j < 4; ++j) {
+            const int32_t here = page >= 0 ? length - tv - 4 * j : 0;
+            mask[j] = here <= 0 ? 0 : here >= 4 ? ~0u : (1u << (8 * here)) - 1;
+        }
+        uint32_t any = 0;
+#pragma unroll
+        for (int i = 0; i < VT; ++i) {
+            u32x4 v = *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024);
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                v[j] &= mask[j];
+                any |= any_nan(v[j]);
+            }
+        }
+        const bool careful = __any(any);
+#pragma unroll
+        for (int i = 0; i < VT; ++i) {
+            u32x4 v = *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024), bad;
+            v &= mask;
+            if (careful) {
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t nan = nan_bytes(v[j]);
+                    v[j] &= ~nan;
+                    bad[j] = nan & 0x38383838u;              // 1.0 as E4M3
+                }
+#pragma unroll
+                for (int n = 0; n < NT; ++n) {
+                    f32x4 seen = {};
+                    const int32_t sees = limit[n] - tv;
+#pragma unroll
+                    for (int h = 0; h < 2; ++h) {
+                        u32x4 visible;
+#pragma unroll
+                        for (int j = 0; j < 4; ++j) visible[j] = (8 * h + 2 * j <= sees ? 0x3F80u : 0) | (8 * h + 2 * j + 1 <= sees ? 0x3F800000u : 0);
+                        seen = mfma16<BF16>(values8<BF16>(bad[2 * h], bad[2 * h + 1], 1.0f), visible, seen);
+                    }
+#pragma unroll
+                    for (int e = 0; e < 4; ++e) o[n][i][e] = seen[e] > 0 ? __builtin_nanf("") : o[n][i][e];
+                }
+            }
+            add(i, v);
+        }
+    }
+};
+
+// what both kernels know of a workgroup's rows: `end` is where the view of the last of them ends
+struct Span {
+    uint32_t rows;
+    int32_t from, to, end;
+};
+__device__ __forceinline__ Span span_of(const Attend &a, const Sequence &s, uint32_t first_row, uint32_t count, uint32_t split)
+{
+    Span v;
+    v.rows = s.count * a.group.by;
+    const uint32_t last = first_row + count < v.rows ? first_row + count - 1 : v.rows - 1;
+    v.end = s.length - (int32_t)s.count + (int32_t)quotient(last, a.group) + 1;
+    v.from = (int32_t)(split * a.chunk);
+    v.to = v.end - v.from < (int32_t)a.chunk ? v.end : v.from + (int32_t)a.chunk;
+    return v;
+}
+__device__ __forceinline__ Cached cached_of(const Attend &a, const Sequence &s, uint32_t b, uint32_t head)
+{
+    return {&a.c, (const __attribute__((address_space(4))) int32_t *)(a.c.table + (size_t)b * a.c.table_stride), s.length, head, false};
+}
+
+// ---- few rows: the card reads the cache, everything else is small ----------------------------------------------------------------
+
+// A workgroup has 16 NT rows; its WAVES waves take tiles in turn and meet in LDS in the end.  Each wave copies its own tiles, one ahead, and waits for
+// its own copies only: no barrier until the end.
+template <int DT, int D, int NT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, D == 64 ? 2 : 1) attend_few_kernel(Attend a)
+{
+    constexpr int KC = D / 64, COPIES = D / 8;
+    extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
     const Pages &c = a.c;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
-    // Workgroups are dealt out to the eight dies one by one.  Each die takes a run of (sequence, head)s, whose keys and values stay in its cache,
-    // and of their rows the last ones first: they see most.
-    const uint32_t groups = c.batch * c.heads, each = a.row_tiles * a.splits, total_tiles = groups * each, per_die = (total_tiles + 7) / 8;
-    const uint32_t tile = blockIdx.x % 8 * per_die + blockIdx.x / 8;
-    if (blockIdx.x / 8 >= per_die || tile >= total_tiles) return;
-    const uint32_t group = tile / each, within = tile % each, b = group / c.heads, head = group % c.heads;
-    const uint32_t split = within % a.splits, row_tile = a.row_tiles - 1 - within / a.splits;
+    const uint32_t split = blockIdx.x % a.splits, rest = blockIdx.x / a.splits, b = rest / a.row_tiles, head = blockIdx.y, row0 = rest % a.row_tiles * (16 * NT);
     const Sequence s = sequence_of(a, b);
     if (!s.good) {
         complain(c);
         return;
     }
-    const uint32_t rows = s.count * a.group.by, first_row = row_tile * ROWS;
-    if (first_row >= rows) return;
-    const int32_t begin = s.length - (int32_t)s.count;
-    const uint32_t last_row = first_row + ROWS < rows ? first_row + ROWS - 1 : rows - 1;
-    const int32_t end = begin + (int32_t)quotient(last_row, a.group) + 1;     // no row here sees a position from here on
-    const int32_t from = (int32_t)(split * a.chunk), to = end - from < (int32_t)a.chunk ? end : from + (int32_t)a.chunk;
-    if (split > 0 && from >= to) return;
+    if (row0 >= s.count * a.group.by) return;
+    const Span v = span_of(a, s, row0, 16 * NT, split);
+    if (split > 0 && v.from >= v.to) return;
+    Cached cache = cached_of(a, s, b, head);
+    Tile<D> *tiles = reinterpret_cast<Tile<D> *>(shared) + 2 * wave;
+    auto scale_bytes = [&](int32_t page, uint32_t &k, uint32_t &w) {
+        const size_t at = (size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + head;
+        k = c.k_scales[at], w = c.v_scales[at];
+    };
+    const int32_t first = v.from + 64 * (int32_t)wave;
+    constexpr int32_t STEP = 64 * WAVES;
+    int32_t raw[4], page = -1, next_page = -1;
+    uint32_t kb = 0, vb = 0, next_kb = 0, next_vb = 0;
+    bool whole = true, next_whole = true;
+    auto ask = [&](int32_t t0, Tile<D> &to, int32_t &pg, bool &all, uint32_t &k, uint32_t &w) {
+        const Runs p = cache.runs(t0, raw);
+        all = (p.page[0] | p.page[1] | p.page[2] | p.page[3]) >= 0;
+        copy_tile<D, 1>(cache, p, t0, to, 0);
+        pg = select4(p, g);
+        scale_bytes(pg, k, w);
+    };
+    if (first < v.to) {
+        cache.table_entries(first, raw);
+        ask(first, tiles[0], page, whole, kb, vb);
+        cache.table_entries(first + STEP, raw);
+    }
+    Rows<DT, D, NT> r;
+    r.begin(a, s, row0, v.rows, head);
+    int buffer = 0;
+    for (int32_t t0 = first; t0 < v.to; t0 += STEP, buffer ^= 1) {
+        __builtin_amdgcn_sched_barrier(0);
+        if (t0 + STEP < v.to) {
+            ask(t0 + STEP, tiles[buffer ^ 1], next_page, next_whole, next_kb, next_vb);
+            cache.table_entries(t0 + 2 * STEP, raw);
+            __builtin_amdgcn_sched_barrier(0);
+            // copies and loads come back in their order: with as many left as copies of the next tile were issued, this tile's are in LDS
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES < 63 ? COPIES : 63) : "memory");
+        } else {
+            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+        }
+        __builtin_amdgcn_sched_barrier(0);
+        r.step(tiles[buffer], t0, s.length, whole, page, power_of(kb) * a.scale, power_of(vb));
+        // (its codes have been read before the tile after the next one is copied there)
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+        page = next_page, whole = next_whole, kb = next_kb, vb = next_vb;
+    }
+    if (cache.bad && lane == 0) complain(c);
 
-    const uint32_t row0 = first_row + wave * (16 * NT);
-    uint32_t token[NT], q_head[NT];
-    int32_t limit[NT];                                                        // the last position that the row sees
-    u32x4 q[NT][KC][2] = {};
+    // the waves' sums, in their order; the tiles' LDS is free now
+    __syncthreads();
+    float *most_of = reinterpret_cast<float *>(shared), *total_of = most_of + WAVES * 16 * NT;
+    f32x4 *sums = reinterpret_cast<f32x4 *>(shared + 2 * WAVES * 16 * NT * sizeof(float));       // [WAVES][16 NT][17]
+    if (g == 0) {
+#pragma unroll
+        for (int n = 0; n < NT; ++n) most_of[(wave * NT + n) * 16 + col] = r.most[n], total_of[(wave * NT + n) * 16 + col] = r.total[n][0];
+    }
+    __syncthreads();
+    float mine[NT];
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const uint32_t row = row0 + 16 * n + col;
-        token[n] = quotient(row, a.group), q_head[n] = head * a.group.by + (row - token[n] * a.group.by);
-        limit[n] = row < rows ? begin + (int32_t)token[n] : -1;
-        if (row < rows) {
-            const uint16_t *p = static_cast<const uint16_t *>(a.q) + (size_t)(s.start + token[n]) * a.q_token + (size_t)q_head[n] * a.q_head;
-#pragma unroll
-            for (int i = 0; i < KC; ++i)
-#pragma unroll
-                for (int h = 0; h < 2; ++h) q[n][i][h] = *reinterpret_cast<const u32x4_a2 *>(p + 64 * i + 16 * g + 8 * h);
-        }
+        float top = -__builtin_inff();
+        for (int w = 0; w < WAVES; ++w) top = fmaxf(top, most_of[(w * NT + n) * 16 + col]);
+        mine[n] = r.most[n] == -__builtin_inff() ? 0.0f : exp2_of(r.most[n] - top);
     }
-    // of this wave's rows: what the first sees, and where the last one's view ends (none: nothing)
-    const int32_t least = row0 < rows ? begin + (int32_t)quotient(row0, a.group) : 0;
-    const uint32_t my_last = row0 + 16 * NT - 1 < last_row ? row0 + 16 * NT - 1 : last_row;
-    const int32_t my_end = row0 < rows ? begin + (int32_t)quotient(my_last, a.group) + 1 : 0;
-
-    f32x4 o[NT][VT] = {};
-    float most[NT], total[NT];
-#pragma unroll
-    for (int n = 0; n < NT; ++n) most[n] = -__builtin_inff(), total[n] = 0;
-    const uint32_t page_mask = (1u << c.log_page) - 1;
-    const size_t head_values = (size_t)D << c.log_page;
-    const int32_t *table = c.table + (size_t)b * c.table_stride;
-
-    // The page of 16 tokens from position t on, -1 where there is none.  Copies from no page take page 0, which exists, and are not looked at.
-    auto page_at = [&](int32_t t) {
-        const int32_t p = t < s.length ? table[t >> c.log_page] : -1;
-        if ((uint32_t)p < c.n_pages) return p;
-        if (t < s.length) complain(c);
-        return -1;
-    };
-    // wave w copies the keys of 16 tokens and a quarter of the dimensions' values
-    const uint32_t value_group = (lane & 3) ^ value_turn(lane >> 2);
-    auto copy = [&](int32_t t0, int buffer, int32_t key_page, int32_t value_page) {
-        using from_t = const __attribute__((address_space(1))) void *;
-        using to_t = __attribute__((address_space(3))) void *;
-        const uint8_t *k = c.k_codes + ((size_t)(uint32_t)(key_page < 0 ? 0 : key_page) * c.heads + head) * head_values + (size_t)((t0 + 16 * wave) & page_mask) * D;
-        const uint8_t *v = c.v_codes + ((size_t)(uint32_t)(value_page < 0 ? 0 : value_page) * c.heads + head) * head_values + ((t0 + 16 * value_group) & page_mask);
-#pragma unroll
-        for (int r = 0; r < COPIES; ++r) {
-            const uint32_t place = r * 64 + lane, row = place / (D / 16), chunk = place % (D / 16) ^ key_turn<D>(16 * wave + row);
-            __builtin_amdgcn_global_load_lds((from_t)(k + row * D + 16 * chunk), (to_t)(keys[buffer] + 16 * wave * D + r * 1024), 16, 0, 0);
-        }
-#pragma unroll
-        for (int r = 0; r < COPIES; ++r) {
-            const uint32_t dim = (wave * COPIES + r) * 16 + (lane >> 2);
-            __builtin_amdgcn_global_load_lds((from_t)(v + ((size_t)dim << c.log_page)), (to_t)(values[buffer] + (wave * COPIES + r) * 1024), 16, 0, 0);
-        }
-    };
-    uint32_t key_at[4], value_at = col * 64 + ((g ^ value_turn(col)) << 4);
 #pragma unroll
     for (int i = 0; i < KC; ++i) {
-        const uint32_t t = 16 * (col >> 2) + (col & 3);                       // (+ 4 j, which does not turn)
-        key_at[i] = t * D + (((4 * i + g) ^ key_turn<D>(t)) << 4);
+        if (i) __syncthreads();
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int e = 0; e < 4; ++e) sums[(wave * 16 * NT + 16 * n + col) * 17 + 4 * e + g] = r.o[n][4 * i + e] * mine[n];
+        __syncthreads();
+        for (uint32_t at = threadIdx.x; at < 16 * NT * 16; at += 64 * WAVES) {
+            const uint32_t row = at >> 4, d4 = at & 15, out_row = row0 + row;
+            if (out_row >= v.rows) continue;
+            float top = -__builtin_inff(), total = 0;
+            for (int w = 0; w < WAVES; ++w) top = fmaxf(top, most_of[(w * NT + row / 16) * 16 + row % 16]);
+            for (int w = 0; w < WAVES; ++w) {
+                const float m = most_of[(w * NT + row / 16) * 16 + row % 16];
+                total += m == -__builtin_inff() ? 0.0f : total_of[(w * NT + row / 16) * 16 + row % 16] * exp2_of(m - top);
+            }
+            f32x4 sum = sums[row * 17 + d4];
+            for (int w = 1; w < WAVES; ++w) sum += sums[(w * 16 * NT + row) * 17 + d4];
+            const uint32_t token = quotient(out_row, a.group), q_head = head * a.group.by + (out_row - token * a.group.by), d = 64 * i + 4 * d4;
+            if (a.splits == 1) {
+                const float by = total == 0 ? 0.0f : 1.0f / total;
+                uint16_t *p = static_cast<uint16_t *>(a.out) + (size_t)(s.start + token) * a.out_token + (size_t)q_head * a.out_head + d;
+                *reinterpret_cast<u32x2_a2 *>(p) = u32x2{pack2<DT>(sum[0] * by, sum[1] * by), pack2<DT>(sum[2] * by, sum[3] * by)};
+            } else {
+                const size_t to = ((size_t)split * c.n_tokens + s.start + token) * a.q_heads + q_head;
+                *reinterpret_cast<f32x4 *>(a.part + to * D + d) = sum;
+                if (i == 0 && d4 == 0) *reinterpret_cast<f32x2 *>(a.part_stat + 2 * to) = f32x2{top, total};
+            }
+        }
     }
+}
 
-    int32_t page = page_at(from + 16 * (int32_t)g), next_page = -1;           // of the tokens that this lane has weights of
-    {
-        const int32_t kp = page_at(from + 16 * (int32_t)wave), vp = page_at(from + 16 * (int32_t)value_group);
-        if (from < to) copy(from, 0, kp, vp);
+// ---- many rows: the matrix and vector units work, the cache's codes come from the die's own cache ---------------------------------------
+
+// 16 NT rows to each of four waves, which share the tiles: a wave has all of them, so nothing is joined in the end.  The memory unit copies the codes
+// of a tile into LDS while the one before is worked on.  Every wave makes 16-bit values of the codes by itself: a conversion makes two of
+// them in the time of any vector instruction, and NT tiles of rows use each.
+template <int DT, int D, int NT>
+__global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
+{
+    constexpr int VT = D / 16, ROWS = 64 * NT;
+    __shared__ __attribute__((aligned(16))) Tile<D> tiles[2];
+    const Pages &c = a.c;
+    const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
+    // The last rows first, as they see most; workgroups are dealt out to the eight dies one by one, so where (sequence, head)s are a multiple of
+    // eight each of them stays with one die and its cache.
+    const uint32_t groups = c.batch * c.heads, within = blockIdx.x % (groups * a.splits), b = within % groups / c.heads, head = within % groups % c.heads;
+    const uint32_t split = within / groups, first_row = (a.row_tiles - 1 - blockIdx.x / (groups * a.splits)) * ROWS;
+    const Sequence s = sequence_of(a, b);
+    if (!s.good) {
+        complain(c);
+        return;
     }
-    auto scales_of = [&](int32_t p, float &k, float &v) {
-        const size_t at = (size_t)(uint32_t)(p < 0 ? 0 : p) * c.heads + head;
-        k = power_of(c.k_scales[at]), v = power_of(c.v_scales[at]);
+    if (first_row >= s.count * a.group.by) return;
+    const Span v = span_of(a, s, first_row, ROWS, split);
+    if (split > 0 && v.from >= v.to) return;
+    const uint32_t row0 = first_row + wave * (16 * NT);
+    const int32_t my_end = row0 < v.rows ? span_of(a, s, row0, 16 * NT, split).end : 0;
+    Cached cache = cached_of(a, s, b, head);
+    int32_t raw[4], page = -1, next_page = -1;
+    uint32_t kb = 0, vb = 0, next_kb = 0, next_vb = 0;
+    bool whole = true, next_whole = true;
+    auto ask = [&](int32_t t0, Tile<D> &to, int32_t &pg, bool &all, uint32_t &k, uint32_t &w) {
+        const Runs p = cache.runs(t0, raw);
+        all = (p.page[0] | p.page[1] | p.page[2] | p.page[3]) >= 0;
+        copy_tile<D, 4>(cache, p, t0, to, wave);
+        pg = select4(p, g);
+        const size_t at = (size_t)(uint32_t)(pg < 0 ? 0 : pg) * c.heads + head;
+        k = c.k_scales[at], w = c.v_scales[at];
     };
-    float ks, vs, next_ks = 0, next_vs = 0;
-    scales_of(page, ks, vs);
-    int32_t next_kp = page_at(from + 64 + 16 * (int32_t)wave), next_vp = page_at(from + 64 + 16 * (int32_t)value_group);
-    next_page = page_at(from + 64 + 16 * (int32_t)g);
-
+    if (v.from < v.to) {
+        cache.table_entries(v.from, raw);
+        ask(v.from, tiles[0], page, whole, kb, vb);
+        cache.table_entries(v.from + 64, raw);
+    }
+    Rows<DT, D, NT> r;
+    r.begin(a, s, row0, v.rows, head);
     int buffer = 0;
-    for (int32_t t0 = from; t0 < to; t0 += 64, buffer ^= 1) {
+    for (int32_t t0 = v.from; t0 < v.to; t0 += 64, buffer ^= 1) {
         __builtin_amdgcn_sched_barrier(0);
         // this wave's copies are in LDS, then all waves' are, and nobody reads the tile before any more
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
-        int32_t far_page = -1, far_kp = -1, far_vp = -1;
-        if (t0 + 64 < to) {
-            copy(t0 + 64, buffer ^ 1, next_kp, next_vp);
-            scales_of(next_page, next_ks, next_vs);
-            far_page = page_at(t0 + 128 + 16 * (int32_t)g);
-            far_kp = page_at(t0 + 128 + 16 * (int32_t)wave);
-            far_vp = page_at(t0 + 128 + 16 * (int32_t)value_group);
+        if (t0 + 64 < v.to) {
+            ask(t0 + 64, tiles[buffer ^ 1], next_page, next_whole, next_kb, next_vb);
+            cache.table_entries(t0 + 128, raw);
         }
-        if (t0 < my_end) {
-            const int32_t tv = t0 + 16 * (int32_t)g;
-            const bool partial = t0 + 63 > least || t0 + 64 > s.length || __any(page < 0);
-            f32x4 x[NT][4] = {};
-#pragma unroll
-            for (int i = 0; i < KC; ++i) {
-                u32x4 k[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const u32x4 *>(keys[buffer] + key_at[i] + 4 * j * D);
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const u32x4 v = values8<DT>(k[j][2 * h], k[j][2 * h + 1], 1.0f);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) x[n][j] = mfma16<DT>(v, q[n][i][h], x[n][j]);
-                    }
-            }
-            const float by = ks * a.scale;
-            u32x4 p[NT][2], rest_of[NT][2];
-#pragma unroll
-            for (int n = 0; n < NT; ++n) {
-                if (partial) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j)
-#pragma unroll
-                        for (int i = 0; i < 4; ++i) x[n][j][i] = page >= 0 && tv + 4 * j + i <= limit[n] ? x[n][j][i] * by : -__builtin_inff();
-                } else {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[n][j] *= by;
-                }
-                float high = -__builtin_inff();
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int i = 0; i < 4; ++i) high = fmaxf(high, x[n][j][i]);
-                high = over_groups_max(high);
-                // Weights are taken relative to a maximum that may lag behind by up to 2^8, which costs nothing in 32 bits: most tiles need no
-                // change of what is summed already.
-                if (__any(high > most[n] + 8.0f)) {
-                    const float now = fmaxf(most[n], high), fade = now == -__builtin_inff() ? 1.0f : exp2_of(most[n] - now);
-                    most[n] = now;
-                    total[n] *= fade;
-#pragma unroll
-                    for (int i = 0; i < VT; ++i) o[n][i] *= fade;
-                }
-                const float base = most[n] == -__builtin_inff() ? 0.0f : most[n];
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const float lo = exp2_of(x[n][2 * h + j / 2][2 * (j & 1)] - base), hi = exp2_of(x[n][2 * h + j / 2][2 * (j & 1) + 1] - base);
-                        total[n] += lo;
-                        total[n] += hi;
-                        p[n][h][j] = pack2<BF16>(lo, hi);
-                        if constexpr (DT == FP16) {
-                            const f32x2 r = unpack2<BF16>(p[n][h][j]);
-                            rest_of[n][h][j] = pack2<BF16>(lo - r[0], hi - r[1]);
-                        }
-                    }
-            }
-            // in a tile that not every row sees whole: bytes behind the sequence's end and of no page are anyone's, and a NaN is
-            // told to the rows that see it, as above
-            uint32_t mask[4] = {~0u, ~0u, ~0u, ~0u};
-            bool careful = false;
-            if (partial) {
-                uint32_t any = 0;
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const int32_t here = s.length - tv - 4 * j;
-                    mask[j] = page < 0 || here <= 0 ? 0 : here >= 4 ? ~0u : (1u << (8 * here)) - 1;
-                }
-                for (int i = 0; i < VT; ++i) {
-                    const u32x4 v = *reinterpret_cast<const u32x4 *>(values[buffer] + value_at + i * 1024);
-                    for (int j = 0; j < 4; ++j) any |= nan_bytes(v[j] & mask[j]);
-                }
-                careful = __any(any);
-            }
-#pragma unroll
-            for (int i = 0; i < VT; ++i) {
-                u32x4 v = *reinterpret_cast<const u32x4 *>(values[buffer] + value_at + i * 1024);
-                if (partial) {
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) v[j] &= mask[j];
-                    if (careful) {
-                        u32x4 bad;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) {
-                            const uint32_t nan = nan_bytes(v[j]);
-                            v[j] &= ~nan;
-                            bad[j] = nan & 0x38383838u;              // 1.0 as E4M3
-                        }
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) {
-                            f32x4 seen = {};
-#pragma unroll
-                            for (int h = 0; h < 2; ++h) {
-                                u32x4 sees;
-#pragma unroll
-                                for (int j = 0; j < 4; ++j) {
-                                    const int32_t at = tv + 8 * h + 2 * j;
-                                    sees[j] = (at <= limit[n] ? 0x3F80u : 0) | (at + 1 <= limit[n] ? 0x3F800000u : 0);
-                                }
-                                seen = mfma16<BF16>(values8<BF16>(bad[2 * h], bad[2 * h + 1], 1.0f), sees, seen);
-                            }
-#pragma unroll
-                            for (int e = 0; e < 4; ++e) o[n][i][e] = seen[e] > 0 ? __builtin_nanf("") : o[n][i][e];
-                        }
-                    }
-                }
-#pragma unroll
-                for (int h = 0; h < 2; ++h) {
-                    const u32x4 vv = values8<BF16>(v[2 * h], v[2 * h + 1], vs);
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) {
-                        o[n][i] = mfma16<BF16>(vv, p[n][h], o[n][i]);
-                        if constexpr (DT == FP16) o[n][i] = mfma16<BF16>(vv, rest_of[n][h], o[n][i]);
-                    }
-                }
-            }
-        }
-        page = next_page, ks = next_ks, vs = next_vs;
-        next_page = far_page, next_kp = far_kp, next_vp = far_vp;
+        if (t0 < my_end) r.step(tiles[buffer], t0, s.length, whole, page, power_of(kb) * a.scale, power_of(vb));
+        page = next_page, whole = next_whole, kb = next_kb, vb = next_vb;
     }
+    if (cache.bad && threadIdx.x == 0) complain(c);
 #pragma unroll
     for (int n = 0; n < NT; ++n) {
-        const float sum = over_groups_sum(total[n]);
-        if (row0 + 16 * n + col >= rows) continue;
-        const float by = sum == 0 ? 0.0f : 1.0f / sum;
-        const size_t at = ((size_t)split * c.n_tokens + s.start + token[n]) * a.q_heads + q_head[n];
-        uint16_t *out = static_cast<uint16_t *>(a.out) + (size_t)(s.start + token[n]) * a.out_token + (size_t)q_head[n] * a.out_head;
+        const uint32_t row = row0 + 16 * n + col;
+        if (row >= v.rows) continue;
+        const uint32_t token = quotient(row, a.group), q_head = head * a.group.by + (row - token * a.group.by);
+        const float sum = r.total[n][0], by = sum == 0 ? 0.0f : 1.0f / sum;
+        const size_t at = ((size_t)split * c.n_tokens + s.start + token) * a.q_heads + q_head;
+        uint16_t *out = static_cast<uint16_t *>(a.out) + (size_t)(s.start + token) * a.out_token + (size_t)q_head * a.out_head;
 #pragma unroll
         for (int i = 0; i < VT; ++i) {
             const uint32_t d = 16 * i + 4 * g;
-            if (a.splits == 1) *reinterpret_cast<u32x2_a2 *>(out + d) = u32x2{pack2<DT>(o[n][i][0] * by, o[n][i][1] * by), pack2<DT>(o[n][i][2] * by, o[n][i][3] * by)};
-            else *reinterpret_cast<f32x4 *>(a.part + at * D + d) = o[n][i];
+            const f32x4 &o = r.o[n][i];
+            if (a.splits == 1) *reinterpret_cast<u32x2_a2 *>(out + d) = u32x2{pack2<DT>(o[0] * by, o[1] * by), pack2<DT>(o[2] * by, o[3] * by)};
+            else *reinterpret_cast<f32x4 *>(a.part + at * D + d) = o;
         }
-        if (a.splits > 1 && g == 0) *reinterpret_cast<f32x2 *>(a.part_stat + 2 * at) = f32x2{most[n], sum};
+        if (a.splits > 1 && g == 0) *reinterpret_cast<f32x2 *>(a.part_stat + 2 * at) = f32x2{r.most[n], sum};
     }
 }
 
@@ -588,7 +589,7 @@ using namespace enec::lowbit;
 
 struct Plan {
     bool many;                          // the kernel for many rows
-    uint32_t row_tiles, chunk, splits;
+    uint32_t rows, row_tiles, chunk, splits;      // rows of a workgroup
 };
 
 inline uint32_t rows_of_many(uint32_t head_dim) { return head_dim == 256 ? 64 : 128; }
@@ -599,8 +600,9 @@ Plan plan_of(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t head_di
     Plan p;
     const uint64_t rows = (uint64_t)max_new * group;
     p.many = rows > 32;
-    const uint32_t tile = p.many ? rows_of_many(head_dim) : 16, slots = p.many ? 512 : 1024;
-    p.row_tiles = (uint32_t)((rows + tile - 1) / tile);
+    p.rows = p.many ? rows_of_many(head_dim) : rows > 16 && head_dim < 256 ? 32 : 16;       // (32 rows of 256 dimensions do not fit the registers)
+    const uint32_t slots = p.many ? 512 : 1024;
+    p.row_tiles = (uint32_t)((rows + p.rows - 1) / p.rows);
     const uint64_t others = (uint64_t)batch * kv_heads * p.row_tiles;
     const uint64_t want = others >= slots ? 1 : (slots + others - 1) / others;
     const uint64_t tokens = (max_length + want - 1) / want;
@@ -609,18 +611,29 @@ Plan plan_of(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t head_di
     return p;
 }
 
-template <int DT, int D> void launch(const Attend &a, bool many, hipStream_t s)
+template <int DT, int D, int NT> bool launch_few(const Attend &a, uint32_t tiles, hipStream_t s)
+{
+    constexpr int WAVES = D == 256 ? 2 : 4;
+    constexpr size_t LDS = 2 * WAVES * sizeof(Tile<D>);
+    static_assert(LDS >= 2 * WAVES * 16 * NT * sizeof(float) + WAVES * 16 * NT * 17 * sizeof(f32x4) && LDS <= 160 * 1024, "what is joined takes the tiles' place");
+    const auto kernel = attend_few_kernel<DT, D, NT, WAVES>;
+    if (LDS > 65536 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS) != hipSuccess) return false;
+    kernel<<<dim3(tiles, a.c.heads), 64 * WAVES, LDS, s>>>(a);
+    return true;
+}
+template <int DT, int D> bool launch(const Attend &a, const Plan &p, hipStream_t s)
 {
     const uint32_t tiles = a.splits * a.c.batch * a.row_tiles;
-    if (many) attend_many_kernel<DT, D, D == 256 ? 1 : 2><<<(tiles * a.c.heads + 7) / 8 * 8, 256, 0, s>>>(a);
-    else attend_kernel<DT, D><<<dim3(tiles, a.c.heads), 256, 0, s>>>(a);
-    if (a.splits > 1) attend_join_kernel<DT, D><<<dim3(a.c.n_tokens, a.q_heads), 64, 0, s>>>(a);
+    bool ok = true;
+    if (p.many) attend_many_kernel<DT, D, D == 256 ? 1 : 2><<<tiles * a.c.heads, 256, 0, s>>>(a);
+    else if (D == 256 || p.rows == 16) ok = launch_few<DT, D, 1>(a, tiles, s);
+    else ok = launch_few<DT, D, D == 256 ? 1 : 2>(a, tiles, s);
+    if (ok && a.splits > 1) attend_join_kernel<DT, D><<<dim3(a.c.n_tokens, a.q_heads), 64, 0, s>>>(a);
+    return ok;
 }
-template <int DT> void launch(const Attend &a, bool many, hipStream_t s)
+template <int DT> bool launch(const Attend &a, const Plan &p, hipStream_t s)
 {
-    if (a.c.head_dim == 64) launch<DT, 64>(a, many, s);
-    else if (a.c.head_dim == 128) launch<DT, 128>(a, many, s);
-    else launch<DT, 256>(a, many, s);
+    return a.c.head_dim == 64 ? launch<DT, 64>(a, p, s) : a.c.head_dim == 128 ? launch<DT, 128>(a, p, s) : launch<DT, 256>(a, p, s);
 }
 
 // one call's arguments; 0 = none of its kernels can count with these
@@ -651,7 +664,7 @@ int enec_cache_attention(const enec_cache *cache, const enec_cache_batch *batch,
     if (const int rc = pages_of(cache, batch, a.c)) return rc;
     if (!shape_ok(cache, a.c.batch, a.c.n_tokens, q_heads, max_new, max_length)) return ENEC_E_ARG;
     if (a.c.batch == 0 || a.c.n_tokens == 0) return ENEC_OK;
-    if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 1) || max_new == 0) return ENEC_E_ARG;
+    if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 1) || max_new == 0 || !(scale > 0)) return ENEC_E_ARG;
     const uint32_t group = q_heads / a.c.heads;
     const Plan p = plan_of(a.c.batch, a.c.heads, group, a.c.head_dim, max_new, max_length);
     if ((uint64_t)p.splits * a.c.batch * p.row_tiles > 0x3FFFFFFFu / a.c.heads) return ENEC_E_ARG;
@@ -664,9 +677,8 @@ int enec_cache_attention(const enec_cache *cache, const enec_cache_batch *batch,
     a.max_new = max_new, a.max_length = max_length, a.chunk = p.chunk, a.splits = p.splits, a.row_tiles = p.row_tiles;
     a.part = static_cast<float *>(workspace);
     a.part_stat = a.part + (size_t)p.splits * a.c.n_tokens * q_heads * a.c.head_dim;
-    if (dtype == ENEC_BF16) launch<BF16>(a, p.many, (hipStream_t)stream);
-    else launch<FP16>(a, p.many, (hipStream_t)stream);
-    return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
+    const bool ok = dtype == ENEC_BF16 ? launch<BF16>(a, p, (hipStream_t)stream) : launch<FP16>(a, p, (hipStream_t)stream);
+    return ok && hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
 }
 
 }  // extern "C"

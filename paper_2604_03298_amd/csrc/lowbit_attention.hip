@@ -131,29 +131,38 @@ __device__ __forceinline__ int32_t select4(const Runs &p, uint32_t i)
     return i & 2 ? hi : lo;
 }
 
-// Copies part `part` of `parts` of a tile into LDS, 1024 bytes an instruction: PARTS waves share it, or one takes all.  No page: page 0, which exists, and
+// Copies of a tile's keys, or values, into LDS, 1024 bytes an instruction: PARTS waves share them, or one takes all.  No page: page 0, which exists, and
 // whose codes are not looked at.
-template <int D, int PARTS> __device__ __forceinline__ void copy_tile(const Cached &s, const Runs &p, int32_t t0, Tile<D> &to, uint32_t part)
+template <int D, int PARTS> __device__ __forceinline__ void copy_keys(const Cached &s, const Runs &p, int32_t t0, Tile<D> &to, uint32_t part)
 {
-    constexpr int COPIES = D / 16 / PARTS, TOKENS = 1024 / D;             // of keys, and as many of values; tokens of one
+    constexpr int COPIES = D / 16 / PARTS, TOKENS = 1024 / D, OF_RUN = 16 / TOKENS;      // tokens of a copy, copies of a run
     const Pages &c = *s.c;
     const uint32_t lane = threadIdx.x & 63, mask = (1u << c.log_page) - 1;
     const size_t head_values = (size_t)D << c.log_page;
 #pragma unroll
-    for (int r = 0; r < COPIES; ++r) {
-        const uint32_t n = part * COPIES + r, first = n * TOKENS;                           // TOKENS divides 16, so it is of one run
-        const int32_t page = PARTS == 1 ? p.page[first / 16 % 4] : select4(p, first / 16);
-        const uint32_t token = first + lane / (D / 16), chunk = lane % (D / 16) ^ key_turn<D>(token);
-        const uint8_t *k = c.k_codes + ((size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + s.head) * head_values + (size_t)((t0 + first) & mask) * D;
-        copy_to_lds(k + (lane / (D / 16) * D + 16 * chunk), to.keys + n * 1024);
+    for (int q = 0; q < (COPIES + OF_RUN - 1) / OF_RUN; ++q) {
+        const uint32_t run = PARTS == 1 ? q : part * COPIES / OF_RUN + q;
+        const int32_t page = PARTS == 1 ? p.page[q & 3] : select4(p, run);
+        const uint8_t *k = c.k_codes + ((size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + s.head) * head_values + (size_t)((t0 + 16 * run) & mask) * D;
+#pragma unroll
+        for (int r = 0; r < OF_RUN && r < COPIES; ++r) {
+            const uint32_t token = TOKENS * r + lane / (D / 16), chunk = lane % (D / 16) ^ key_turn<D>(16 * run + token);
+            copy_to_lds(k + token * D + 16 * chunk, to.keys + (16 * run + TOKENS * r) * D);
+        }
     }
+}
+template <int D, int PARTS> __device__ __forceinline__ void copy_values(const Cached &s, const Runs &p, int32_t t0, Tile<D> &to, uint32_t part)
+{
+    constexpr int COPIES = D / 16 / PARTS;
+    const Pages &c = *s.c;
+    const uint32_t lane = threadIdx.x & 63, mask = (1u << c.log_page) - 1;
     const uint32_t run = (lane & 3) ^ value_turn(lane >> 2);
     const int32_t page = select4(p, run);
-    const uint8_t *v = c.v_codes + ((size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + s.head) * head_values + ((t0 + 16 * run) & mask);
+    const uint8_t *v = c.v_codes + (((size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + s.head) * D << c.log_page) + ((t0 + 16 * run) & mask);
 #pragma unroll
     for (int r = 0; r < COPIES; ++r) {
         const uint32_t n = part * COPIES + r;
-        copy_to_lds(v + ((size_t)(n * 16 + (lane >> 2)) << c.log_page), to.values + n * 1024);
+        copy_to_lds(v + ((n * 16 + (lane >> 2)) << c.log_page), to.values + n * 1024);
     }
 }
 
@@ -203,12 +212,12 @@ template <int DT, int D, int NT> struct Rows {
         value_at = col * 64 + ((g ^ value_turn(col)) << 4);
     }
 
-    // page, ks, vs: of the lane group's run.  by: its keys' scale, the call's and log2 e
-    __device__ __forceinline__ void step(const Tile<D> &tile, int32_t t0, int32_t length, bool whole_pages, int32_t page, float by, float vs)
+    __device__ __forceinline__ void scores(const Tile<D> &tile, f32x4 (&x)[NT][4]) const
     {
-        const uint32_t g = threadIdx.x >> 4 & 3;
-        const int32_t tv = t0 + 16 * (int32_t)g;
-        f32x4 x[NT][4] = {};
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[n][j] = f32x4{};
 #pragma unroll
         for (int i = 0; i < KC; ++i) {
             u32x4 k[4];
@@ -223,6 +232,15 @@ template <int DT, int D, int NT> struct Rows {
                     for (int n = 0; n < NT; ++n) x[n][j] = mfma16<DT>(v, q[n][i][h], x[n][j]);
                 }
         }
+    }
+
+    // page, vs: of the lane group's run.  by: its keys' scale, the call's and log2 e.  arrived(): waits for the tile's values.
+    template <typename F>
+    __device__ __forceinline__ void add(const Tile<D> &tile, f32x4 (&x)[NT][4], int32_t t0, int32_t length, bool whole_pages, int32_t page, float by, float vs,
+                                        F arrived)
+    {
+        const uint32_t g = threadIdx.x >> 4 & 3;
+        const int32_t tv = t0 + 16 * (int32_t)g;
         // what a row does not see takes no part, whatever its codes are
         const bool partial = t0 + 63 > least || t0 + 64 > length || !whole_pages;
         if (partial) {
@@ -274,7 +292,8 @@ template <int DT, int D, int NT> struct Rows {
                 total[n] = mfma16<BF16>(ones, p[n][h], total[n]);
                 if constexpr (DT == FP16) total[n] = mfma16<BF16>(ones, rest_of[n][h], total[n]);
             }
-        auto add = [&](int i, const u32x4 &v) {
+        arrived();
+        auto product = [&](int i, const u32x4 &v) {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 const u32x4 vv = values8<BF16>(v[2 * h], v[2 * h + 1], vs);
@@ -287,7 +306,7 @@ template <int DT, int D, int NT> struct Rows {
         };
         if (!partial) {
 #pragma unroll
-            for (int i = 0; i < VT; ++i) add(i, *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024));
+            for (int i = 0; i < VT; ++i) product(i, *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024));
             return;
         }
         // Bytes behind the sequence's end and of no page are anyone's.  A value that is NaN has to reach the rows that see it, and no other: 0 * NaN would.
@@ -335,7 +354,7 @@ template <int DT, int D, int NT> struct Rows {
                     for (int e = 0; e < 4; ++e) o[n][i][e] = seen[e] > 0 ? __builtin_nanf("") : o[n][i][e];
                 }
             }
-            add(i, v);
+            product(i, v);
         }
     }
 };
@@ -362,12 +381,14 @@ __device__ __forceinline__ Cached cached_of(const Attend &a, const Sequence &s, 
 
 // ---- few rows: the card reads the cache, everything else is small ----------------------------------------------------------------
 
-// A workgroup has 16 NT rows; its WAVES waves take tiles in turn and meet in LDS in the end.  Each wave copies its own tiles, one ahead, and waits for
-// its own copies only: no barrier until the end.
+// A workgroup has 16 NT rows; its WAVES waves take tiles in turn and meet in LDS in the end.  A wave has LDS for one tile of its own: when its keys have
+// been multiplied, the next tile's are copied there while the weights are computed and the values multiplied, and the next values while the next keys are.
+// It waits for its own copies only: no barrier until the end.  Two waves to a SIMD (head_dim 256: one) did more than copies further ahead: a tile's
+// chain of steps leaves half of a wave's cycles idle (64 sequences of up to 8191 tokens: 4 waves with two tiles each 150 us).
 template <int DT, int D, int NT, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES, D == 64 ? 2 : 1) attend_few_kernel(Attend a)
+__global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kernel(Attend a)
 {
-    constexpr int KC = D / 64, COPIES = D / 8;
+    constexpr int KC = D / 64, COPIES = D / 16;              // of a tile's keys, and of its values
     extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
     const Pages &c = a.c;
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
@@ -381,47 +402,55 @@ __global__ void __launch_bounds__(64 * WAVES, D == 64 ? 2 : 1) attend_few_kernel
     const Span v = span_of(a, s, row0, 16 * NT, split);
     if (split > 0 && v.from >= v.to) return;
     Cached cache = cached_of(a, s, b, head);
-    Tile<D> *tiles = reinterpret_cast<Tile<D> *>(shared) + 2 * wave;
-    auto scale_bytes = [&](int32_t page, uint32_t &k, uint32_t &w) {
-        const size_t at = (size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + head;
-        k = c.k_scales[at], w = c.v_scales[at];
-    };
-    const int32_t first = v.from + 64 * (int32_t)wave;
+    Tile<D> &tile = reinterpret_cast<Tile<D> *>(shared)[wave];
     constexpr int32_t STEP = 64 * WAVES;
-    int32_t raw[4], page = -1, next_page = -1;
-    uint32_t kb = 0, vb = 0, next_kb = 0, next_vb = 0;
-    bool whole = true, next_whole = true;
-    auto ask = [&](int32_t t0, Tile<D> &to, int32_t &pg, bool &all, uint32_t &k, uint32_t &w) {
-        const Runs p = cache.runs(t0, raw);
-        all = (p.page[0] | p.page[1] | p.page[2] | p.page[3]) >= 0;
-        copy_tile<D, 1>(cache, p, t0, to, 0);
-        pg = select4(p, g);
-        scale_bytes(pg, k, w);
+    const int32_t first = v.from + 64 * (int32_t)wave;
+    int32_t raw[4];
+    Runs runs{};
+    uint32_t k_byte = 0, v_byte = 0;
+    auto ask_keys = [&](int32_t t0) {                        // and the scales, before them
+        runs = cache.runs(t0, raw);
+        const int32_t page = select4(runs, g);
+        const size_t at = (size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + head;
+        k_byte = c.k_scales[at], v_byte = c.v_scales[at];
+        __builtin_amdgcn_sched_barrier(0);
+        copy_keys<D, 1>(cache, runs, t0, tile, 0);
+        cache.table_entries(t0 + STEP, raw);
     };
     if (first < v.to) {
         cache.table_entries(first, raw);
-        ask(first, tiles[0], page, whole, kb, vb);
-        cache.table_entries(first + STEP, raw);
+        ask_keys(first);
+        __builtin_amdgcn_sched_barrier(0);
+        copy_values<D, 1>(cache, runs, first, tile, 0);
     }
     Rows<DT, D, NT> r;
     r.begin(a, s, row0, v.rows, head);
-    int buffer = 0;
-    for (int32_t t0 = first; t0 < v.to; t0 += STEP, buffer ^= 1) {
+    for (int32_t t0 = first; t0 < v.to; t0 += STEP) {
+        const Runs now = runs;
+        const int32_t page = select4(now, g);
+        const bool whole = (now.page[0] | now.page[1] | now.page[2] | now.page[3]) >= 0, more = t0 + STEP < v.to;
+        // Copies and loads come back in the order in which they were issued: with as many left as were issued of the values behind the keys, the keys are
+        // in LDS.
         __builtin_amdgcn_sched_barrier(0);
-        if (t0 + STEP < v.to) {
-            ask(t0 + STEP, tiles[buffer ^ 1], next_page, next_whole, next_kb, next_vb);
-            cache.table_entries(t0 + 2 * STEP, raw);
+        asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+        __builtin_amdgcn_sched_barrier(0);
+        f32x4 x[NT][4];
+        r.scores(tile, x);
+        const float by = power_of(k_byte) * a.scale, vs = power_of(v_byte);
+        __builtin_amdgcn_sched_barrier(0);
+        asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (the keys have been read)
+        if (more) ask_keys(t0 + STEP);
+        __builtin_amdgcn_sched_barrier(0);
+        r.add(tile, x, t0, s.length, whole, page, by, vs, [&] {
+            // the same for the values, with the next keys behind them
             __builtin_amdgcn_sched_barrier(0);
-            // copies and loads come back in their order: with as many left as copies of the next tile were issued, this tile's are in LDS
-            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES < 63 ? COPIES : 63) : "memory");
-        } else {
-            asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
-        }
+            if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
+            else asm volatile("s_waitcnt vmcnt(0)" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+        });
         __builtin_amdgcn_sched_barrier(0);
-        r.step(tiles[buffer], t0, s.length, whole, page, power_of(kb) * a.scale, power_of(vb));
-        // (its codes have been read before the tile after the next one is copied there)
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
-        page = next_page, whole = next_whole, kb = next_kb, vb = next_vb;
+        if (more) copy_values<D, 1>(cache, runs, t0 + STEP, tile, 0);
     }
     if (cache.bad && lane == 0) complain(c);
 
@@ -507,7 +536,8 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
     auto ask = [&](int32_t t0, Tile<D> &to, int32_t &pg, bool &all, uint32_t &k, uint32_t &w) {
         const Runs p = cache.runs(t0, raw);
         all = (p.page[0] | p.page[1] | p.page[2] | p.page[3]) >= 0;
-        copy_tile<D, 4>(cache, p, t0, to, wave);
+        copy_keys<D, 4>(cache, p, t0, to, wave);
+        copy_values<D, 4>(cache, p, t0, to, wave);
         pg = select4(p, g);
         const size_t at = (size_t)(uint32_t)(pg < 0 ? 0 : pg) * c.heads + head;
         k = c.k_scales[at], w = c.v_scales[at];
@@ -529,7 +559,11 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
             ask(t0 + 64, tiles[buffer ^ 1], next_page, next_whole, next_kb, next_vb);
             cache.table_entries(t0 + 128, raw);
         }
-        if (t0 < my_end) r.step(tiles[buffer], t0, s.length, whole, page, power_of(kb) * a.scale, power_of(vb));
+        if (t0 < my_end) {
+            f32x4 x[NT][4];
+            r.scores(tiles[buffer], x);
+            r.add(tiles[buffer], x, t0, s.length, whole, page, power_of(kb) * a.scale, power_of(vb), [] {});
+        }
         page = next_page, whole = next_whole, kb = next_kb, vb = next_vb;
     }
     if (cache.bad && threadIdx.x == 0) complain(c);
@@ -552,12 +586,14 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
     }
 }
 
-// The splits of a row, in their order: one wave a row.
+// The splits of a row: a workgroup a row, D / 4 threads to a split, 1024 / D splits at a time; each thread's sums in the order of the splits, then theirs.
 template <int DT, int D>
-__global__ void __launch_bounds__(64) attend_join_kernel(Attend a)
+__global__ void __launch_bounds__(256) attend_join_kernel(Attend a)
 {
-    constexpr int N = D / 64;
-    const uint32_t lane = threadIdx.x, token = blockIdx.x, q_head = blockIdx.y;
+    constexpr uint32_t LANES = D / 4, AT_ONCE = 256 / LANES;
+    __shared__ f32x4 sums[AT_ONCE][LANES];
+    __shared__ float tops[4], totals[AT_ONCE];
+    const uint32_t token = blockIdx.x, q_head = blockIdx.y, lane = threadIdx.x & 63, d4 = threadIdx.x % LANES, mine = threadIdx.x / LANES;
     // the token's sequence: the last one that starts at or before it
     uint32_t n = 0;
     for (uint32_t b = 0; b < a.c.batch; b += 64) n += (uint32_t)__popcll(__ballot(b + lane < a.c.batch && a.c.starts[b + lane] <= (int32_t)token));
@@ -567,17 +603,31 @@ __global__ void __launch_bounds__(64) attend_join_kernel(Attend a)
     const int32_t sees = s.length - (int32_t)s.count + (int32_t)(token - s.start) + 1;
     const uint32_t splits = sees <= 0 ? 1 : ((uint32_t)sees + a.chunk - 1) / a.chunk;
     const size_t at = (size_t)token * a.q_heads + q_head, step = (size_t)a.c.n_tokens * a.q_heads;
-    float top = -__builtin_inff(), total = 0, o[N] = {};
-    for (uint32_t i = 0; i < splits; ++i) top = fmaxf(top, a.part_stat[2 * (at + i * step)]);
-    for (uint32_t i = 0; i < splits; ++i) {
+    float top = -__builtin_inff();
+    for (uint32_t i = threadIdx.x; i < splits; i += 256) top = fmaxf(top, a.part_stat[2 * (at + i * step)]);
+    for (int k = 1; k < 64; k *= 2) top = fmaxf(top, __shfl_xor(top, k));
+    if (lane == 0) tops[threadIdx.x >> 6] = top;
+    __syncthreads();
+    top = fmaxf(fmaxf(tops[0], tops[1]), fmaxf(tops[2], tops[3]));
+    f32x4 o = {};
+    float total = 0;
+#pragma unroll 4
+    for (uint32_t i = mine; i < splits; i += AT_ONCE) {
         const size_t j = at + i * step;
-        const float high = a.part_stat[2 * j], w = high == -__builtin_inff() ? 0.0f : exp2_of(high - top);
-        total += w * a.part_stat[2 * j + 1];
-        for (int e = 0; e < N; ++e) o[e] += w * a.part[j * D + N * lane + e];
+        const f32x2 stat = *reinterpret_cast<const f32x2 *>(a.part_stat + 2 * j);
+        const f32x4 part = *reinterpret_cast<const f32x4 *>(a.part + j * D + 4 * d4);
+        const float w = stat[0] == -__builtin_inff() ? 0.0f : exp2_of(stat[0] - top);
+        total += w * stat[1];
+        o += w * part;
     }
+    sums[mine][d4] = o;
+    if (d4 == 0) totals[mine] = total;
+    __syncthreads();
+    if (mine != 0) return;
+    for (uint32_t i = 1; i < AT_ONCE; ++i) o += sums[i][d4], total += totals[i];
     const float by = total == 0 ? 0.0f : 1.0f / total;
-    for (int e = 0; e < N; ++e)
-        store1<DT>(a.out, (size_t)token * a.out_token + (size_t)q_head * a.out_head + N * lane + e, o[e] * by);
+    uint16_t *p = static_cast<uint16_t *>(a.out) + (size_t)token * a.out_token + (size_t)q_head * a.out_head + 4 * d4;
+    *reinterpret_cast<u32x2_a2 *>(p) = u32x2{pack2<DT>(o[0] * by, o[1] * by), pack2<DT>(o[2] * by, o[3] * by)};
 }
 
 }  // namespace lowbit
@@ -601,21 +651,25 @@ Plan plan_of(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t head_di
     const uint64_t rows = (uint64_t)max_new * group;
     p.many = rows > 32;
     p.rows = p.many ? rows_of_many(head_dim) : rows > 16 && head_dim < 256 ? 32 : 16;       // (32 rows of 256 dimensions do not fit the registers)
-    const uint32_t slots = p.many ? 512 : 1024;
     p.row_tiles = (uint32_t)((rows + p.rows - 1) / p.rows);
+    // One round of workgroups, as many as the card holds, each with at least `least` tokens: a workgroup's start and end, and joining, cost as much as
+    // some hundred tokens.
+    const uint32_t slots = p.many || head_dim == 64 ? 512 : 256, least = p.many ? 512 : 1024;
     const uint64_t others = (uint64_t)batch * kv_heads * p.row_tiles;
-    const uint64_t want = others >= slots ? 1 : (slots + others - 1) / others;
+    const uint64_t want = others >= slots ? 1 : slots / others;
     const uint64_t tokens = (max_length + want - 1) / want;
-    p.chunk = (uint32_t)(tokens <= 256 ? 256 : (tokens + 255) / 256 * 256);
+    p.chunk = (uint32_t)(tokens <= least ? least : (tokens + 255) / 256 * 256);
     p.splits = max_length <= p.chunk ? 1 : (max_length + p.chunk - 1) / p.chunk;
     return p;
 }
 
 template <int DT, int D, int NT> bool launch_few(const Attend &a, uint32_t tiles, hipStream_t s)
 {
-    constexpr int WAVES = D == 256 ? 2 : 4;
-    constexpr size_t LDS = 2 * WAVES * sizeof(Tile<D>);
-    static_assert(LDS >= 2 * WAVES * 16 * NT * sizeof(float) + WAVES * 16 * NT * 17 * sizeof(f32x4) && LDS <= 160 * 1024, "what is joined takes the tiles' place");
+    constexpr int WAVES = D == 256 ? 4 : 8;
+    // what is joined in the end takes the tiles' place
+    constexpr size_t JOINED = 2 * WAVES * 16 * NT * sizeof(float) + WAVES * 16 * NT * 17 * sizeof(f32x4), TILES = WAVES * sizeof(Tile<D>);
+    constexpr size_t LDS = JOINED > TILES ? JOINED : TILES;
+    static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
     const auto kernel = attend_few_kernel<DT, D, NT, WAVES>;
     if (LDS > 65536 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS) != hipSuccess) return false;
     kernel<<<dim3(tiles, a.c.heads), 64 * WAVES, LDS, s>>>(a);
@@ -628,7 +682,7 @@ template <int DT, int D> bool launch(const Attend &a, const Plan &p, hipStream_t
     if (p.many) attend_many_kernel<DT, D, D == 256 ? 1 : 2><<<tiles * a.c.heads, 256, 0, s>>>(a);
     else if (D == 256 || p.rows == 16) ok = launch_few<DT, D, 1>(a, tiles, s);
     else ok = launch_few<DT, D, D == 256 ? 1 : 2>(a, tiles, s);
-    if (ok && a.splits > 1) attend_join_kernel<DT, D><<<dim3(a.c.n_tokens, a.q_heads), 64, 0, s>>>(a);
+    if (ok && a.splits > 1) attend_join_kernel<DT, D><<<dim3(a.c.n_tokens, a.q_heads), 256, 0, s>>>(a);
     return ok;
 }
 template <int DT> bool launch(const Attend &a, const Plan &p, hipStream_t s)

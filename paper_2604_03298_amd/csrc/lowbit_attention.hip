@@ -36,6 +36,13 @@ __device__ __forceinline__ float over_groups_max(float v)
     asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
     return fmaxf(a, b);
 }
+// (fmaxf passes each operand through an instruction of its own first, in case it is a signalling NaN: these are products)
+__device__ __forceinline__ float max3(float a, float b, float c)
+{
+    float r;
+    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
+    return r;
+}
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
 
 template <int DT> __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, const f32x4 &c)
@@ -241,26 +248,34 @@ template <int DT, int D, int NT> struct Rows {
     {
         const uint32_t g = threadIdx.x >> 4 & 3;
         const int32_t tv = t0 + 16 * (int32_t)g;
-        // what a row does not see takes no part, whatever its codes are
+        // What a row does not see takes no part, whatever its codes are.  (The empty instructions keep what few tiles need out of the others' way, where
+        // the compiler would compute both and select.)
         const bool partial = t0 + 63 > least || t0 + 64 > length || !whole_pages;
+#pragma unroll
+        for (int n = 0; n < NT; ++n)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) x[n][j] *= by;
         if (partial) {
+            asm volatile("");
 #pragma unroll
             for (int n = 0; n < NT; ++n) {
                 const int32_t sees = page >= 0 ? limit[n] - tv : -1;
 #pragma unroll
                 for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int i = 0; i < 4; ++i) x[n][j][i] = 4 * j + i <= sees ? x[n][j][i] * by : -__builtin_inff();
+                    for (int i = 0; i < 4; ++i) x[n][j][i] = 4 * j + i <= sees ? x[n][j][i] : -__builtin_inff();
             }
-            by = 1.0f;
         }
         u32x4 p[NT][2], rest_of[NT][2];
 #pragma unroll
         for (int n = 0; n < NT; ++n) {
-            float high = fmaxf(fmaxf(x[n][0][0], x[n][0][1]), fmaxf(x[n][0][2], x[n][0][3]));
+            float high = x[n][0][0];
 #pragma unroll
-            for (int j = 1; j < 4; ++j) high = fmaxf(high, fmaxf(fmaxf(x[n][j][0], x[n][j][1]), fmaxf(x[n][j][2], x[n][j][3])));
-            high = over_groups_max(high * by);
+            for (int j = 0; j < 4; ++j) {
+                high = max3(high, x[n][j][0], x[n][j][1]);
+                high = max3(high, x[n][j][2], x[n][j][3]);
+            }
+            high = over_groups_max(high);
             // Weights are taken relative to a maximum that may lag behind by up to 2^8, which costs nothing in 32 bits: most tiles need no
             // change of what is summed already.
             if (__any(high > most[n] + 8.0f)) {
@@ -275,8 +290,8 @@ template <int DT, int D, int NT> struct Rows {
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float lo = exp2_of(__builtin_fmaf(x[n][2 * h + j / 2][2 * (j & 1)], by, -base));
-                    const float hi = exp2_of(__builtin_fmaf(x[n][2 * h + j / 2][2 * (j & 1) + 1], by, -base));
+                    const float lo = exp2_of(x[n][2 * h + j / 2][2 * (j & 1)] - base);
+                    const float hi = exp2_of(x[n][2 * h + j / 2][2 * (j & 1) + 1] - base);
                     p[n][h][j] = pack2<BF16>(lo, hi);
                     if constexpr (DT == FP16) {
                         const f32x2 r = unpack2<BF16>(p[n][h][j]);
@@ -293,69 +308,66 @@ template <int DT, int D, int NT> struct Rows {
                 if constexpr (DT == FP16) total[n] = mfma16<BF16>(ones, rest_of[n][h], total[n]);
             }
         arrived();
-        auto product = [&](int i, const u32x4 &v) {
+        u32x4 v[VT];
+#pragma unroll
+        for (int i = 0; i < VT; ++i) v[i] = *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024);
+        if (partial) {
+            asm volatile("");
+            // Bytes behind the sequence's end and of no page are anyone's.  A value that is NaN has to reach the rows that see it, and no other:
+            // 0 * NaN would.  Such values are taken out, and the rows that see one are told.
+            u32x4 mask;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                const int32_t here = page >= 0 ? length - tv - 4 * j : 0;
+                mask[j] = here <= 0 ? 0 : here >= 4 ? ~0u : (1u << (8 * here)) - 1;
+            }
+            uint32_t any = 0;
+#pragma unroll
+            for (int i = 0; i < VT; ++i)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    v[i][j] &= mask[j];
+                    any |= any_nan(v[i][j]);
+                }
+            if (__any(any)) {
+                asm volatile("");
+#pragma unroll
+                for (int i = 0; i < VT; ++i) {
+                    u32x4 bad;
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const uint32_t nan = nan_bytes(v[i][j]);
+                        v[i][j] &= ~nan;
+                        bad[j] = nan & 0x38383838u;              // 1.0 as E4M3
+                    }
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) {
+                        f32x4 seen = {};
+                        const int32_t sees = limit[n] - tv;
+#pragma unroll
+                        for (int h = 0; h < 2; ++h) {
+                            u32x4 visible;
+#pragma unroll
+                            for (int j = 0; j < 4; ++j) visible[j] = (8 * h + 2 * j <= sees ? 0x3F80u : 0) | (8 * h + 2 * j + 1 <= sees ? 0x3F800000u : 0);
+                            seen = mfma16<BF16>(values8<BF16>(bad[2 * h], bad[2 * h + 1], 1.0f), visible, seen);
+                        }
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) o[n][i][e] = seen[e] > 0 ? __builtin_nanf("") : o[n][i][e];
+                    }
+                }
+            }
+        }
+#pragma unroll
+        for (int i = 0; i < VT; ++i)
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
-                const u32x4 vv = values8<BF16>(v[2 * h], v[2 * h + 1], vs);
+                const u32x4 vv = values8<BF16>(v[i][2 * h], v[i][2 * h + 1], vs);
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     o[n][i] = mfma16<BF16>(vv, p[n][h], o[n][i]);
                     if constexpr (DT == FP16) o[n][i] = mfma16<BF16>(vv, rest_of[n][h], o[n][i]);
                 }
             }
-        };
-        if (!partial) {
-#pragma unroll
-            for (int i = 0; i < VT; ++i) product(i, *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024));
-            return;
-        }
-        // Bytes behind the sequence's end and of no page are anyone's.  A value that is NaN has to reach the rows that see it, and no other: 0 * NaN would.
-        // Such values are taken out, and the rows that see one are told.
-        u32x4 mask;
-#pragma unroll
-        for (int j = 0; j < 4; ++j) {
-            const int32_t here = page >= 0 ? length - tv - 4 * j : 0;
-            mask[j] = here <= 0 ? 0 : here >= 4 ? ~0u : (1u << (8 * here)) - 1;
-        }
-        uint32_t any = 0;
-#pragma unroll
-        for (int i = 0; i < VT; ++i) {
-            u32x4 v = *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024);
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                v[j] &= mask[j];
-                any |= any_nan(v[j]);
-            }
-        }
-        const bool careful = __any(any);
-#pragma unroll
-        for (int i = 0; i < VT; ++i) {
-            u32x4 v = *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024), bad;
-            v &= mask;
-            if (careful) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t nan = nan_bytes(v[j]);
-                    v[j] &= ~nan;
-                    bad[j] = nan & 0x38383838u;              // 1.0 as E4M3
-                }
-#pragma unroll
-                for (int n = 0; n < NT; ++n) {
-                    f32x4 seen = {};
-                    const int32_t sees = limit[n] - tv;
-#pragma unroll
-                    for (int h = 0; h < 2; ++h) {
-                        u32x4 visible;
-#pragma unroll
-                        for (int j = 0; j < 4; ++j) visible[j] = (8 * h + 2 * j <= sees ? 0x3F80u : 0) | (8 * h + 2 * j + 1 <= sees ? 0x3F800000u : 0);
-                        seen = mfma16<BF16>(values8<BF16>(bad[2 * h], bad[2 * h + 1], 1.0f), visible, seen);
-                    }
-#pragma unroll
-                    for (int e = 0; e < 4; ++e) o[n][i][e] = seen[e] > 0 ? __builtin_nanf("") : o[n][i][e];
-                }
-            }
-            product(i, v);
-        }
     }
 };
 
@@ -528,7 +540,6 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
     const Span v = span_of(a, s, first_row, ROWS, split);
     if (split > 0 && v.from >= v.to) return;
     const uint32_t row0 = first_row + wave * (16 * NT);
-    const int32_t my_end = row0 < v.rows ? span_of(a, s, row0, 16 * NT, split).end : 0;
     Cached cache = cached_of(a, s, b, head);
     int32_t raw[4], page = -1, next_page = -1;
     uint32_t kb = 0, vb = 0, next_kb = 0, next_vb = 0;
@@ -559,11 +570,13 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
             ask(t0 + 64, tiles[buffer ^ 1], next_page, next_whole, next_kb, next_vb);
             cache.table_entries(t0 + 128, raw);
         }
-        if (t0 < my_end) {
-            f32x4 x[NT][4];
-            r.scores(tiles[buffer], x);
-            r.add(tiles[buffer], x, t0, s.length, whole, page, power_of(kb) * a.scale, power_of(vb), [] {});
-        }
+        // (also the last tiles, of which the first waves' rows see nothing: a branch around them cost every tile a copy of all sums)
+        f32x4 x[NT][4];
+        r.scores(tiles[buffer], x);
+        // (a wave between its products goes first: the other one of its SIMD has matrix instructions running meanwhile; 400 -> 378 us for two prompts of
+        // 4000 tokens over 5003)
+        __builtin_amdgcn_s_setprio(1);
+        r.add(tiles[buffer], x, t0, s.length, whole, page, power_of(kb) * a.scale, power_of(vb), [] { __builtin_amdgcn_s_setprio(0); });
         page = next_page, whole = next_whole, kb = next_kb, vb = next_vb;
     }
     if (cache.bad && threadIdx.x == 0) complain(c);

@@ -56,22 +56,21 @@ struct Page {
     uint32_t first, end;        // slots of the page that the call's tokens have
     uint32_t token;             // the call's token in slot 0 (may lie before the sequence's first one: mod 2^32)
     int32_t position;           // of slot 0
-    int32_t page;               // page number; -1: none
+    const int32_t *entry;       // where its number is; null: it has none
     bool good;
 };
 __device__ __forceinline__ Page page_of_item(const Pages &c, uint32_t item)
 {
-    uint32_t first_item = 0;
-    const int32_t b = sequence_of_item(c, item, first_item);
+    const Found f = sequence_of_item(c, item);
+    const Sequence &s = f.s;
     Page p{};
-    if (b < 0) return p;
-    const Sequence s = sequence_of(c, (uint32_t)b, MAX_SEQUENCE);
+    if (f.b < 0) return p;
     if (!s.good) {
         complain(c);
         return p;
     }
     const int32_t begin = s.length - (int32_t)s.count;           // position of the sequence's first token in the call; may be negative
-    const int32_t slot = ((begin >> c.log_page) + (int32_t)(item - first_item));
+    const int32_t slot = ((begin >> c.log_page) + (int32_t)(item - f.first));
     p.position = slot << c.log_page;
     const int32_t lo = begin > p.position ? begin : p.position;
     const int32_t hi = s.length < p.position + (1 << c.log_page) ? s.length : p.position + (1 << c.log_page);
@@ -79,16 +78,18 @@ __device__ __forceinline__ Page page_of_item(const Pages &c, uint32_t item)
     p.first = (uint32_t)(lo - p.position);
     p.end = (uint32_t)(hi - p.position);
     p.token = s.start + (uint32_t)(p.position - begin);
-    p.page = -1;
+    p.entry = slot >= 0 ? c.table + (size_t)f.b * c.table_stride + (uint32_t)slot : nullptr;
     p.good = true;
-    if (slot >= 0) {
-        p.page = c.table[(size_t)b * c.table_stride + (uint32_t)slot];
-        if (p.page < 0 || (uint32_t)p.page >= c.n_pages) {
-            p.page = -1;
-            complain(c);
-        }
-    }
     return p;
+}
+// its number; -1: none, or none of the cache's
+__device__ __forceinline__ int32_t number_of(const Pages &c, const Page &p)
+{
+    if (!p.entry) return -1;
+    const int32_t n = *p.entry;
+    if ((uint32_t)n < c.n_pages) return n;
+    complain(c);
+    return -1;
 }
 
 // A workgroup has one page of one head, keys or values: it alone knows all tokens that the scale depends on, and nothing is
@@ -96,8 +97,8 @@ __device__ __forceinline__ Page page_of_item(const Pages &c, uint32_t item)
 // both ways a thread's codes are two runs of 16 bytes; consecutive threads have consecutive dimensions, so that the loads of a
 // token are one run.  The tiles stay in registers between finding the scale and writing; pages of more than 8192 values are read
 // twice (the second time from the cache).
-// Bound by HBM for prompts (3 bytes a bf16 value) and by its chain of dependent reads for single tokens: starts and lengths, table,
-// old scale and new values.
+// Bound by HBM for prompts (3 bytes a bf16 value) and by its chain of dependent reads for single tokens: starts and lengths, table
+// beside the new values, old scale, old codes.  A workgroup has a thread for each tile, 64 to 256.
 template <int DT, bool V> struct Tile {
     uint32_t slot, dim;         // first slot and dimension
     float x[32];
@@ -175,23 +176,26 @@ template <int DT, bool V>
 __device__ __forceinline__ void write_page(const Pages &c, const Page &p, uint32_t head, const void *in, size_t token_stride, size_t head_stride,
                                            uint32_t *shared)
 {
-    const size_t page_head = (size_t)(uint32_t)p.page * c.heads + head, values = (size_t)c.head_dim << c.log_page;
-    uint8_t *codes = (V ? c.v_codes : c.k_codes) + page_head * values;
-    uint8_t *scales = (V ? c.v_scales : c.k_scales) + page_head;
-    const uint32_t kept = *scales, old = kept < 255 ? kept : 254;
+    const size_t values = (size_t)c.head_dim << c.log_page;
     const uint32_t log_dims = (uint32_t)__builtin_ctz(c.head_dim / (V ? 2u : 16u)), tiles = (uint32_t)(values / 32);
     Tile<DT, V> t;
     uint32_t a = 0;
-    for (uint32_t i = threadIdx.x; i < tiles; i += 256) {
+    const int32_t number = number_of(c, p);
+    for (uint32_t i = threadIdx.x; i < tiles; i += blockDim.x) {
         t.at(i, log_dims);
         t.load(in, token_stride, head * head_stride, p);
         const uint32_t b = t.largest();
         a = a > b ? a : b;
     }
+    if (number < 0) return;
+    const size_t page_head = (size_t)(uint32_t)number * c.heads + head;
+    uint8_t *codes = (V ? c.v_codes : c.k_codes) + page_head * values;
+    uint8_t *scales = (V ? c.v_scales : c.k_scales) + page_head;
+    const uint32_t kept = *scales, old = kept < 255 ? kept : 254;
     a = wave_max(a);
     if ((threadIdx.x & 63) == 0) shared[threadIdx.x >> 6] = a;
     __syncthreads();
-    for (int i = 0; i < 4; ++i) a = a > shared[i] ? a : shared[i];
+    for (uint32_t i = 0; i < blockDim.x / 64; ++i) a = a > shared[i] ? a : shared[i];
     uint32_t byte = scale_byte(a);
     // slots before the first new one hold earlier tokens of the sequence, unless they are slots of negative positions
     const bool held = p.first > 0 && p.position >= 0;
@@ -199,8 +203,8 @@ __device__ __forceinline__ void write_page(const Pages &c, const Page &p, uint32
     if (held && old > byte) byte = old;
     const float inverse = power_of(254 - byte), by = move ? power_of(127 - (byte - old > 126 ? 126 : byte - old)) : 1.0f;
     if (threadIdx.x == 0) *scales = (uint8_t)byte;
-    for (uint32_t i = threadIdx.x; i < tiles; i += 256) {
-        if (tiles > 256) {
+    for (uint32_t i = threadIdx.x; i < tiles; i += blockDim.x) {
+        if (tiles > blockDim.x) {
             t.at(i, log_dims);
             t.load(in, token_stride, head * head_stride, p);
         }
@@ -218,7 +222,7 @@ __global__ void __launch_bounds__(256) cache_write_kernel(Pages c, NewTokens n)
 {
     __shared__ uint32_t shared[4];
     const Page p = page_of_item(c, blockIdx.x);
-    if (!p.good || p.page < 0) return;
+    if (!p.good) return;
     if (blockIdx.z == 0) write_page<DT, false>(c, p, blockIdx.y, n.k, n.k_token, n.k_head, shared);
     else write_page<DT, true>(c, p, blockIdx.y, n.v, n.v_token, n.v_head, shared);
 }
@@ -227,18 +231,19 @@ __global__ void __launch_bounds__(256) cache_write_kernel(Pages c, NewTokens n)
 template <int DT, bool V>
 __device__ __forceinline__ void read_page(const Pages &c, const Page &p, uint32_t head, void *out, size_t token_stride, size_t head_stride)
 {
-    const size_t page_head = (size_t)(uint32_t)(p.page < 0 ? 0 : p.page) * c.heads + head, values = (size_t)c.head_dim << c.log_page;
+    const int32_t number = number_of(c, p);
+    const size_t page_head = (size_t)(uint32_t)(number < 0 ? 0 : number) * c.heads + head, values = (size_t)c.head_dim << c.log_page;
     const uint8_t *codes = (V ? c.v_codes : c.k_codes) + page_head * values;
-    const float scale = p.page < 0 ? 0.0f : power_of((V ? c.v_scales : c.k_scales)[page_head]);
+    const float scale = number < 0 ? 0.0f : power_of((V ? c.v_scales : c.k_scales)[page_head]);
     const uint32_t log_dims = (uint32_t)__builtin_ctz(c.head_dim / (V ? 2u : 16u)), tiles = (uint32_t)(values / 32);
-    for (uint32_t i = threadIdx.x; i < tiles; i += 256) {
+    for (uint32_t i = threadIdx.x; i < tiles; i += blockDim.x) {
         const uint32_t dim = (i & ((1u << log_dims) - 1)) * (V ? 2 : 16), slot = (i >> log_dims) * (V ? 16 : 2);
         if (slot >= p.end || slot + (V ? 16 : 2) <= p.first) continue;
         float x[2][16];
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
             const size_t at = V ? ((size_t)(dim + r) << c.log_page) + slot : (size_t)(slot + r) * c.head_dim + dim;
-            const u32x4 w = p.page < 0 ? u32x4{} : *reinterpret_cast<const u32x4 *>(codes + at);
+            const u32x4 w = number < 0 ? u32x4{} : *reinterpret_cast<const u32x4 *>(codes + at);
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
                 const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w[j], true);
@@ -311,6 +316,13 @@ int pages_of(const enec_cache *cache, const enec_cache_batch *batch, Pages &p)
 }  // namespace lowbit
 }  // namespace enec
 
+// a thread for each tile of a page, in whole waves
+static unsigned threads_of(const Pages &p)
+{
+    const unsigned tiles = (p.head_dim << p.log_page) / 32;
+    return tiles < 64 ? 64 : tiles > 256 ? 256 : tiles;
+}
+
 extern "C" {
 
 int enec_cache_write(const enec_cache *cache, const enec_cache_batch *batch, const void *k, size_t k_token_stride, size_t k_head_stride,
@@ -323,7 +335,7 @@ int enec_cache_write(const enec_cache *cache, const enec_cache_batch *batch, con
     if (!k || !v || (((uintptr_t)k | (uintptr_t)v) & 1)) return ENEC_E_ARG;
     const dim3 grid((p.n_tokens >> p.log_page) + 2 * p.batch, p.heads, 2);
     auto kernel = dtype == ENEC_BF16 ? cache_write_kernel<BF16> : cache_write_kernel<FP16>;
-    kernel<<<grid, 256, 0, (hipStream_t)stream>>>(p, NewTokens{k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride});
+    kernel<<<grid, threads_of(p), 0, (hipStream_t)stream>>>(p, NewTokens{k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride});
     return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
 }
 
@@ -337,7 +349,7 @@ int enec_cache_read(const enec_cache *cache, const enec_cache_batch *batch, void
     if (!k || !v || (((uintptr_t)k | (uintptr_t)v) & (dtype == ENEC_FP32 ? 3 : 1))) return ENEC_E_ARG;
     const dim3 grid((p.n_tokens >> p.log_page) + 2 * p.batch, p.heads, 2);
     auto kernel = dtype == ENEC_BF16 ? cache_read_kernel<BF16> : dtype == ENEC_FP16 ? cache_read_kernel<FP16> : cache_read_kernel<FP32>;
-    kernel<<<grid, 256, 0, (hipStream_t)stream>>>(p, Returned{k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride});
+    kernel<<<grid, threads_of(p), 0, (hipStream_t)stream>>>(p, Returned{k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride});
     return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
 }
 

@@ -55,7 +55,8 @@ int enec_mx4_dequantize(const void *codes, const void *scales, size_t rows, size
  *   codes, scales  DEVICE, an n x k matrix as enec_mx4_quantize writes it
  *   y       DEVICE, m x n values of the same dtype, y_stride (>= n); must not overlap the inputs
  *   workspace      DEVICE, 16-byte aligned, or NULL if workspace_bytes = enec_mx4_linear_workspace(m, n, k) is 0
- * Products are exact and summed in 32 bits; y is rounded once. */
+ * Products are exact and summed in 32 bits; y is rounded once.
+ * ENEC_E_ARG also beyond m = 2^21, n = 2^26, k = 2^21, m k = 2^34 or m n = 2^40. */
 size_t enec_mx4_linear_workspace(size_t m, size_t n, size_t k);
 int enec_mx4_linear(const void *x, size_t m, size_t x_stride, int dtype, const void *codes, const void *scales, size_t n, size_t k,
                     void *y, size_t y_stride, void *workspace, size_t workspace_bytes, void *stream);

@@ -2,6 +2,7 @@
 #pragma once
 
 #include <hip/hip_runtime.h>
+#include <atomic>
 #include <cstdint>
 
 namespace enec {
@@ -104,6 +105,18 @@ inline Divide divide_by(uint32_t d)
 __device__ __forceinline__ uint32_t quotient(uint32_t v, const Divide &d)
 {
     return (uint32_t)(((uint64_t)v * d.mul) >> d.shift);
+}
+
+// More LDS than 64 KB has to be allowed, once for a kernel and device; `allowed` keeps a bit for each device that it is on.
+inline bool allow_lds(const void *kernel, size_t bytes, std::atomic<uint64_t> &allowed)
+{
+    int device = 0;
+    if (hipGetDevice(&device) != hipSuccess) return false;
+    const uint64_t bit = device < 64 ? (uint64_t)1 << device : 0;
+    if (allowed.load(std::memory_order_relaxed) & bit) return true;
+    if (hipFuncSetAttribute(kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)bytes) != hipSuccess) return false;
+    allowed.fetch_or(bit, std::memory_order_relaxed);
+    return true;
 }
 
 }  // namespace lowbit

@@ -684,7 +684,8 @@ template <int DT, int D, int NT> bool launch_few(const Attend &a, uint32_t tiles
     constexpr size_t LDS = JOINED > TILES ? JOINED : TILES;
     static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
     const auto kernel = attend_few_kernel<DT, D, NT, WAVES>;
-    if (LDS > 65536 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS) != hipSuccess) return false;
+    static std::atomic<uint64_t> allowed{0};
+    if (LDS > 65536 && !allow_lds((const void *)kernel, LDS, allowed)) return false;
     kernel<<<dim3(tiles, a.c.heads), 64 * WAVES, LDS, s>>>(a);
     return true;
 }

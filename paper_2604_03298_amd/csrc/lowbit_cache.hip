@@ -139,12 +139,16 @@ template <int DT, bool V> struct Tile {
         }
         return a;
     }
+    __device__ __forceinline__ size_t run_at(int r, uint32_t log_page, uint32_t head_dim) const
+    {
+        return V ? ((size_t)(dim + r) << log_page) + slot : (size_t)(slot + r) * head_dim + dim;
+    }
     // the 16-byte runs: keys, of each token; values, of each dimension.  `move`: earlier codes of the page follow a larger scale.
     __device__ __forceinline__ void store(uint8_t *codes, uint32_t log_page, uint32_t head_dim, const Page &p, float inverse, bool move, float by) const
     {
 #pragma unroll
         for (int r = 0; r < 2; ++r) {
-            const size_t i = V ? ((size_t)(dim + r) << log_page) + slot : (size_t)(slot + r) * head_dim + dim;
+            const size_t i = run_at(r, log_page, head_dim);
             // slots of the run: one (keys) or sixteen (values)
             const uint32_t lo = V ? slot : slot + r, hi = lo + (V ? 16 : 1);
             const bool fresh = hi > p.first && lo < p.end, whole = lo >= p.first && hi <= p.end, older = move && lo < p.first;

@@ -2,7 +2,7 @@
 #include "enec_lowbit.h"
 #include "lowbit.hpp"
 
-#include <type_traits>
+#include <atomic>
 
 namespace enec {
 namespace lowbit {
@@ -75,109 +75,6 @@ __device__ __forceinline__ void store4(void *y, int dtype, size_t at, uint32_t v
     }
 }
 
-// Weights are the left operand, 16 rows, activations the right one, 16 tokens.  A product over a row does not care about the order of
-// its columns, so they are dealt out for the loads: of 512 columns a lane takes 128 in a row, four blocks, whose codes are 64
-// consecutive bytes and whose scales are one word; at step s it multiplies with its block s.
-// The waves of a workgroup share the rows and split the columns; their sums meet in LDS, in a fixed order.
-template <int ACT, int RT, int MT, int W>
-__global__ void __launch_bounds__(64 * W) product_few_kernel(Product a)
-{
-    __shared__ f32x4 sums[W][RT * MT][64];
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, g = lane >> 4, c = lane & 15;
-    const uint32_t n0 = blockIdx.x * (16 * RT), m0 = blockIdx.y * (16 * MT);
-    f32x4 acc[RT][MT] = {};
-    const uint32_t steps = (a.groups + 3) / 4;
-    for (uint32_t step = wave; step < steps; step += W) {
-        const uint32_t group = 4 * step + g;
-        const bool in = group < a.groups;
-        u32x4 w[RT][4] = {};
-        uint32_t ws[RT] = {};
-#pragma unroll
-        for (int t = 0; t < RT; ++t) {
-            const uint32_t row = n0 + 16 * t + c;
-            if (in && row < a.n) {
-                const size_t at = (size_t)row * a.groups + group;
-                ws[t] = reinterpret_cast<const uint32_t *>(a.scales)[at];
-#pragma unroll
-                for (int s = 0; s < 4; ++s) w[t][s] = reinterpret_cast<const u32x4 *>(a.codes)[at * 4 + s];
-            }
-        }
-        if constexpr (ACT == MX4) {
-            u32x4 x[MT][4] = {};
-            uint32_t xs[MT] = {};
-#pragma unroll
-            for (int u = 0; u < MT; ++u) {
-                const uint32_t token = m0 + 16 * u + c;
-                if (in && token < a.m) {
-                    const size_t at = (size_t)token * a.groups + group;
-                    xs[u] = reinterpret_cast<const uint32_t *>(a.x_scales)[at];
-#pragma unroll
-                    for (int s = 0; s < 4; ++s) x[u][s] = static_cast<const u32x4 *>(a.x)[at * 4 + s];
-                }
-            }
-#pragma unroll
-            for (int s = 0; s < 4; ++s)
-#pragma unroll
-                for (int t = 0; t < RT; ++t)
-#pragma unroll
-                    for (int u = 0; u < MT; ++u) acc[t][u] = mfma_mx4(s, w[t][s], x[u][s], acc[t][u], (int)ws[t], (int)xs[u]);
-        } else {
-            const uint16_t *x = static_cast<const uint16_t *>(a.x);
-#pragma unroll
-            for (int s = 0; s < 4; ++s) {
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t col = group * 128 + s * 32 + j * 8;
-                    bf16x8 wv[RT];
-#pragma unroll
-                    for (int t = 0; t < RT; ++t) wv[t] = values_of(w[t][s][j], power_of(ws[t] >> (8 * s) & 255));
-#pragma unroll
-                    for (int u = 0; u < MT; ++u) {
-                        const uint32_t token = m0 + 16 * u + c;
-                        u32x4 v = {};
-                        if (token < a.m) {
-                            const uint16_t *p = x + (size_t)token * a.x_stride + col;
-                            if (col + 8 <= a.k) {
-                                v = *reinterpret_cast<const u32x4_a2 *>(p);
-                            } else {
-                                for (uint32_t i = 0; i < 8; ++i)
-                                    if (col + i < a.k) v[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
-                            }
-                        }
-                        if constexpr (ACT == BF16) {
-                            const bf16x8 xv = __builtin_bit_cast(bf16x8, v);
-#pragma unroll
-                            for (int t = 0; t < RT; ++t) acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[t], xv, acc[t][u], 0, 0, 0);
-                        } else {
-                            bf16x8 hi, lo;
-                            split_fp16(v, hi, lo);
-#pragma unroll
-                            for (int t = 0; t < RT; ++t) {
-                                acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[t], lo, acc[t][u], 0, 0, 0);
-                                acc[t][u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(wv[t], hi, acc[t][u], 0, 0, 0);
-                            }
-                        }
-                    }
-                }
-            }
-        }
-    }
-#pragma unroll
-    for (int t = 0; t < RT; ++t)
-#pragma unroll
-        for (int u = 0; u < MT; ++u) sums[wave][t * MT + u][lane] = acc[t][u];
-    __syncthreads();
-    for (uint32_t i = threadIdx.x; i < RT * MT * 64; i += 64 * W) {
-        const uint32_t tile = i >> 6, l = i & 63;
-        f32x4 v = sums[0][tile][l];
-        for (int w = 1; w < W; ++w) v += sums[w][tile][l];
-        const uint32_t row = n0 + 16 * (tile / MT) + 4 * (l >> 4), token = m0 + 16 * (tile % MT) + (l & 15);
-        if (token < a.m && row < a.n) store4(a.y, a.y_dtype, (size_t)token * a.y_stride + row, a.n - row, v);
-    }
-}
-
-// ---- many tokens -------------------------------------------------------------------------------------------------------
-
 // Memory through a descriptor, whose range the memory unit checks: rows behind a matrix's last one need no branch.  Offsets are 32 bits wide,
 // from a tile's first row.
 using Range = __amdgpu_buffer_rsrc_t;
@@ -204,19 +101,23 @@ template <int ROW> __device__ __forceinline__ uint32_t turn(uint32_t r)
     return 2 * (r >> 3 & 1);
 }
 
-// A workgroup has 16 RT WN rows of weights and 16 MT WM tokens; a wave 16 RT rows and 16 MT tokens of them.  A stage is 128 columns (4-bit activations: 256),
+// Weights are the left operand of the matrix instructions, activations the right one.
+// A workgroup has 16 RT WN rows of weights and 16 MT WM tokens; a wave 16 RT rows and 16 MT tokens of them.  Where there are few tokens the rows of a
+// workgroup are few too, so that all compute units have some, and KG groups of waves take its stages in turn; their sums meet in LDS.  A stage is 128 columns (4-bit activations: 256),
 // whose codes, scales and activations the memory unit brings into LDS, BUFFERS stages in turn.  Loads straight into registers were slower: a lane has
 // a row of its own there, so that each lane's 16 bytes are an access by themselves to the vector cache, where four neighbouring lanes of a copy make one
 // (2048 tokens x 4096 x 16384: 125 million accesses and 272 us then; the cache takes about one in a cycle).
 // As left operand a lane has row lane mod 16, and of a stage's blocks of 32 columns block lane / 16 (or 4 s + lane / 16 at step s).
-template <int ACT, int RT, int MT, int WN, int WM, int BUFFERS>
-__global__ void __launch_bounds__(64 * WN * WM, RT * MT > 32 ? 1 : 2) product_tile_kernel(Product a)
+template <int ACT, int RT, int MT, int WN, int WM, int KG, int BUFFERS>
+__global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) product_tile_kernel(Product a)
 {
-    constexpr int THREADS = 64 * WN * WM, TOKENS = 16 * MT * WM, ROWS = 16 * RT * WN, PLANES = ACT == FP16 ? 2 : 1;
+    constexpr int THREADS = 64 * WN * WM, ALL = THREADS * KG, TOKENS = 16 * MT * WM, ROWS = 16 * RT * WN, PLANES = ACT == FP16 ? 2 : 1;
     constexpr int X_ROW = ACT == MX4 ? 128 : 256, W_ROW = ACT == MX4 ? 128 : 64, X_CHUNKS = X_ROW / 16, W_CHUNKS = W_ROW / 16;
     constexpr int X_SIZE = TOKENS * X_ROW, W_SIZE = ROWS * W_ROW, S_SIZE = ROWS * 16, XS_SIZE = ACT == MX4 ? TOKENS * 16 : 0;
     constexpr uint32_t S_STAGES = ACT == MX4 ? 2 : 4;                    // that sixteen bytes of scales are for
+    constexpr int BLOCKS = KG > (int)S_STAGES ? KG / S_STAGES : 1;       // of scales that a round of stages needs
     constexpr int X_COPIES = X_SIZE / 16 / THREADS, W_COPIES = W_SIZE / 16 / THREADS;
+    static_assert(KG == 1 || KG % S_STAGES == 0, "a round needs whole blocks of scales");
     static_assert(X_SIZE % (16 * THREADS) == 0 && W_SIZE % (16 * THREADS) == 0 && S_SIZE % 256 == 0 && XS_SIZE % 256 == 0, "whole copies of a wave");
     constexpr int U = MT < 4 ? MT : 4, STEPS = ACT == MX4 ? 2 : 4, UNITS = STEPS * (MT / U);
     struct Stage {
@@ -224,9 +125,10 @@ __global__ void __launch_bounds__(64 * WN * WM, RT * MT > 32 ? 1 : 2) product_ti
     };
     extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
     Stage *stage = reinterpret_cast<Stage *>(shared);
-    uint8_t *scale_bytes = shared + BUFFERS * sizeof(Stage);             // two of S_SIZE + XS_SIZE, in turn
+    uint8_t *scale_bytes = shared + BUFFERS * KG * sizeof(Stage);        // two of BLOCKS (S_SIZE + XS_SIZE), in turn
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-    const uint32_t wn = wave % WN, wm = wave / WN;
+    const uint32_t kg = wave / (WN * WM), mate = wave % (WN * WM), thread = threadIdx.x % THREADS;      // wave and thread of the group
+    const uint32_t wn = mate % WN, wm = mate / WN;
     // Workgroups are dealt out to the eight dies one by one.  Each die takes a run of tiles, tokens first, so that it reads few rows of weights.
     const uint32_t tiles = a.n_tiles * a.m_tiles, per_die = (tiles + 7) / 8, tile = blockIdx.x % 8 * per_die + blockIdx.x / 8;
     if (tile >= tiles) return;
@@ -240,31 +142,34 @@ __global__ void __launch_bounds__(64 * WN * WM, RT * MT > 32 ? 1 : 2) product_ti
     const uint32_t first = blockIdx.y * a.split_stages, stages = ACT == MX4 ? (a.groups + 1) / 2 : a.groups;
     const uint32_t end = first + a.split_stages < stages ? first + a.split_stages : stages;
 
-    // (the places of a thread's copies are whole multiples of sixteen rows apart, so its chunk is the same in all of them)
-    const uint32_t x_token = threadIdx.x / X_CHUNKS, w_row = threadIdx.x / W_CHUNKS;
-    const uint32_t x_from = x_token * x_pitch + 16 * ((threadIdx.x % X_CHUNKS) ^ turn<X_ROW>(x_token & 15));
-    const uint32_t w_from = w_row * w_pitch + 16 * ((threadIdx.x % W_CHUNKS) ^ turn<W_ROW>(w_row & 15));
+    // the chunk of row r that belongs to this thread's place
+    auto x_from = [&](uint32_t r) { return r * x_pitch + 16 * ((thread % X_CHUNKS) ^ turn<X_ROW>(r & 15)); };
+    auto w_from = [&](uint32_t r) { return r * w_pitch + 16 * ((thread % W_CHUNKS) ^ turn<W_ROW>(r & 15)); };
     const uint32_t s_from = threadIdx.x / 4 * s_pitch + 4 * (threadIdx.x % 4);
-    auto copy = [&](uint32_t unit) {                        // unit: a stage, or one plane of it
+    auto copy = [&](uint32_t unit, uint32_t buffer) {       // unit: a stage, or one plane of it
         const uint32_t i = unit / PLANES, p = unit % PLANES;
-        Stage *to = stage + unit % BUFFERS;
+        Stage *to = stage + buffer * KG + kg;
 #pragma unroll
         for (int r = 0; r < X_COPIES; ++r)
-            copy_to_lds<16>(x, x_from + r * (THREADS / X_CHUNKS) * x_pitch + i * X_ROW + p * a.x_plane, to->x + (r * THREADS + wave * 64) * 16);
+            copy_to_lds<16>(x, x_from(thread / X_CHUNKS + r * (THREADS / X_CHUNKS)) + i * X_ROW + p * a.x_plane, to->x + (r * THREADS + mate * 64) * 16);
 #pragma unroll
         for (int r = 0; r < W_COPIES; ++r)
-            copy_to_lds<16>(codes, w_from + r * (THREADS / W_CHUNKS) * w_pitch + i * W_ROW, to->w + (r * THREADS + wave * 64) * 16);
+            copy_to_lds<16>(codes, w_from(thread / W_CHUNKS + r * (THREADS / W_CHUNKS)) + i * W_ROW, to->w + (r * THREADS + mate * 64) * 16);
     };
     // Scales come for several stages at once, sixteen bytes of each row: four lanes' words are one access.
-    auto copy_scales = [&](uint32_t block) {
-        uint8_t *to = scale_bytes + (block & 1) * (S_SIZE + XS_SIZE);
+    auto copy_scales = [&](uint32_t block, uint32_t turn_of) {
 #pragma unroll
-        for (int r = 0; r * THREADS * 4 < S_SIZE; ++r)
-            if ((r * THREADS + wave * 64) * 4 < S_SIZE) copy_to_lds<4>(scales, s_from + r * (THREADS / 4) * s_pitch + block * 16, to + (r * THREADS + wave * 64) * 4);
+        for (int k = 0; k < BLOCKS; ++k) {
+            uint8_t *to = scale_bytes + ((turn_of & 1) * BLOCKS + k) * (S_SIZE + XS_SIZE);
 #pragma unroll
-        for (int r = 0; r * THREADS * 4 < XS_SIZE; ++r)
-            if ((r * THREADS + wave * 64) * 4 < XS_SIZE)
-                copy_to_lds<4>(x_scales, s_from + r * (THREADS / 4) * s_pitch + block * 16, to + S_SIZE + (r * THREADS + wave * 64) * 4);
+            for (int r = 0; r * ALL * 4 < S_SIZE; ++r)
+                if ((r * ALL + wave * 64) * 4 < S_SIZE)
+                    copy_to_lds<4>(scales, s_from + r * (ALL / 4) * s_pitch + (block + k) * 16, to + (r * ALL + wave * 64) * 4);
+#pragma unroll
+            for (int r = 0; r * ALL * 4 < XS_SIZE; ++r)
+                if ((r * ALL + wave * 64) * 4 < XS_SIZE)
+                    copy_to_lds<4>(x_scales, s_from + r * (ALL / 4) * s_pitch + (block + k) * 16, to + S_SIZE + (r * ALL + wave * 64) * 4);
+        }
     };
     // A wave's copies are counted, and done in the order in which they were issued: with at most AHEAD left, those before them are in LDS.  Then
     // all waves' are, and nobody reads the stage before any more.
@@ -286,17 +191,25 @@ __global__ void __launch_bounds__(64 * WN * WM, RT * MT > 32 ? 1 : 2) product_ti
     auto w_chunk = [&](const Stage *t, int j, int r) { return *reinterpret_cast<const u32x4 *>(t->w + w_at[j] + r * (16 * W_ROW)); };
 
     f32x4 acc[RT][MT] = {};
-    const uint32_t begin = first * PLANES, finish = end * PLANES;
-    copy_scales(first / S_STAGES);                          // (a split begins with such a block)
-    copy(begin);
-    if (BUFFERS == 3 && begin + 1 < finish) copy(begin + 1);
-    for (uint32_t unit = begin; unit < finish; ++unit) {
-        landed(unit + 1 >= finish);
-        const uint32_t i = unit / PLANES;
-        if (unit % (PLANES * S_STAGES) == 0 && i + S_STAGES < end) copy_scales(i / S_STAGES + 1);
-        if (unit + BUFFERS - 1 < finish) copy(unit + BUFFERS - 1);
-        const Stage *now = stage + unit % BUFFERS;
-        const uint8_t *ws_now = scale_bytes + (i / S_STAGES & 1) * (S_SIZE + XS_SIZE) + (16 / S_STAGES) * (i % S_STAGES);
+    // Group kg takes stages first + kg, first + KG + kg, ..., in rounds that all groups begin together.
+    constexpr uint32_t ROUND = KG > 1 ? KG : 1;
+    const uint32_t rounds = (end - first + ROUND - 1) / ROUND * PLANES, per_block = KG > 1 ? PLANES * (S_STAGES > KG ? S_STAGES / KG : 1) : PLANES * S_STAGES;
+    auto stage_of = [&](uint32_t round) { return first + round / PLANES * ROUND + (KG > 1 ? kg : 0); };
+    auto fetch = [&](uint32_t round) {
+        const uint32_t i = stage_of(round);
+        copy((i < end ? i : end - 1) * PLANES + round % PLANES, round % BUFFERS);
+    };
+    copy_scales(first / S_STAGES, 0);                       // (a split begins with such a block)
+    fetch(0);
+    if (BUFFERS == 3 && rounds > 1) fetch(1);
+    for (uint32_t round = 0; round < rounds; ++round) {
+        landed(round + 1 >= rounds);
+        const uint32_t i = stage_of(round);
+        if (round % per_block == 0 && round + per_block < rounds) copy_scales(first / S_STAGES + (round / per_block + 1) * BLOCKS, round / per_block + 1);
+        if (round + BUFFERS - 1 < rounds) fetch(round + BUFFERS - 1);
+        if (KG > 1 && i >= end) continue;
+        const Stage *now = stage + round % BUFFERS * KG + kg;
+        const uint8_t *ws_now = scale_bytes + ((round / per_block & 1) * BLOCKS + (KG > 1 ? kg / S_STAGES : 0)) * (S_SIZE + XS_SIZE) + (16 / S_STAGES) * (i % S_STAGES);
         // tokens' tiles are taken U at a time; the next ones' chunks are asked for before these are multiplied, and no earlier
         u32x4 xv[2][U];
         if constexpr (ACT == MX4) {
@@ -315,7 +228,7 @@ __global__ void __launch_bounds__(64 * WN * WM, RT * MT > 32 ? 1 : 2) product_ti
                 const u32x2 v = *reinterpret_cast<const u32x2 *>(ws_now + S_SIZE + (wm * (16 * MT) + 16 * u + c) * 16);
                 xs[u] = __builtin_amdgcn_perm(v[1], v[0], pick);
             }
-            if (unit == a.groups / 2) {                                  // one group only: the other's bytes are not this row's
+            if (i == a.groups / 2) {                                     // one group only: the other's bytes are not this row's
 #pragma unroll
                 for (int t = 0; t < RT; ++t) ws[t] &= 255;
 #pragma unroll
@@ -374,6 +287,24 @@ __global__ void __launch_bounds__(64 * WN * WM, RT * MT > 32 ? 1 : 2) product_ti
         }
         __builtin_amdgcn_sched_barrier(0);
     }
+    if constexpr (KG > 1) {                                 // the groups' sums, in their order; LDS is free now
+        f32x4 *sums = reinterpret_cast<f32x4 *>(shared);
+        __syncthreads();
+        if (kg != 0) {
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int u = 0; u < MT; ++u) sums[(((kg - 1) * WN * WM + mate) * RT * MT + t * MT + u) * 64 + lane] = acc[t][u];
+        }
+        __syncthreads();
+        if (kg != 0) return;
+#pragma unroll
+        for (int k = 1; k < KG; ++k)
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int u = 0; u < MT; ++u) acc[t][u] += sums[(((k - 1) * WN * WM + mate) * RT * MT + t * MT + u) * 64 + lane];
+    }
 #pragma unroll
     for (int u = 0; u < MT; ++u) {
         const uint32_t token = m0 + wm * (16 * MT) + 16 * u + c;
@@ -415,15 +346,15 @@ __global__ void __launch_bounds__(256) lay_out_kernel(const uint16_t *__restrict
     }
 }
 
-// The sums of the splits, in their order.
+// The sums of the splits, in their order (none, where there are no columns: zeros).
 __global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ parts, uint32_t splits, uint32_t m, uint32_t n, size_t part_row, Divide per_row,
                                                    void *y, size_t y_stride, int y_dtype)
 {
     const uint32_t at = blockIdx.x * 256u + threadIdx.x, token = quotient(at, per_row), r = (at - token * per_row.by) * 4u;
     if (token >= m) return;
     const float *p = parts + (size_t)token * part_row + r;
-    f32x4 v = *reinterpret_cast<const f32x4 *>(p);
-    for (uint32_t i = 1; i < splits; ++i) v += *reinterpret_cast<const f32x4 *>(p + i * (m * part_row));
+    f32x4 v = {};
+    for (uint32_t i = 0; i < splits; ++i) v += *reinterpret_cast<const f32x4 *>(p + i * (m * part_row));
     store4(y, y_dtype, (size_t)token * y_stride + r, n - r, v);
 }
 
@@ -436,68 +367,75 @@ using namespace enec::lowbit;
 
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
+// The tiles there are.  `resident` workgroups of one fit a compute unit (by LDS), and with all of them there a round of stages, `stages` of them, takes
+// `us` (measured: 16-bit 2048 tokens x 4096 x 16384, both in 4 bits 4096 x 8192 x 32768, and few tokens x 4096 x 11008).
+struct Shape {
+    uint32_t rows, tokens, resident, stages;
+    double us;
+};
+constexpr Shape SHAPES[2][6] = {{{256, 128, 1, 1, 1.92}, {256, 64, 2, 1, 1.93}, {128, 64, 3, 1, 1.52}, {128, 32, 3, 1, 0.90}, {64, 32, 1, 4, 0.80}, {32, 16, 2, 4, 0.60}},
+                                {{256, 256, 1, 1, 2.49}, {128, 128, 2, 1, 1.68}, {128, 64, 2, 1, 1.39}, {128, 32, 2, 1, 0.90}, {64, 32, 1, 4, 0.70}, {32, 16, 2, 4, 0.50}}};
+constexpr uint32_t UNITS = 256;                     // compute units
+
 // How a product is cut up: the tile, and the splits of the columns where tiles alone leave the card empty.
 struct Plan {
-    int kind;                           // 0: the kernel for few tokens
-    uint32_t rows, tokens, splits, split_stages;
+    int shape;
+    uint32_t splits, split_stages;
     size_t laid_out, parts;             // bytes of the workspace
 };
-
-constexpr uint32_t MOST_COLUMNS = 1u << 21;         // offsets inside a tile are 31 bits wide
 
 inline uint32_t up(uint32_t v, uint32_t by) { return (v + by - 1) / by; }
 inline size_t part_row(uint32_t n) { return ((size_t)n + 15) / 16 * 16; }
 
 Plan plan_of(uint32_t m, uint32_t n, uint32_t k, bool mx4)
 {
-    const uint32_t shapes[][2] = {{256, mx4 ? 256u : 128u}, {mx4 ? 128u : 256u, mx4 ? 128u : 64u}, {128, 64}, {128, 32}, {64, 32}};
     Plan p{};
-    // (the counts of vectors that are laid out, and of tiles, have 31 bits)
-    if (m <= 16 || k > MOST_COLUMNS || k == 0 || (uint64_t)m * up(k, 128) >= 1u << 27 || (uint64_t)up(n, 128) * up(m, 32) >= 1u << 27) return p;
-    const uint32_t groups = up(k, 128), unit = mx4 ? 2 : 4, stages = mx4 ? up(groups, 2) : groups;      // a split is whole blocks of scales
-
+    if (!mx4) p.laid_out = 4 * (size_t)m * (up(k, 128) * 128);
+    const uint32_t groups = up(k, 128), unit = 4, stages = mx4 ? up(groups, 2) : groups;     // a split is whole blocks of scales and whole rounds
     double best = 1e300;
-    for (int kind = 1; kind <= 5; ++kind) {
-        const uint32_t rows = shapes[kind - 1][0], tokens = shapes[kind - 1][1];
-        if (tokens > 32 && m <= tokens / 2) continue;
-        const uint64_t tiles = (uint64_t)up(n, rows) * up(m, tokens);
-        for (uint32_t splits = 1; splits <= 16 && splits * unit <= stages && (splits == 1 || (uint64_t)m * up(n, 4) < 1u << 31); splits *= 2) {
-            const uint32_t each = up(up(stages, splits), unit) * unit;
-            const uint64_t rounds = (tiles * up(stages, each) + 511) / 512;
-            // a stage costs its matrix instructions, or bringing its bytes; joining costs the sums' way out and back
-            const double stage = (double)rows * tokens / 128 / 128 + 0.5 + 0.25 * rows / 128;
-            const double cost = rounds * (each + 4.0) * stage + (splits > 1 ? 8 + (double)splits * m * n * 8 / 4e6 : 0);
-            if (cost < best) best = cost, p = {kind, rows, tokens, up(stages, each), each, 0, 0};
+    for (int i = 0; i < 6; ++i) {
+        const Shape &s = SHAPES[mx4][i];
+        if ((i == 5) != (m <= 16)) continue;                 // half of a larger tile would be empty; more of these would read the weights again
+        const uint64_t tiles = (uint64_t)up(n, s.rows) * up(m, s.tokens), slots = (uint64_t)UNITS * s.resident;
+        for (uint32_t splits = 1; splits <= 16 && splits * unit <= (stages > unit ? stages : unit) && (splits == 1 || (uint64_t)m * up(n, 4) < 1u << 31); splits *= 2) {
+            const uint32_t each = up(up(stages, splits), unit) * unit, count = up(stages, each);
+            // a workgroup alone on its compute unit is no faster than 0.6 of that; its start and end are 3 us, and joining is a launch, the sums' way out
+            // and back
+            const double filled = (double)(tiles * count) / slots;
+            const double turns = filled > 1 ? (double)((tiles * count + slots - 1) / slots) : filled > 0.6 ? filled : 0.6;
+            const double us = turns * (up(each, s.stages) * s.us + 3) + (count > 1 ? 4 + (double)count * m * n * 8 / 4e6 : 0);
+            if (us < best) best = us, p.shape = i, p.splits = count, p.split_stages = each;
         }
     }
-    if (!mx4) p.laid_out = 4 * (size_t)m * (up(k, 128) * 128);
     if (p.splits > 1) p.parts = p.splits * (size_t)m * part_row(n) * sizeof(float);
     return p;
 }
 
-template <int ACT, int RT, int MT, int WN, int WM, int BUFFERS> bool launch_tile(const Product &a, uint32_t splits, hipStream_t s)
+template <int ACT, int RT, int MT, int WN, int WM, int KG, int BUFFERS> bool launch_tile(const Product &a, uint32_t splits, hipStream_t s)
 {
     constexpr size_t TOKENS = 16 * MT * WM, ROWS = 16 * RT * WN;
-    constexpr size_t LDS = BUFFERS * (ACT == MX4 ? (TOKENS + ROWS) * 128 : TOKENS * 256 + ROWS * 64) + 2 * 16 * (ACT == MX4 ? TOKENS + ROWS : ROWS);
-    static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
-    const auto kernel = product_tile_kernel<ACT, RT, MT, WN, WM, BUFFERS>;
-    if (LDS > 65536 && hipFuncSetAttribute((const void *)kernel, hipFuncAttributeMaxDynamicSharedMemorySize, (int)LDS) != hipSuccess) return false;
-    kernel<<<dim3(up(a.n_tiles * a.m_tiles, 8) * 8, splits), 64 * WN * WM, LDS, s>>>(a);
+    static std::atomic<uint64_t> allowed{0};
+    constexpr size_t STAGES = BUFFERS * KG * (ACT == MX4 ? (TOKENS + ROWS) * 128 : TOKENS * 256 + ROWS * 64);
+    constexpr size_t BLOCKS = ACT == MX4 && KG == 4 ? 2 : 1, LDS = STAGES + 2 * BLOCKS * 16 * (ACT == MX4 ? TOKENS + ROWS : ROWS);
+    static_assert(LDS <= 160 * 1024 && (KG - 1) * 4 * TOKENS * ROWS <= LDS, "LDS of a compute unit; the groups' sums take the stages' place");
+    const auto kernel = product_tile_kernel<ACT, RT, MT, WN, WM, KG, BUFFERS>;
+    if (LDS > 65536 && !allow_lds((const void *)kernel, LDS, allowed)) return false;
+    kernel<<<dim3(up(a.n_tiles * a.m_tiles, 8) * 8, splits), 64 * WN * WM * KG, LDS, s>>>(a);
     return true;
 }
 
 template <int ACT> int launch(Product a, void *workspace, hipStream_t s)
 {
-    const Plan p = plan_of(a.m, a.n, a.k, ACT == MX4);
-    if (p.kind == 0) {
-        const uint32_t rows = up(a.n, 16);
-        if (a.m <= 16) product_few_kernel<ACT, 1, 1, 4><<<dim3(rows, 1), 256, 0, s>>>(a);
-        else product_few_kernel<ACT, 1, 4, 4><<<dim3(rows, up(a.m, 64)), 256, 0, s>>>(a);
+    if (a.k == 0) {
+        const uint32_t per_row = up(a.n, 4);
+        join_kernel<<<up(a.m * per_row, 256), 256, 0, s>>>(nullptr, 0, a.m, a.n, 0, divide_by(per_row), a.y, a.y_stride, a.y_dtype);
         return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
     }
+    const Plan p = plan_of(a.m, a.n, a.k, ACT == MX4);
+    const Shape &shape = SHAPES[ACT == MX4][p.shape];
     if constexpr (ACT == MX4) {
         a.x_row = a.x_bytes = a.groups * 64;
-    } else if (ACT == BF16 && a.k % 128 == 0 && a.x_stride % 8 == 0 && a.x_stride <= MOST_COLUMNS && aligned(a.x, 16)) {
+    } else if (ACT == BF16 && a.k % 128 == 0 && a.x_stride % 8 == 0 && a.x_stride <= (1u << 22) && aligned(a.x, 16)) {
         a.x_row = a.x_stride * 2, a.x_bytes = a.k * 2;
     } else {
         const uint32_t cols = up(a.k, 128) * 128, n_vec = a.m * (cols / 8);
@@ -507,15 +445,16 @@ template <int ACT> int launch(Product a, void *workspace, hipStream_t s)
         a.x_plane = cols * 2;
         a.x_row = a.x_bytes = ACT == FP16 ? 2 * a.x_plane : a.x_plane;
     }
-    a.n_tiles = up(a.n, p.rows), a.m_tiles = up(a.m, p.tokens), a.split_stages = p.split_stages;
+    a.n_tiles = up(a.n, shape.rows), a.m_tiles = up(a.m, shape.tokens), a.split_stages = p.split_stages;
     if (p.splits > 1) a.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.laid_out), a.part_row = part_row(a.n);
     bool ok;
-    switch (p.kind) {
-    case 1: ok = ACT == MX4 ? launch_tile<ACT, 4, ACT == MX4 ? 8 : 4, 4, 2, 2>(a, p.splits, s) : launch_tile<ACT, 4, 4, 4, 2, 2>(a, p.splits, s); break;
-    case 2: ok = ACT == MX4 ? launch_tile<ACT, 4, 4, 2, 2, 2>(a, p.splits, s) : launch_tile<ACT, 4, 4, 4, 1, 2>(a, p.splits, s); break;
-    case 3: ok = launch_tile<ACT, 2, 4, 4, 1, 2>(a, p.splits, s); break;
-    case 4: ok = launch_tile<ACT, 2, 2, 4, 1, 3>(a, p.splits, s); break;
-    default: ok = launch_tile<ACT, 1, 2, 4, 1, 3>(a, p.splits, s); break;
+    switch (p.shape) {
+    case 0: ok = launch_tile<ACT, 4, ACT == MX4 ? 8 : 4, 4, 2, 1, 2>(a, p.splits, s); break;
+    case 1: ok = launch_tile<ACT, 4, 4, ACT == MX4 ? 2 : 4, ACT == MX4 ? 2 : 1, 1, 2>(a, p.splits, s); break;
+    case 2: ok = launch_tile<ACT, 2, 4, 4, 1, 1, 2>(a, p.splits, s); break;
+    case 3: ok = launch_tile<ACT, 2, 2, 4, 1, 1, 3>(a, p.splits, s); break;
+    case 4: ok = launch_tile<ACT, 1, 2, 4, 1, 4, 2>(a, p.splits, s); break;
+    default: ok = launch_tile<ACT, 1, 1, 2, 1, 4, 3>(a, p.splits, s); break;
     }
     if (!ok) return ENEC_E_HIP;
     if (p.splits > 1) {
@@ -525,8 +464,11 @@ template <int ACT> int launch(Product a, void *workspace, hipStream_t s)
     return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
 }
 
-// sizes that every kernel here can count with: columns in 32 bits with the padding, tokens and rows in a grid
-inline bool sizes_ok(size_t m, size_t n, size_t k) { return m <= (1u << 21) && n <= (1u << 30) && k <= (1u << 30); }
+// sizes that every kernel here can count with: offsets inside a tile have 31 bits, and so have the counts of vectors that are laid out and of tiles
+inline bool sizes_ok(size_t m, size_t n, size_t k)
+{
+    return m <= (1u << 21) && n <= (1u << 26) && k <= (1u << 21) && m * k <= (size_t)1 << 34 && m * n <= (size_t)1 << 40 && (k != 0 || m * n < (size_t)1 << 33);
+}
 
 }  // namespace
 
@@ -534,13 +476,13 @@ extern "C" {
 
 size_t enec_mx4_linear_workspace(size_t m, size_t n, size_t k)
 {
-    if (!sizes_ok(m, n, k) || m == 0 || n == 0) return 0;
+    if (!sizes_ok(m, n, k) || m == 0 || n == 0 || k == 0) return 0;
     const Plan p = plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, false);
     return p.laid_out + p.parts;
 }
 size_t enec_mx4_matmul_workspace(size_t m, size_t n, size_t k)
 {
-    if (!sizes_ok(m, n, k) || m == 0 || n == 0) return 0;
+    if (!sizes_ok(m, n, k) || m == 0 || n == 0 || k == 0) return 0;
     const Plan p = plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, true);
     return p.laid_out + p.parts;
 }

@@ -7,6 +7,7 @@ fallback.  The tensors' shapes are checked here, where C sees pointers only; a w
 from __future__ import annotations
 
 import ctypes as C
+import struct
 
 from . import enec
 from .enec import BF16, E_ARG, E_BLOCK, E_CAPACITY, E_DTYPE, FP16, FP32, OK, strerror  # noqa: F401
@@ -35,7 +36,7 @@ def lib():
     if _lib is None:
         L = enec.lib()
         vp, sz, u32, i = C.c_void_p, C.c_size_t, C.c_uint32, C.c_int
-        cache, batch = C.POINTER(CacheStruct), C.POINTER(BatchStruct)
+        cache, batch = C.POINTER(CacheStruct), vp            # (a batch is handed over packed, see _BATCH)
         for name, result, arguments in (
                 ("enec_mx4_bytes", i, [sz, sz, C.POINTER(sz), C.POINTER(sz)]),
                 ("enec_mx4_quantize", i, [vp, sz, sz, sz, i, vp, vp, vp]),
@@ -68,16 +69,18 @@ def _dtype(t) -> int:
 
 def _rows(t, what):
     """(rows, columns, row stride) of a matrix whose rows are runs."""
-    if t.dim() != 2 or (t.stride(1) != 1 and t.shape[1] > 1):
+    stride = t.stride()
+    if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1):
         raise ValueError(f"{what}: a matrix whose columns lie side by side is wanted")
     rows, cols = t.shape
-    return rows, cols, t.stride(0) if rows > 1 else cols
+    return rows, cols, stride[0] if rows > 1 else cols
 
 
 def _mx4(codes, scales, what):
     """(rows, padded columns) of a matrix in 4 bits."""
     rows, half = codes.shape
-    if half % 64 or scales.shape != (rows, half // 16) or codes.element_size() != 1 or scales.element_size() != 1 \
+    n, blocks = scales.shape
+    if half & 63 or half != 16 * blocks or n != rows or codes.element_size() != 1 or scales.element_size() != 1 \
             or not codes.is_contiguous() or not scales.is_contiguous():
         raise ValueError(f"{what}: codes (rows, padded / 2) and scales (rows, padded / 32) of bytes without gaps are wanted, padded a multiple of 128")
     return rows, 2 * half
@@ -103,7 +106,7 @@ def mx4_empty(rows: int, cols: int, device="cuda") -> tuple:
 
 
 def _same_padding(padded, cols):
-    if padded != -(-cols // 128) * 128:
+    if not 0 <= padded - cols < 128:
         raise ValueError(f"{cols} columns are padded to {-(-cols // 128) * 128}, not {padded}")
 
 
@@ -188,22 +191,28 @@ class Cache:
         return cls(make(*codes), make(*scales), make(n_pages, heads, head_dim, page_tokens), make(*scales))
 
 
+_BATCH = struct.Struct("=QQQIII4xQ")          # a BatchStruct: packed in one go, a structure's fields cost 0.2 us each
+assert _BATCH.size == C.sizeof(BatchStruct)
+
+
 def _batch(table, starts, lengths, n_tokens, status):
-    if table.dim() != 2 or table.element_size() != 4 or starts.element_size() != 4 or lengths.element_size() != 4 \
-            or not table.is_contiguous() or not starts.is_contiguous() or not lengths.is_contiguous():
-        raise ValueError("table (batch, pages), starts and lengths are int32 without gaps")
+    shape = table.shape
     batch = lengths.numel()
-    if table.shape[0] != batch or starts.numel() != batch + 1:
-        raise ValueError("table has a row for each of lengths, starts one entry more")
-    return BatchStruct(table.data_ptr(), starts.data_ptr(), lengths.data_ptr(), table.shape[1], batch, n_tokens,
-                       None if status is None else status.data_ptr())
+    if len(shape) != 2 or shape[0] != batch or starts.numel() != batch + 1:
+        raise ValueError("table (batch, pages) has a row for each of lengths, starts one entry more")
+    if table.element_size() != 4 or starts.element_size() != 4 or lengths.element_size() != 4 \
+            or not table.is_contiguous() or not starts.is_contiguous() or not lengths.is_contiguous():
+        raise ValueError("table, starts and lengths are int32 without gaps")
+    return _BATCH.pack(table.data_ptr(), starts.data_ptr(), lengths.data_ptr(), shape[1], batch, n_tokens,
+                       0 if status is None else status.data_ptr())
 
 
 def _tokens(t, heads, dim, what):
     """(token stride, head stride) of (tokens, heads, head_dim) values."""
-    if t.dim() != 3 or t.shape[1] != heads or t.shape[2] != dim or t.stride(2) != 1:
+    stride = t.stride()
+    if len(stride) != 3 or stride[2] != 1 or t.shape[1:] != (heads, dim):
         raise ValueError(f"{what}: (tokens, {heads}, {dim}) values, a head's side by side, are wanted")
-    return t.stride(0), t.stride(1)
+    return stride[0], stride[1]
 
 
 def _keys_values(cache, k, v):
@@ -218,14 +227,14 @@ def cache_write(cache, k, v, table, starts, lengths, status=None, stream=None) -
     pages), starts (batch + 1) and lengths (batch, new tokens included): int32 on the device; status: None or an int32 word holding 0."""
     ks, vs = _keys_values(cache, k, v)
     b = _batch(table, starts, lengths, k.shape[0], status)
-    return int(lib().enec_cache_write(cache.ref, C.byref(b), k.data_ptr(), *ks, v.data_ptr(), *vs, _dtype(k), enec._stream_handle(stream)))
+    return int(lib().enec_cache_write(cache.ref, b, k.data_ptr(), *ks, v.data_ptr(), *vs, _dtype(k), enec._stream_handle(stream)))
 
 
 def cache_read(cache, k, v, table, starts, lengths, status=None, stream=None) -> int:
     """Enqueues enec_cache_read: the newest tokens' keys and values into k, v (bf16, fp16 or fp32); starts of whole lengths read all."""
     ks, vs = _keys_values(cache, k, v)
     b = _batch(table, starts, lengths, k.shape[0], status)
-    return int(lib().enec_cache_read(cache.ref, C.byref(b), k.data_ptr(), *ks, v.data_ptr(), *vs, _dtype(k), enec._stream_handle(stream)))
+    return int(lib().enec_cache_read(cache.ref, b, k.data_ptr(), *ks, v.data_ptr(), *vs, _dtype(k), enec._stream_handle(stream)))
 
 
 def cache_attention_workspace(cache, batch: int, n_tokens: int, q_heads: int, max_new: int, max_length: int) -> int:
@@ -241,5 +250,5 @@ def cache_attention(cache, q, out, table, starts, lengths, max_new: int, max_len
         raise ValueError("q and out differ in shape or format")
     b = _batch(table, starts, lengths, q.shape[0], status)
     ws, size = _space(workspace)
-    return int(lib().enec_cache_attention(cache.ref, C.byref(b), q.data_ptr(), *qs, out.data_ptr(), *os_, _dtype(q), heads, max_new, max_length,
+    return int(lib().enec_cache_attention(cache.ref, b, q.data_ptr(), *qs, out.data_ptr(), *os_, _dtype(q), heads, max_new, max_length,
                                           cache.head_dim ** -0.5 if scale is None else scale, ws, size, enec._stream_handle(stream)))

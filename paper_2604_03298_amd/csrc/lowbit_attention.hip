@@ -112,17 +112,26 @@ struct Cached {
     uint32_t head;
     bool bad;                                                      // a page number outside the cache was met
 
+    // (pages of 64 tokens and more hold whole tiles: one entry is all)
+    __device__ __forceinline__ bool one() const { return c->log_page >= 6; }
     __device__ __forceinline__ void table_entries(int32_t t0, int32_t (&raw)[4]) const
     {
-#pragma unroll
-        for (int r = 0; r < 4; ++r) {
-            const int32_t t = t0 + 16 * r < length ? t0 + 16 * r : length - 1;        // (a length of zero has no tiles)
-            raw[r] = table[t >> c->log_page];
+        if (one()) {
+            raw[0] = table[(t0 < length ? t0 : length - 1) >> c->log_page];                 // (a length of zero has no tiles)
+            return;
         }
+#pragma unroll
+        for (int r = 0; r < 4; ++r) raw[r] = table[(t0 + 16 * r < length ? t0 + 16 * r : length - 1) >> c->log_page];
     }
     __device__ __forceinline__ Runs runs(int32_t t0, const int32_t (&raw)[4])
     {
         Runs p;
+        if (one()) {
+            const bool in = (uint32_t)raw[0] < c->n_pages;
+            bad |= !in;
+            p.page[0] = p.page[1] = p.page[2] = p.page[3] = in ? raw[0] : -1;
+            return p;
+        }
 #pragma unroll
         for (int r = 0; r < 4; ++r) {
             const bool in = (uint32_t)raw[r] < c->n_pages, there = t0 + 16 * r < length;
@@ -131,6 +140,11 @@ struct Cached {
         }
         return p;
     }
+    // where a page's keys, or values, of the head begin: in page 0, which exists, where there is none
+    __device__ __forceinline__ size_t place_of(int32_t page, uint32_t log_values) const
+    {
+        return ((size_t)(uint32_t)(page < 0 ? 0 : page) * c->heads + head) << log_values;
+    }
 };
 __device__ __forceinline__ int32_t select4(const Runs &p, uint32_t i)
 {
@@ -138,38 +152,48 @@ __device__ __forceinline__ int32_t select4(const Runs &p, uint32_t i)
     return i & 2 ? hi : lo;
 }
 
-// Copies of a tile's keys, or values, into LDS, 1024 bytes an instruction: PARTS waves share them, or one takes all.  No page: page 0, which exists, and
-// whose codes are not looked at.
+// Copies of a tile's keys, or values, into LDS, 1024 bytes an instruction: PARTS waves share them, or one takes all.  What is copied of no page is not
+// looked at.
 template <int D, int PARTS> __device__ __forceinline__ void copy_keys(const Cached &s, const Runs &p, int32_t t0, Tile<D> &to, uint32_t part)
 {
     constexpr int COPIES = D / 16 / PARTS, TOKENS = 1024 / D, OF_RUN = 16 / TOKENS;      // tokens of a copy, copies of a run
+    constexpr uint32_t LOG_D = D == 64 ? 6 : D == 128 ? 7 : 8;
     const Pages &c = *s.c;
     const uint32_t lane = threadIdx.x & 63, mask = (1u << c.log_page) - 1;
-    const size_t head_values = (size_t)D << c.log_page;
+    if (s.one()) {
+        const uint8_t *k = c.k_codes + s.place_of(p.page[0], LOG_D + c.log_page) + (size_t)((t0 & mask) + part * COPIES * TOKENS) * D;
+#pragma unroll
+        for (int r = 0; r < COPIES; ++r) {
+            const uint32_t token = TOKENS * r + lane / (D / 16), chunk = lane % (D / 16) ^ key_turn<D>(part * COPIES * TOKENS + token);
+            copy_to_lds(k + (token * D + 16 * chunk), to.keys + (part * COPIES + r) * 1024);
+        }
+        return;
+    }
 #pragma unroll
     for (int q = 0; q < (COPIES + OF_RUN - 1) / OF_RUN; ++q) {
         const uint32_t run = PARTS == 1 ? q : part * COPIES / OF_RUN + q;
-        const int32_t page = PARTS == 1 ? p.page[q & 3] : select4(p, run);
-        const uint8_t *k = c.k_codes + ((size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + s.head) * head_values + (size_t)((t0 + 16 * run) & mask) * D;
+        const uint8_t *k = c.k_codes + s.place_of(PARTS == 1 ? p.page[q & 3] : select4(p, run), LOG_D + c.log_page) + (size_t)((t0 + 16 * run) & mask) * D;
 #pragma unroll
         for (int r = 0; r < OF_RUN && r < COPIES; ++r) {
             const uint32_t token = TOKENS * r + lane / (D / 16), chunk = lane % (D / 16) ^ key_turn<D>(16 * run + token);
-            copy_to_lds(k + token * D + 16 * chunk, to.keys + (16 * run + TOKENS * r) * D);
+            copy_to_lds(k + (token * D + 16 * chunk), to.keys + (16 * run + TOKENS * r) * D);
         }
     }
 }
 template <int D, int PARTS> __device__ __forceinline__ void copy_values(const Cached &s, const Runs &p, int32_t t0, Tile<D> &to, uint32_t part)
 {
     constexpr int COPIES = D / 16 / PARTS;
+    constexpr uint32_t LOG_D = D == 64 ? 6 : D == 128 ? 7 : 8;
     const Pages &c = *s.c;
     const uint32_t lane = threadIdx.x & 63, mask = (1u << c.log_page) - 1;
-    const uint32_t run = (lane & 3) ^ value_turn(lane >> 2);
-    const int32_t page = select4(p, run);
-    const uint8_t *v = c.v_codes + (((size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + s.head) * D << c.log_page) + ((t0 + 16 * run) & mask);
+    const uint32_t run = (lane & 3) ^ value_turn(lane >> 2), own = ((lane >> 2) << c.log_page) + (s.one() ? 16 * run : 0);
+    const uint8_t *v = c.v_codes;
+    if (s.one()) v += s.place_of(p.page[0], LOG_D + c.log_page) + (t0 & mask);
+    else v += s.place_of(select4(p, run), LOG_D + c.log_page) + ((t0 + 16 * run) & mask);
 #pragma unroll
     for (int r = 0; r < COPIES; ++r) {
         const uint32_t n = part * COPIES + r;
-        copy_to_lds(v + ((n * 16 + (lane >> 2)) << c.log_page), to.values + n * 1024);
+        copy_to_lds(v + ((size_t)(n * 16) << c.log_page) + own, to.values + n * 1024);
     }
 }
 

@@ -120,12 +120,10 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
     static_assert(KG == 1 || KG % S_STAGES == 0, "a round needs whole blocks of scales");
     static_assert(X_SIZE % (16 * THREADS) == 0 && W_SIZE % (16 * THREADS) == 0 && S_SIZE % 256 == 0 && XS_SIZE % 256 == 0, "whole copies of a wave");
     constexpr int U = MT < 4 ? MT : 4, STEPS = ACT == MX4 ? 2 : 4, UNITS = STEPS * (MT / U);
-    struct Stage {
-        uint8_t x[X_SIZE], w[W_SIZE];
-    };
+    constexpr int W_BUFFERS = PLANES == 2 ? 2 : BUFFERS;                 // (both planes of a stage are multiplied with the same weights)
     extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
-    Stage *stage = reinterpret_cast<Stage *>(shared);
-    uint8_t *scale_bytes = shared + BUFFERS * KG * sizeof(Stage);        // two of BLOCKS (S_SIZE + XS_SIZE), in turn
+    uint8_t *x_stages = shared, *w_stages = shared + BUFFERS * KG * X_SIZE;
+    uint8_t *scale_bytes = w_stages + W_BUFFERS * KG * W_SIZE;           // two of BLOCKS (S_SIZE + XS_SIZE), in turn
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
     const uint32_t kg = wave / (WN * WM), mate = wave % (WN * WM), thread = threadIdx.x % THREADS;      // wave and thread of the group
     const uint32_t wn = mate % WN, wm = mate / WN;
@@ -146,15 +144,15 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
     auto x_from = [&](uint32_t r) { return r * x_pitch + 16 * ((thread % X_CHUNKS) ^ turn<X_ROW>(r & 15)); };
     auto w_from = [&](uint32_t r) { return r * w_pitch + 16 * ((thread % W_CHUNKS) ^ turn<W_ROW>(r & 15)); };
     const uint32_t s_from = threadIdx.x / 4 * s_pitch + 4 * (threadIdx.x % 4);
-    auto copy = [&](uint32_t unit, uint32_t buffer) {       // unit: a stage, or one plane of it
-        const uint32_t i = unit / PLANES, p = unit % PLANES;
-        Stage *to = stage + buffer * KG + kg;
+    auto copy = [&](uint32_t i, uint32_t plane, uint32_t x_buffer, uint32_t w_buffer) {
+        uint8_t *x_to = x_stages + (x_buffer * KG + kg) * X_SIZE, *w_to = w_stages + (w_buffer * KG + kg) * W_SIZE;
 #pragma unroll
         for (int r = 0; r < X_COPIES; ++r)
-            copy_to_lds<16>(x, x_from(thread / X_CHUNKS + r * (THREADS / X_CHUNKS)) + i * X_ROW + p * a.x_plane, to->x + (r * THREADS + mate * 64) * 16);
+            copy_to_lds<16>(x, x_from(thread / X_CHUNKS + r * (THREADS / X_CHUNKS)) + i * X_ROW + plane * a.x_plane, x_to + (r * THREADS + mate * 64) * 16);
+        if (plane != 0) return;
 #pragma unroll
         for (int r = 0; r < W_COPIES; ++r)
-            copy_to_lds<16>(codes, w_from(thread / W_CHUNKS + r * (THREADS / W_CHUNKS)) + i * W_ROW, to->w + (r * THREADS + mate * 64) * 16);
+            copy_to_lds<16>(codes, w_from(thread / W_CHUNKS + r * (THREADS / W_CHUNKS)) + i * W_ROW, w_to + (r * THREADS + mate * 64) * 16);
     };
     // Scales come for several stages at once, sixteen bytes of each row: four lanes' words are one access.
     auto copy_scales = [&](uint32_t block, uint32_t turn_of) {
@@ -173,7 +171,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
     };
     // A wave's copies are counted, and done in the order in which they were issued: with at most AHEAD left, those before them are in LDS.  Then
     // all waves' are, and nobody reads the stage before any more.
-    constexpr int AHEAD = (BUFFERS - 2) * (X_COPIES + W_COPIES);         // (scales' copies make it more)
+    constexpr int AHEAD = (BUFFERS - 2) * (PLANES == 2 ? X_COPIES : X_COPIES + W_COPIES);         // at least so many copies are of the next round
     auto landed = [&](bool last) {
         __builtin_amdgcn_sched_barrier(0);
         if (AHEAD == 0 || last) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -187,8 +185,8 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
     for (int j = 0; j < STEPS; ++j) x_at[j] = (wm * (16 * MT) + c) * X_ROW + (((ACT == MX4 ? 4 * j + g : 4 * g + j) ^ turn<X_ROW>(c)) << 4);
 #pragma unroll
     for (int j = 0; j < 2; ++j) w_at[j] = (wn * (16 * RT) + c) * W_ROW + (((ACT == MX4 ? 4 * j + g : g) ^ turn<W_ROW>(c)) << 4);
-    auto x_chunk = [&](const Stage *t, int j, int u) { return *reinterpret_cast<const u32x4 *>(t->x + x_at[j] + u * (16 * X_ROW)); };
-    auto w_chunk = [&](const Stage *t, int j, int r) { return *reinterpret_cast<const u32x4 *>(t->w + w_at[j] + r * (16 * W_ROW)); };
+    auto x_chunk = [&](const uint8_t *t, int j, int u) { return *reinterpret_cast<const u32x4 *>(t + x_at[j] + u * (16 * X_ROW)); };
+    auto w_chunk = [&](const uint8_t *t, int j, int r) { return *reinterpret_cast<const u32x4 *>(t + w_at[j] + r * (16 * W_ROW)); };
 
     f32x4 acc[RT][MT] = {};
     // Group kg takes stages first + kg, first + KG + kg, ..., in rounds that all groups begin together.
@@ -197,7 +195,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
     auto stage_of = [&](uint32_t round) { return first + round / PLANES * ROUND + (KG > 1 ? kg : 0); };
     auto fetch = [&](uint32_t round) {
         const uint32_t i = stage_of(round);
-        copy((i < end ? i : end - 1) * PLANES + round % PLANES, round % BUFFERS);
+        copy(i < end ? i : end - 1, round % PLANES, round % BUFFERS, round / PLANES % W_BUFFERS);
     };
     copy_scales(first / S_STAGES, 0);                       // (a split begins with such a block)
     fetch(0);
@@ -208,7 +206,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
         if (round % per_block == 0 && round + per_block < rounds) copy_scales(first / S_STAGES + (round / per_block + 1) * BLOCKS, round / per_block + 1);
         if (round + BUFFERS - 1 < rounds) fetch(round + BUFFERS - 1);
         if (KG > 1 && i >= end) continue;
-        const Stage *now = stage + round % BUFFERS * KG + kg;
+        const uint8_t *x_now = x_stages + (round % BUFFERS * KG + kg) * X_SIZE, *w_now = w_stages + (round / PLANES % W_BUFFERS * KG + kg) * W_SIZE;
         const uint8_t *ws_now = scale_bytes + ((round / per_block & 1) * BLOCKS + (KG > 1 ? kg / S_STAGES : 0)) * (S_SIZE + XS_SIZE) + (16 / S_STAGES) * (i % S_STAGES);
         // tokens' tiles are taken U at a time; the next ones' chunks are asked for before these are multiplied, and no earlier
         u32x4 xv[2][U];
@@ -217,7 +215,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
             uint32_t ws[RT], xs[MT];
             const uint32_t pick = 0x0c0c0400u + 0x101u * g;              // of a row's eight bytes this lane's block's two
 #pragma unroll
-            for (int t = 0; t < RT; ++t) w[0][t] = w_chunk(now, 0, t);
+            for (int t = 0; t < RT; ++t) w[0][t] = w_chunk(w_now, 0, t);
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
                 const u32x2 v = *reinterpret_cast<const u32x2 *>(ws_now + (wn * (16 * RT) + 16 * t + c) * 16);
@@ -235,18 +233,18 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
                 for (int u = 0; u < MT; ++u) xs[u] &= 255;
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) xv[0][u] = x_chunk(now, 0, u);
+            for (int u = 0; u < U; ++u) xv[0][u] = x_chunk(x_now, 0, u);
 #pragma unroll
             for (int k = 0; k < UNITS; ++k) {
                 const int s = k / (MT / U), b = k % (MT / U), next = k + 1;
                 __builtin_amdgcn_sched_barrier(0);
                 if (next < UNITS) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) xv[next & 1][u] = x_chunk(now, next / (MT / U), next % (MT / U) * U + u);
+                    for (int u = 0; u < U; ++u) xv[next & 1][u] = x_chunk(x_now, next / (MT / U), next % (MT / U) * U + u);
                 }
                 if (k == 0) {
 #pragma unroll
-                    for (int t = 0; t < RT; ++t) w[1][t] = w_chunk(now, 1, t);
+                    for (int t = 0; t < RT; ++t) w[1][t] = w_chunk(w_now, 1, t);
                 }
 #pragma unroll
                 for (int u = 0; u < U; ++u)
@@ -259,11 +257,11 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
             bf16x8 wv[2][RT];
 #pragma unroll
             for (int t = 0; t < RT; ++t) {
-                w[t] = w_chunk(now, 0, t);
+                w[t] = w_chunk(w_now, 0, t);
                 ws[t] = ws_now[(wn * (16 * RT) + 16 * t + c) * 16 + g];
             }
 #pragma unroll
-            for (int u = 0; u < U; ++u) xv[0][u] = x_chunk(now, 0, u);
+            for (int u = 0; u < U; ++u) xv[0][u] = x_chunk(x_now, 0, u);
 #pragma unroll
             for (int t = 0; t < RT; ++t) wv[0][t] = values_of(w[t][0], f32_of_bits(ws[t] << 23));
 #pragma unroll
@@ -272,7 +270,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
                 __builtin_amdgcn_sched_barrier(0);
                 if (next < UNITS) {
 #pragma unroll
-                    for (int u = 0; u < U; ++u) xv[next & 1][u] = x_chunk(now, next / (MT / U), next % (MT / U) * U + u);
+                    for (int u = 0; u < U; ++u) xv[next & 1][u] = x_chunk(x_now, next / (MT / U), next % (MT / U) * U + u);
                 }
                 if (b == MT / U - 1 && j < 3) {
 #pragma unroll
@@ -332,9 +330,12 @@ __global__ void __launch_bounds__(256) lay_out_kernel(const uint16_t *__restrict
     u32x4 v = {};
     if (col + 8 <= k) {
         v = *reinterpret_cast<const u32x4_a2 *>(p);
-    } else {
-        for (uint32_t i = 0; i < 8; ++i)
-            if (col + i < k) v[i >> 1] |= (uint32_t)p[i] << (16 * (i & 1));
+    } else if (col < k) {                                   // (loads that do not wait for one another)
+        uint32_t e[8];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) e[i] = p[col + i < k ? i : k - 1 - col];
+#pragma unroll
+        for (uint32_t i = 0; i < 8; ++i) v[i >> 1] |= (col + i < k ? e[i] : 0) << (16 * (i & 1));
     }
     if constexpr (DT == BF16) {
         out[at] = v;
@@ -368,13 +369,13 @@ using namespace enec::lowbit;
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 // The tiles there are.  `resident` workgroups of one fit a compute unit (by LDS), and with all of them there a round of stages, `stages` of them, takes
-// `us` (measured: 16-bit 2048 tokens x 4096 x 16384, both in 4 bits 4096 x 8192 x 32768, and few tokens x 4096 x 11008).
+// `us` (measured: 1 to 3000 tokens with matrices of 4096 x 1024 to 11008).
 struct Shape {
     uint32_t rows, tokens, resident, stages;
     double us;
 };
-constexpr Shape SHAPES[2][6] = {{{256, 128, 1, 1, 1.92}, {256, 64, 2, 1, 1.93}, {128, 64, 3, 1, 1.52}, {128, 32, 3, 1, 0.90}, {64, 32, 1, 4, 0.80}, {32, 16, 2, 4, 0.60}},
-                                {{256, 256, 1, 1, 2.49}, {128, 128, 2, 1, 1.68}, {128, 64, 2, 1, 1.39}, {128, 32, 2, 1, 0.90}, {64, 32, 1, 4, 0.70}, {32, 16, 2, 4, 0.50}}};
+constexpr Shape SHAPES[2][6] = {{{256, 128, 1, 1, 1.92}, {256, 64, 2, 1, 1.90}, {128, 64, 3, 1, 1.48}, {128, 32, 3, 1, 1.20}, {64, 32, 1, 4, 0.70}, {32, 16, 2, 4, 0.60}},
+                                {{256, 256, 1, 1, 2.49}, {128, 128, 2, 1, 1.50}, {128, 64, 2, 1, 1.39}, {128, 32, 2, 1, 0.90}, {64, 32, 1, 4, 0.60}, {32, 16, 2, 4, 0.50}}};
 constexpr uint32_t UNITS = 256;                     // compute units
 
 // How a product is cut up: the tile, and the splits of the columns where tiles alone leave the card empty.
@@ -395,14 +396,15 @@ Plan plan_of(uint32_t m, uint32_t n, uint32_t k, bool mx4)
     double best = 1e300;
     for (int i = 0; i < 6; ++i) {
         const Shape &s = SHAPES[mx4][i];
-        if ((i == 5) != (m <= 16)) continue;                 // half of a larger tile would be empty; more of these would read the weights again
-        const uint64_t tiles = (uint64_t)up(n, s.rows) * up(m, s.tokens), slots = (uint64_t)UNITS * s.resident;
+        const uint64_t tiles = (uint64_t)up(n, s.rows) * up(m, s.tokens);
         for (uint32_t splits = 1; splits <= 16 && splits * unit <= (stages > unit ? stages : unit) && (splits == 1 || (uint64_t)m * up(n, 4) < 1u << 31); splits *= 2) {
             const uint32_t each = up(up(stages, splits), unit) * unit, count = up(stages, each);
-            // a workgroup alone on its compute unit is no faster than 0.6 of that; its start and end are 3 us, and joining is a launch, the sums' way out
-            // and back
-            const double filled = (double)(tiles * count) / slots;
-            const double turns = filled > 1 ? (double)((tiles * count + slots - 1) / slots) : filled > 0.6 ? filled : 0.6;
+            // The busiest compute unit has `most` workgroups.  Fewer than fit take their share of the time and a little more; where one fits and not all
+            // units have one, memory has less to do; past two rounds the units drift apart and no one waits.  A workgroup's start and end are 3 us, and joining is a launch, the sums' way out and back.
+            const uint64_t all = tiles * count, most = (all + UNITS - 1) / UNITS, left = most % s.resident;
+            double turns = (double)(most / s.resident) + (left ? (double)left / s.resident + 0.07 : 0);
+            if (s.resident == 1 && all * 4 < most * UNITS * 3) turns *= 0.88;
+            if (turns > 2) turns = (double)all / UNITS / s.resident;
             const double us = turns * (up(each, s.stages) * s.us + 3) + (count > 1 ? 4 + (double)count * m * n * 8 / 4e6 : 0);
             if (us < best) best = us, p.shape = i, p.splits = count, p.split_stages = each;
         }
@@ -415,7 +417,7 @@ template <int ACT, int RT, int MT, int WN, int WM, int KG, int BUFFERS> bool lau
 {
     constexpr size_t TOKENS = 16 * MT * WM, ROWS = 16 * RT * WN;
     static std::atomic<uint64_t> allowed{0};
-    constexpr size_t STAGES = BUFFERS * KG * (ACT == MX4 ? (TOKENS + ROWS) * 128 : TOKENS * 256 + ROWS * 64);
+    constexpr size_t STAGES = KG * (BUFFERS * TOKENS * (ACT == MX4 ? 128 : 256) + (ACT == FP16 ? 2 : BUFFERS) * ROWS * (ACT == MX4 ? 128 : 64));
     constexpr size_t BLOCKS = ACT == MX4 && KG == 4 ? 2 : 1, LDS = STAGES + 2 * BLOCKS * 16 * (ACT == MX4 ? TOKENS + ROWS : ROWS);
     static_assert(LDS <= 160 * 1024 && (KG - 1) * 4 * TOKENS * ROWS <= LDS, "LDS of a compute unit; the groups' sums take the stages' place");
     const auto kernel = product_tile_kernel<ACT, RT, MT, WN, WM, KG, BUFFERS>;

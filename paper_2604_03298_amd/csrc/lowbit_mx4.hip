@@ -22,8 +22,11 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const void *__restric
         const size_t i = (size_t)row * stride + col;
         if (at < n_vec && col + 8 <= cols) {
             load8<DT>(in, i, v[u]);
+        } else if (at < n_vec && col < cols) {              // (loads that do not wait for one another)
+            for (int j = 0; j < 8; ++j) v[u][j] = load1<DT>(in, i + (col + j < cols ? j : cols - 1 - col));
+            for (int j = 0; j < 8; ++j) v[u][j] = col + j < cols ? v[u][j] : 0.0f;
         } else {
-            for (int j = 0; j < 8; ++j) v[u][j] = at < n_vec && col + j < cols ? load1<DT>(in, i + j) : 0.0f;
+            for (int j = 0; j < 8; ++j) v[u][j] = 0.0f;
         }
     }
     for (int u = 0; u < U; ++u) {

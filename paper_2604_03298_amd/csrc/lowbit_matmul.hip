@@ -374,7 +374,7 @@ struct Shape {
     uint32_t rows, tokens, resident, stages;
     double us;
 };
-constexpr Shape SHAPES[2][6] = {{{256, 128, 1, 1, 1.92}, {256, 64, 2, 1, 1.90}, {128, 64, 3, 1, 1.48}, {128, 32, 3, 1, 1.20}, {64, 32, 1, 4, 0.70}, {32, 16, 2, 4, 0.60}},
+constexpr Shape SHAPES[2][6] = {{{256, 128, 1, 1, 1.72}, {256, 64, 2, 1, 1.85}, {128, 64, 3, 1, 1.48}, {128, 32, 3, 1, 1.20}, {64, 32, 1, 4, 0.70}, {32, 16, 2, 4, 0.60}},
                                 {{256, 256, 1, 1, 2.49}, {128, 128, 2, 1, 1.50}, {128, 64, 2, 1, 1.39}, {128, 32, 2, 1, 0.90}, {64, 32, 1, 4, 0.60}, {32, 16, 2, 4, 0.50}}};
 constexpr uint32_t UNITS = 256;                     // compute units
 

@@ -73,7 +73,7 @@ int enec_mx4_matmul(const void *x_codes, const void *x_scales, size_t m, const v
  *   k_codes   n_pages x kv_heads x page_tokens x head_dim bytes
  *   v_codes   n_pages x kv_heads x head_dim x page_tokens bytes   (a head's values, transposed: a product over tokens reads runs)
  *   k_scales, v_scales  n_pages x kv_heads bytes
- * page_tokens is a power of two from 16 to 256, head_dim 64, 128 or 256.  Which pages a sequence owns says
+ * n_pages is at least 1, page_tokens a power of two from 16 to 256, head_dim 64, 128 or 256.  Which pages a sequence owns says
  *   table     DEVICE, int32, batch rows of table_stride entries: entry i is the page of tokens i page_tokens ...
  * A batch of sequences is described by
  *   starts    DEVICE, int32, batch + 1 entries, ascending from 0 to n_tokens: where the sequence's tokens begin among those the
@@ -82,9 +82,9 @@ int enec_mx4_matmul(const void *x_codes, const void *x_scales, size_t m, const v
  * so token i of a sequence's t tokens in the call has position lengths[b] - t + i.  A negative position (an idle slot of a batch,
  * with length 0) belongs to no page: such a token is not stored, reads back as zeros, and its attention is zeros.
  * What only the device can see is checked there.  A sequence whose starts are out of order, or whose length exceeds
- * table_stride * page_tokens or 2^30 (attention: or max_length, or whose tokens in the call exceed max_new), is left out: nothing of it is stored or returned.  The tokens of a
- * page whose number lies outside the cache are not stored, read back as zeros and are not seen.  In both cases ENEC_E_ARG is
- * stored to
+ * table_stride * page_tokens or 2^30 (attention: or max_length, or whose tokens in the call exceed max_new), is left out: nothing of
+ * it is stored or returned.  The tokens of a page whose number lies outside the cache are not stored, read back as zeros and are not
+ * seen.  In both cases ENEC_E_ARG is stored to
  *   status    NULL, or a DEVICE-ACCESSIBLE word that the caller has set to 0
  */
 typedef struct {
@@ -119,7 +119,7 @@ int enec_cache_read(const enec_cache *cache, const enec_cache_batch *batch, void
  *   q, out  DEVICE, n_tokens x q_heads x head_dim values (bf16 or fp16), token and head strides; must not overlap
  *   q_heads a multiple of kv_heads
  *   max_new, max_length  HOST: no sequence has more tokens in the call, or more in all (they shape the launch)
- *   scale   above zero, usually head_dim^-1/2
+ *   scale   above zero and finite, usually head_dim^-1/2
  *   workspace  DEVICE, 16-byte aligned, or NULL if workspace_bytes = enec_cache_attention_workspace(...) is 0
  * Scores, softmax and sums are held in 32 bits; the probabilities are rounded to bf16 for the product with v (to the sum of two
  * bf16 numbers for fp16 tensors). */

@@ -2,6 +2,8 @@
 #include "enec_lowbit.h"
 #include "lowbit_pages.hpp"
 
+#include <cmath>
+
 namespace enec {
 namespace lowbit {
 
@@ -757,7 +759,7 @@ int enec_cache_attention(const enec_cache *cache, const enec_cache_batch *batch,
     if (const int rc = pages_of(cache, batch, a.c)) return rc;
     if (!shape_ok(cache, a.c.batch, a.c.n_tokens, q_heads, max_new, max_length)) return ENEC_E_ARG;
     if (a.c.batch == 0 || a.c.n_tokens == 0) return ENEC_OK;
-    if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 1) || max_new == 0 || !(scale > 0)) return ENEC_E_ARG;
+    if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 1) || max_new == 0 || !(scale > 0) || !std::isfinite(scale)) return ENEC_E_ARG;
     const uint32_t group = q_heads / a.c.heads;
     const Plan p = plan_of(a.c.batch, a.c.heads, group, a.c.head_dim, max_new, max_length);
     if ((uint64_t)p.splits * a.c.batch * p.row_tiles > 0x3FFFFFFFu / a.c.heads) return ENEC_E_ARG;

@@ -103,9 +103,9 @@ def test_caches_that_are_refused(lowbit):
         c, b = structs(**s)
         return L.enec_cache_read(C.byref(c), C.byref(b), k, 512, 128, v, 512, 128, dtype, None)
 
-    def attend(k=P, v=P, dtype=0, q_heads=8, new=1, most=500, ws=P, size=1 << 40, **s):
+    def attend(k=P, v=P, dtype=0, q_heads=8, new=1, most=500, ws=P, size=1 << 40, scale=0.1, **s):
         c, b = structs(**s)
-        return L.enec_cache_attention(C.byref(c), C.byref(b), k, 1024, 128, v, 1024, 128, dtype, q_heads, new, most, 0.1, ws, size, None)
+        return L.enec_cache_attention(C.byref(c), C.byref(b), k, 1024, 128, v, 1024, 128, dtype, q_heads, new, most, scale, ws, size, None)
 
     for call in (write, read, attend):
         for page in (0, 1, 8, 24, 100, 512):
@@ -117,6 +117,7 @@ def test_caches_that_are_refused(lowbit):
                     {"stride": 0}, {"heads": 0}, {"heads": 70000}, {"batch": 70000}, {"tokens": 1 << 31}, {"pages": 1 << 31}, {"k": None}, {"v": None},
                     {"k": ODD}, {"v": ODD}):
             assert call(**bad) == lowbit.E_ARG, bad
+        assert call(pages=0) == lowbit.E_ARG
         assert call(dtype=3) == call(dtype=-1) == lowbit.E_DTYPE
         assert call(batch=0) == call(tokens=0) == lowbit.OK
         assert call(batch=0, table=None, starts=None, lengths=None) == lowbit.OK
@@ -124,6 +125,8 @@ def test_caches_that_are_refused(lowbit):
     assert read(dtype=2, k=0x1002) == lowbit.E_ARG
     for bad in ({"q_heads": 0}, {"q_heads": 6}, {"q_heads": 1 << 20}, {"new": 0}, {"new": 1 << 31}, {"most": (1 << 30) + 1}):
         assert attend(**bad) == lowbit.E_ARG, bad
+    for scale in (0.0, -0.1, float("nan"), float("inf")):
+        assert attend(scale=scale) == lowbit.E_ARG, scale
     assert L.enec_cache_write(None, None, P, 1, 1, P, 1, 1, 0, None) == lowbit.E_ARG
     c, _ = structs()
     need = L.enec_cache_attention_workspace(C.byref(c), 3, 3, 8, 1, 100000)

@@ -79,7 +79,8 @@ int enec_mx4_matmul(const void *x_codes, const void *x_scales, size_t m, const v
  *   starts    DEVICE, int32, batch + 1 entries, ascending from 0 to n_tokens: where the sequence's tokens begin among those the
  *             call takes or returns, which are the newest of their sequence
  *   lengths   DEVICE, int32, batch entries: tokens of the sequence, those of the call among them
- * so token i of a sequence's t tokens in the call has position lengths[b] - t + i.  A negative position (an idle slot of a batch,
+ * batch and kv_heads are at most 65535 and n_tokens below 2^24.
+ * Token i of a sequence's t tokens in the call has position lengths[b] - t + i.  A negative position (an idle slot of a batch,
  * with length 0) belongs to no page: such a token is not stored, reads back as zeros, and its attention is zeros.
  * What only the device can see is checked there.  A sequence whose starts are out of order, or whose length exceeds
  * table_stride * page_tokens or 2^30 (attention: or max_length, or whose tokens in the call exceed max_new), is left out: nothing of
@@ -119,6 +120,7 @@ int enec_cache_read(const enec_cache *cache, const enec_cache_batch *batch, void
  *   q, out  DEVICE, n_tokens x q_heads x head_dim values (bf16 or fp16), token and head strides; must not overlap
  *   q_heads a multiple of kv_heads
  *   max_new, max_length  HOST: no sequence has more tokens in the call, or more in all (they shape the launch)
+ *           ENEC_E_ARG from max_new (q_heads / kv_heads) = 2^21 or batch kv_heads = 2^23 on
  *   scale   above zero and finite, usually head_dim^-1/2
  *   workspace  DEVICE, 16-byte aligned, or NULL if workspace_bytes = enec_cache_attention_workspace(...) is 0
  * Scores, softmax and sums are held in 32 bits; the probabilities are rounded to bf16 for the product with v (to the sum of two

@@ -28,6 +28,17 @@ __device__ __forceinline__ Sequence sequence_of(const Attend &a, uint32_t b)
     return s;
 }
 
+// What a row's sum is multiplied with in the end.  The weights' sum is zero where no score is above minus infinity: such a row has no softmax (NaN), unless
+// it sees no token at all.
+__device__ __forceinline__ float share_of(const Attend &a, const Sequence &s, uint32_t b, uint32_t token, float total)
+{
+    if (total != 0) return 1.0f / total;                     // (NaN too)
+    const int32_t *table = a.c.table + (size_t)b * a.c.table_stride;
+    for (int32_t at = s.length - (int32_t)s.count + (int32_t)token; at >= 0; at -= 1 << a.c.log_page)
+        if ((uint32_t)table[at >> a.c.log_page] < a.c.n_pages) return __builtin_nanf("");
+    return 0;
+}
+
 // The largest of four lanes sixteen apart.  The exchanges swap rows of lanes of two registers that hold the same; as instructions of their own, since the
 // compiler takes the two results for equal.
 __device__ __forceinline__ float over_groups_max(float v)
@@ -475,7 +486,7 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
         __builtin_amdgcn_sched_barrier(0);
         f32x4 x[NT][4];
         r.scores(tile, x);
-        const float by = power_of(k_byte) * a.scale, vs = power_of(v_byte);
+        const float by = power_of(k_byte) * a.scale, vs = page >= 0 ? power_of(v_byte) : 1.0f;       // (no page: another one's, and 0 * NaN would be one)
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (the keys have been read)
         if (more) ask_keys(t0 + STEP);
@@ -530,7 +541,7 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
             for (int w = 1; w < WAVES; ++w) sum += sums[(w * 16 * NT + row) * 17 + d4];
             const uint32_t token = quotient(out_row, a.group), q_head = head * a.group.by + (out_row - token * a.group.by), d = 64 * i + 4 * d4;
             if (a.splits == 1) {
-                const float by = total == 0 ? 0.0f : 1.0f / total;
+                const float by = share_of(a, s, b, token, total);
                 uint16_t *p = static_cast<uint16_t *>(a.out) + (size_t)(s.start + token) * a.out_token + (size_t)q_head * a.out_head + d;
                 *reinterpret_cast<u32x2_a2 *>(p) = u32x2{pack2<DT>(sum[0] * by, sum[1] * by), pack2<DT>(sum[2] * by, sum[3] * by)};
             } else {
@@ -556,8 +567,8 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, col = lane & 15;
     // The last rows first, as they see most; workgroups are dealt out to the eight dies one by one, so where (sequence, head)s are a multiple of
     // eight each of them stays with one die and its cache.
-    const uint32_t groups = c.batch * c.heads, within = blockIdx.x % (groups * a.splits), b = within % groups / c.heads, head = within % groups % c.heads;
-    const uint32_t split = within / groups, first_row = (a.row_tiles - 1 - blockIdx.x / (groups * a.splits)) * ROWS;
+    const uint32_t groups = c.batch * c.heads, split = blockIdx.x / groups, within = blockIdx.x - split * groups, b = within / c.heads, head = within - b * c.heads;
+    const uint32_t first_row = (a.row_tiles - 1 - blockIdx.y) * ROWS;
     const Sequence s = sequence_of(a, b);
     if (!s.good) {
         complain(c);
@@ -603,7 +614,7 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
         // (a wave between its products goes first: the other one of its SIMD has matrix instructions running meanwhile; 400 -> 378 us for two prompts of
         // 4000 tokens over 5003)
         __builtin_amdgcn_s_setprio(1);
-        r.add(tiles[buffer], x, t0, s.length, whole, page, power_of(kb) * a.scale, power_of(vb), [] { __builtin_amdgcn_s_setprio(0); });
+        r.add(tiles[buffer], x, t0, s.length, whole, page, power_of(kb) * a.scale, page >= 0 ? power_of(vb) : 1.0f, [] { __builtin_amdgcn_s_setprio(0); });
         page = next_page, whole = next_whole, kb = next_kb, vb = next_vb;
     }
     if (cache.bad && threadIdx.x == 0) complain(c);
@@ -612,7 +623,7 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
         const uint32_t row = row0 + 16 * n + col;
         if (row >= v.rows) continue;
         const uint32_t token = quotient(row, a.group), q_head = head * a.group.by + (row - token * a.group.by);
-        const float sum = r.total[n][0], by = sum == 0 ? 0.0f : 1.0f / sum;
+        const float sum = r.total[n][0], by = a.splits == 1 ? share_of(a, s, b, token, sum) : 0;
         const size_t at = ((size_t)split * c.n_tokens + s.start + token) * a.q_heads + q_head;
         uint16_t *out = static_cast<uint16_t *>(a.out) + (size_t)(s.start + token) * a.out_token + (size_t)q_head * a.out_head;
 #pragma unroll
@@ -665,7 +676,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(Attend a)
     __syncthreads();
     if (mine != 0) return;
     for (uint32_t i = 1; i < AT_ONCE; ++i) o += sums[i][d4], total += totals[i];
-    const float by = total == 0 ? 0.0f : 1.0f / total;
+    const float by = share_of(a, s, n - 1, token - s.start, total);
     uint16_t *p = static_cast<uint16_t *>(a.out) + (size_t)token * a.out_token + (size_t)q_head * a.out_head + 4 * d4;
     *reinterpret_cast<u32x2_a2 *>(p) = u32x2{pack2<DT>(o[0] * by, o[1] * by), pack2<DT>(o[2] * by, o[3] * by)};
 }
@@ -720,7 +731,7 @@ template <int DT, int D> bool launch(const Attend &a, const Plan &p, hipStream_t
 {
     const uint32_t tiles = a.splits * a.c.batch * a.row_tiles;
     bool ok = true;
-    if (p.many) attend_many_kernel<DT, D, D == 256 ? 1 : 2><<<tiles * a.c.heads, 256, 0, s>>>(a);
+    if (p.many) attend_many_kernel<DT, D, D == 256 ? 1 : 2><<<dim3(a.splits * a.c.batch * a.c.heads, a.row_tiles), 256, 0, s>>>(a);
     else if (D == 256 || p.rows == 16) ok = launch_few<DT, D, 1>(a, tiles, s);
     else ok = launch_few<DT, D, D == 256 ? 1 : 2>(a, tiles, s);
     if (ok && a.splits > 1) attend_join_kernel<DT, D><<<dim3(a.c.n_tokens, a.q_heads), 256, 0, s>>>(a);
@@ -731,12 +742,14 @@ template <int DT> bool launch(const Attend &a, const Plan &p, hipStream_t s)
     return a.c.head_dim == 64 ? launch<DT, 64>(a, p, s) : a.c.head_dim == 128 ? launch<DT, 128>(a, p, s) : launch<DT, 256>(a, p, s);
 }
 
+constexpr uint32_t MAX_ROWS = 1u << 21, MAX_GROUPS = 1u << 23;      // what a launch holds: 65535 tiles of rows, 2^32 threads side by side
+
 // one call's arguments; 0 = none of its kernels can count with these
 bool shape_ok(const enec_cache *cache, uint32_t batch, uint32_t n_tokens, uint32_t q_heads, uint32_t max_new, uint32_t max_length)
 {
     if (cache->kv_heads == 0 || q_heads == 0 || q_heads > 65535 || q_heads % cache->kv_heads || max_length > (uint32_t)MAX_SEQUENCE) return false;
     const uint64_t rows = (uint64_t)max_new * (q_heads / cache->kv_heads);
-    return rows < (1u << 30) && n_tokens <= 0x7FFFFFFFu && batch <= 65535;
+    return rows < MAX_ROWS && n_tokens < MAX_TOKENS && (uint64_t)batch * cache->kv_heads < MAX_GROUPS;
 }
 
 }  // namespace
@@ -762,7 +775,6 @@ int enec_cache_attention(const enec_cache *cache, const enec_cache_batch *batch,
     if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 1) || max_new == 0 || !(scale > 0) || !std::isfinite(scale)) return ENEC_E_ARG;
     const uint32_t group = q_heads / a.c.heads;
     const Plan p = plan_of(a.c.batch, a.c.heads, group, a.c.head_dim, max_new, max_length);
-    if ((uint64_t)p.splits * a.c.batch * p.row_tiles > 0x3FFFFFFFu / a.c.heads) return ENEC_E_ARG;
     const size_t need = enec_cache_attention_workspace(cache, a.c.batch, a.c.n_tokens, q_heads, max_new, max_length);
     if (workspace_bytes < need || (need && !workspace)) return ENEC_E_CAPACITY;
     if (need && ((uintptr_t)workspace & 15)) return ENEC_E_ARG;

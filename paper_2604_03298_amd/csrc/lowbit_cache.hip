@@ -299,7 +299,7 @@ int pages_of(const enec_cache *cache, const enec_cache_batch *batch, Pages &p)
     if (!cache || !batch) return ENEC_E_ARG;
     const uint32_t P = cache->page_tokens, D = cache->head_dim;
     if (P < 16 || P > 256 || (P & (P - 1)) || (D != 64 && D != 128 && D != 256)) return ENEC_E_BLOCK;
-    if (cache->kv_heads == 0 || cache->kv_heads > 65535 || cache->n_pages == 0 || cache->n_pages > 0x7FFFFFFFu || batch->batch > 65535 || batch->n_tokens > 0x7FFFFFFFu)
+    if (cache->kv_heads == 0 || cache->kv_heads > 65535 || cache->n_pages == 0 || cache->n_pages > 0x7FFFFFFFu || batch->batch > 65535 || batch->n_tokens >= MAX_TOKENS)
         return ENEC_E_ARG;
     // (an empty batch needs no arrays)
     if (batch->batch && batch->n_tokens) {

@@ -396,15 +396,18 @@ Plan plan_of(uint32_t m, uint32_t n, uint32_t k, bool mx4)
     double best = 1e300;
     for (int i = 0; i < 6; ++i) {
         const Shape &s = SHAPES[mx4][i];
-        const uint64_t tiles = (uint64_t)up(n, s.rows) * up(m, s.tokens);
-        for (uint32_t splits = 1; splits <= 16 && splits * unit <= (stages > unit ? stages : unit) && (splits == 1 || (uint64_t)m * up(n, 4) < 1u << 31); splits *= 2) {
+        if (s.tokens > 16 && s.tokens >= 2 * up(m, 16) * 16) continue;       // half of the tile or more would be empty
+        const uint64_t tiles = (uint64_t)up(n, s.rows) * up(m, s.tokens), full = UNITS * s.resident;
+        const bool splittable = (uint64_t)m * up(n, 4) < 1u << 31;
+        for (uint32_t splits = 1; splits == 1 || (splittable && splits <= 16 && splits * unit <= stages && tiles * (splits / 2) < full); splits *= 2) {
             const uint32_t each = up(up(stages, splits), unit) * unit, count = up(stages, each);
             // The busiest compute unit has `most` workgroups.  Fewer than fit take their share of the time and a little more; where one fits and not all
-            // units have one, memory has less to do; past two rounds the units drift apart and no one waits.  A workgroup's start and end are 3 us, and joining is a launch, the sums' way out and back.
+            // units have one, memory has less to do; past two rounds the units drift apart and no one waits.  A workgroup's start and end are 3 us,
+            // and joining is a launch, the sums' way out and back.
             const uint64_t all = tiles * count, most = (all + UNITS - 1) / UNITS, left = most % s.resident;
             double turns = (double)(most / s.resident) + (left ? (double)left / s.resident + 0.07 : 0);
             if (s.resident == 1 && all * 4 < most * UNITS * 3) turns *= 0.88;
-            if (turns > 2) turns = (double)all / UNITS / s.resident;
+            if (turns > 2) turns = (double)all / full;
             const double us = turns * (up(each, s.stages) * s.us + 3) + (count > 1 ? 4 + (double)count * m * n * 8 / 4e6 : 0);
             if (us < best) best = us, p.shape = i, p.splits = count, p.split_stages = each;
         }

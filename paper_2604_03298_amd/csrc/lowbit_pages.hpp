@@ -20,6 +20,7 @@ __device__ __forceinline__ void complain(const Pages &c)
     if (c.status) *reinterpret_cast<volatile uint32_t *>(c.status) = STATUS_ARG;
 }
 
+constexpr uint32_t MAX_TOKENS = 1u << 24;       // of a call: a workgroup of 256 each is what a launch holds
 constexpr int32_t MAX_SEQUENCE = 1 << 30;       // tokens: positions and the ends of pages stay below 2^31
 
 // A sequence's part of a call: tokens start ... start + count - 1 of the call end a sequence of `length` tokens.

@@ -420,3 +420,39 @@ def test_another_stream_and_a_graph_give_the_same(lowbit, counts, lengths):
         graph.replay()
         torch.cuda.synchronize()
         assert all(torch.equal(a, b) for a, b in zip((out, *back), want[i]))
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("page,dim,counts,lengths", [(16, 64, [1, 1, 1], [1, 17, 0]), (32, 128, [1, 1], [33, 70]), (16, 128, [3, 40], [3, 50]), (64, 256, [1, 30], [5, 65])])
+def test_pages_that_nothing_was_written_to_hold_anything(lowbit, page, dim, counts, lengths, dtype):
+    """Every byte of them is a NaN, scales too, and one of them is the first page."""
+    c = Both(lowbit, lengths, page, 2, dim, 21)
+    c.table[c.table >= 0] = [p for p in range(1, c.cache.n_pages) if p != 2][:int((c.table >= 0).sum())]
+    c.gpu_table.copy_(torch.from_numpy(c.table))
+    for t in c.cache.tensors:
+        t.fill_(255)
+    c.fill(lengths, dtype)
+    q = torch.from_numpy(c.rng.standard_normal((sum(counts), 6, dim)).astype(np.float32)).to(dtype)
+    check_attention(c, attend(c, q, counts, lengths), q, counts, lengths)
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("counts,lengths", [([1, 1], [1, 0]), ([1, 1], [300, 40]), ([5], [2]), ([1], [9000]), ([90], [200]), ([40], [5000])])
+def test_infinite_and_undefined_scores(lowbit, counts, lengths, dtype):
+    """A row whose scores are all minus infinity, one with plus infinity and one with NaN have no softmax: NaN.  One that sees nothing is zeros."""
+    c = Both(lowbit, lengths, 64, 1, 64, 22)
+    n = sum(lengths)
+    k, v = c.values(n, dtype), c.values(n, dtype)
+    k[0][:, :, 7] = 1.0
+    c.write(lengths, lengths, (k[0], k[0].cuda()), v)
+    for what in (float("-inf"), float("inf"), float("nan")):
+        q = torch.zeros(sum(counts), 3, 64, dtype=dtype)
+        q[:, 1, 7] = what                                  # of three heads the middle one
+        out = attend(c, q, counts, lengths).cpu()
+        at = 0
+        for count, length in zip(counts, lengths):
+            for i in range(count):
+                sees = length - count + i + 1 > 0
+                assert torch.isnan(out[at, 1]).all() if sees else (out[at] == 0).all(), (what, count, length, i)
+                assert torch.isfinite(out[at, ::2]).all()
+                at += 1

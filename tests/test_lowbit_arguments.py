@@ -117,13 +117,13 @@ def test_caches_that_are_refused(lowbit):
                     {"stride": 0}, {"heads": 0}, {"heads": 70000}, {"batch": 70000}, {"tokens": 1 << 31}, {"pages": 1 << 31}, {"k": None}, {"v": None},
                     {"k": ODD}, {"v": ODD}):
             assert call(**bad) == lowbit.E_ARG, bad
-        assert call(pages=0) == lowbit.E_ARG
+        assert call(pages=0) == call(tokens=1 << 24) == lowbit.E_ARG
         assert call(dtype=3) == call(dtype=-1) == lowbit.E_DTYPE
         assert call(batch=0) == call(tokens=0) == lowbit.OK
         assert call(batch=0, table=None, starts=None, lengths=None) == lowbit.OK
     assert write(dtype=2) == attend(dtype=2) == lowbit.E_DTYPE
     assert read(dtype=2, k=0x1002) == lowbit.E_ARG
-    for bad in ({"q_heads": 0}, {"q_heads": 6}, {"q_heads": 1 << 20}, {"new": 0}, {"new": 1 << 31}, {"most": (1 << 30) + 1}):
+    for bad in ({"q_heads": 0}, {"q_heads": 6}, {"q_heads": 1 << 20}, {"new": 0}, {"new": 1 << 31}, {"new": 1 << 20}, {"batch": 65535, "heads": 256, "q_heads": 256}, {"most": (1 << 30) + 1}):
         assert attend(**bad) == lowbit.E_ARG, bad
     for scale in (0.0, -0.1, float("nan"), float("inf")):
         assert attend(scale=scale) == lowbit.E_ARG, scale

@@ -16,9 +16,9 @@ struct Product {
     size_t x_stride, y_stride;          // elements
     uint32_t m, n, k, groups;           // groups of 128 columns
     int y_dtype;
-    // for many tokens: bytes between rows of x, and between its planes; the tiles; the stages of a split and where their sums go
+    // bytes between rows of x, and of a row; the tiles; the stages of a split and where their sums go
     size_t x_row, part_row;
-    uint32_t x_bytes, x_plane, n_tiles, m_tiles, split_stages;
+    uint32_t x_bytes, n_tiles, m_tiles, split_stages;
     float *parts;
 };
 
@@ -42,22 +42,30 @@ __device__ __forceinline__ bf16x8 values_of(uint32_t codes, float scale)
     const bf16x2 c = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 2), d = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 3);
     return bf16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-// An fp16 value is the sum of two bf16 values, exactly: eight of its eleven bits and the rest, whose exponents bf16 has room for.  The weights' scales
-// have bf16's range and not fp16's, so fp16 activations are multiplied as these two.
-__device__ __forceinline__ void split_fp16(const u32x4 &v, bf16x8 &hi, bf16x8 &lo)
+// The same as fp16 values without their scale, whose range is bf16's and not fp16's: each block's sum takes it instead, which is five instructions for
+// a matrix instruction.  (fp16 activations as the sum of two bf16 numbers need none, but twice the matrix instructions: 2048 tokens x 4096 x 11008
+// 300 us instead of 255, one token x 8192 x 28672 41 instead of 28.)
+__device__ __forceinline__ f16x8 unscaled_values_of(uint32_t codes)
 {
-#pragma unroll
-    for (int j = 0; j < 4; ++j) {
-        const f32x2 f = unpack2<FP16>(v[j]);
-#pragma unroll
-        for (int i = 0; i < 2; ++i) {
-            const __bf16 h = (__bf16)f[i];
-            hi[2 * j + i] = h;
-            lo[2 * j + i] = __builtin_isinf(f[i]) ? (__bf16)0.0f : (__bf16)(f[i] - (float)h);
-        }
-    }
+    const f16x2 a = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 0), b = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 1);
+    const f16x2 c = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 2), d = __builtin_amdgcn_cvt_scalef32_pk_f16_fp4(codes, 1.0f, 3);
+    return f16x8{a[0], a[1], b[0], b[1], c[0], c[1], d[0], d[1]};
 }
-
+// Word j of the four lanes sixteen apart becomes lane j's, in the order of the lanes: exchanges of halves, then of quarters.  As instructions of their own,
+// see over_groups_max in lowbit_attention.hip.
+__device__ __forceinline__ void exchange_words(u32x4 &v)
+{
+    uint32_t a = v[0], b = v[1], c = v[2], d = v[3];
+    asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %2\n\tv_permlane32_swap_b32 %1, %3\n\ts_nop 1\n\tv_permlane16_swap_b32 %0, %1\n\tv_permlane16_swap_b32 %2, %3"
+        : "+v"(a), "+v"(b), "+v"(c), "+v"(d));
+    v = u32x4{a, b, c, d};
+}
+// 2^(byte - 127), byte j of a word; 255: infinity
+__device__ __forceinline__ float scale_of(uint32_t bytes, int j)
+{
+    const uint32_t e = (j < 3 ? bytes << (23 - 8 * j) : bytes >> 1) & 0x7F800000u;
+    return f32_of_bits(e > 0x00400000u ? e : 0x00400000u);
+}
 __device__ __forceinline__ void store4(void *y, int dtype, size_t at, uint32_t valid, const f32x4 &v)
 {
     if (dtype == FP32) {
@@ -93,7 +101,7 @@ template <int BYTES> __device__ __forceinline__ void copy_to_lds(Range r, uint32
 // How a stage lies in LDS.  A row (of weights, or a token's) is a run of chunks of 16 bytes, chunk i at place i ^ turn(row).  A wave reads 16 bytes a lane
 // in four goes of sixteen lanes, lanes {0-3, 12-15, 20-27} the first: rows {0-3, 12-15} of one lane group and rows {4-11} of its neighbour.  Each
 // turn puts such sixteen chunks into the sixteen different places of 256 bytes, so that no bank is asked twice:
-//   256 bytes a row, the groups' chunks four apart (16-bit activations); 128 bytes, one apart (4-bit ones, and their weights); 64 bytes, one apart
+//   256 bytes a row, the groups' chunks four apart (16-bit activations; one apart, where a step is one block: the row itself); 128 bytes, one apart (4-bit ones, and their weights); 64 bytes, one apart
 template <int ROW> __device__ __forceinline__ uint32_t turn(uint32_t r)
 {
     if constexpr (ROW == 256) return (r & 3) + 12 * (r >> 3 & 1);
@@ -111,19 +119,19 @@ template <int ROW> __device__ __forceinline__ uint32_t turn(uint32_t r)
 template <int ACT, int RT, int MT, int WN, int WM, int KG, int BUFFERS>
 __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) product_tile_kernel(Product a)
 {
-    constexpr int THREADS = 64 * WN * WM, ALL = THREADS * KG, TOKENS = 16 * MT * WM, ROWS = 16 * RT * WN, PLANES = ACT == FP16 ? 2 : 1;
+    constexpr int THREADS = 64 * WN * WM, ALL = THREADS * KG, TOKENS = 16 * MT * WM, ROWS = 16 * RT * WN;
     constexpr int X_ROW = ACT == MX4 ? 128 : 256, W_ROW = ACT == MX4 ? 128 : 64, X_CHUNKS = X_ROW / 16, W_CHUNKS = W_ROW / 16;
     constexpr int X_SIZE = TOKENS * X_ROW, W_SIZE = ROWS * W_ROW, S_SIZE = ROWS * 16, XS_SIZE = ACT == MX4 ? TOKENS * 16 : 0;
     constexpr uint32_t S_STAGES = ACT == MX4 ? 2 : 4;                    // that sixteen bytes of scales are for
     constexpr int BLOCKS = KG > (int)S_STAGES ? KG / S_STAGES : 1;       // of scales that a round of stages needs
     constexpr int X_COPIES = X_SIZE / 16 / THREADS, W_COPIES = W_SIZE / 16 / THREADS;
     static_assert(KG == 1 || KG % S_STAGES == 0, "a round needs whole blocks of scales");
+    static_assert(ACT != FP16 || MT <= 4, "all tokens' tiles at once");
     static_assert(X_SIZE % (16 * THREADS) == 0 && W_SIZE % (16 * THREADS) == 0 && S_SIZE % 256 == 0 && XS_SIZE % 256 == 0, "whole copies of a wave");
     constexpr int U = MT < 4 ? MT : 4, STEPS = ACT == MX4 ? 2 : 4, UNITS = STEPS * (MT / U);
-    constexpr int W_BUFFERS = PLANES == 2 ? 2 : BUFFERS;                 // (both planes of a stage are multiplied with the same weights)
     extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
     uint8_t *x_stages = shared, *w_stages = shared + BUFFERS * KG * X_SIZE;
-    uint8_t *scale_bytes = w_stages + W_BUFFERS * KG * W_SIZE;           // two of BLOCKS (S_SIZE + XS_SIZE), in turn
+    uint8_t *scale_bytes = w_stages + BUFFERS * KG * W_SIZE;           // two of BLOCKS (S_SIZE + XS_SIZE), in turn
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
     const uint32_t kg = wave / (WN * WM), mate = wave % (WN * WM), thread = threadIdx.x % THREADS;      // wave and thread of the group
     const uint32_t wn = mate % WN, wm = mate / WN;
@@ -141,15 +149,15 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
     const uint32_t end = first + a.split_stages < stages ? first + a.split_stages : stages;
 
     // the chunk of row r that belongs to this thread's place
-    auto x_from = [&](uint32_t r) { return r * x_pitch + 16 * ((thread % X_CHUNKS) ^ turn<X_ROW>(r & 15)); };
+    auto x_turn = [](uint32_t r) { return ACT == FP16 ? r : turn<X_ROW>(r); };
+    auto x_from = [&](uint32_t r) { return r * x_pitch + 16 * ((thread % X_CHUNKS) ^ x_turn(r & 15)); };
     auto w_from = [&](uint32_t r) { return r * w_pitch + 16 * ((thread % W_CHUNKS) ^ turn<W_ROW>(r & 15)); };
     const uint32_t s_from = threadIdx.x / 4 * s_pitch + 4 * (threadIdx.x % 4);
-    auto copy = [&](uint32_t i, uint32_t plane, uint32_t x_buffer, uint32_t w_buffer) {
-        uint8_t *x_to = x_stages + (x_buffer * KG + kg) * X_SIZE, *w_to = w_stages + (w_buffer * KG + kg) * W_SIZE;
+    auto copy = [&](uint32_t i, uint32_t buffer) {
+        uint8_t *x_to = x_stages + (buffer * KG + kg) * X_SIZE, *w_to = w_stages + (buffer * KG + kg) * W_SIZE;
 #pragma unroll
         for (int r = 0; r < X_COPIES; ++r)
-            copy_to_lds<16>(x, x_from(thread / X_CHUNKS + r * (THREADS / X_CHUNKS)) + i * X_ROW + plane * a.x_plane, x_to + (r * THREADS + mate * 64) * 16);
-        if (plane != 0) return;
+            copy_to_lds<16>(x, x_from(thread / X_CHUNKS + r * (THREADS / X_CHUNKS)) + i * X_ROW, x_to + (r * THREADS + mate * 64) * 16);
 #pragma unroll
         for (int r = 0; r < W_COPIES; ++r)
             copy_to_lds<16>(codes, w_from(thread / W_CHUNKS + r * (THREADS / W_CHUNKS)) + i * W_ROW, w_to + (r * THREADS + mate * 64) * 16);
@@ -171,7 +179,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
     };
     // A wave's copies are counted, and done in the order in which they were issued: with at most AHEAD left, those before them are in LDS.  Then
     // all waves' are, and nobody reads the stage before any more.
-    constexpr int AHEAD = (BUFFERS - 2) * (PLANES == 2 ? X_COPIES : X_COPIES + W_COPIES);         // at least so many copies are of the next round
+    constexpr int AHEAD = (BUFFERS - 2) * (X_COPIES + W_COPIES);         // at least so many copies are of the next round
     auto landed = [&](bool last) {
         __builtin_amdgcn_sched_barrier(0);
         if (AHEAD == 0 || last) asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
@@ -182,7 +190,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
     // where this lane's chunks lie: of tokens c, 16 + c, ..., and of rows c, 16 + c, ...
     uint32_t x_at[STEPS], w_at[2];
 #pragma unroll
-    for (int j = 0; j < STEPS; ++j) x_at[j] = (wm * (16 * MT) + c) * X_ROW + (((ACT == MX4 ? 4 * j + g : 4 * g + j) ^ turn<X_ROW>(c)) << 4);
+    for (int j = 0; j < STEPS; ++j) x_at[j] = (wm * (16 * MT) + c) * X_ROW + (((ACT != BF16 ? 4 * j + g : 4 * g + j) ^ x_turn(c)) << 4);
 #pragma unroll
     for (int j = 0; j < 2; ++j) w_at[j] = (wn * (16 * RT) + c) * W_ROW + (((ACT == MX4 ? 4 * j + g : g) ^ turn<W_ROW>(c)) << 4);
     auto x_chunk = [&](const uint8_t *t, int j, int u) { return *reinterpret_cast<const u32x4 *>(t + x_at[j] + u * (16 * X_ROW)); };
@@ -191,11 +199,11 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
     f32x4 acc[RT][MT] = {};
     // Group kg takes stages first + kg, first + KG + kg, ..., in rounds that all groups begin together.
     constexpr uint32_t ROUND = KG > 1 ? KG : 1;
-    const uint32_t rounds = (end - first + ROUND - 1) / ROUND * PLANES, per_block = KG > 1 ? PLANES * (S_STAGES > KG ? S_STAGES / KG : 1) : PLANES * S_STAGES;
-    auto stage_of = [&](uint32_t round) { return first + round / PLANES * ROUND + (KG > 1 ? kg : 0); };
+    const uint32_t rounds = (end - first + ROUND - 1) / ROUND, per_block = KG > 1 ? (S_STAGES > KG ? S_STAGES / KG : 1) : S_STAGES;
+    auto stage_of = [&](uint32_t round) { return first + round * ROUND + (KG > 1 ? kg : 0); };
     auto fetch = [&](uint32_t round) {
         const uint32_t i = stage_of(round);
-        copy(i < end ? i : end - 1, round % PLANES, round % BUFFERS, round / PLANES % W_BUFFERS);
+        copy(i < end ? i : end - 1, round % BUFFERS);
     };
     copy_scales(first / S_STAGES, 0);                       // (a split begins with such a block)
     fetch(0);
@@ -206,7 +214,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
         if (round % per_block == 0 && round + per_block < rounds) copy_scales(first / S_STAGES + (round / per_block + 1) * BLOCKS, round / per_block + 1);
         if (round + BUFFERS - 1 < rounds) fetch(round + BUFFERS - 1);
         if (KG > 1 && i >= end) continue;
-        const uint8_t *x_now = x_stages + (round % BUFFERS * KG + kg) * X_SIZE, *w_now = w_stages + (round / PLANES % W_BUFFERS * KG + kg) * W_SIZE;
+        const uint8_t *x_now = x_stages + (round % BUFFERS * KG + kg) * X_SIZE, *w_now = w_stages + (round % BUFFERS * KG + kg) * W_SIZE;
         const uint8_t *ws_now = scale_bytes + ((round / per_block & 1) * BLOCKS + (KG > 1 ? kg / S_STAGES : 0)) * (S_SIZE + XS_SIZE) + (16 / S_STAGES) * (i % S_STAGES);
         // tokens' tiles are taken U at a time; the next ones' chunks are asked for before these are multiplied, and no earlier
         u32x4 xv[2][U];
@@ -250,6 +258,38 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
                 for (int u = 0; u < U; ++u)
 #pragma unroll
                     for (int t = 0; t < RT; ++t) acc[t][b * U + u] = mfma_mx4(s, w[s][t], xv[k & 1][u], acc[t][b * U + u], (int)ws[t], (int)xs[b * U + u]);
+            }
+        } else if constexpr (ACT == FP16) {
+            // A step is a block of 32 columns.  Weights are the right operand here: all sums of a lane are of one row, and so is the scale.
+            u32x4 w[RT];
+            uint32_t ws[RT];
+#pragma unroll
+            for (int t = 0; t < RT; ++t) {
+                w[t] = w_chunk(w_now, 0, t);
+                ws[t] = *reinterpret_cast<const uint32_t *>(ws_now + (wn * (16 * RT) + 16 * t + c) * 16);
+                if ((ws[t] >> (8 * g) & 255) == 255) w[t] = u32x4{};    // 0 * infinity, whatever the codes are
+                exchange_words(w[t]);
+            }
+#pragma unroll
+            for (int u = 0; u < U; ++u) xv[0][u] = x_chunk(x_now, 0, u);
+#pragma unroll
+            for (int j = 0; j < STEPS; ++j) {
+                __builtin_amdgcn_sched_barrier(0);
+                if (j + 1 < STEPS) {
+#pragma unroll
+                    for (int u = 0; u < U; ++u) xv[(j + 1) & 1][u] = x_chunk(x_now, j + 1, u);
+                }
+#pragma unroll
+                for (int t = 0; t < RT; ++t) {
+                    const f16x8 wv = unscaled_values_of(w[t][j]);
+                    const float by = scale_of(ws[t], j);
+#pragma unroll
+                    for (int u = 0; u < U; ++u) {
+                        const f32x4 sum = __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, xv[j & 1][u]), wv, f32x4{}, 0, 0, 0);
+#pragma unroll
+                        for (int e = 0; e < 4; ++e) acc[t][u][e] = __builtin_fmaf(sum[e], by, acc[t][u][e]);
+                    }
+                }
             }
         } else {
             u32x4 w[RT];
@@ -303,6 +343,20 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
 #pragma unroll
                 for (int u = 0; u < MT; ++u) acc[t][u] += sums[(((k - 1) * WN * WM + mate) * RT * MT + t * MT + u) * 64 + lane];
     }
+    if constexpr (ACT == FP16) {                            // four tokens of a row
+#pragma unroll
+        for (int u = 0; u < MT; ++u)
+#pragma unroll
+            for (int t = 0; t < RT; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t token = m0 + wm * (16 * MT) + 16 * u + 4 * g + e, r = n0 + 16 * (wn * RT + t) + c;
+                    if (token >= a.m || r >= a.n) continue;
+                    if (a.parts) a.parts[((size_t)blockIdx.y * a.m + token) * a.part_row + r] = acc[t][u][e];
+                    else static_cast<_Float16 *>(a.y)[(size_t)token * a.y_stride + r] = (_Float16)acc[t][u][e];
+                }
+        return;
+    }
 #pragma unroll
     for (int u = 0; u < MT; ++u) {
         const uint32_t token = m0 + wm * (16 * MT) + 16 * u + c;
@@ -317,9 +371,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
     }
 }
 
-// Activations as the kernel above copies them: bf16, rows of a multiple of 128 columns, zeros behind the last one; of fp16 two
-// such rows one behind the other, the values' parts.
-template <int DT>
+// Activations as the kernel above copies them: rows of a multiple of 128 columns, zeros behind the last one.
 __global__ void __launch_bounds__(256) lay_out_kernel(const uint16_t *__restrict__ x, size_t x_stride, uint32_t k, Divide per_row, uint32_t n_vec,
                                                       u32x4 *__restrict__ out)
 {
@@ -337,14 +389,7 @@ __global__ void __launch_bounds__(256) lay_out_kernel(const uint16_t *__restrict
 #pragma unroll
         for (uint32_t i = 0; i < 8; ++i) v[i >> 1] |= (col + i < k ? e[i] : 0) << (16 * (i & 1));
     }
-    if constexpr (DT == BF16) {
-        out[at] = v;
-    } else {
-        bf16x8 hi, lo;
-        split_fp16(v, hi, lo);
-        out[(size_t)row * (2 * per_row.by) + (at - row * per_row.by)] = __builtin_bit_cast(u32x4, hi);
-        out[(size_t)row * (2 * per_row.by) + (at - row * per_row.by) + per_row.by] = __builtin_bit_cast(u32x4, lo);
-    }
+    out[at] = v;
 }
 
 // The sums of the splits, in their order (none, where there are no columns: zeros).
@@ -369,13 +414,17 @@ using namespace enec::lowbit;
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 // The tiles there are.  `resident` workgroups of one fit a compute unit (by LDS), and with all of them there a round of stages, `stages` of them, takes
-// `us` (measured: 1 to 3000 tokens with matrices of 4096 x 1024 to 11008).
+// `us` (measured: 1 to 4096 tokens with matrices of 4096 x 1024 to 8192 x 28672).
 struct Shape {
     uint32_t rows, tokens, resident, stages;
     double us;
 };
-constexpr Shape SHAPES[2][6] = {{{256, 128, 1, 1, 1.72}, {256, 64, 2, 1, 1.85}, {128, 64, 3, 1, 1.48}, {128, 32, 3, 1, 1.20}, {64, 32, 1, 4, 0.70}, {32, 16, 2, 4, 0.60}},
+constexpr Shape SHAPES[3][6] = {{{256, 128, 1, 1, 1.72}, {256, 64, 2, 1, 1.85}, {128, 64, 3, 1, 1.48}, {128, 32, 3, 1, 1.20}, {64, 32, 1, 4, 0.70}, {32, 16, 2, 4, 0.60}},
+                                {{256, 128, 1, 1, 2.75}, {256, 64, 2, 1, 2.80}, {128, 64, 3, 1, 2.10}, {128, 32, 3, 1, 1.45}, {64, 32, 1, 4, 0.90}, {32, 16, 2, 4, 0.75}},
                                 {{256, 256, 1, 1, 2.49}, {128, 128, 2, 1, 1.50}, {128, 64, 2, 1, 1.39}, {128, 32, 2, 1, 0.90}, {64, 32, 1, 4, 0.60}, {32, 16, 2, 4, 0.50}}};
+constexpr double THIN[3] = {0.05, 0.10, 0.05};      // what a workgroup that is not there costs of the time saved: less overlaps
+constexpr const Shape *shapes_of(int act) { return SHAPES[act == MX4 ? 2 : act]; }
+static_assert(BF16 == 0 && FP16 == 1, "the tables' order");
 constexpr uint32_t UNITS = 256;                     // compute units
 
 // How a product is cut up: the tile, and the splits of the columns where tiles alone leave the card empty.
@@ -388,24 +437,25 @@ struct Plan {
 inline uint32_t up(uint32_t v, uint32_t by) { return (v + by - 1) / by; }
 inline size_t part_row(uint32_t n) { return ((size_t)n + 15) / 16 * 16; }
 
-Plan plan_of(uint32_t m, uint32_t n, uint32_t k, bool mx4)
+Plan plan_of(uint32_t m, uint32_t n, uint32_t k, int act)
 {
     Plan p{};
-    if (!mx4) p.laid_out = 4 * (size_t)m * (up(k, 128) * 128);
+    const bool mx4 = act == MX4;
+    if (!mx4) p.laid_out = 2 * (size_t)m * (up(k, 128) * 128);
     const uint32_t groups = up(k, 128), unit = 4, stages = mx4 ? up(groups, 2) : groups;     // a split is whole blocks of scales and whole rounds
     double best = 1e300;
     for (int i = 0; i < 6; ++i) {
-        const Shape &s = SHAPES[mx4][i];
+        const Shape &s = shapes_of(act)[i];
         if (s.tokens > 16 && s.tokens >= 2 * up(m, 16) * 16) continue;       // half of the tile or more would be empty
         const uint64_t tiles = (uint64_t)up(n, s.rows) * up(m, s.tokens), full = UNITS * s.resident;
         const bool splittable = (uint64_t)m * up(n, 4) < 1u << 31;
         for (uint32_t splits = 1; splits == 1 || (splittable && splits <= 16 && splits * unit <= stages && tiles * (splits / 2) < full); splits *= 2) {
             const uint32_t each = up(up(stages, splits), unit) * unit, count = up(stages, each);
-            // The busiest compute unit has `most` workgroups.  Fewer than fit take their share of the time and a little more; where one fits and not all
+            // The busiest compute unit has `most` workgroups.  Fewer than fit take their share of the time and some more; where one fits and not all
             // units have one, memory has less to do; past two rounds the units drift apart and no one waits.  A workgroup's start and end are 3 us,
             // and joining is a launch, the sums' way out and back.
             const uint64_t all = tiles * count, most = (all + UNITS - 1) / UNITS, left = most % s.resident;
-            double turns = (double)(most / s.resident) + (left ? (double)left / s.resident + 0.07 : 0);
+            double turns = (double)(most / s.resident) + (left ? (double)left / s.resident + (s.resident - left) * THIN[mx4 ? 2 : act] : 0);
             if (s.resident == 1 && all * 4 < most * UNITS * 3) turns *= 0.88;
             if (turns > 2) turns = (double)all / full;
             const double us = turns * (up(each, s.stages) * s.us + 3) + (count > 1 ? 4 + (double)count * m * n * 8 / 4e6 : 0);
@@ -416,11 +466,14 @@ Plan plan_of(uint32_t m, uint32_t n, uint32_t k, bool mx4)
     return p;
 }
 
+// (the workspace is the same for both formats of activations)
+inline size_t space_of(const Plan &a, const Plan &b) { return a.laid_out + (a.parts > b.parts ? a.parts : b.parts); }
+
 template <int ACT, int RT, int MT, int WN, int WM, int KG, int BUFFERS> bool launch_tile(const Product &a, uint32_t splits, hipStream_t s)
 {
     constexpr size_t TOKENS = 16 * MT * WM, ROWS = 16 * RT * WN;
     static std::atomic<uint64_t> allowed{0};
-    constexpr size_t STAGES = KG * (BUFFERS * TOKENS * (ACT == MX4 ? 128 : 256) + (ACT == FP16 ? 2 : BUFFERS) * ROWS * (ACT == MX4 ? 128 : 64));
+    constexpr size_t STAGES = KG * BUFFERS * (TOKENS * (ACT == MX4 ? 128 : 256) + ROWS * (ACT == MX4 ? 128 : 64));
     constexpr size_t BLOCKS = ACT == MX4 && KG == 4 ? 2 : 1, LDS = STAGES + 2 * BLOCKS * 16 * (ACT == MX4 ? TOKENS + ROWS : ROWS);
     static_assert(LDS <= 160 * 1024 && (KG - 1) * 4 * TOKENS * ROWS <= LDS, "LDS of a compute unit; the groups' sums take the stages' place");
     const auto kernel = product_tile_kernel<ACT, RT, MT, WN, WM, KG, BUFFERS>;
@@ -429,26 +482,24 @@ template <int ACT, int RT, int MT, int WN, int WM, int KG, int BUFFERS> bool lau
     return true;
 }
 
-template <int ACT> int launch(Product a, void *workspace, hipStream_t s)
+template <int ACT> int launch(Product a, const Plan &p, void *workspace, hipStream_t s)
 {
     if (a.k == 0) {
         const uint32_t per_row = up(a.n, 4);
         join_kernel<<<up(a.m * per_row, 256), 256, 0, s>>>(nullptr, 0, a.m, a.n, 0, divide_by(per_row), a.y, a.y_stride, a.y_dtype);
         return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
     }
-    const Plan p = plan_of(a.m, a.n, a.k, ACT == MX4);
-    const Shape &shape = SHAPES[ACT == MX4][p.shape];
+    const Shape &shape = shapes_of(ACT)[p.shape];
     if constexpr (ACT == MX4) {
         a.x_row = a.x_bytes = a.groups * 64;
-    } else if (ACT == BF16 && a.k % 128 == 0 && a.x_stride % 8 == 0 && a.x_stride <= (1u << 22) && aligned(a.x, 16)) {
+    } else if (a.k % 128 == 0 && a.x_stride % 8 == 0 && a.x_stride <= (1u << 22) && aligned(a.x, 16)) {
         a.x_row = a.x_stride * 2, a.x_bytes = a.k * 2;
     } else {
         const uint32_t cols = up(a.k, 128) * 128, n_vec = a.m * (cols / 8);
-        lay_out_kernel<ACT><<<up(n_vec, 256), 256, 0, s>>>(static_cast<const uint16_t *>(a.x), a.x_stride, a.k, divide_by(cols / 8), n_vec,
-                                                           static_cast<u32x4 *>(workspace));
+        lay_out_kernel<<<up(n_vec, 256), 256, 0, s>>>(static_cast<const uint16_t *>(a.x), a.x_stride, a.k, divide_by(cols / 8), n_vec,
+                                                      static_cast<u32x4 *>(workspace));
         a.x = workspace;
-        a.x_plane = cols * 2;
-        a.x_row = a.x_bytes = ACT == FP16 ? 2 * a.x_plane : a.x_plane;
+        a.x_row = a.x_bytes = cols * 2;
     }
     a.n_tiles = up(a.n, shape.rows), a.m_tiles = up(a.m, shape.tokens), a.split_stages = p.split_stages;
     if (p.splits > 1) a.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.laid_out), a.part_row = part_row(a.n);
@@ -482,14 +533,12 @@ extern "C" {
 size_t enec_mx4_linear_workspace(size_t m, size_t n, size_t k)
 {
     if (!sizes_ok(m, n, k) || m == 0 || n == 0 || k == 0) return 0;
-    const Plan p = plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, false);
-    return p.laid_out + p.parts;
+    return space_of(plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, BF16), plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, FP16));
 }
 size_t enec_mx4_matmul_workspace(size_t m, size_t n, size_t k)
 {
     if (!sizes_ok(m, n, k) || m == 0 || n == 0 || k == 0) return 0;
-    const Plan p = plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, true);
-    return p.laid_out + p.parts;
+    return plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, MX4).parts;
 }
 
 int enec_mx4_linear(const void *x, size_t m, size_t x_stride, int dtype, const void *codes, const void *scales, size_t n, size_t k, void *y,
@@ -500,12 +549,15 @@ int enec_mx4_linear(const void *x, size_t m, size_t x_stride, int dtype, const v
     if (m == 0 || n == 0) return ENEC_OK;
     if (!y || !aligned(y, 2) || y_stride < n) return ENEC_E_ARG;
     if (k != 0 && (!x || !codes || !scales || !aligned(x, 2) || !aligned(codes, 16) || !aligned(scales, 4) || x_stride < k)) return ENEC_E_ARG;
-    const size_t need = enec_mx4_linear_workspace(m, n, k);
+    Plan p[2] = {};
+    if (k != 0)
+        for (int t : {BF16, FP16}) p[t] = plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, t);
+    const size_t need = space_of(p[BF16], p[FP16]);
     if (workspace_bytes < need || (need && !workspace)) return ENEC_E_CAPACITY;
     if (need && !aligned(workspace, 16)) return ENEC_E_ARG;
     const Product a{x, nullptr, static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), y, x_stride, y_stride,
-                    (uint32_t)m, (uint32_t)n, (uint32_t)k, (uint32_t)((k + 127) / 128), dtype, 0, 0, 0, 0, 0, 0, 0, nullptr};
-    return dtype == ENEC_BF16 ? launch<BF16>(a, workspace, (hipStream_t)stream) : launch<FP16>(a, workspace, (hipStream_t)stream);
+                    (uint32_t)m, (uint32_t)n, (uint32_t)k, (uint32_t)((k + 127) / 128), dtype, 0, 0, 0, 0, 0, 0, nullptr};
+    return dtype == ENEC_BF16 ? launch<BF16>(a, p[BF16], workspace, (hipStream_t)stream) : launch<FP16>(a, p[FP16], workspace, (hipStream_t)stream);
 }
 
 int enec_mx4_matmul(const void *x_codes, const void *x_scales, size_t m, const void *codes, const void *scales, size_t n, size_t k, void *y,
@@ -517,12 +569,13 @@ int enec_mx4_matmul(const void *x_codes, const void *x_scales, size_t m, const v
     if (!y || !aligned(y, dtype == ENEC_FP32 ? 4 : 2) || y_stride < n) return ENEC_E_ARG;
     if (k != 0 && (!x_codes || !x_scales || !codes || !scales || !aligned(x_codes, 16) || !aligned(x_scales, 4) || !aligned(codes, 16) || !aligned(scales, 4)))
         return ENEC_E_ARG;
-    const size_t need = enec_mx4_matmul_workspace(m, n, k);
+    const Plan p = k == 0 ? Plan{} : plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, MX4);
+    const size_t need = p.parts;
     if (workspace_bytes < need || (need && !workspace)) return ENEC_E_CAPACITY;
     if (need && !aligned(workspace, 16)) return ENEC_E_ARG;
     const Product a{x_codes, static_cast<const uint8_t *>(x_scales), static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), y, 0, y_stride,
-                    (uint32_t)m, (uint32_t)n, (uint32_t)k, (uint32_t)((k + 127) / 128), dtype, 0, 0, 0, 0, 0, 0, 0, nullptr};
-    return launch<MX4>(a, workspace, (hipStream_t)stream);
+                    (uint32_t)m, (uint32_t)n, (uint32_t)k, (uint32_t)((k + 127) / 128), dtype, 0, 0, 0, 0, 0, 0, nullptr};
+    return launch<MX4>(a, p, workspace, (hipStream_t)stream);
 }
 
 }  // extern "C"

@@ -274,3 +274,71 @@ def test_another_stream_and_a_graph_give_the_same(lowbit):
         torch.cuda.synchronize()
         for a, b in zip((y, z, back), want[i]):
             assert torch.equal(a, b)
+
+
+def any_codes(n, k, seed):
+    """A matrix of any codes, with scales around 1 / 50: as it might come from elsewhere."""
+    g = np.random.default_rng(seed)
+    padded = -(-k // 128) * 128
+    codes = g.integers(0, 256, (n, padded // 2), dtype=np.uint8)
+    for c in range(k, padded):                            # padding is zeros
+        codes[:, c // 2] &= 0xF0 if c % 2 == 0 else 0x0F
+    return codes, g.integers(118, 125, (n, padded // 32), dtype=np.uint8)
+
+
+# ragged sizes that are large enough, in one direction or another, for large tiles and for columns that are split over workgroups
+LARGE = [(1000, 4100, 300), (2100, 5000, 129), (700, 8200, 200), (40, 9000, 1200), (300, 5000, 1200), (3, 20, 8100), (20, 1030, 16380), (70, 500, 16380),
+         (40, 1030, 16380), (130, 5000, 16380), (300, 5000, 16380), (300, 2050, 40000), (20, 1030, 40000)]
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("m,n,k", LARGE)
+def test_large_products_with_16_bit_activations(lowbit, m, n, k, dtype):
+    codes, scales = any_codes(n, k, m + n + k)
+    x = torch.randn(m, k, generator=torch.Generator().manual_seed(k)).to(dtype)
+    out = torch.empty(m, n, dtype=dtype, device="cuda")
+    ws = space(lowbit.mx4_linear_workspace(m, n, k))
+    gpu = [torch.from_numpy(t).cuda() for t in (codes, scales)]
+    w = plain.mx4_decode(codes, scales, k)
+    for src in (x.cuda(), on_gpu(x, k + 1, 1)):
+        out.fill_(float("nan"))
+        assert lowbit.mx4_linear(src, *gpu, out, ws) == lowbit.OK
+        close(out, x.double().numpy(), w, dtype)
+
+
+@pytest.mark.parametrize("m,n,k", LARGE + [(2050, 4097, 130)])
+def test_large_products_with_both_in_4_bits(lowbit, m, n, k):
+    codes, scales = any_codes(n, k, m + n + k)
+    x_codes, x_scales = any_codes(m, k, 8)
+    out = torch.full((m, n), float("nan"), device="cuda")
+    ws = space(lowbit.mx4_matmul_workspace(m, n, k))
+    gpu = [torch.from_numpy(t).cuda() for t in (x_codes, x_scales, codes, scales)]
+    assert lowbit.mx4_matmul(*gpu, out, ws) == lowbit.OK
+    close(out, plain.mx4_decode(x_codes, x_scales, k), plain.mx4_decode(codes, scales, k), torch.float32)
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("m", [1, 30, 50, 600])
+def test_least_and_largest_activations(lowbit, m, dtype):
+    """Values of the format's smallest exponents are not lost: beside weights that bring them back, and alone."""
+    n, k = 1030, 256
+    codes, scales = any_codes(n, k, 9)
+    x = torch.randn(m, k, generator=torch.Generator().manual_seed(10)).double()
+    x[:, ::3] *= 2.0 ** -22
+    x[:, 1::3] *= 2.0 ** 13
+    x = x.to(dtype)
+    x[:, 128:] = x[:, 128:] * 2.0 ** -10
+    scales[::2] += 20
+    codes[1::2, :32] = 0
+    out = torch.empty(m, n, dtype=dtype, device="cuda")
+    w = plain.mx4_decode(codes, scales, k)
+    if dtype == torch.float16:                            # results within the format
+        x[:, :128] = x[:, :128] * 2.0 ** -14
+        w = plain.mx4_decode(codes, scales, k)
+    ws = space(lowbit.mx4_linear_workspace(m, n, k))
+    assert lowbit.mx4_linear(x.cuda(), torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), out, ws) == lowbit.OK
+    got, xx = out.double().cpu().numpy(), x.double().numpy()
+    want = xx @ w.T
+    fits = np.abs(want) < 60000 if dtype == torch.float16 else np.isfinite(want)
+    off = np.abs(got - want) - plain.product_bound(xx, w, want, dtype)
+    assert fits.mean() > 0.4 and (off[fits] <= 0).all()

@@ -63,6 +63,13 @@ template <int DT> __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const 
     if constexpr (DT == BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
+// 32 E4M3 codes a lane on both sides, each side with a power of two for them; PIECE: which byte of sb
+template <int PIECE> __device__ __forceinline__ f32x4 mfma_codes(const u32x4 &a0, const u32x4 &a1, const u32x4 &b0, const u32x4 &b1, const f32x4 &c, uint32_t sa, uint32_t sb)
+{
+    const i32x8 a = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
+    const i32x8 b = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3], (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
+    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, (int)sa, PIECE, (int)sb);
+}
 // eight E4M3 codes as values of the 16-bit format: all of them are numbers of it (bf16: also with a power of two)
 template <int DT> __device__ __forceinline__ u32x4 values8(uint32_t lo, uint32_t hi, float scale)
 {
@@ -161,7 +168,8 @@ struct Cached {
 };
 __device__ __forceinline__ int32_t select4(const Runs &p, uint32_t i)
 {
-    const int32_t lo = i & 1 ? p.page[1] : p.page[0], hi = i & 1 ? p.page[3] : p.page[2];
+    const int32_t p0 = p.page[0], p1 = p.page[1], p2 = p.page[2], p3 = p.page[3];
+    const int32_t lo = i & 1 ? p1 : p0, hi = i & 1 ? p3 : p2;
     return i & 2 ? hi : lo;
 }
 
@@ -218,9 +226,18 @@ template <int D, int PARTS> __device__ __forceinline__ void copy_values(const Ca
 // 16 consecutive tokens a lane: one run of 16 bytes.  A run of 16 keys' bytes is two steps of the first product, whose order of
 // dimensions is the same for the queries.
 // Query rows are pairs of (token, head of the key head's group).  A wave has 16 NT of them.
-template <int DT, int D, int NT, int LAG> struct Rows {
+//
+// Scores of bf16 queries take the keys' codes as they are (BYTES): a bf16 number has eight significant bits, so a query is the sum of two E4M3 numbers,
+// of which the second has what the first one's rounding left.  A row has a power of two for each: the largest value is 128 to 256 in the first, and in the second
+// 32 times as much, which loses less than 2^-22 of the row's largest value.  The two products cost what one of bf16 does, the page's scale comes with
+// them, and the vector unit has no keys to convert (two prompts of 4000 tokens over 5003: 358 -> 336 us; where rows are few it is the memory's time, and
+// one sequence's call would take 11.7 us instead of 10.9).  Values are converted: the weights would cost more as two E4M3 numbers than the values do as bf16.
+template <int DT, int D, int NT, bool MANY> struct Rows {
+    static constexpr bool BYTES = MANY && DT == BF16 && D >= 128;
+    static constexpr float LAG = MANY ? 8 : 0;
     static constexpr int KC = D / 64, VT = D / 16;
-    u32x4 q[NT][KC][2];
+    u32x4 q[NT][KC][2];                 // eight values each; BYTES: sixteen of the first numbers, and of the second ones
+    uint32_t q_scale[NT];               // BYTES: a byte for each of the two
     // The weights' sum is a product too, with a row of ones: every register of `total` has it, and it is that of the rounded weights, whose
     // errors the division takes out again where one weight outdoes the others.
     f32x4 o[NT][VT], total[NT];
@@ -245,6 +262,7 @@ template <int DT, int D, int NT, int LAG> struct Rows {
 #pragma unroll
             for (int i = 0; i < VT; ++i) o[n][i] = f32x4{};
             total[n] = f32x4{};
+            if constexpr (BYTES) in_two(n);
             most[n] = -__builtin_inff();
         }
         least = row0 < rows ? first + (int32_t)quotient(row0, a.group) : -1;
@@ -256,42 +274,127 @@ template <int DT, int D, int NT, int LAG> struct Rows {
         value_at = col * 64 + ((g ^ value_turn(col)) << 4);
     }
 
-    __device__ __forceinline__ void scores(const Tile<D> &tile, f32x4 (&x)[NT][4]) const
+    __device__ __forceinline__ void in_two(int n)
+    {
+        uint32_t top = 0;                                    // the largest finite magnitude
+#pragma unroll
+        for (int i = 0; i < KC; ++i)
+#pragma unroll
+            for (int h = 0; h < 2; ++h)
+#pragma unroll
+                for (int j = 0; j < 4; ++j) {
+                    const uint32_t a = q[n][i][h][j] & 0x7FFF, b = q[n][i][h][j] >> 16 & 0x7FFF;
+                    top = a < 0x7F80 && a > top ? a : top;
+                    top = b < 0x7F80 && b > top ? b : top;
+                }
+        top = bits_of(over_groups_max(f32_of_bits(top << 16))) >> 23;
+        const uint32_t byte = top > 13 ? top - 7 : 6;
+        const float by = power_of(254 - byte);
+        q_scale[n] = byte | (byte - 5) << 8;
+#pragma unroll
+        for (int i = 0; i < KC; ++i) {
+            u32x4 first, second;
+#pragma unroll
+            for (int j = 0; j < 4; ++j) {
+                float v[4], r[4];
+#pragma unroll
+                for (int k = 0; k < 2; ++k) {
+                    const f32x2 u = unpack2<BF16>(q[n][i][j >> 1][2 * (j & 1) + k]);
+                    v[2 * k] = u[0] * by, v[2 * k + 1] = u[1] * by;
+                }
+                // (a row with an infinity has no softmax: NaN)
+#pragma unroll
+                for (int k = 0; k < 4; ++k) v[k] = __builtin_isinf(v[k]) ? __builtin_nanf("") : v[k];
+                uint32_t w = 0;
+                w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], w, false);
+                w = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w, true);
+                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+                r[0] = v[0] - lo[0], r[1] = v[1] - lo[1], r[2] = v[2] - hi[0], r[3] = v[3] - hi[1];
+                first[j] = w;
+                w = 0;
+                w = __builtin_amdgcn_cvt_pk_fp8_f32(32 * r[0], 32 * r[1], w, false);
+                w = __builtin_amdgcn_cvt_pk_fp8_f32(32 * r[2], 32 * r[3], w, true);
+                second[j] = w;
+            }
+            q[n][i][0] = first, q[n][i][1] = second;
+        }
+    }
+
+    static constexpr int EARLY = KC < 2 ? KC : 2;            // keys that fit registers before they are needed
+    __device__ __forceinline__ u32x4 keys_of(const Tile<D> &tile, int i, int j) const { return *reinterpret_cast<const u32x4 *>(tile.keys + key_at[i] + 4 * j * D); }
+    __device__ __forceinline__ void load_keys(const Tile<D> &tile, u32x4 (&k)[EARLY][4]) const
+    {
+#pragma unroll
+        for (int i = 0; i < EARLY; ++i)
+#pragma unroll
+            for (int j = 0; j < 4; ++j) k[i][j] = keys_of(tile, i, j);
+    }
+    // early: what load_keys read.  k_byte: BYTES: the scale of the keys of this lane's row of the product
+    __device__ __forceinline__ void scores(const Tile<D> &tile, const u32x4 (&early)[EARLY][4], f32x4 (&x)[NT][4], uint32_t k_byte) const
     {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[n][j] = f32x4{};
+        if constexpr (BYTES) {
 #pragma unroll
-        for (int i = 0; i < KC; ++i) {
-            u32x4 k[4];
+            for (int i = 0; i < KC; i += 2) {
+                u32x4 k[2][4];
 #pragma unroll
-            for (int j = 0; j < 4; ++j) k[j] = *reinterpret_cast<const u32x4 *>(tile.keys + key_at[i] + 4 * j * D);
+                for (int h = 0; h < 2; ++h)
 #pragma unroll
-            for (int h = 0; h < 2; ++h)
+                    for (int j = 0; j < 4; ++j) k[h][j] = i < EARLY ? early[h][j] : keys_of(tile, i + h, j);
 #pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const u32x4 v = values8<DT>(k[j][2 * h], k[j][2 * h + 1], 1.0f);
+                for (int j = 0; j < 4; ++j)
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) x[n][j] = mfma16<DT>(v, q[n][i][h], x[n][j]);
-                }
+                    for (int n = 0; n < NT; ++n) x[n][j] = mfma_codes<0>(k[0][j], k[1][j], q[n][i][0], q[n][i + 1][0], x[n][j], k_byte, q_scale[n]);
+#pragma unroll
+                for (int j = 0; j < 4; ++j)
+#pragma unroll
+                    for (int n = 0; n < NT; ++n) x[n][j] = mfma_codes<1>(k[0][j], k[1][j], q[n][i][1], q[n][i + 1][1], x[n][j], k_byte, q_scale[n]);
+            }
+        } else {
+#pragma unroll
+            for (int i = 0; i < KC; ++i) {
+                u32x4 k[4];
+#pragma unroll
+                for (int j = 0; j < 4; ++j) k[j] = i < EARLY ? early[i][j] : keys_of(tile, i, j);
+#pragma unroll
+                for (int h = 0; h < 2; ++h)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) {
+                        const u32x4 v = values8<DT>(k[j][2 * h], k[j][2 * h + 1], 1.0f);
+#pragma unroll
+                        for (int n = 0; n < NT; ++n) x[n][j] = mfma16<DT>(v, q[n][i][h], x[n][j]);
+                    }
+            }
         }
     }
 
-    // page, vs: of the lane group's run.  by: its keys' scale, the call's and log2 e.  arrived(): waits for the tile's values.
+    // the run whose keys' scale the lane needs
+    static __device__ __forceinline__ uint32_t scale_run() { return BYTES ? threadIdx.x >> 2 & 3 : threadIdx.x >> 4 & 3; }
+
+    // page, vs: of the lane group's run.  ks: its keys' scale (BYTES: scores have it).  by: the call's scale and log2 e.  arrived(): waits for the tile's values.
     template <typename F>
-    __device__ __forceinline__ void add(const Tile<D> &tile, f32x4 (&x)[NT][4], int32_t t0, int32_t length, bool whole_pages, int32_t page, float by, float vs,
+    __device__ __forceinline__ void add(const Tile<D> &tile, f32x4 (&x)[NT][4], int32_t t0, int32_t length, bool whole_pages, int32_t page, float ks, float by, float vs,
                                         F arrived)
     {
         const uint32_t g = threadIdx.x >> 4 & 3;
         const int32_t tv = t0 + 16 * (int32_t)g;
         // What a row does not see takes no part, whatever its codes are.  (The empty instructions keep what few tiles need out of the others' way, where
         // the compiler would compute both and select.)
+        constexpr int AHEAD = MANY ? VT / 2 : 0;             // values on their way while the weights are computed
+        u32x4 v[VT];
+#pragma unroll
+        for (int i = 0; i < AHEAD; ++i) v[i] = *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024);
+        if (AHEAD) __builtin_amdgcn_sched_barrier(0);
         const bool partial = t0 + 63 > least || t0 + 64 > length || !whole_pages;
+        if constexpr (!BYTES) {
 #pragma unroll
-        for (int n = 0; n < NT; ++n)
+            for (int n = 0; n < NT; ++n)
 #pragma unroll
-            for (int j = 0; j < 4; ++j) x[n][j] *= by;
+                for (int j = 0; j < 4; ++j) x[n][j] *= ks;
+        }
         if (partial) {
             asm volatile("");
 #pragma unroll
@@ -312,11 +415,11 @@ template <int DT, int D, int NT, int LAG> struct Rows {
                 high = max3(high, x[n][j][0], x[n][j][1]);
                 high = max3(high, x[n][j][2], x[n][j][3]);
             }
-            high = over_groups_max(high);
+            high = over_groups_max(high) * by;
             // Weights are taken relative to a maximum that may lag behind by up to 2^LAG: in 32 bits that costs nothing, and most tiles need no change of
             // what is summed already.  It does cost the one weight that would be 1, exactly, its exactness in bf16 (error against 64 bits 0.0022 instead of 0.0018),
             // so where time is the memory's the maximum is kept (many rows: 354 us with a lag of 8, 376 with none).
-            if (__any(high > most[n] + (float)LAG)) {
+            if (__any(high > most[n] + LAG)) {
                 const float now = fmaxf(most[n], high), fade = now == -__builtin_inff() ? 1.0f : exp2_of(most[n] - now);
                 most[n] = now;
                 total[n] *= fade;
@@ -328,8 +431,8 @@ template <int DT, int D, int NT, int LAG> struct Rows {
             for (int h = 0; h < 2; ++h)
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
-                    const float lo = exp2_of(x[n][2 * h + j / 2][2 * (j & 1)] - base);
-                    const float hi = exp2_of(x[n][2 * h + j / 2][2 * (j & 1) + 1] - base);
+                    const float lo = exp2_of(__builtin_fmaf(x[n][2 * h + j / 2][2 * (j & 1)], by, -base));
+                    const float hi = exp2_of(__builtin_fmaf(x[n][2 * h + j / 2][2 * (j & 1) + 1], by, -base));
                     p[n][h][j] = pack2<BF16>(lo, hi);
                     if constexpr (DT == FP16) {
                         const f32x2 r = unpack2<BF16>(p[n][h][j]);
@@ -346,9 +449,8 @@ template <int DT, int D, int NT, int LAG> struct Rows {
                 if constexpr (DT == FP16) total[n] = mfma16<BF16>(ones, rest_of[n][h], total[n]);
             }
         arrived();
-        u32x4 v[VT];
 #pragma unroll
-        for (int i = 0; i < VT; ++i) v[i] = *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024);
+        for (int i = AHEAD; i < VT; ++i) v[i] = *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024);
         if (partial) {
             asm volatile("");
             // Bytes behind the sequence's end and of no page are anyone's.  A value that is NaN has to reach the rows that see it, and no other:
@@ -459,12 +561,12 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
     Runs runs{};
     uint32_t k_byte = 0, v_byte = 0;
     auto ask_keys = [&](int32_t t0) {                        // and the scales, before them
-        runs = cache.runs(t0, raw);
-        const int32_t page = select4(runs, g);
-        const size_t at = (size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + head;
-        k_byte = c.k_scales[at], v_byte = c.v_scales[at];
+        const Runs next = cache.runs(t0, raw);
+        runs = next;
+        const int32_t keys = select4(next, Rows<DT, D, NT, false>::scale_run()), values = select4(next, g);
+        k_byte = c.k_scales[(size_t)(uint32_t)(keys < 0 ? 0 : keys) * c.heads + head], v_byte = c.v_scales[(size_t)(uint32_t)(values < 0 ? 0 : values) * c.heads + head];
         __builtin_amdgcn_sched_barrier(0);
-        copy_keys<D, 1>(cache, runs, t0, tile, 0);
+        copy_keys<D, 1>(cache, next, t0, tile, 0);
         cache.table_entries(t0 + STEP, raw);
     };
     if (first < v.to) {
@@ -473,7 +575,7 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
         __builtin_amdgcn_sched_barrier(0);
         copy_values<D, 1>(cache, runs, first, tile, 0);
     }
-    Rows<DT, D, NT, 0> r;
+    Rows<DT, D, NT, false> r;
     r.begin(a, s, row0, v.rows, head);
     for (int32_t t0 = first; t0 < v.to; t0 += STEP) {
         const Runs now = runs;
@@ -485,13 +587,15 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
         asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
         __builtin_amdgcn_sched_barrier(0);
         f32x4 x[NT][4];
-        r.scores(tile, x);
-        const float by = power_of(k_byte) * a.scale, vs = page >= 0 ? power_of(v_byte) : 1.0f;       // (no page: another one's, and 0 * NaN would be one)
+        u32x4 k[Rows<DT, D, NT, false>::EARLY][4];
+        r.load_keys(tile, k);
+        r.scores(tile, k, x, k_byte);
+        const float ks = power_of(k_byte), vs = page >= 0 ? power_of(v_byte) : 1.0f;       // (no page: another one's, and 0 * NaN would be one)
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (the keys have been read)
         if (more) ask_keys(t0 + STEP);
         __builtin_amdgcn_sched_barrier(0);
-        r.add(tile, x, t0, s.length, whole, page, by, vs, [&] {
+        r.add(tile, x, t0, s.length, whole, page, ks, a.scale, vs, [&] {
             // the same for the values, with the next keys behind them
             __builtin_amdgcn_sched_barrier(0);
             if (more) asm volatile("s_waitcnt vmcnt(%0)" ::"n"(COPIES) : "memory");
@@ -588,15 +692,15 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
         copy_keys<D, 4>(cache, p, t0, to, wave);
         copy_values<D, 4>(cache, p, t0, to, wave);
         pg = select4(p, g);
-        const size_t at = (size_t)(uint32_t)(pg < 0 ? 0 : pg) * c.heads + head;
-        k = c.k_scales[at], w = c.v_scales[at];
+        const int32_t keys = select4(p, Rows<DT, D, NT, true>::scale_run());
+        k = c.k_scales[(size_t)(uint32_t)(keys < 0 ? 0 : keys) * c.heads + head], w = c.v_scales[(size_t)(uint32_t)(pg < 0 ? 0 : pg) * c.heads + head];
     };
     if (v.from < v.to) {
         cache.table_entries(v.from, raw);
         ask(v.from, tiles[0], page, whole, kb, vb);
         cache.table_entries(v.from + 64, raw);
     }
-    Rows<DT, D, NT, 8> r;
+    Rows<DT, D, NT, true> r;
     r.begin(a, s, row0, v.rows, head);
     int buffer = 0;
     for (int32_t t0 = v.from; t0 < v.to; t0 += 64, buffer ^= 1) {
@@ -604,17 +708,20 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
         // this wave's copies are in LDS, then all waves' are, and nobody reads the tile before any more
         asm volatile("s_waitcnt vmcnt(0) lgkmcnt(0)\n\ts_barrier" ::: "memory");
         __builtin_amdgcn_sched_barrier(0);
+        u32x4 k[Rows<DT, D, NT, true>::EARLY][4];            // (on their way while the next tile is asked for)
+        r.load_keys(tiles[buffer], k);
+        __builtin_amdgcn_sched_barrier(0);
         if (t0 + 64 < v.to) {
             ask(t0 + 64, tiles[buffer ^ 1], next_page, next_whole, next_kb, next_vb);
             cache.table_entries(t0 + 128, raw);
         }
         // (also the last tiles, of which the first waves' rows see nothing: a branch around them cost every tile a copy of all sums)
         f32x4 x[NT][4];
-        r.scores(tiles[buffer], x);
+        r.scores(tiles[buffer], k, x, kb);
         // (a wave between its products goes first: the other one of its SIMD has matrix instructions running meanwhile; 400 -> 378 us for two prompts of
         // 4000 tokens over 5003)
         __builtin_amdgcn_s_setprio(1);
-        r.add(tiles[buffer], x, t0, s.length, whole, page, power_of(kb) * a.scale, page >= 0 ? power_of(vb) : 1.0f, [] { __builtin_amdgcn_s_setprio(0); });
+        r.add(tiles[buffer], x, t0, s.length, whole, page, power_of(kb), a.scale, page >= 0 ? power_of(vb) : 1.0f, [] { __builtin_amdgcn_s_setprio(0); });
         page = next_page, whole = next_whole, kb = next_kb, vb = next_vb;
     }
     if (cache.bad && threadIdx.x == 0) complain(c);

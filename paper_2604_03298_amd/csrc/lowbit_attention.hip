@@ -537,6 +537,8 @@ __device__ __forceinline__ Cached cached_of(const Attend &a, const Sequence &s, 
 // been multiplied, the next tile's are copied there while the weights are computed and the values multiplied, and the next values while the next keys are.
 // It waits for its own copies only: no barrier until the end.  Two waves to a SIMD (head_dim 256: one) did more than copies further ahead: a tile's
 // chain of steps leaves half of a wave's cycles idle (64 sequences of up to 8191 tokens: 4 waves with two tiles each 150 us).
+// Bound by HBM: 64 sequences of up to 8191 tokens, 8 heads of 128, bf16 130 us (5.1 TB/s, what a copy reaches); two of 131072, fp16, pages of 16,
+// 83 us and the join 4.5.  One sequence of 1000 tokens: 10 us, a chain of dependent reads.
 template <int DT, int D, int NT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kernel(Attend a)
 {
@@ -660,8 +662,11 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
 // ---- many rows: the matrix and vector units work, the cache's codes come from the die's own cache ---------------------------------------
 
 // 16 NT rows to each of four waves, which share the tiles: a wave has all of them, so nothing is joined in the end.  The memory unit copies the codes
-// of a tile into LDS while the one before is worked on.  Every wave makes 16-bit values of the codes by itself: a conversion makes two of
+// of a tile into LDS while the one before is worked on.  Every wave makes 16-bit values of the codes by itself, where it needs them: a conversion makes two of
 // them in the time of any vector instruction, and NT tiles of rows use each.
+// Bound by the vector and the matrix unit together: two prompts of 4000 tokens over 5003, 32 heads of 128, bf16 338 us (880 TFLOP/s); matrix instructions take
+// 39 % of the cycles, vector instructions 58 % (the issue of the former among them).  Multiplying a tile's values while the next tile's weights are computed, instruction by instruction, did
+// not help (360 us), nor did four tiles of rows to a wave, which do not fit the registers.
 template <int DT, int D, int NT>
 __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
 {

@@ -101,7 +101,8 @@ template <int BYTES> __device__ __forceinline__ void copy_to_lds(Range r, uint32
 // How a stage lies in LDS.  A row (of weights, or a token's) is a run of chunks of 16 bytes, chunk i at place i ^ turn(row).  A wave reads 16 bytes a lane
 // in four goes of sixteen lanes, lanes {0-3, 12-15, 20-27} the first: rows {0-3, 12-15} of one lane group and rows {4-11} of its neighbour.  Each
 // turn puts such sixteen chunks into the sixteen different places of 256 bytes, so that no bank is asked twice:
-//   256 bytes a row, the groups' chunks four apart (16-bit activations; one apart, where a step is one block: the row itself); 128 bytes, one apart (4-bit ones, and their weights); 64 bytes, one apart
+//   256 bytes a row: the groups' chunks four apart (bf16 activations), or one apart (fp16, where a step is one block: the turn is the row itself)
+//   128 bytes, one apart (4-bit ones, and their weights); 64 bytes, one apart
 template <int ROW> __device__ __forceinline__ uint32_t turn(uint32_t r)
 {
     if constexpr (ROW == 256) return (r & 3) + 12 * (r >> 3 & 1);
@@ -109,13 +110,17 @@ template <int ROW> __device__ __forceinline__ uint32_t turn(uint32_t r)
     return 2 * (r >> 3 & 1);
 }
 
-// Weights are the left operand of the matrix instructions, activations the right one.
+// Weights are the left operand of the matrix instructions, activations the right one (fp16: the other way round).
 // A workgroup has 16 RT WN rows of weights and 16 MT WM tokens; a wave 16 RT rows and 16 MT tokens of them.  Where there are few tokens the rows of a
-// workgroup are few too, so that all compute units have some, and KG groups of waves take its stages in turn; their sums meet in LDS.  A stage is 128 columns (4-bit activations: 256),
-// whose codes, scales and activations the memory unit brings into LDS, BUFFERS stages in turn.  Loads straight into registers were slower: a lane has
+// workgroup are few too, so that all compute units have some, and KG groups of waves take its stages in turn; their sums meet in LDS.  A stage is 128 columns
+// (4-bit activations: 256), whose codes, scales and activations the memory unit brings into LDS, BUFFERS stages in turn.  Loads straight into registers were slower: a lane has
 // a row of its own there, so that each lane's 16 bytes are an access by themselves to the vector cache, where four neighbouring lanes of a copy make one
 // (2048 tokens x 4096 x 16384: 125 million accesses and 272 us then; the cache takes about one in a cycle).
 // As left operand a lane has row lane mod 16, and of a stage's blocks of 32 columns block lane / 16 (or 4 s + lane / 16 at step s).
+// Few tokens: bound by the weights' way from memory; 4096 x 11008 bf16 with one token 7.3 us a call (3.3 TB/s), 32 tokens 10, 8192 x 28672 with one token
+// 22 (5.7 TB/s).
+// Many: by the matrix unit and LDS; 4096 tokens x 8192 x 28672 bf16 1400 us (1375 TFLOP/s, what a large library product of bf16 reaches on this card),
+// fp16 255 us for 2048 x 4096 x 11008 (725 TFLOP/s), 4-bit activations 500 us for 4096 x 8192 x 28672 (3850 TFLOP/s; LDS is asked for nearly all it can give).
 template <int ACT, int RT, int MT, int WN, int WM, int KG, int BUFFERS>
 __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) product_tile_kernel(Product a)
 {

@@ -9,7 +9,8 @@ namespace lowbit {
 // consecutive values (one 16-byte load, one 4-byte store), four threads a block of 32, so a wave's accesses are whole lines both
 // ways; the largest magnitude of a block takes two exchanges between neighbouring lanes.  It is found on the bits: magnitudes of
 // floats order as whole numbers do, and a NaN or an infinity has the exponent field 255.  U vectors per thread are asked for
-// before the first is used: 11008 x 4096 bf16 take 21.5 us with two (5.3 TB/s), 24 with four, 27.6 with eight.
+// before the first is used: 11008 x 4096 bf16 took 21.5 us with two, 24 with four, 27.6 with eight; with stores that stream past the cache 17.6
+// (6.5 TB/s: the matrix fits the last-level cache).  One row of 4096 takes 1.9 us, and its call 5.4 on the host.
 template <int DT, int U>
 __global__ void __launch_bounds__(256) mx4_quantize_kernel(const void *__restrict__ in, uint32_t cols, size_t stride, Divide per_row,
                                                            uint32_t n_vec, uint32_t *__restrict__ codes, uint8_t *__restrict__ scales)
@@ -54,7 +55,7 @@ __global__ void __launch_bounds__(256) mx4_quantize_kernel(const void *__restric
     }
 }
 
-// The way back: four bytes of codes and a scale in, eight values out.  Bound by HBM as well.
+// The way back: four bytes of codes and a scale in, eight values out.  Bound by HBM as well: 11008 x 4096 bf16 16.5 us (6.9 TB/s).
 template <int DT, int U>
 __global__ void __launch_bounds__(256) mx4_dequantize_kernel(const uint32_t *__restrict__ codes, const uint8_t *__restrict__ scales, uint32_t cols,
                                                              size_t stride, Divide per_row, uint32_t n_vec, void *__restrict__ out)

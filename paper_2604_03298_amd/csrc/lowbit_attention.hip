@@ -41,21 +41,16 @@ __device__ __forceinline__ float share_of(const Attend &a, const Sequence &s, ui
 
 // The largest of four lanes sixteen apart.  The exchanges swap rows of lanes of two registers that hold the same; as instructions of their own, since the
 // compiler takes the two results for equal.
+// (`maximum` is one instruction for three operands; fmaxf passes each through an instruction of its own first.  It gives NaN where one of them is, which is the row's result.)
 __device__ __forceinline__ float over_groups_max(float v)
 {
     float a = v, b = v;
     asm("s_nop 1\n\tv_permlane32_swap_b32 %0, %1" : "+v"(a), "+v"(b));
-    a = b = fmaxf(a, b);
+    a = b = __builtin_elementwise_maximum(a, b);
     asm("s_nop 1\n\tv_permlane16_swap_b32 %0, %1" : "+v"(a), "+v"(b));
-    return fmaxf(a, b);
+    return __builtin_elementwise_maximum(a, b);
 }
-// (fmaxf passes each operand through an instruction of its own first, in case it is a signalling NaN: these are products)
-__device__ __forceinline__ float max3(float a, float b, float c)
-{
-    float r;
-    asm("v_max3_f32 %0, %1, %2, %3" : "=v"(r) : "v"(a), "v"(b), "v"(c));
-    return r;
-}
+__device__ __forceinline__ float max3(float a, float b, float c) { return __builtin_elementwise_maximum(__builtin_elementwise_maximum(a, b), c); }
 __device__ __forceinline__ float exp2_of(float v) { return __builtin_amdgcn_exp2f(v); }
 
 template <int DT> __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const u32x4 &b, const f32x4 &c)

@@ -69,25 +69,27 @@ def _dtype(t) -> int:
 
 def _rows(t, what):
     """(rows, columns, row stride) of a matrix whose rows are runs."""
-    stride = t.stride()
-    if len(stride) != 2 or (stride[1] != 1 and t.shape[1] > 1):
-        raise ValueError(f"{what}: a matrix whose columns lie side by side is wanted")
-    rows, cols = t.shape
-    return rows, cols, stride[0] if rows > 1 else cols
+    shape = t.shape                                         # (an attribute of a tensor costs 0.1 us: each is asked for once)
+    if len(shape) == 2:
+        rows, cols = shape
+        stride, side = t.stride()
+        if side == 1 or cols <= 1:
+            return rows, cols, stride if rows > 1 else cols
+    raise ValueError(f"{what}: a matrix whose columns lie side by side is wanted")
 
 
 def _mx4(codes, scales, what):
     """(rows, padded columns) of a matrix in 4 bits."""
     rows, half = codes.shape
     n, blocks = scales.shape
-    if half & 63 or half != 16 * blocks or n != rows or codes.element_size() != 1 or scales.element_size() != 1 \
+    if half & 63 or half != 16 * blocks or n != rows or codes.itemsize != 1 or scales.itemsize != 1 \
             or not codes.is_contiguous() or not scales.is_contiguous():
         raise ValueError(f"{what}: codes (rows, padded / 2) and scales (rows, padded / 32) of bytes without gaps are wanted, padded a multiple of 128")
     return rows, 2 * half
 
 
 def _space(workspace):
-    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.numel() * workspace.element_size())
+    return (None, 0) if workspace is None else (workspace.data_ptr(), workspace.nbytes)
 
 
 # ---- matrices in 4 bits -------------------------------------------------------------
@@ -117,8 +119,8 @@ def mx4_quantize(src, codes, scales, stream=None) -> int:
     _same_padding(padded, cols)
     if n != rows:
         raise ValueError("src and codes differ in their rows")
-    return int(lib().enec_mx4_quantize(src.data_ptr(), rows, cols, stride, _dtype(src), codes.data_ptr(), scales.data_ptr(),
-                                       enec._stream_handle(stream)))
+    return lib().enec_mx4_quantize(src.data_ptr(), rows, cols, stride, _dtype(src), codes.data_ptr(), scales.data_ptr(),
+                                   enec._stream_handle(stream))
 
 
 def mx4_dequantize(codes, scales, out, stream=None) -> int:
@@ -128,8 +130,8 @@ def mx4_dequantize(codes, scales, out, stream=None) -> int:
     _same_padding(padded, cols)
     if n != rows:
         raise ValueError("out and codes differ in their rows")
-    return int(lib().enec_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), stride, _dtype(out),
-                                         enec._stream_handle(stream)))
+    return lib().enec_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), stride, _dtype(out),
+                                     enec._stream_handle(stream))
 
 
 def mx4_linear_workspace(m: int, n: int, k: int) -> int:
@@ -145,8 +147,8 @@ def mx4_linear(x, codes, scales, out, workspace=None, stream=None) -> int:
     if (rows, cols) != (m, n) or out.dtype != x.dtype:
         raise ValueError(f"out: ({m}, {n}) of x's format is wanted")
     ws, size = _space(workspace)
-    return int(lib().enec_mx4_linear(x.data_ptr(), m, x_stride, _dtype(x), codes.data_ptr(), scales.data_ptr(), n, k, out.data_ptr(), y_stride,
-                                     ws, size, enec._stream_handle(stream)))
+    return lib().enec_mx4_linear(x.data_ptr(), m, x_stride, _dtype(x), codes.data_ptr(), scales.data_ptr(), n, k, out.data_ptr(), y_stride,
+                                 ws, size, enec._stream_handle(stream))
 
 
 def mx4_matmul_workspace(m: int, n: int, k: int) -> int:
@@ -161,8 +163,8 @@ def mx4_matmul(x_codes, x_scales, codes, scales, out, workspace=None, stream=Non
     if padded != other or (rows, cols) != (m, n):
         raise ValueError(f"matrices of as many columns and out ({m}, {n}) are wanted")
     ws, size = _space(workspace)
-    return int(lib().enec_mx4_matmul(x_codes.data_ptr(), x_scales.data_ptr(), m, codes.data_ptr(), scales.data_ptr(), n, padded, out.data_ptr(),
-                                     y_stride, _dtype(out), ws, size, enec._stream_handle(stream)))
+    return lib().enec_mx4_matmul(x_codes.data_ptr(), x_scales.data_ptr(), m, codes.data_ptr(), scales.data_ptr(), n, padded, out.data_ptr(),
+                                 y_stride, _dtype(out), ws, size, enec._stream_handle(stream))
 
 
 # ---- the cache ----------------------------------------------------------------------
@@ -200,41 +202,39 @@ def _batch(table, starts, lengths, n_tokens, status):
     batch = lengths.numel()
     if len(shape) != 2 or shape[0] != batch or starts.numel() != batch + 1:
         raise ValueError("table (batch, pages) has a row for each of lengths, starts one entry more")
-    if table.element_size() != 4 or starts.element_size() != 4 or lengths.element_size() != 4 \
+    if table.itemsize != 4 or starts.itemsize != 4 or lengths.itemsize != 4 \
             or not table.is_contiguous() or not starts.is_contiguous() or not lengths.is_contiguous():
         raise ValueError("table, starts and lengths are int32 without gaps")
     return _BATCH.pack(table.data_ptr(), starts.data_ptr(), lengths.data_ptr(), shape[1], batch, n_tokens,
                        0 if status is None else status.data_ptr())
 
 
-def _tokens(t, heads, dim, what):
-    """(token stride, head stride) of (tokens, heads, head_dim) values."""
-    stride = t.stride()
-    if len(stride) != 3 or stride[2] != 1 or t.shape[1:] != (heads, dim):
+def _tokens(t, other, heads, dim, what):
+    """(tokens, token stride, head stride, other's token stride, head stride) of two tensors of (tokens, heads, head_dim) values."""
+    shape = t.shape
+    if len(shape) != 3 or shape != other.shape or t.dtype != other.dtype:
+        raise ValueError(f"{what} are two tensors of (tokens, heads, head_dim) values, alike in shape and format")
+    tokens, h, d = shape
+    token, head, side = t.stride()
+    other_token, other_head, other_side = other.stride()
+    if h != heads or d != dim or side != 1 or other_side != 1:
         raise ValueError(f"{what}: (tokens, {heads}, {dim}) values, a head's side by side, are wanted")
-    return stride[0], stride[1]
-
-
-def _keys_values(cache, k, v):
-    ks, vs = _tokens(k, cache.heads, cache.head_dim, "k"), _tokens(v, cache.heads, cache.head_dim, "v")
-    if k.shape != v.shape or k.dtype != v.dtype:
-        raise ValueError("k and v differ in shape or format")
-    return ks, vs
+    return tokens, token, head, other_token, other_head
 
 
 def cache_write(cache, k, v, table, starts, lengths, status=None, stream=None) -> int:
     """Enqueues enec_cache_write.  k, v: (tokens, heads, head_dim) of bf16 or fp16, the newest tokens of their sequences; table (batch,
     pages), starts (batch + 1) and lengths (batch, new tokens included): int32 on the device; status: None or an int32 word holding 0."""
-    ks, vs = _keys_values(cache, k, v)
-    b = _batch(table, starts, lengths, k.shape[0], status)
-    return int(lib().enec_cache_write(cache.ref, b, k.data_ptr(), *ks, v.data_ptr(), *vs, _dtype(k), enec._stream_handle(stream)))
+    tokens, kt, kh, vt, vh = _tokens(k, v, cache.heads, cache.head_dim, "k and v")
+    b = _batch(table, starts, lengths, tokens, status)
+    return lib().enec_cache_write(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, _dtype(k), enec._stream_handle(stream))
 
 
 def cache_read(cache, k, v, table, starts, lengths, status=None, stream=None) -> int:
     """Enqueues enec_cache_read: the newest tokens' keys and values into k, v (bf16, fp16 or fp32); starts of whole lengths read all."""
-    ks, vs = _keys_values(cache, k, v)
-    b = _batch(table, starts, lengths, k.shape[0], status)
-    return int(lib().enec_cache_read(cache.ref, b, k.data_ptr(), *ks, v.data_ptr(), *vs, _dtype(k), enec._stream_handle(stream)))
+    tokens, kt, kh, vt, vh = _tokens(k, v, cache.heads, cache.head_dim, "k and v")
+    b = _batch(table, starts, lengths, tokens, status)
+    return lib().enec_cache_read(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, _dtype(k), enec._stream_handle(stream))
 
 
 def cache_attention_workspace(cache, batch: int, n_tokens: int, q_heads: int, max_new: int, max_length: int) -> int:
@@ -244,11 +244,9 @@ def cache_attention_workspace(cache, batch: int, n_tokens: int, q_heads: int, ma
 def cache_attention(cache, q, out, table, starts, lengths, max_new: int, max_length: int, workspace=None, scale: float | None = None,
                     status=None, stream=None) -> int:
     """Enqueues enec_cache_attention.  q, out: (tokens, q_heads, head_dim) of bf16 or fp16; scale: head_dim ** -0.5 unless given."""
-    heads = q.shape[1]
-    qs, os_ = _tokens(q, heads, cache.head_dim, "q"), _tokens(out, heads, cache.head_dim, "out")
-    if q.shape != out.shape or q.dtype != out.dtype:
-        raise ValueError("q and out differ in shape or format")
-    b = _batch(table, starts, lengths, q.shape[0], status)
+    heads, dim = q.shape[1], cache.head_dim
+    tokens, qt, qh, ot, oh = _tokens(q, out, heads, dim, "q and out")
+    b = _batch(table, starts, lengths, tokens, status)
     ws, size = _space(workspace)
-    return int(lib().enec_cache_attention(cache.ref, b, q.data_ptr(), *qs, out.data_ptr(), *os_, _dtype(q), heads, max_new, max_length,
-                                          cache.head_dim ** -0.5 if scale is None else scale, ws, size, enec._stream_handle(stream)))
+    return lib().enec_cache_attention(cache.ref, b, q.data_ptr(), qt, qh, out.data_ptr(), ot, oh, _dtype(q), heads, max_new, max_length,
+                                      dim ** -0.5 if scale is None else scale, ws, size, enec._stream_handle(stream))

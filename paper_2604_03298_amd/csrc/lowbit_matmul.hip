@@ -112,8 +112,8 @@ template <int ROW> __device__ __forceinline__ uint32_t turn(uint32_t r)
 
 // Weights are the left operand of the matrix instructions, activations the right one (fp16: the other way round).
 // A workgroup has 16 RT WN rows of weights and 16 MT WM tokens; a wave 16 RT rows and 16 MT tokens of them.  Where there are few tokens the rows of a
-// workgroup are few too, so that all compute units have some, and KG groups of waves take its stages in turn; their sums meet in LDS.  A stage is 128 columns
-// (4-bit activations: 256), whose codes, scales and activations the memory unit brings into LDS, BUFFERS stages in turn.  Loads straight into registers were slower: a lane has
+// workgroup are few too, so that all compute units have some, and KG groups of waves take its stages in turn; their sums meet in LDS (128 tokens x 4096 x 11008 bf16:
+// two groups 19 us, one 22; one token x 8192 x 28672: four groups 22, one 41).  A stage is 128 columns (4-bit activations: 256), whose codes, scales and activations the memory unit brings into LDS, BUFFERS stages in turn.  Loads straight into registers were slower: a lane has
 // a row of its own there, so that each lane's 16 bytes are an access by themselves to the vector cache, where four neighbouring lanes of a copy make one
 // (2048 tokens x 4096 x 16384: 125 million accesses and 272 us then; the cache takes about one in a cycle).
 // As left operand a lane has row lane mod 16, and of a stage's blocks of 32 columns block lane / 16 (or 4 s + lane / 16 at step s).
@@ -130,7 +130,7 @@ __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) produ
     constexpr uint32_t S_STAGES = ACT == MX4 ? 2 : 4;                    // that sixteen bytes of scales are for
     constexpr int BLOCKS = KG > (int)S_STAGES ? KG / S_STAGES : 1;       // of scales that a round of stages needs
     constexpr int X_COPIES = X_SIZE / 16 / THREADS, W_COPIES = W_SIZE / 16 / THREADS;
-    static_assert(KG == 1 || KG % S_STAGES == 0, "a round needs whole blocks of scales");
+    static_assert(KG == 1 || KG % S_STAGES == 0 || S_STAGES % KG == 0, "rounds and blocks of scales end together");
     static_assert(ACT != FP16 || MT <= 4, "all tokens' tiles at once");
     static_assert(X_SIZE % (16 * THREADS) == 0 && W_SIZE % (16 * THREADS) == 0 && S_SIZE % 256 == 0 && XS_SIZE % 256 == 0, "whole copies of a wave");
     constexpr int U = MT < 4 ? MT : 4, STEPS = ACT == MX4 ? 2 : 4, UNITS = STEPS * (MT / U);
@@ -428,9 +428,14 @@ struct Shape {
     uint32_t rows, tokens, resident, stages;
     double us;
 };
-constexpr Shape SHAPES[3][6] = {{{256, 128, 1, 1, 1.72}, {256, 64, 2, 1, 1.85}, {128, 64, 3, 1, 1.48}, {128, 32, 3, 1, 1.20}, {64, 32, 1, 4, 0.70}, {32, 16, 2, 4, 0.60}},
-                                {{256, 128, 1, 1, 2.75}, {256, 64, 2, 1, 2.80}, {128, 64, 3, 1, 2.10}, {128, 32, 3, 1, 1.45}, {64, 32, 1, 4, 0.90}, {32, 16, 2, 4, 0.75}},
-                                {{256, 256, 1, 1, 2.49}, {128, 128, 2, 1, 1.50}, {128, 64, 2, 1, 1.39}, {128, 32, 2, 1, 0.90}, {64, 32, 1, 4, 0.60}, {32, 16, 2, 4, 0.50}}};
+constexpr Shape SHAPES[3][7] = {
+    {{256, 128, 1, 1, 1.72}, {256, 64, 2, 1, 1.90}, {128, 64, 3, 1, 1.48}, {128, 32, 3, 1, 1.20}, {64, 32, 1, 4, 0.70},
+     {32, 16, 2, 4, 0.60}, {128, 64, 1, 2, 1.08}},
+    {{256, 128, 1, 1, 2.75}, {256, 64, 2, 1, 2.80}, {128, 64, 3, 1, 2.10}, {128, 32, 3, 1, 1.45}, {64, 32, 1, 4, 0.90},
+     {32, 16, 2, 4, 0.75}, {128, 64, 1, 2, 1.80}},
+    {{256, 256, 1, 1, 2.49}, {128, 128, 2, 1, 1.40}, {128, 64, 2, 1, 1.39}, {128, 32, 2, 1, 0.90}, {64, 32, 1, 4, 0.80},
+     {32, 16, 2, 4, 0.50}, {128, 64, 1, 2, 1.10}},
+};
 constexpr double THIN[3] = {0.05, 0.10, 0.05};      // what a workgroup that is not there costs of the time saved: less overlaps
 constexpr const Shape *shapes_of(int act) { return SHAPES[act == MX4 ? 2 : act]; }
 static_assert(BF16 == 0 && FP16 == 1, "the tables' order");
@@ -453,7 +458,7 @@ Plan plan_of(uint32_t m, uint32_t n, uint32_t k, int act)
     if (!mx4) p.laid_out = 2 * (size_t)m * (up(k, 128) * 128);
     const uint32_t groups = up(k, 128), unit = 4, stages = mx4 ? up(groups, 2) : groups;     // a split is whole blocks of scales and whole rounds
     double best = 1e300;
-    for (int i = 0; i < 6; ++i) {
+    for (int i = 0; i < 7; ++i) {
         const Shape &s = shapes_of(act)[i];
         if (s.tokens > 16 && s.tokens >= 2 * up(m, 16) * 16) continue;       // half of the tile or more would be empty
         const uint64_t tiles = (uint64_t)up(n, s.rows) * up(m, s.tokens), full = UNITS * s.resident;
@@ -461,12 +466,12 @@ Plan plan_of(uint32_t m, uint32_t n, uint32_t k, int act)
         for (uint32_t splits = 1; splits == 1 || (splittable && splits <= 16 && splits * unit <= stages && tiles * (splits / 2) < full); splits *= 2) {
             const uint32_t each = up(up(stages, splits), unit) * unit, count = up(stages, each);
             // The busiest compute unit has `most` workgroups.  Fewer than fit take their share of the time and some more; where one fits and not all
-            // units have one, memory has less to do; past two rounds the units drift apart and no one waits.  A workgroup's start and end are 3 us,
+            // units have one, memory has less to do; past that the units drift apart, and half of the last round's waste goes.  A workgroup's start and end are 3 us,
             // and joining is a launch, the sums' way out and back.
             const uint64_t all = tiles * count, most = (all + UNITS - 1) / UNITS, left = most % s.resident;
             double turns = (double)(most / s.resident) + (left ? (double)left / s.resident + (s.resident - left) * THIN[mx4 ? 2 : act] : 0);
             if (s.resident == 1 && all * 4 < most * UNITS * 3) turns *= 0.88;
-            if (turns > 2) turns = (double)all / full;
+            if (turns > 2 || (s.resident > 1 && all > UNITS)) turns = (turns + (double)all / full) / 2;
             const double us = turns * (up(each, s.stages) * s.us + 3) + (count > 1 ? 4 + (double)count * m * n * 8 / 4e6 : 0);
             if (us < best) best = us, p.shape = i, p.splits = count, p.split_stages = each;
         }
@@ -519,7 +524,8 @@ template <int ACT> int launch(Product a, const Plan &p, void *workspace, hipStre
     case 2: ok = launch_tile<ACT, 2, 4, 4, 1, 1, 2>(a, p.splits, s); break;
     case 3: ok = launch_tile<ACT, 2, 2, 4, 1, 1, 3>(a, p.splits, s); break;
     case 4: ok = launch_tile<ACT, 1, 2, 4, 1, 4, 2>(a, p.splits, s); break;
-    default: ok = launch_tile<ACT, 1, 1, 2, 1, 4, 3>(a, p.splits, s); break;
+    case 5: ok = launch_tile<ACT, 1, 1, 2, 1, 4, 3>(a, p.splits, s); break;
+    default: ok = launch_tile<ACT, 2, 4, 4, 1, 2, 2>(a, p.splits, s); break;
     }
     if (!ok) return ENEC_E_HIP;
     if (p.splits > 1) {

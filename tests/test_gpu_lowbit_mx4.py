@@ -288,7 +288,8 @@ def any_codes(n, k, seed):
 
 # ragged sizes that are large enough, in one direction or another, for large tiles and for columns that are split over workgroups
 LARGE = [(1000, 4100, 300), (2100, 5000, 129), (700, 8200, 200), (40, 9000, 1200), (300, 5000, 1200), (3, 20, 8100), (20, 1030, 16380), (70, 500, 16380),
-         (40, 1030, 16380), (130, 5000, 16380), (300, 5000, 16380), (300, 2050, 40000), (20, 1030, 40000)]
+         (40, 1030, 16380), (130, 5000, 16380), (300, 5000, 16380), (300, 2050, 40000), (20, 1030, 40000),
+         (2000, 4090, 130), (500, 2050, 1300), (700, 2050, 1300), (300, 500, 16380), (500, 1030, 8100), (500, 4090, 130), (130, 8100, 130)]
 
 
 @pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])

@@ -659,9 +659,9 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
 // 16 NT rows to each of four waves, which share the tiles: a wave has all of them, so nothing is joined in the end.  The memory unit copies the codes
 // of a tile into LDS while the one before is worked on.  Every wave makes 16-bit values of the codes by itself, where it needs them: a conversion makes two of
 // them in the time of any vector instruction, and NT tiles of rows use each.
-// Bound by the vector and the matrix unit together: two prompts of 4000 tokens over 5003, 32 heads of 128, bf16 332 us (895 TFLOP/s); matrix instructions take
-// 39 % of the cycles, vector instructions 58 % (the issue of the former among them).  Multiplying a tile's values while the next tile's weights are computed, instruction by instruction, did
-// not help (360 us), nor did four tiles of rows to a wave, which do not fit the registers.
+// Bound by the vector and the matrix unit together: two prompts of 4000 tokens over 5003, 32 heads of 128, bf16 332 us (895 TFLOP/s); matrix instructions
+// take 39 % of the cycles, vector instructions 58 % (the issue of the former among them).  Multiplying a tile's values while the next tile's weights are
+// computed, instruction by instruction, did not help (360 us), nor did four tiles of rows to a wave, which do not fit the registers.
 template <int DT, int D, int NT>
 __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
 {

@@ -112,9 +112,10 @@ template <int ROW> __device__ __forceinline__ uint32_t turn(uint32_t r)
 
 // Weights are the left operand of the matrix instructions, activations the right one (fp16: the other way round).
 // A workgroup has 16 RT WN rows of weights and 16 MT WM tokens; a wave 16 RT rows and 16 MT tokens of them.  Where there are few tokens the rows of a
-// workgroup are few too, so that all compute units have some, and KG groups of waves take its stages in turn; their sums meet in LDS (128 tokens x 4096 x 11008 bf16:
-// two groups 19 us, one 22; one token x 8192 x 28672: four groups 22, one 41).  A stage is 128 columns (4-bit activations: 256), whose codes, scales and activations the memory unit brings into LDS, BUFFERS stages in turn.  Loads straight into registers were slower: a lane has
-// a row of its own there, so that each lane's 16 bytes are an access by themselves to the vector cache, where four neighbouring lanes of a copy make one
+// workgroup are few too, so that all compute units have some, and KG groups of waves take its stages in turn; their sums meet in LDS (128 tokens x 4096
+// x 11008 bf16: two groups 19 us, one 22; one token x 8192 x 28672: four groups 22, one 41).  A stage is 128 columns (4-bit activations: 256), whose
+// codes, scales and activations the memory unit brings into LDS, BUFFERS stages in turn.  Loads straight into registers were slower: a lane has a row of
+// its own there, so that each lane's 16 bytes are an access by themselves to the vector cache, where four neighbouring lanes of a copy make one
 // (2048 tokens x 4096 x 16384: 125 million accesses and 272 us then; the cache takes about one in a cycle).
 // As left operand a lane has row lane mod 16, and of a stage's blocks of 32 columns block lane / 16 (or 4 s + lane / 16 at step s).
 // Few tokens: bound by the weights' way from memory; 4096 x 11008 bf16 with one token 7.3 us a call (3.3 TB/s), 32 tokens 10, 8192 x 28672 with one token

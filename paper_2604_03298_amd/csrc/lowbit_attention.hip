@@ -223,16 +223,20 @@ template <int D, int PARTS> __device__ __forceinline__ void copy_values(const Ca
 // Query rows are pairs of (token, head of the key head's group).  A wave has 16 NT of them.
 //
 // Scores of bf16 queries take the keys' codes as they are (BYTES): a bf16 number has eight significant bits, so a query is the sum of two E4M3 numbers,
-// of which the second has what the first one's rounding left.  A row has a power of two for each: the largest value is 128 to 256 in the first, and in the second
-// 32 times as much, which loses less than 2^-22 of the row's largest value.  The two products cost what one of bf16 does, the page's scale comes with
-// them, and the vector unit has no keys to convert (two prompts of 4000 tokens over 5003: 358 -> 336 us; where rows are few it is the memory's time, and
-// one sequence's call would take 11.7 us instead of 10.9).  Values are converted: the weights would cost more as two E4M3 numbers than the values do as bf16.
+// of which the second has what the first one's rounding left.  A row has a power of two for each: the largest value is 128 to 256 in the first, and the second
+// is 32 times as large.  That is exact for values down to 2^-14 of the row's largest, and smaller ones lose less than 2^-22 of it.  That is less than the
+// rounding of sums in 32 bits where most values are far larger, and is taken only where half of a lane's are above 2^-9 of the largest: a wave with a row
+// of other values that lose anything, or of values that are not finite, takes 16-bit keys (not `whole`).  The two products cost what one of bf16 does, the
+// page's scale comes with them, and the vector unit has no keys to convert (two prompts of 4000 tokens over 5003: 354 -> 333 us; where rows are few it is
+// the memory's time, and one sequence's call would take 11.7 us instead of 10.9).  Values are converted: the weights would cost more as two E4M3 numbers
+// than the values do as bf16.
 template <int DT, int D, int NT, bool MANY> struct Rows {
     static constexpr bool BYTES = MANY && DT == BF16 && D >= 128;
     static constexpr float LAG = MANY ? 8 : 0;
     static constexpr int KC = D / 64, VT = D / 16;
     u32x4 q[NT][KC][2];                 // eight values each; BYTES: sixteen of the first numbers, and of the second ones
     uint32_t q_scale[NT];               // BYTES: a byte for each of the two
+    bool whole;                         // BYTES: all rows of the wave are such sums
     // The weights' sum is a product too, with a row of ones: every register of `total` has it, and it is that of the rounded weights, whose
     // errors the division takes out again where one weight outdoes the others.
     f32x4 o[NT][VT], total[NT];
@@ -257,8 +261,17 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
 #pragma unroll
             for (int i = 0; i < VT; ++i) o[n][i] = f32x4{};
             total[n] = f32x4{};
-            if constexpr (BYTES) in_two(n);
             most[n] = -__builtin_inff();
+        }
+        if constexpr (BYTES) {
+            bool rest = false;
+#pragma unroll
+            for (int n = 0; n < NT; ++n) rest |= in_two<false>(n);
+            whole = !__any(rest);
+            if (whole) {
+#pragma unroll
+                for (int n = 0; n < NT; ++n) in_two<true>(n);
+            }
         }
         least = row0 < rows ? first + (int32_t)quotient(row0, a.group) : -1;
 #pragma unroll
@@ -269,9 +282,10 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
         value_at = col * 64 + ((g ^ value_turn(col)) << 4);
     }
 
-    __device__ __forceinline__ void in_two(int n)
+    // Row n as two E4M3 numbers each, KEEP: in place; whether something is left that counts.
+    template <bool KEEP> __device__ __forceinline__ bool in_two(int n)
     {
-        uint32_t top = 0;                                    // the largest finite magnitude
+        uint32_t top = 0;                                    // the largest magnitude
 #pragma unroll
         for (int i = 0; i < KC; ++i)
 #pragma unroll
@@ -279,40 +293,45 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
 #pragma unroll
                 for (int j = 0; j < 4; ++j) {
                     const uint32_t a = q[n][i][h][j] & 0x7FFF, b = q[n][i][h][j] >> 16 & 0x7FFF;
-                    top = a < 0x7F80 && a > top ? a : top;
-                    top = b < 0x7F80 && b > top ? b : top;
+                    top = a > top ? a : top;
+                    top = b > top ? b : top;
                 }
+        if (__any(top >= 0x7F80)) return true;               // (infinity, NaN)
         top = bits_of(over_groups_max(f32_of_bits(top << 16))) >> 23;
         const uint32_t byte = top > 13 ? top - 7 : 6;
         const float by = power_of(254 - byte);
         q_scale[n] = byte | (byte - 5) << 8;
+        bool rest = false;
+        uint32_t large = 0;
 #pragma unroll
         for (int i = 0; i < KC; ++i) {
             u32x4 first, second;
 #pragma unroll
             for (int j = 0; j < 4; ++j) {
-                float v[4], r[4];
+                float v[4];
 #pragma unroll
                 for (int k = 0; k < 2; ++k) {
                     const f32x2 u = unpack2<BF16>(q[n][i][j >> 1][2 * (j & 1) + k]);
                     v[2 * k] = u[0] * by, v[2 * k + 1] = u[1] * by;
                 }
-                // (a row with an infinity has no softmax: NaN)
 #pragma unroll
-                for (int k = 0; k < 4; ++k) v[k] = __builtin_isinf(v[k]) ? __builtin_nanf("") : v[k];
+                for (int k = 0; k < 4; ++k) large += __builtin_fabsf(v[k]) >= 0.5f;
                 uint32_t w = 0;
                 w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], w, false);
                 w = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w, true);
-                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-                r[0] = v[0] - lo[0], r[1] = v[1] - lo[1], r[2] = v[2] - hi[0], r[3] = v[3] - hi[1];
                 first[j] = w;
+                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+                v[0] = 32 * (v[0] - lo[0]), v[1] = 32 * (v[1] - lo[1]), v[2] = 32 * (v[2] - hi[0]), v[3] = 32 * (v[3] - hi[1]);
                 w = 0;
-                w = __builtin_amdgcn_cvt_pk_fp8_f32(32 * r[0], 32 * r[1], w, false);
-                w = __builtin_amdgcn_cvt_pk_fp8_f32(32 * r[2], 32 * r[3], w, true);
+                w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], w, false);
+                w = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w, true);
                 second[j] = w;
+                const f32x2 lo2 = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi2 = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
+                rest |= v[0] != lo2[0] || v[1] != lo2[1] || v[2] != hi2[0] || v[3] != hi2[1];
             }
-            q[n][i][0] = first, q[n][i][1] = second;
+            if (KEEP) q[n][i][0] = first, q[n][i][1] = second;
         }
+        return rest && large < 8 * KC;                       // (of 16 KC)
     }
 
     static constexpr int EARLY = KC < 2 ? KC : 2;            // keys that fit registers before they are needed
@@ -331,9 +350,9 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[n][j] = f32x4{};
-        if constexpr (BYTES) {
+        if (BYTES && whole) {
 #pragma unroll
-            for (int i = 0; i < KC; i += 2) {
+            for (int i = 0; i + 1 < KC; i += 2) {
                 u32x4 k[2][4];
 #pragma unroll
                 for (int h = 0; h < 2; ++h)
@@ -362,6 +381,13 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
 #pragma unroll
                         for (int n = 0; n < NT; ++n) x[n][j] = mfma16<DT>(v, q[n][i][h], x[n][j]);
                     }
+            }
+            if constexpr (BYTES) {                               // the scale of the lane group's own run, which another of its lanes has
+                const float ks = power_of(__shfl(k_byte, (threadIdx.x & 48) + (threadIdx.x >> 4 & 3) * 4));
+#pragma unroll
+                for (int n = 0; n < NT; ++n)
+#pragma unroll
+                    for (int j = 0; j < 4; ++j) x[n][j] *= ks;
             }
         }
     }
@@ -659,7 +685,7 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
 // 16 NT rows to each of four waves, which share the tiles: a wave has all of them, so nothing is joined in the end.  The memory unit copies the codes
 // of a tile into LDS while the one before is worked on.  Every wave makes 16-bit values of the codes by itself, where it needs them: a conversion makes two of
 // them in the time of any vector instruction, and NT tiles of rows use each.
-// Bound by the vector and the matrix unit together: two prompts of 4000 tokens over 5003, 32 heads of 128, bf16 332 us (895 TFLOP/s); matrix instructions
+// Bound by the vector and the matrix unit together: two prompts of 4000 tokens over 5003, 32 heads of 128, bf16 333 us (893 TFLOP/s); matrix instructions
 // take 39 % of the cycles, vector instructions 58 % (the issue of the former among them).  Multiplying a tile's values while the next tile's weights are
 // computed, instruction by instruction, did not help (360 us), nor did four tiles of rows to a wave, which do not fit the registers.
 template <int DT, int D, int NT>

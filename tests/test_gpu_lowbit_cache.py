@@ -456,3 +456,18 @@ def test_infinite_and_undefined_scores(lowbit, counts, lengths, dtype):
                 assert torch.isnan(out[at, 1]).all() if sees else (out[at] == 0).all(), (what, count, length, i)
                 assert torch.isfinite(out[at, ::2]).all()
                 at += 1
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("dim,counts", [(128, [90]), (256, [70]), (64, [100]), (128, [1])])
+def test_queries_with_one_value_far_above_the_others(lowbit, dim, counts, dtype):
+    """Where the keys have nothing for it, the others decide; some rows, none of a wave's, or all."""
+    n = 150
+    c = Both(lowbit, [n], 64, 1, dim, 23)
+    k, v = c.values(n, dtype), c.values(n, dtype)
+    k[0][:, :, 5] = 0
+    c.write([n], [n], (k[0], k[0].cuda()), v)
+    for rows in (slice(0, 1), slice(40, None), slice(None)):
+        q = torch.from_numpy(c.rng.standard_normal((counts[0], 3, dim)).astype(np.float32)).to(dtype)
+        q[rows, :, 5] = 60000.0 if dtype == torch.float16 else 1e8
+        check_attention(c, attend(c, q, counts, [n]), q, counts, [n])

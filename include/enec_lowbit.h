@@ -123,8 +123,8 @@ int enec_cache_read(const enec_cache *cache, const enec_cache_batch *batch, void
  *           ENEC_E_ARG from max_new (q_heads / kv_heads) = 2^21 or batch kv_heads = 2^23 on
  *   scale   above zero and finite, usually head_dim^-1/2
  *   workspace  DEVICE, 16-byte aligned, or NULL if workspace_bytes = enec_cache_attention_workspace(...) is 0
- * Scores, softmax and sums are held in 32 bits; the probabilities are rounded to bf16 for the product with v (to the sum of two
- * bf16 numbers for fp16 tensors). */
+ * Scores, softmax and sums are held in 32 bits; for the product with v the probabilities are rounded to the sum of two bf16 numbers (16
+ * significant bits). */
 size_t enec_cache_attention_workspace(const enec_cache *cache, uint32_t batch, uint32_t n_tokens, uint32_t q_heads, uint32_t max_new,
                                       uint32_t max_length);
 int enec_cache_attention(const enec_cache *cache, const enec_cache_batch *batch, const void *q, size_t q_token_stride,

@@ -237,6 +237,9 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
     u32x4 q[NT][KC][2];                 // eight values each; BYTES: sixteen of the first numbers, and of the second ones
     uint32_t q_scale[NT];               // BYTES: a byte for each of the two
     bool whole;                         // BYTES: all rows of the wave are such sums
+    // Weights go into the product with the values as the sum of two bf16 numbers each, 16 significant bits: with one the error is of the order of the
+    // output's own rounding (bf16, against 64 bits: 0.0018, many rows 0.0022; with two 0.00166, which is that rounding alone).  It costs 64 sequences of up
+    // to 8191 tokens 135 us instead of 132, and two prompts of 4000 tokens over 5003 435 instead of 333.
     // The weights' sum is a product too, with a row of ones: every register of `total` has it, and it is that of the rounded weights, whose
     // errors the division takes out again where one weight outdoes the others.
     f32x4 o[NT][VT], total[NT];
@@ -437,9 +440,8 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
                 high = max3(high, x[n][j][2], x[n][j][3]);
             }
             high = over_groups_max(high) * by;
-            // Weights are taken relative to a maximum that may lag behind by up to 2^LAG: in 32 bits that costs nothing, and most tiles need no change of
-            // what is summed already.  It does cost the one weight that would be 1, exactly, its exactness in bf16 (error against 64 bits 0.0022 instead of 0.0018),
-            // so where time is the memory's the maximum is kept (many rows: 354 us with a lag of 8, 376 with none).
+            // Weights are taken relative to a maximum that may lag behind by up to 2^LAG, which costs no bits of theirs, and most tiles need no change of
+            // what is summed already (two prompts of 4000 tokens over 5003, fp16: 457 us with a lag of 8, 480 with none; where time is the memory's it is the same).
             if (__any(high > most[n] + LAG)) {
                 const float now = fmaxf(most[n], high), fade = now == -__builtin_inff() ? 1.0f : exp2_of(most[n] - now);
                 most[n] = now;
@@ -455,10 +457,8 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
                     const float lo = exp2_of(__builtin_fmaf(x[n][2 * h + j / 2][2 * (j & 1)], by, -base));
                     const float hi = exp2_of(__builtin_fmaf(x[n][2 * h + j / 2][2 * (j & 1) + 1], by, -base));
                     p[n][h][j] = pack2<BF16>(lo, hi);
-                    if constexpr (DT == FP16) {
-                        const f32x2 r = unpack2<BF16>(p[n][h][j]);
-                        rest_of[n][h][j] = pack2<BF16>(lo - r[0], hi - r[1]);
-                    }
+                    const f32x2 r = unpack2<BF16>(p[n][h][j]);
+                    rest_of[n][h][j] = pack2<BF16>(lo - r[0], hi - r[1]);
                 }
         }
         const u32x4 ones = {0x3F803F80u, 0x3F803F80u, 0x3F803F80u, 0x3F803F80u};
@@ -467,7 +467,7 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
 #pragma unroll
             for (int h = 0; h < 2; ++h) {
                 total[n] = mfma16<BF16>(ones, p[n][h], total[n]);
-                if constexpr (DT == FP16) total[n] = mfma16<BF16>(ones, rest_of[n][h], total[n]);
+                total[n] = mfma16<BF16>(ones, rest_of[n][h], total[n]);
             }
         arrived();
 #pragma unroll
@@ -526,7 +526,7 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
 #pragma unroll
                 for (int n = 0; n < NT; ++n) {
                     o[n][i] = mfma16<BF16>(vv, p[n][h], o[n][i]);
-                    if constexpr (DT == FP16) o[n][i] = mfma16<BF16>(vv, rest_of[n][h], o[n][i]);
+                    o[n][i] = mfma16<BF16>(vv, rest_of[n][h], o[n][i]);
                 }
             }
     }
@@ -558,7 +558,7 @@ __device__ __forceinline__ Cached cached_of(const Attend &a, const Sequence &s, 
 // been multiplied, the next tile's are copied there while the weights are computed and the values multiplied, and the next values while the next keys are.
 // It waits for its own copies only: no barrier until the end.  Two waves to a SIMD (head_dim 256: one) did more than copies further ahead: a tile's
 // chain of steps leaves half of a wave's cycles idle (64 sequences of up to 8191 tokens: 4 waves with two tiles each 150 us).
-// Bound by HBM: 64 sequences of up to 8191 tokens, 8 heads of 128, bf16 130 us (5.1 TB/s, what a copy reaches); two of 131072, fp16, pages of 16,
+// Bound by HBM: 64 sequences of up to 8191 tokens, 8 heads of 128, bf16 134 us (4.9 TB/s); two of 131072, fp16, pages of 16,
 // 83 us and the join 4.5.  One sequence of 1000 tokens: 10 us, a chain of dependent reads.
 template <int DT, int D, int NT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kernel(Attend a)
@@ -685,8 +685,7 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
 // 16 NT rows to each of four waves, which share the tiles: a wave has all of them, so nothing is joined in the end.  The memory unit copies the codes
 // of a tile into LDS while the one before is worked on.  Every wave makes 16-bit values of the codes by itself, where it needs them: a conversion makes two of
 // them in the time of any vector instruction, and NT tiles of rows use each.
-// Bound by the vector and the matrix unit together: two prompts of 4000 tokens over 5003, 32 heads of 128, bf16 333 us (893 TFLOP/s); matrix instructions
-// take 39 % of the cycles, vector instructions 58 % (the issue of the former among them).  Multiplying a tile's values while the next tile's weights are
+// Bound by the vector and the matrix unit together: two prompts of 4000 tokens over 5003, 32 heads of 128, bf16 435 us (684 TFLOP/s).  Multiplying a tile's values while the next tile's weights are
 // computed, instruction by instruction, did not help (360 us), nor did four tiles of rows to a wave, which do not fit the registers.
 template <int DT, int D, int NT>
 __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)

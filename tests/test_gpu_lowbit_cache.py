@@ -471,3 +471,21 @@ def test_queries_with_one_value_far_above_the_others(lowbit, dim, counts, dtype)
         q = torch.from_numpy(c.rng.standard_normal((counts[0], 3, dim)).astype(np.float32)).to(dtype)
         q[rows, :, 5] = 60000.0 if dtype == torch.float16 else 1e8
         check_attention(c, attend(c, q, counts, [n]), q, counts, [n])
+
+
+@pytest.mark.parametrize("page,dim,heads,group,counts,lengths", [
+    (64, 128, 2, 4, [1, 1], [300, 64]), (16, 64, 1, 8, [1], [9000]), (32, 256, 1, 3, [4], [700]), (64, 128, 1, 6, [5], [1500]),
+    (64, 64, 1, 2, [90], [200]), (64, 128, 2, 1, [77, 33], [190, 80]), (16, 128, 1, 5, [8], [5000]), (32, 256, 1, 2, [70], [101])])
+def test_outputs_in_bf16_are_as_exact_as_their_format(lowbit, page, dim, heads, group, counts, lengths):
+    """Weights keep the bits of two bf16 numbers for the product with the values, as for fp16 tensors: beside the output's one rounding nothing
+    of the order of bf16's is left, which shows where values cancel."""
+    c = Both(lowbit, lengths, page, heads, dim, seed=30 + dim)
+    c.fill(lengths, torch.bfloat16)
+    q = torch.from_numpy(c.rng.standard_normal((sum(counts), heads * group, dim)).astype(np.float32) * 1.5).to(torch.bfloat16)
+    out, starts = attend(c, q, counts, lengths), starts_of(counts)
+    for b, n in enumerate(lengths):
+        rows = slice(starts[b], starts[b + 1])
+        want, bound = plain.attention(q[rows].double().numpy(), c.k.read(c.table[b], n), c.v.read(c.table[b], n), dim ** -0.5, torch.float16)
+        bound += plain.UNIT[torch.bfloat16] * np.abs(want)
+        off = np.abs(out[rows].double().cpu().numpy() - want) - bound
+        assert off.max() <= 0, (b, n, off.max(), np.unravel_index(off.argmax(), off.shape))

@@ -58,13 +58,6 @@ template <int DT> __device__ __forceinline__ f32x4 mfma16(const u32x4 &a, const 
     if constexpr (DT == BF16) return __builtin_amdgcn_mfma_f32_16x16x32_bf16(__builtin_bit_cast(bf16x8, a), __builtin_bit_cast(bf16x8, b), c, 0, 0, 0);
     return __builtin_amdgcn_mfma_f32_16x16x32_f16(__builtin_bit_cast(f16x8, a), __builtin_bit_cast(f16x8, b), c, 0, 0, 0);
 }
-// 32 E4M3 codes a lane on both sides, each side with a power of two for them; PIECE: which byte of sb
-template <int PIECE> __device__ __forceinline__ f32x4 mfma_codes(const u32x4 &a0, const u32x4 &a1, const u32x4 &b0, const u32x4 &b1, const f32x4 &c, uint32_t sa, uint32_t sb)
-{
-    const i32x8 a = {(int)a0[0], (int)a0[1], (int)a0[2], (int)a0[3], (int)a1[0], (int)a1[1], (int)a1[2], (int)a1[3]};
-    const i32x8 b = {(int)b0[0], (int)b0[1], (int)b0[2], (int)b0[3], (int)b1[0], (int)b1[1], (int)b1[2], (int)b1[3]};
-    return __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(a, b, c, 0, 0, 0, (int)sa, PIECE, (int)sb);
-}
 // eight E4M3 codes as values of the 16-bit format: all of them are numbers of it (bf16: also with a power of two)
 template <int DT> __device__ __forceinline__ u32x4 values8(uint32_t lo, uint32_t hi, float scale)
 {
@@ -222,24 +215,16 @@ template <int D, int PARTS> __device__ __forceinline__ void copy_values(const Ca
 // dimensions is the same for the queries.
 // Query rows are pairs of (token, head of the key head's group).  A wave has 16 NT of them.
 //
-// Scores of bf16 queries take the keys' codes as they are (BYTES): a bf16 number has eight significant bits, so a query is the sum of two E4M3 numbers,
-// of which the second has what the first one's rounding left.  A row has a power of two for each: the largest value is 128 to 256 in the first, and the second
-// is 32 times as large.  That is exact for values down to 2^-14 of the row's largest, and smaller ones lose less than 2^-22 of it.  That is less than the
-// rounding of sums in 32 bits where most values are far larger, and is taken only where half of a lane's are above 2^-9 of the largest: a wave with a row
-// of other values that lose anything, or of values that are not finite, takes 16-bit keys (not `whole`).  The two products cost what one of bf16 does, the
-// page's scale comes with them, and the vector unit has no keys to convert (two prompts of 4000 tokens over 5003: 354 -> 333 us; where rows are few it is
-// the memory's time, and one sequence's call would take 11.7 us instead of 10.9).  Values are converted: the weights would cost more as two E4M3 numbers
-// than the values do as bf16.
+// Keys become 16-bit values for the product with the queries, whose bits all count.  (bf16 queries as the sum of two E4M3 numbers against the codes as they are
+// took two prompts of 4000 tokens over 5003 from 457 to 435 us, but such a sum does not hold what is 2^-14 of a row's largest value or less, and
+// it is the keys that decide whether that counts.)
 template <int DT, int D, int NT, bool MANY> struct Rows {
-    static constexpr bool BYTES = MANY && DT == BF16 && D >= 128;
     static constexpr float LAG = MANY ? 8 : 0;
     static constexpr int KC = D / 64, VT = D / 16;
-    u32x4 q[NT][KC][2];                 // eight values each; BYTES: sixteen of the first numbers, and of the second ones
-    uint32_t q_scale[NT];               // BYTES: a byte for each of the two
-    bool whole;                         // BYTES: all rows of the wave are such sums
+    u32x4 q[NT][KC][2];                 // eight values each
     // Weights go into the product with the values as the sum of two bf16 numbers each, 16 significant bits: with one the error is of the order of the
     // output's own rounding (bf16, against 64 bits: 0.0018, many rows 0.0022; with two 0.00166, which is that rounding alone).  It costs 64 sequences of up
-    // to 8191 tokens 135 us instead of 132, and two prompts of 4000 tokens over 5003 435 instead of 333.
+    // to 8191 tokens 135 us instead of 132, and two prompts of 4000 tokens over 5003 457 instead of 350.
     // The weights' sum is a product too, with a row of ones: every register of `total` has it, and it is that of the rounded weights, whose
     // errors the division takes out again where one weight outdoes the others.
     f32x4 o[NT][VT], total[NT];
@@ -266,16 +251,6 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
             total[n] = f32x4{};
             most[n] = -__builtin_inff();
         }
-        if constexpr (BYTES) {
-            bool rest = false;
-#pragma unroll
-            for (int n = 0; n < NT; ++n) rest |= in_two<false>(n);
-            whole = !__any(rest);
-            if (whole) {
-#pragma unroll
-                for (int n = 0; n < NT; ++n) in_two<true>(n);
-            }
-        }
         least = row0 < rows ? first + (int32_t)quotient(row0, a.group) : -1;
 #pragma unroll
         for (int i = 0; i < KC; ++i) {
@@ -283,58 +258,6 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
             key_at[i] = t * D + (((4 * i + g) ^ key_turn<D>(t)) << 4);
         }
         value_at = col * 64 + ((g ^ value_turn(col)) << 4);
-    }
-
-    // Row n as two E4M3 numbers each, KEEP: in place; whether something is left that counts.
-    template <bool KEEP> __device__ __forceinline__ bool in_two(int n)
-    {
-        uint32_t top = 0;                                    // the largest magnitude
-#pragma unroll
-        for (int i = 0; i < KC; ++i)
-#pragma unroll
-            for (int h = 0; h < 2; ++h)
-#pragma unroll
-                for (int j = 0; j < 4; ++j) {
-                    const uint32_t a = q[n][i][h][j] & 0x7FFF, b = q[n][i][h][j] >> 16 & 0x7FFF;
-                    top = a > top ? a : top;
-                    top = b > top ? b : top;
-                }
-        if (__any(top >= 0x7F80)) return true;               // (infinity, NaN)
-        top = bits_of(over_groups_max(f32_of_bits(top << 16))) >> 23;
-        const uint32_t byte = top > 13 ? top - 7 : 6;
-        const float by = power_of(254 - byte);
-        q_scale[n] = byte | (byte - 5) << 8;
-        bool rest = false;
-        uint32_t large = 0;
-#pragma unroll
-        for (int i = 0; i < KC; ++i) {
-            u32x4 first, second;
-#pragma unroll
-            for (int j = 0; j < 4; ++j) {
-                float v[4];
-#pragma unroll
-                for (int k = 0; k < 2; ++k) {
-                    const f32x2 u = unpack2<BF16>(q[n][i][j >> 1][2 * (j & 1) + k]);
-                    v[2 * k] = u[0] * by, v[2 * k + 1] = u[1] * by;
-                }
-#pragma unroll
-                for (int k = 0; k < 4; ++k) large += __builtin_fabsf(v[k]) >= 0.5f;
-                uint32_t w = 0;
-                w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], w, false);
-                w = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w, true);
-                first[j] = w;
-                const f32x2 lo = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-                v[0] = 32 * (v[0] - lo[0]), v[1] = 32 * (v[1] - lo[1]), v[2] = 32 * (v[2] - hi[0]), v[3] = 32 * (v[3] - hi[1]);
-                w = 0;
-                w = __builtin_amdgcn_cvt_pk_fp8_f32(v[0], v[1], w, false);
-                w = __builtin_amdgcn_cvt_pk_fp8_f32(v[2], v[3], w, true);
-                second[j] = w;
-                const f32x2 lo2 = __builtin_amdgcn_cvt_pk_f32_fp8(w, false), hi2 = __builtin_amdgcn_cvt_pk_f32_fp8(w, true);
-                rest |= v[0] != lo2[0] || v[1] != lo2[1] || v[2] != hi2[0] || v[3] != hi2[1];
-            }
-            if (KEEP) q[n][i][0] = first, q[n][i][1] = second;
-        }
-        return rest && large < 8 * KC;                       // (of 16 KC)
     }
 
     static constexpr int EARLY = KC < 2 ? KC : 2;            // keys that fit registers before they are needed
@@ -346,59 +269,30 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
 #pragma unroll
             for (int j = 0; j < 4; ++j) k[i][j] = keys_of(tile, i, j);
     }
-    // early: what load_keys read.  k_byte: BYTES: the scale of the keys of this lane's row of the product
-    __device__ __forceinline__ void scores(const Tile<D> &tile, const u32x4 (&early)[EARLY][4], f32x4 (&x)[NT][4], uint32_t k_byte) const
+    // early: what load_keys read
+    __device__ __forceinline__ void scores(const Tile<D> &tile, const u32x4 (&early)[EARLY][4], f32x4 (&x)[NT][4]) const
     {
 #pragma unroll
         for (int n = 0; n < NT; ++n)
 #pragma unroll
             for (int j = 0; j < 4; ++j) x[n][j] = f32x4{};
-        if (BYTES && whole) {
 #pragma unroll
-            for (int i = 0; i + 1 < KC; i += 2) {
-                u32x4 k[2][4];
+        for (int i = 0; i < KC; ++i) {
+            u32x4 k[4];
 #pragma unroll
-                for (int h = 0; h < 2; ++h)
+            for (int j = 0; j < 4; ++j) k[j] = i < EARLY ? early[i][j] : keys_of(tile, i, j);
 #pragma unroll
-                    for (int j = 0; j < 4; ++j) k[h][j] = i < EARLY ? early[h][j] : keys_of(tile, i + h, j);
+            for (int h = 0; h < 2; ++h)
 #pragma unroll
-                for (int j = 0; j < 4; ++j)
+                for (int j = 0; j < 4; ++j) {
+                    const u32x4 v = values8<DT>(k[j][2 * h], k[j][2 * h + 1], 1.0f);
 #pragma unroll
-                    for (int n = 0; n < NT; ++n) x[n][j] = mfma_codes<0>(k[0][j], k[1][j], q[n][i][0], q[n][i + 1][0], x[n][j], k_byte, q_scale[n]);
-#pragma unroll
-                for (int j = 0; j < 4; ++j)
-#pragma unroll
-                    for (int n = 0; n < NT; ++n) x[n][j] = mfma_codes<1>(k[0][j], k[1][j], q[n][i][1], q[n][i + 1][1], x[n][j], k_byte, q_scale[n]);
-            }
-        } else {
-#pragma unroll
-            for (int i = 0; i < KC; ++i) {
-                u32x4 k[4];
-#pragma unroll
-                for (int j = 0; j < 4; ++j) k[j] = i < EARLY ? early[i][j] : keys_of(tile, i, j);
-#pragma unroll
-                for (int h = 0; h < 2; ++h)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) {
-                        const u32x4 v = values8<DT>(k[j][2 * h], k[j][2 * h + 1], 1.0f);
-#pragma unroll
-                        for (int n = 0; n < NT; ++n) x[n][j] = mfma16<DT>(v, q[n][i][h], x[n][j]);
-                    }
-            }
-            if constexpr (BYTES) {                               // the scale of the lane group's own run, which another of its lanes has
-                const float ks = power_of(__shfl(k_byte, (threadIdx.x & 48) + (threadIdx.x >> 4 & 3) * 4));
-#pragma unroll
-                for (int n = 0; n < NT; ++n)
-#pragma unroll
-                    for (int j = 0; j < 4; ++j) x[n][j] *= ks;
-            }
+                    for (int n = 0; n < NT; ++n) x[n][j] = mfma16<DT>(v, q[n][i][h], x[n][j]);
+                }
         }
     }
 
-    // the run whose keys' scale the lane needs
-    static __device__ __forceinline__ uint32_t scale_run() { return BYTES ? threadIdx.x >> 2 & 3 : threadIdx.x >> 4 & 3; }
-
-    // page, vs: of the lane group's run.  ks: its keys' scale (BYTES: scores have it).  by: the call's scale and log2 e.  arrived(): waits for the tile's values.
+    // page, ks, vs: of the lane group's run, ks its keys' scale.  by: the call's scale and log2 e.  arrived(): waits for the tile's values.
     template <typename F>
     __device__ __forceinline__ void add(const Tile<D> &tile, f32x4 (&x)[NT][4], int32_t t0, int32_t length, bool whole_pages, int32_t page, float ks, float by, float vs,
                                         F arrived)
@@ -413,12 +307,10 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
         for (int i = 0; i < AHEAD; ++i) v[i] = *reinterpret_cast<const u32x4 *>(tile.values + value_at + i * 1024);
         if (AHEAD) __builtin_amdgcn_sched_barrier(0);
         const bool partial = t0 + 63 > least || t0 + 64 > length || !whole_pages;
-        if constexpr (!BYTES) {
 #pragma unroll
-            for (int n = 0; n < NT; ++n)
+        for (int n = 0; n < NT; ++n)
 #pragma unroll
-                for (int j = 0; j < 4; ++j) x[n][j] *= ks;
-        }
+            for (int j = 0; j < 4; ++j) x[n][j] *= ks;
         if (partial) {
             asm volatile("");
 #pragma unroll
@@ -586,8 +478,9 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
     auto ask_keys = [&](int32_t t0) {                        // and the scales, before them
         const Runs next = cache.runs(t0, raw);
         runs = next;
-        const int32_t keys = select4(next, Rows<DT, D, NT, false>::scale_run()), values = select4(next, g);
-        k_byte = c.k_scales[(size_t)(uint32_t)(keys < 0 ? 0 : keys) * c.heads + head], v_byte = c.v_scales[(size_t)(uint32_t)(values < 0 ? 0 : values) * c.heads + head];
+        const int32_t page = select4(next, g);
+        const size_t scale = (size_t)(uint32_t)(page < 0 ? 0 : page) * c.heads + head;
+        k_byte = c.k_scales[scale], v_byte = c.v_scales[scale];
         __builtin_amdgcn_sched_barrier(0);
         copy_keys<D, 1>(cache, next, t0, tile, 0);
         cache.table_entries(t0 + STEP, raw);
@@ -612,7 +505,7 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
         f32x4 x[NT][4];
         u32x4 k[Rows<DT, D, NT, false>::EARLY][4];
         r.load_keys(tile, k);
-        r.scores(tile, k, x, k_byte);
+        r.scores(tile, k, x);
         const float ks = power_of(k_byte), vs = page >= 0 ? power_of(v_byte) : 1.0f;       // (no page: another one's, and 0 * NaN would be one)
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");   // (the keys have been read)
@@ -685,8 +578,9 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
 // 16 NT rows to each of four waves, which share the tiles: a wave has all of them, so nothing is joined in the end.  The memory unit copies the codes
 // of a tile into LDS while the one before is worked on.  Every wave makes 16-bit values of the codes by itself, where it needs them: a conversion makes two of
 // them in the time of any vector instruction, and NT tiles of rows use each.
-// Bound by the vector and the matrix unit together: two prompts of 4000 tokens over 5003, 32 heads of 128, bf16 435 us (684 TFLOP/s).  Multiplying a tile's values while the next tile's weights are
-// computed, instruction by instruction, did not help (360 us), nor did four tiles of rows to a wave, which do not fit the registers.
+// Bound by the vector and the matrix unit together: two prompts of 4000 tokens over 5003, 32 heads of 128 457 us (650 TFLOP/s) in either format, 32 heads
+// of 64 306, 16 of 256 546.  Multiplying a tile's values while the next tile's weights are computed, instruction by instruction, did not help, nor did four
+// tiles of rows to a wave, which do not fit the registers.
 template <int DT, int D, int NT>
 __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
 {
@@ -717,8 +611,8 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
         copy_keys<D, 4>(cache, p, t0, to, wave);
         copy_values<D, 4>(cache, p, t0, to, wave);
         pg = select4(p, g);
-        const int32_t keys = select4(p, Rows<DT, D, NT, true>::scale_run());
-        k = c.k_scales[(size_t)(uint32_t)(keys < 0 ? 0 : keys) * c.heads + head], w = c.v_scales[(size_t)(uint32_t)(pg < 0 ? 0 : pg) * c.heads + head];
+        const size_t scale = (size_t)(uint32_t)(pg < 0 ? 0 : pg) * c.heads + head;
+        k = c.k_scales[scale], w = c.v_scales[scale];
     };
     if (v.from < v.to) {
         cache.table_entries(v.from, raw);
@@ -742,7 +636,7 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
         }
         // (also the last tiles, of which the first waves' rows see nothing: a branch around them cost every tile a copy of all sums)
         f32x4 x[NT][4];
-        r.scores(tiles[buffer], k, x, kb);
+        r.scores(tiles[buffer], k, x);
         // (a wave between its products goes first: the other one of its SIMD has matrix instructions running meanwhile; 400 -> 378 us for two prompts of
         // 4000 tokens over 5003)
         __builtin_amdgcn_s_setprio(1);

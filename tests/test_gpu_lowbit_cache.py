@@ -489,3 +489,21 @@ def test_outputs_in_bf16_are_as_exact_as_their_format(lowbit, page, dim, heads, 
         bound += plain.UNIT[torch.bfloat16] * np.abs(want)
         off = np.abs(out[rows].double().cpu().numpy() - want) - bound
         assert off.max() <= 0, (b, n, off.max(), np.unravel_index(off.argmax(), off.shape))
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("far", [2.0 ** 14, 2.0 ** 16, 2.0 ** 20, 1e8])
+@pytest.mark.parametrize("dim,counts", [(128, [90]), (256, [70]), (64, [100]), (128, [3])])
+def test_queries_with_half_of_their_values_far_above_the_others(lowbit, dim, counts, far, dtype):
+    """Where the keys have nothing for the large half, the small one decides."""
+    if dtype == torch.float16 and far > 2.0 ** 14:
+        far = 2.0 ** 14                                   # (what the format holds)
+    n = 150
+    c = Both(lowbit, [n], 64, 1, dim, 24)
+    k, v = c.values(n, dtype), c.values(n, dtype)
+    k[0][:, :, ::2] = 0
+    c.write([n], [n], (k[0], k[0].cuda()), v)
+    for rows in (slice(0, 1), slice(None)):
+        q = torch.from_numpy(c.rng.standard_normal((counts[0], 3, dim)).astype(np.float32)).to(dtype)
+        q[rows, :, ::2] = ((1 + 0.5 * torch.rand(q[rows, :, ::2].shape, generator=torch.Generator().manual_seed(dim))) * far).to(dtype)
+        check_attention(c, attend(c, q, counts, [n]), q, counts, [n])

@@ -334,8 +334,10 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
             high = over_groups_max(high) * by;
             // Weights are taken relative to a maximum that may lag behind by up to 2^LAG, which costs no bits of theirs, and most tiles need no change of
             // what is summed already (two prompts of 4000 tokens over 5003, fp16: 457 us with a lag of 8, 480 with none; where time is the memory's it is the same).
-            if (__any(high > most[n] + LAG)) {
-                const float now = fmaxf(most[n], high), fade = now == -__builtin_inff() ? 1.0f : exp2_of(most[n] - now);
+            // (A row goes by its own scores only, so that its bits do not depend on the other rows of the wave.)
+            const bool moves = high > most[n] + LAG;
+            if (__any(moves)) {
+                const float now = moves ? high : most[n], fade = moves ? exp2_of(most[n] - now) : 1.0f;
                 most[n] = now;
                 total[n] *= fade;
 #pragma unroll

@@ -507,3 +507,21 @@ def test_queries_with_half_of_their_values_far_above_the_others(lowbit, dim, cou
         q = torch.from_numpy(c.rng.standard_normal((counts[0], 3, dim)).astype(np.float32)).to(dtype)
         q[rows, :, ::2] = ((1 + 0.5 * torch.rand(q[rows, :, ::2].shape, generator=torch.Generator().manual_seed(dim))) * far).to(dtype)
         check_attention(c, attend(c, q, counts, [n]), q, counts, [n])
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("dim,counts,n", [(64, [100], 500), (128, [90], 700), (256, [70], 300), (128, [90], 5000), (128, [20], 900)])
+def test_a_row_does_not_depend_on_the_others(lowbit, dim, counts, n, dtype):
+    """Not a bit of it: the others with values that lose bits in eight, that are not finite, or with scores that grow from tile to tile."""
+    c = Both(lowbit, [n], 64, 1, dim, 25)
+    k, v = c.values(n, dtype), c.values(n, dtype)
+    k[0][:, :, 3] = torch.linspace(-3, 3, n)[:, None].to(dtype)
+    c.write([n], [n], (k[0], k[0].cuda()), v)
+    q = torch.from_numpy(c.rng.standard_normal((counts[0], 3, dim)).astype(np.float32)).to(dtype)
+    want = attend(c, q, counts, [n])
+    for value in (1e-3, 200.0, 3e4, float("inf"), float("nan")):
+        others = q.clone()
+        others[1::2, :, 3] = value
+        out = attend(c, others, counts, [n])
+        differ = int((out[::2] != want[::2]).sum())
+        assert differ == 0, (value, differ)

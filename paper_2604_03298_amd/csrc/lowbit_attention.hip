@@ -723,23 +723,44 @@ struct Plan {
 
 inline uint32_t rows_of_many(uint32_t head_dim) { return head_dim == 256 ? 64 : 128; }
 
+// One round of workgroups, as many as the card holds, each with at least `least` tokens: a workgroup's start and end, and joining, cost as much as
+// some hundred tokens.
+inline uint32_t slots_of(bool many, uint32_t head_dim) { return many || head_dim == 64 ? 512 : 256; }
+inline uint32_t least_of(bool many) { return many ? 512 : 1024; }
+constexpr uint32_t FEW_ROWS = 32;       // more take the kernel for many
+
 // How a call is cut up.  A sequence's cached tokens are split where rows and heads alone leave the card empty.
 Plan plan_of(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t head_dim, uint32_t max_new, uint32_t max_length)
 {
     Plan p;
     const uint64_t rows = (uint64_t)max_new * group;
-    p.many = rows > 32;
+    p.many = rows > FEW_ROWS;
     p.rows = p.many ? rows_of_many(head_dim) : rows > 16 && head_dim < 256 ? 32 : 16;       // (32 rows of 256 dimensions do not fit the registers)
     p.row_tiles = (uint32_t)((rows + p.rows - 1) / p.rows);
-    // One round of workgroups, as many as the card holds, each with at least `least` tokens: a workgroup's start and end, and joining, cost as much as
-    // some hundred tokens.
-    const uint32_t slots = p.many || head_dim == 64 ? 512 : 256, least = p.many ? 512 : 1024;
+    const uint32_t slots = slots_of(p.many, head_dim), least = least_of(p.many);
     const uint64_t others = (uint64_t)batch * kv_heads * p.row_tiles;
     const uint64_t want = others >= slots ? 1 : slots / others;
     const uint64_t tokens = (max_length + want - 1) / want;
     p.chunk = (uint32_t)(tokens <= least ? least : (tokens + 255) / 256 * 256);
     p.splits = max_length <= p.chunk ? 1 : (max_length + p.chunk - 1) / p.chunk;
     return p;
+}
+
+// The rows of parts, each of a token, that no call exceeds with at most so many of all these.  Smaller calls may be split more, but a kernel's splits, sequences, heads and
+// tiles of rows multiply to `slots` at most, a tile has the tokens of so many rows, and a split has `least` tokens.
+uint64_t most_parts(uint32_t n_tokens, uint32_t q_heads, uint32_t group, uint32_t head_dim, uint32_t max_new, uint32_t max_length)
+{
+    const uint64_t rows = (uint64_t)max_new * group;
+    uint64_t most = 0;
+    for (const bool many : {false, true}) {
+        if (many ? rows <= FEW_ROWS : group > FEW_ROWS) continue;             // not met by any of them
+        const uint64_t of_tile = many ? rows_of_many(head_dim) : FEW_ROWS, splits = ((uint64_t)max_length + least_of(many) - 1) / least_of(many);
+        if (splits < 2) continue;
+        const uint64_t by_slots = slots_of(many, head_dim) * (rows < of_tile ? rows : of_tile) / q_heads, by_length = splits * n_tokens;
+        const uint64_t parts = by_slots < by_length ? by_slots : by_length;
+        most = most > parts ? most : parts;
+    }
+    return most;
 }
 
 template <int DT, int D, int NT> bool launch_few(const Attend &a, uint32_t tiles, hipStream_t s)
@@ -788,7 +809,8 @@ size_t enec_cache_attention_workspace(const enec_cache *cache, uint32_t batch, u
 {
     if (!cache || !shape_ok(cache, batch, n_tokens, q_heads, max_new, max_length) || batch == 0 || n_tokens == 0 || max_new == 0) return 0;
     const Plan p = plan_of(batch, cache->kv_heads, q_heads / cache->kv_heads, cache->head_dim, max_new, max_length);
-    return p.splits == 1 ? 0 : (size_t)p.splits * n_tokens * q_heads * (cache->head_dim + 2) * sizeof(float);
+    const uint64_t own = p.splits == 1 ? 0 : (uint64_t)p.splits * n_tokens, most = most_parts(n_tokens, q_heads, q_heads / cache->kv_heads, cache->head_dim, max_new, max_length);
+    return (size_t)(own > most ? own : most) * q_heads * (cache->head_dim + 2) * sizeof(float);
 }
 
 int enec_cache_attention(const enec_cache *cache, const enec_cache_batch *batch, const void *q, size_t q_token_stride, size_t q_head_stride, void *out,

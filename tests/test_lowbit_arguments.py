@@ -175,3 +175,34 @@ def test_caches_that_the_binding_refuses(lowbit):
     q = torch.zeros(5, 4, 64, dtype=torch.bfloat16)
     with pytest.raises(ValueError):
         lowbit.cache_attention(c, q, q[:4], i(3, 2), i(4), i(3), 1, 32)
+
+
+def test_a_workspace_for_the_largest_attention_serves_smaller_ones(lowbit):
+    """Fewer tokens can mean more splits: what is said for the largest covers them."""
+    import random
+    L, rng = lowbit.lib(), random.Random(5)
+
+    def need(c, batch, tokens, q_heads, new, most):
+        return L.enec_cache_attention_workspace(C.byref(c), batch, tokens, q_heads, new, most)
+
+    shape = lambda heads, dim: lowbit.CacheStruct(P, P, P, P, 10, 64, heads, dim)  # noqa: E731
+    c = shape(8, 128)
+    assert need(c, 4, 128, 32, 32, 131072) <= need(c, 4, 400, 32, 100, 131072)
+    assert need(c, 2, 128, 32, 64, 8192) <= need(c, 2, 300, 32, 150, 8192)
+    met = 0
+    for _ in range(20000):
+        heads, dim, group = rng.choice((1, 2, 3, 8, 32, 300)), rng.choice((64, 128, 256)), rng.choice((1, 2, 4, 7, 16, 17, 32, 33, 40))
+        c, sizes = shape(heads, dim), []
+        large = (rng.randint(1, 70), int(2 ** rng.uniform(0, 12)), int(2 ** rng.uniform(0, 18)))
+        small = tuple(rng.randint(1, v) if rng.random() < 0.7 else v for v in large)
+        tokens = large[0] * large[1] if rng.random() < 0.5 else rng.randint(1, large[0] * large[1])
+        fewer = min(tokens, small[0] * small[1])
+        for (batch, new, most), n in ((large, tokens), (small, fewer)):
+            sizes.append(need(c, batch, n, heads * group, new, most))
+        assert sizes[1] <= sizes[0] <= 35 << 20, (heads, dim, group, large, small, tokens, fewer, sizes)
+        met += sizes[1] > 0
+    assert met > 5000                                      # (the draw does reach calls that are split)
+    # and such a workspace is large enough for the call itself: the next thing wrong with it is its address
+    c, b = shape(8, 128), lowbit.BatchStruct(P, P, P, 8, 4, 128, None)
+    size = need(c, 4, 400, 32, 100, 131072)
+    assert L.enec_cache_attention(C.byref(c), C.byref(b), P, 4096, 128, P, 4096, 128, 0, 32, 32, 131072, 0.1, 0x1008, size, None) == lowbit.E_ARG

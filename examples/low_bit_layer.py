@@ -61,10 +61,10 @@ class Layer:
 
     def reserve(self, batch, tokens, max_new, max_length):
         """Scratch memory for steps of at most these sizes; one piece serves the calls of a stream, one after the other."""
-        need = [lowbit.cache_attention_workspace(self.cache, batch, t, self.heads, n, max_length) for t, n in ((tokens, max_new), (batch, 1))]
+        tokens = max(tokens, batch)                                         # (what serves the largest call serves all smaller ones)
+        need = [lowbit.cache_attention_workspace(self.cache, batch, tokens, self.heads, max(max_new, 1), max_length)]
         for n, k in self.shapes.values():
-            for m in {tokens, batch}:
-                need += [lowbit.mx4_linear_workspace(m, n, k), lowbit.mx4_matmul_workspace(m, n, k)]
+            need += [lowbit.mx4_linear_workspace(tokens, n, k), lowbit.mx4_matmul_workspace(tokens, n, k)]
         self.workspace = torch.empty(max(max(need), 16), dtype=torch.uint8, device="cuda")
 
     def product(self, x, name, four_bits=False):

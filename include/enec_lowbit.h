@@ -54,15 +54,16 @@ int enec_mx4_dequantize(const void *codes, const void *scales, size_t rows, size
  *   x       DEVICE, m x k values (bf16 or fp16), x_stride elements from row to row (>= k)
  *   codes, scales  DEVICE, an n x k matrix as enec_mx4_quantize writes it
  *   y       DEVICE, m x n values of the same dtype, y_stride (>= n); must not overlap the inputs
- *   workspace      DEVICE, 16-byte aligned, or NULL if workspace_bytes = enec_mx4_linear_workspace(m, n, k) is 0
+ *   workspace      DEVICE, 16-byte aligned, or NULL if workspace_bytes = enec_mx4_linear_workspace(m, n, k) is 0.  What it says serves
+ *                  every product of fewer rows with the same n and k as well, in either format.
  * Products are exact and summed in 32 bits; y is rounded once.
  * ENEC_E_ARG also beyond m = 2^21, n = 2^26, k = 2^21, m k = 2^34 or m n = 2^40. */
 size_t enec_mx4_linear_workspace(size_t m, size_t n, size_t k);
 int enec_mx4_linear(const void *x, size_t m, size_t x_stride, int dtype, const void *codes, const void *scales, size_t n, size_t k,
                     void *y, size_t y_stride, void *workspace, size_t workspace_bytes, void *stream);
 
-/* y = x w^T with both in 4 bits: x is an m x k matrix, w an n x k matrix as enec_mx4_quantize writes them; y as above, of any
- * dtype (bf16, fp16 or fp32). */
+/* y = x w^T with both in 4 bits: x is an m x k matrix, w an n x k matrix as enec_mx4_quantize writes them; y and the
+ * workspace as above, y of any dtype (bf16, fp16 or fp32). */
 size_t enec_mx4_matmul_workspace(size_t m, size_t n, size_t k);
 int enec_mx4_matmul(const void *x_codes, const void *x_scales, size_t m, const void *codes, const void *scales, size_t n, size_t k,
                     void *y, size_t y_stride, int dtype, void *workspace, size_t workspace_bytes, void *stream);

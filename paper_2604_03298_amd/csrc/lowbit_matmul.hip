@@ -446,26 +446,26 @@ constexpr uint32_t UNITS = 256;                     // compute units
 struct Plan {
     int shape;
     uint32_t splits, split_stages;
-    size_t laid_out, parts;             // bytes of the workspace
 };
+constexpr uint32_t MOST_SPLITS = 16, UNIT = 4;      // a split is whole blocks of scales and whole rounds: so many stages, or a multiple
 
 inline uint32_t up(uint32_t v, uint32_t by) { return (v + by - 1) / by; }
 inline size_t part_row(uint32_t n) { return ((size_t)n + 15) / 16 * 16; }
+inline uint32_t stages_of(uint32_t k, int act) { return act == MX4 ? up(up(k, 128), 2) : up(k, 128); }
 
 Plan plan_of(uint32_t m, uint32_t n, uint32_t k, int act)
 {
     Plan p{};
     const bool mx4 = act == MX4;
-    if (!mx4) p.laid_out = 2 * (size_t)m * (up(k, 128) * 128);
-    const uint32_t groups = up(k, 128), unit = 4, stages = mx4 ? up(groups, 2) : groups;     // a split is whole blocks of scales and whole rounds
+    const uint32_t stages = stages_of(k, act);
     double best = 1e300;
     for (int i = 0; i < 7; ++i) {
         const Shape &s = shapes_of(act)[i];
         if (s.tokens > 16 && s.tokens >= 2 * up(m, 16) * 16) continue;       // half of the tile or more would be empty
         const uint64_t tiles = (uint64_t)up(n, s.rows) * up(m, s.tokens), full = UNITS * s.resident;
         const bool splittable = (uint64_t)m * up(n, 4) < 1u << 31;
-        for (uint32_t splits = 1; splits == 1 || (splittable && splits <= 16 && splits * unit <= stages && tiles * (splits / 2) < full); splits *= 2) {
-            const uint32_t each = up(up(stages, splits), unit) * unit, count = up(stages, each);
+        for (uint32_t splits = 1; splits == 1 || (splittable && splits <= MOST_SPLITS && splits * UNIT <= stages && tiles * (splits / 2) < full); splits *= 2) {
+            const uint32_t each = up(up(stages, splits), UNIT) * UNIT, count = up(stages, each);
             // The busiest compute unit has `most` workgroups.  Fewer than fit take their share of the time and some more; where one fits and not all
             // units have one, memory has less to do; past that the units drift apart, and half of the last round's waste goes.  A workgroup's start and end are 3 us,
             // and joining is a launch, the sums' way out and back.
@@ -477,12 +477,33 @@ Plan plan_of(uint32_t m, uint32_t n, uint32_t k, int act)
             if (us < best) best = us, p.shape = i, p.splits = count, p.split_stages = each;
         }
     }
-    if (p.splits > 1) p.parts = p.splits * (size_t)m * part_row(n) * sizeof(float);
     return p;
 }
 
-// (the workspace is the same for both formats of activations)
-inline size_t space_of(const Plan &a, const Plan &b) { return a.laid_out + (a.parts > b.parts ? a.parts : b.parts); }
+// Bytes for the sums of the splits: of no more than m tokens, however few, so that one piece serves products of any number of them (fewer may be split
+// more).  Splits and tiles together are below twice what the card holds, which bounds the splits' tokens by the tile's.
+size_t parts_of(uint32_t m, uint32_t n, uint32_t k, int act)
+{
+    uint32_t splits = 1;
+    while (splits < MOST_SPLITS && splits * 2 * UNIT <= stages_of(k, act)) splits *= 2;
+    uint64_t most = 0;
+    for (int i = 0; i < 7 && splits > 1; ++i) {
+        const Shape &s = shapes_of(act)[i];
+        if (s.tokens > 16 && s.tokens >= 2 * up(m, 16) * 16) continue;
+        const uint64_t full = UNITS * s.resident, by_tiles = s.tokens * (2 * (full - 1) / up(n, s.rows)), by_splits = (uint64_t)splits * m;
+        const uint64_t rows = by_tiles < by_splits ? by_tiles : by_splits;
+        most = most > rows ? most : rows;
+    }
+    return most * part_row(n) * sizeof(float);
+}
+
+// A copy of the activations, and the sums.  (It is the same for both formats, and for activations that need no copy.)
+inline size_t laid_out_bytes(uint32_t m, uint32_t k) { return 2 * (size_t)m * (up(k, 128) * 128); }
+size_t linear_space(uint32_t m, uint32_t n, uint32_t k)
+{
+    const size_t a = parts_of(m, n, k, BF16), b = parts_of(m, n, k, FP16);
+    return laid_out_bytes(m, k) + (a > b ? a : b);
+}
 
 template <int ACT, int RT, int MT, int WN, int WM, int KG, int BUFFERS> bool launch_tile(const Product &a, uint32_t splits, hipStream_t s)
 {
@@ -517,7 +538,7 @@ template <int ACT> int launch(Product a, const Plan &p, void *workspace, hipStre
         a.x_row = a.x_bytes = cols * 2;
     }
     a.n_tiles = up(a.n, shape.rows), a.m_tiles = up(a.m, shape.tokens), a.split_stages = p.split_stages;
-    if (p.splits > 1) a.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + p.laid_out), a.part_row = part_row(a.n);
+    if (p.splits > 1) a.parts = reinterpret_cast<float *>(static_cast<uint8_t *>(workspace) + (ACT == MX4 ? 0 : laid_out_bytes(a.m, a.k))), a.part_row = part_row(a.n);
     bool ok;
     switch (p.shape) {
     case 0: ok = launch_tile<ACT, 4, ACT == MX4 ? 8 : 4, 4, 2, 1, 2>(a, p.splits, s); break;
@@ -549,12 +570,12 @@ extern "C" {
 size_t enec_mx4_linear_workspace(size_t m, size_t n, size_t k)
 {
     if (!sizes_ok(m, n, k) || m == 0 || n == 0 || k == 0) return 0;
-    return space_of(plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, BF16), plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, FP16));
+    return linear_space((uint32_t)m, (uint32_t)n, (uint32_t)k);
 }
 size_t enec_mx4_matmul_workspace(size_t m, size_t n, size_t k)
 {
     if (!sizes_ok(m, n, k) || m == 0 || n == 0 || k == 0) return 0;
-    return plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, MX4).parts;
+    return parts_of((uint32_t)m, (uint32_t)n, (uint32_t)k, MX4);
 }
 
 int enec_mx4_linear(const void *x, size_t m, size_t x_stride, int dtype, const void *codes, const void *scales, size_t n, size_t k, void *y,
@@ -565,15 +586,13 @@ int enec_mx4_linear(const void *x, size_t m, size_t x_stride, int dtype, const v
     if (m == 0 || n == 0) return ENEC_OK;
     if (!y || !aligned(y, 2) || y_stride < n) return ENEC_E_ARG;
     if (k != 0 && (!x || !codes || !scales || !aligned(x, 2) || !aligned(codes, 16) || !aligned(scales, 4) || x_stride < k)) return ENEC_E_ARG;
-    Plan p[2] = {};
-    if (k != 0)
-        for (int t : {BF16, FP16}) p[t] = plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, t);
-    const size_t need = space_of(p[BF16], p[FP16]);
+    const Plan p = k == 0 ? Plan{} : plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, dtype);
+    const size_t need = k == 0 ? 0 : linear_space((uint32_t)m, (uint32_t)n, (uint32_t)k);
     if (workspace_bytes < need || (need && !workspace)) return ENEC_E_CAPACITY;
     if (need && !aligned(workspace, 16)) return ENEC_E_ARG;
     const Product a{x, nullptr, static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), y, x_stride, y_stride,
                     (uint32_t)m, (uint32_t)n, (uint32_t)k, (uint32_t)((k + 127) / 128), dtype, 0, 0, 0, 0, 0, 0, nullptr};
-    return dtype == ENEC_BF16 ? launch<BF16>(a, p[BF16], workspace, (hipStream_t)stream) : launch<FP16>(a, p[FP16], workspace, (hipStream_t)stream);
+    return dtype == ENEC_BF16 ? launch<BF16>(a, p, workspace, (hipStream_t)stream) : launch<FP16>(a, p, workspace, (hipStream_t)stream);
 }
 
 int enec_mx4_matmul(const void *x_codes, const void *x_scales, size_t m, const void *codes, const void *scales, size_t n, size_t k, void *y,
@@ -586,7 +605,7 @@ int enec_mx4_matmul(const void *x_codes, const void *x_scales, size_t m, const v
     if (k != 0 && (!x_codes || !x_scales || !codes || !scales || !aligned(x_codes, 16) || !aligned(x_scales, 4) || !aligned(codes, 16) || !aligned(scales, 4)))
         return ENEC_E_ARG;
     const Plan p = k == 0 ? Plan{} : plan_of((uint32_t)m, (uint32_t)n, (uint32_t)k, MX4);
-    const size_t need = p.parts;
+    const size_t need = k == 0 ? 0 : parts_of((uint32_t)m, (uint32_t)n, (uint32_t)k, MX4);
     if (workspace_bytes < need || (need && !workspace)) return ENEC_E_CAPACITY;
     if (need && !aligned(workspace, 16)) return ENEC_E_ARG;
     const Product a{x_codes, static_cast<const uint8_t *>(x_scales), static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), y, 0, y_stride,

@@ -65,3 +65,23 @@ def test_layer(dtype, four_bits):
         want = np.concatenate([cache.read(table[b], n) for b, n in enumerate(lengths)])
         off = np.sqrt(((got.double().cpu().numpy() - want) ** 2).mean() / (want ** 2).mean())
         assert off < 0.1, off
+
+
+def test_scratch_memory_for_the_largest_step_serves_smaller_ones():
+    import low_bit_layer as example
+    hidden, ffn, heads, kv_heads, dim, batch = 256, 384, 32, 8, 128, 4
+    g = torch.Generator("cuda").manual_seed(2)
+    normal = lambda *shape: (torch.randn(*shape, generator=g, device="cuda") * shape[-1] ** -0.5).to(torch.bfloat16)  # noqa: E731
+    matrices = {"qkv": normal((heads + 2 * kv_heads) * dim, hidden), "out": normal(hidden, heads * dim), "up": normal(2 * ffn, hidden), "down": normal(hidden, ffn)}
+    layer = example.Layer({name: example.stored(w) for name, w in matrices.items()}, hidden, ffn, heads, kv_heads, dim, 2 * batch)
+    table = torch.arange(2 * batch, dtype=torch.int32, device="cuda").view(batch, 2)
+    longest = 131072
+    layer.reserve(batch, 400, 100, longest)
+    for new in (100, 64, 32, 16, 5, 1):
+        x = normal(batch * new, hidden)
+        lengths = torch.full((batch,), 100, dtype=torch.int32, device="cuda")
+        layer.workspace.fill_(0xFF)                        # (NaN, were it read unwritten)
+        for four_bits in (False, True):
+            y = layer.step(x, table, example.starts_of([new] * batch), lengths, new, longest, four_bits)
+            assert torch.isfinite(y).all()
+    assert layer.status.item() == 0

@@ -206,3 +206,24 @@ def test_a_workspace_for_the_largest_attention_serves_smaller_ones(lowbit):
     c, b = shape(8, 128), lowbit.BatchStruct(P, P, P, 8, 4, 128, None)
     size = need(c, 4, 400, 32, 100, 131072)
     assert L.enec_cache_attention(C.byref(c), C.byref(b), P, 4096, 128, P, 4096, 128, 0, 32, 32, 131072, 0.1, 0x1008, size, None) == lowbit.E_ARG
+
+
+def test_a_workspace_for_many_rows_serves_products_of_fewer(lowbit):
+    """Fewer rows can mean more splits: what is said for the most rows covers them."""
+    import random
+    rng = random.Random(6)
+    linear, matmul = lowbit.mx4_linear_workspace, lowbit.mx4_matmul_workspace
+    assert linear(115, 4285, 5818) <= linear(230, 4285, 5818) and matmul(692, 801, 10103) <= matmul(1854, 801, 10103)
+    met = 0
+    for _ in range(20000):
+        n, k, m = int(2 ** rng.uniform(0, 16)), int(2 ** rng.uniform(0, 15)), int(2 ** rng.uniform(0, 13))
+        fewer = rng.randint(1, m)
+        copied = 2 * m * -(-k // 128) * 128
+        assert linear(fewer, n, k) <= linear(m, n, k) <= copied + (68 << 20), (fewer, m, n, k)
+        assert matmul(fewer, n, k) <= matmul(m, n, k) <= 136 << 20, (fewer, m, n, k)
+        met += matmul(fewer, n, k) > 0
+    assert met > 3000
+    # and such a workspace is large enough for the call itself: the next thing wrong with it is its address
+    L = lowbit.lib()
+    assert L.enec_mx4_linear(P, 115, 5818, 0, P, P, 4285, 5818, P, 4285, 0x1008, linear(230, 4285, 5818), None) == lowbit.E_ARG
+    assert L.enec_mx4_matmul(P, P, 692, P, P, 801, 10103, P, 801, 0, 0x1008, matmul(1854, 801, 10103), None) == lowbit.E_ARG

@@ -83,7 +83,7 @@ int enec_mx4_matmul(const void *x_codes, const void *x_scales, size_t m, const v
  * batch and kv_heads are at most 65535 and n_tokens below 2^24.
  * Token i of a sequence's t tokens in the call has position lengths[b] - t + i.  A negative position (an idle slot of a batch,
  * with length 0) belongs to no page: such a token is not stored, reads back as zeros, and its attention is zeros.
- * What only the device can see is checked there.  A sequence whose starts are out of order, or whose length exceeds
+ * What only the device can see is checked there.  A sequence whose two starts are out of order or beyond the call's tokens, or whose length exceeds
  * table_stride * page_tokens or 2^30 (attention: or max_length, or whose tokens in the call exceed max_new), is left out: nothing of
  * it is stored or returned.  The tokens of a page whose number lies outside the cache are not stored, read back as zeros and are not
  * seen.  In both cases ENEC_E_ARG is stored to

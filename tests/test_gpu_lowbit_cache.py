@@ -525,3 +525,40 @@ def test_a_row_does_not_depend_on_the_others(lowbit, dim, counts, n, dtype):
         out = attend(c, others, counts, [n])
         differ = int((out[::2] != want[::2]).sum())
         assert differ == 0, (value, differ)
+
+
+# starts that do not ascend from 0 to the tokens of the call, and the sequences that are in order all the same
+BAD_STARTS = [([100, 1], [], 1), ([-5, 1], [], 1), ([0, 1, -1000, 3], [0], 3), ([0, 100, 2, 3], [2], 3), ([0, 1, 2, 9], [0, 1], 3), ([-1, 1, 2, 3], [1, 2], 3),
+              ([0, 2, 1, 1], [0], 3), ([0, 1, 2, 3, 2 ** 31 - 1, 5], [0, 1, 2], 5), ([0, 1, -2 ** 31, 3, 4, 5], [0, 3, 4], 5),
+              ([5000 if i == 10 else -7 if i == 3 else i for i in range(71)], [i for i in range(70) if i not in (2, 3, 9, 10)], 70),
+              ([-1 if i < 66 else i for i in range(71)], [66, 67, 68, 69], 70)]
+
+
+@pytest.mark.parametrize("page", [16, 64])
+@pytest.mark.parametrize("starts,good,tokens", BAD_STARTS)
+def test_starts_out_of_order_are_told_and_leave_the_other_sequences_alone(lowbit, starts, good, tokens, page):
+    batch, heads, dim = len(starts) - 1, 2, 64
+    prior = [page - 3 + b % 7 for b in range(batch)]
+    c = Both(lowbit, [n + 2 for n in prior], page, heads, dim, 40)
+    c.fill(prior, torch.bfloat16)
+    lengths = list(prior)
+    for b in good:
+        lengths[b] += starts[b + 1] - starts[b]
+    k, v = c.values(tokens, torch.bfloat16), c.values(tokens, torch.bfloat16)
+    status = torch.zeros(1, dtype=torch.int32, device="cuda")
+    assert lowbit.cache_write(c.cache, k[1], v[1], c.gpu_table, ints(starts), ints(lengths), status) == lowbit.OK
+    assert status.item() == lowbit.E_ARG
+    for b in good:
+        rows = slice(starts[b], starts[b + 1])
+        for form, x in ((c.k, k[0]), (c.v, v[0])):
+            form.write(x[rows].double().numpy(), c.table[b:b + 1], [0, starts[b + 1] - starts[b]], [lengths[b]])
+    c.check(lengths)                                       # all that is cached: nothing else was stored
+    status.zero_()
+    out = [torch.full((tokens, heads, dim), 9.0, device="cuda") for _ in range(2)]
+    assert lowbit.cache_read(c.cache, *out, c.gpu_table, ints(starts), ints(lengths), status) == lowbit.OK
+    assert status.item() == lowbit.E_ARG
+    for t, form in zip(out, (c.k, c.v)):
+        want = np.full((tokens, heads, dim), 9.0)
+        for b in good:
+            want[starts[b]:starts[b + 1]] = form.read(c.table[b], lengths[b])[lengths[b] - (starts[b + 1] - starts[b]):]
+        assert np.array_equal(t.cpu().double().numpy(), want)

@@ -673,12 +673,19 @@ __global__ void __launch_bounds__(256) attend_join_kernel(Attend a)
     __shared__ f32x4 sums[AT_ONCE][LANES];
     __shared__ float tops[4], totals[AT_ONCE];
     const uint32_t token = blockIdx.x, q_head = blockIdx.y, lane = threadIdx.x & 63, d4 = threadIdx.x % LANES, mine = threadIdx.x / LANES;
-    // the token's sequence: the last one that starts at or before it
-    uint32_t n = 0;
-    for (uint32_t b = 0; b < a.c.batch; b += 64) n += (uint32_t)__popcll(__ballot(b + lane < a.c.batch && a.c.starts[b + lane] <= (int32_t)token));
-    if (n == 0) return;
-    const Sequence s = sequence_of(a, n - 1);
-    if (!s.good || token - s.start >= s.count) return;
+    // the token's sequence: the one that starts at or before it and ends behind it
+    uint32_t b = 0;
+    for (;; b += 64) {
+        if (b >= a.c.batch) return;
+        const uint32_t i = b + lane < a.c.batch ? b + lane : a.c.batch - 1;
+        const int32_t start = a.c.starts[i], next = a.c.starts[i + 1];
+        const uint64_t has = __ballot(in_order(a.c, start, next) && start <= (int32_t)token && (int32_t)token < next);
+        if (has == 0) continue;
+        b += (uint32_t)__builtin_ctzll(has);
+        break;
+    }
+    const Sequence s = sequence_of(a, b);
+    if (!s.good) return;
     const int32_t sees = s.length - (int32_t)s.count + (int32_t)(token - s.start) + 1;
     const uint32_t splits = sees <= 0 ? 1 : ((uint32_t)sees + a.chunk - 1) / a.chunk;
     const size_t at = (size_t)token * a.q_heads + q_head, step = (size_t)a.c.n_tokens * a.q_heads;
@@ -704,7 +711,7 @@ __global__ void __launch_bounds__(256) attend_join_kernel(Attend a)
     __syncthreads();
     if (mine != 0) return;
     for (uint32_t i = 1; i < AT_ONCE; ++i) o += sums[i][d4], total += totals[i];
-    const float by = share_of(a, s, n - 1, token - s.start, total);
+    const float by = share_of(a, s, b, token - s.start, total);
     uint16_t *p = static_cast<uint16_t *>(a.out) + (size_t)token * a.out_token + (size_t)q_head * a.out_head + 4 * d4;
     *reinterpret_cast<u32x2_a2 *>(p) = u32x2{pack2<DT>(o[0] * by, o[1] * by), pack2<DT>(o[2] * by, o[3] * by)};
 }

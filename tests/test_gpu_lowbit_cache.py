@@ -562,3 +562,27 @@ def test_starts_out_of_order_are_told_and_leave_the_other_sequences_alone(lowbit
         for b in good:
             want[starts[b]:starts[b + 1]] = form.read(c.table[b], lengths[b])[lengths[b] - (starts[b + 1] - starts[b]):]
         assert np.array_equal(t.cpu().double().numpy(), want)
+
+
+@pytest.mark.parametrize("starts,good,tokens", BAD_STARTS)
+def test_starts_out_of_order_leave_the_attention_of_the_other_sequences_alone(lowbit, starts, good, tokens):
+    """Also where the cached tokens are split, and the splits joined."""
+    batch, heads, dim, page = len(starts) - 1, 1, 64, 64
+    lengths = [70 + 31 * (b % 5) for b in range(batch)]
+    lengths[good[0] if good else 0] = 2500
+    c = Both(lowbit, lengths, page, heads, dim, 41)
+    c.fill(lengths, torch.bfloat16)
+    q = torch.from_numpy(c.rng.standard_normal((tokens, 2, dim)).astype(np.float32)).to(torch.bfloat16)
+    for most in (2500, 20000):
+        out = torch.full_like(q, 77.0, device="cuda")
+        ws = torch.full((max(16, lowbit.cache_attention_workspace(c.cache, batch, tokens, 2, 2, most)),), 0xFF, dtype=torch.uint8, device="cuda")
+        status = torch.zeros(1, dtype=torch.int32, device="cuda")
+        assert lowbit.cache_attention(c.cache, q.cuda(), out, c.gpu_table, ints(starts), ints(lengths), 2, most, ws, status=status) == lowbit.OK
+        assert status.item() == lowbit.E_ARG
+        left = torch.ones(tokens, dtype=torch.bool)
+        for b in good:
+            rows = slice(starts[b], starts[b + 1])
+            want, bound = plain.attention(q[rows].double().numpy(), c.k.read(c.table[b], lengths[b]), c.v.read(c.table[b], lengths[b]), dim ** -0.5, q.dtype)
+            assert (np.abs(out[rows].double().cpu().numpy() - want) <= bound).all(), b
+            left[rows] = False
+        assert bool((out.cpu()[left] == 77).all())

@@ -2,7 +2,7 @@
 
 Matrices in microscaled 4-bit floating point with the products that read them, and a paged 8-bit cache with its
 attention.  As in enec.py: argument marshalling only, PyTorch for device memory and streams, status codes returned, no CPU
-fallback.  The tensors' shapes are checked here, where C sees pointers only; a wrong one raises ValueError.
+fallback.  The tensors' shapes, integer types and places are checked here, where C sees pointers only; a wrong one raises ValueError.
 """
 from __future__ import annotations
 
@@ -67,6 +67,21 @@ def _dtype(t) -> int:
     return _codes.get(t.dtype, -1)
 
 
+def _on_gpu(*tensors):
+    """All of them (None: none) lie on one GPU, or in pinned host memory, which its kernels reach too.  (The calls compare the numbers of their tensors' GPUs
+    themselves, 0.04 us each, and ask here where these differ.)"""
+    device = -1
+    for t in tensors:
+        at = -1 if t is None else t.get_device()
+        if at < 0:
+            if t is not None and not t.is_pinned():
+                raise ValueError("tensors on the GPU are wanted")
+        elif device < 0:
+            device = at
+        elif at != device:
+            raise ValueError("tensors on one GPU are wanted")
+
+
 def _rows(t, what):
     """(rows, columns, row stride) of a matrix whose rows are runs."""
     shape = t.shape                                         # (an attribute of a tensor costs 0.1 us: each is asked for once)
@@ -119,6 +134,8 @@ def mx4_quantize(src, codes, scales, stream=None) -> int:
     _same_padding(padded, cols)
     if n != rows:
         raise ValueError("src and codes differ in their rows")
+    if not src.get_device() == codes.get_device() == scales.get_device() >= 0:
+        _on_gpu(src, codes, scales)
     return lib().enec_mx4_quantize(src.data_ptr(), rows, cols, stride, _dtype(src), codes.data_ptr(), scales.data_ptr(),
                                    enec._stream_handle(stream))
 
@@ -130,6 +147,8 @@ def mx4_dequantize(codes, scales, out, stream=None) -> int:
     _same_padding(padded, cols)
     if n != rows:
         raise ValueError("out and codes differ in their rows")
+    if not codes.get_device() == scales.get_device() == out.get_device() >= 0:
+        _on_gpu(codes, scales, out)
     return lib().enec_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), stride, _dtype(out),
                                      enec._stream_handle(stream))
 
@@ -146,6 +165,8 @@ def mx4_linear(x, codes, scales, out, workspace=None, stream=None) -> int:
     rows, cols, y_stride = _rows(out, "out")
     if (rows, cols) != (m, n) or out.dtype != x.dtype:
         raise ValueError(f"out: ({m}, {n}) of x's format is wanted")
+    if not x.get_device() == codes.get_device() == scales.get_device() == out.get_device() == (x if workspace is None else workspace).get_device() >= 0:
+        _on_gpu(x, codes, scales, out, workspace)
     ws, size = _space(workspace)
     return lib().enec_mx4_linear(x.data_ptr(), m, x_stride, _dtype(x), codes.data_ptr(), scales.data_ptr(), n, k, out.data_ptr(), y_stride,
                                  ws, size, enec._stream_handle(stream))
@@ -162,6 +183,9 @@ def mx4_matmul(x_codes, x_scales, codes, scales, out, workspace=None, stream=Non
     rows, cols, y_stride = _rows(out, "out")
     if padded != other or (rows, cols) != (m, n):
         raise ValueError(f"matrices of as many columns and out ({m}, {n}) are wanted")
+    if not x_codes.get_device() == x_scales.get_device() == codes.get_device() == scales.get_device() == out.get_device() \
+            == (out if workspace is None else workspace).get_device() >= 0:
+        _on_gpu(x_codes, x_scales, codes, scales, out, workspace)
     ws, size = _space(workspace)
     return lib().enec_mx4_matmul(x_codes.data_ptr(), x_scales.data_ptr(), m, codes.data_ptr(), scales.data_ptr(), n, padded, out.data_ptr(),
                                  y_stride, _dtype(out), ws, size, enec._stream_handle(stream))
@@ -179,7 +203,10 @@ class Cache:
         for t in (k_codes, k_scales, v_codes, v_scales):
             if t.element_size() != 1 or not t.is_contiguous():
                 raise ValueError("the cache's tensors are bytes without gaps")
+            if t.device != k_codes.device:
+                raise ValueError("the cache's tensors are on one GPU")
         self.tensors = (k_codes, k_scales, v_codes, v_scales)
+        self.device = k_codes.get_device()
         self.page_tokens, self.heads, self.head_dim, self.n_pages = page, heads, dim, pages
         self.struct = CacheStruct(*(t.data_ptr() for t in self.tensors), pages, page, heads, dim)
         self.ref = C.byref(self.struct)
@@ -197,14 +224,26 @@ _BATCH = struct.Struct("=QQQIII4xQ")          # a BatchStruct: packed in one go,
 assert _BATCH.size == C.sizeof(BatchStruct)
 
 
-def _batch(table, starts, lengths, n_tokens, status):
+_int32 = None
+
+
+def _batch(cache, x, y, table, starts, lengths, n_tokens, status, workspace=None):
+    global _int32
+    if _int32 is None:
+        import torch
+        _int32 = torch.int32
     shape = table.shape
     batch = lengths.numel()
     if len(shape) != 2 or shape[0] != batch or starts.numel() != batch + 1:
         raise ValueError("table (batch, pages) has a row for each of lengths, starts one entry more")
-    if table.itemsize != 4 or starts.itemsize != 4 or lengths.itemsize != 4 \
+    if table.dtype is not _int32 or starts.dtype is not _int32 or lengths.dtype is not _int32 \
             or not table.is_contiguous() or not starts.is_contiguous() or not lengths.is_contiguous():
         raise ValueError("table, starts and lengths are int32 without gaps")
+    if status is not None and (status.dtype is not _int32 or status.numel() == 0):
+        raise ValueError("status: an int32 word, or None, is wanted")
+    if not x.get_device() == y.get_device() == table.get_device() == starts.get_device() == lengths.get_device() == (x if status is None else status).get_device() \
+            == (x if workspace is None else workspace).get_device() == cache.device >= 0:
+        _on_gpu(cache.tensors[0], x, y, table, starts, lengths, status, workspace)
     return _BATCH.pack(table.data_ptr(), starts.data_ptr(), lengths.data_ptr(), shape[1], batch, n_tokens,
                        0 if status is None else status.data_ptr())
 
@@ -226,14 +265,14 @@ def cache_write(cache, k, v, table, starts, lengths, status=None, stream=None) -
     """Enqueues enec_cache_write.  k, v: (tokens, heads, head_dim) of bf16 or fp16, the newest tokens of their sequences; table (batch,
     pages), starts (batch + 1) and lengths (batch, new tokens included): int32 on the device; status: None or an int32 word holding 0."""
     tokens, kt, kh, vt, vh = _tokens(k, v, cache.heads, cache.head_dim, "k and v")
-    b = _batch(table, starts, lengths, tokens, status)
+    b = _batch(cache, k, v, table, starts, lengths, tokens, status)
     return lib().enec_cache_write(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, _dtype(k), enec._stream_handle(stream))
 
 
 def cache_read(cache, k, v, table, starts, lengths, status=None, stream=None) -> int:
     """Enqueues enec_cache_read: the newest tokens' keys and values into k, v (bf16, fp16 or fp32); starts of whole lengths read all."""
     tokens, kt, kh, vt, vh = _tokens(k, v, cache.heads, cache.head_dim, "k and v")
-    b = _batch(table, starts, lengths, tokens, status)
+    b = _batch(cache, k, v, table, starts, lengths, tokens, status)
     return lib().enec_cache_read(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, _dtype(k), enec._stream_handle(stream))
 
 
@@ -246,7 +285,7 @@ def cache_attention(cache, q, out, table, starts, lengths, max_new: int, max_len
     """Enqueues enec_cache_attention.  q, out: (tokens, q_heads, head_dim) of bf16 or fp16; scale: head_dim ** -0.5 unless given."""
     heads, dim = q.shape[1], cache.head_dim
     tokens, qt, qh, ot, oh = _tokens(q, out, heads, dim, "q and out")
-    b = _batch(table, starts, lengths, tokens, status)
+    b = _batch(cache, q, out, table, starts, lengths, tokens, status, workspace)
     ws, size = _space(workspace)
     return lib().enec_cache_attention(cache.ref, b, q.data_ptr(), qt, qh, out.data_ptr(), ot, oh, _dtype(q), heads, max_new, max_length,
                                       dim ** -0.5 if scale is None else scale, ws, size, enec._stream_handle(stream))

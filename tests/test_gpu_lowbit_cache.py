@@ -586,3 +586,20 @@ def test_starts_out_of_order_leave_the_attention_of_the_other_sequences_alone(lo
             assert (np.abs(out[rows].double().cpu().numpy() - want) <= bound).all(), b
             left[rows] = False
         assert bool((out.cpu()[left] == 77).all())
+
+
+def test_places_that_the_binding_refuses_and_pinned_memory(lowbit):
+    c = Both(lowbit, [20], 16, 1, 64, 50)
+    c.fill([20], torch.bfloat16)
+    q = torch.randn(1, 2, 64, generator=torch.Generator().manual_seed(1)).to(torch.bfloat16)
+    want = attend(c, q, [1], [20])
+    good = dict(q=q.cuda(), out=torch.empty_like(q, device="cuda"), table=c.gpu_table, starts=ints([0, 1]), lengths=ints([20]), status=torch.zeros(1, dtype=torch.int32, device="cuda"),
+                workspace=torch.empty(1 << 20, dtype=torch.uint8, device="cuda"))
+    call = lambda q, out, table, starts, lengths, status, workspace: lowbit.cache_attention(c.cache, q, out, table, starts, lengths, 1, 20, workspace, status=status)  # noqa: E731
+    for name, t in good.items():
+        with pytest.raises(ValueError, match="GPU"):
+            call(**good | {name: t.cpu()})                  # refused on the host: no kernel sees the address
+    pinned = {name: good[name].cpu().pin_memory() for name in ("table", "starts", "lengths", "status")}
+    assert call(**good | pinned) == lowbit.OK
+    torch.cuda.synchronize()
+    assert torch.equal(good["out"], want) and pinned["status"].item() == 0

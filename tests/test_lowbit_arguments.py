@@ -227,3 +227,37 @@ def test_a_workspace_for_many_rows_serves_products_of_fewer(lowbit):
     L = lowbit.lib()
     assert L.enec_mx4_linear(P, 115, 5818, 0, P, P, 4285, 5818, P, 4285, 0x1008, linear(230, 4285, 5818), None) == lowbit.E_ARG
     assert L.enec_mx4_matmul(P, P, 692, P, P, 801, 10103, P, 801, 0, 0x1008, matmul(1854, 801, 10103), None) == lowbit.E_ARG
+
+
+def test_types_and_places_that_the_binding_refuses(lowbit):
+    """What the kernels would read as something else, or not reach at all."""
+    import torch
+    byte = lambda *s: torch.zeros(*s, dtype=torch.uint8)  # noqa: E731
+    c = lowbit.Cache(byte(4, 2, 16, 64), byte(4, 2), byte(4, 2, 64, 16), byte(4, 2))
+    i = lambda *s: torch.zeros(*s, dtype=torch.int32)  # noqa: E731
+    k, q = torch.zeros(5, 2, 64, dtype=torch.bfloat16), torch.zeros(5, 4, 64, dtype=torch.bfloat16)
+
+    def calls(table, starts, lengths, status=None):
+        yield lambda: lowbit.cache_write(c, k, k, table, starts, lengths, status)
+        yield lambda: lowbit.cache_read(c, k, k, table, starts, lengths, status)
+        yield lambda: lowbit.cache_attention(c, q, q, table, starts, lengths, 1, 32, status=status)
+
+    good = dict(table=i(3, 2), starts=i(4), lengths=i(3))
+    for name in good:
+        for other in (torch.float32, torch.uint8, torch.int64):
+            for call in calls(**good | {name: good[name].to(other)}):
+                with pytest.raises(ValueError, match="int32"):
+                    call()
+    for status in (byte(4), i(0), torch.zeros(1), torch.zeros(1, dtype=torch.int64)):
+        for call in calls(**good, status=status):
+            with pytest.raises(ValueError, match="status"):
+                call()
+    for call in calls(**good):                             # all well, but in the host's memory
+        with pytest.raises(ValueError, match="GPU"):
+            call()
+    x, codes, scales, x4 = torch.zeros(4, 200, dtype=torch.bfloat16), byte(6, 128), byte(6, 8), (byte(4, 128), byte(4, 8))
+    out = torch.zeros(4, 6, dtype=torch.bfloat16)
+    for call in (lambda: lowbit.mx4_quantize(x, *x4), lambda: lowbit.mx4_dequantize(*x4, x), lambda: lowbit.mx4_linear(x, codes, scales, out),
+                 lambda: lowbit.mx4_matmul(*x4, codes, scales, out)):
+        with pytest.raises(ValueError, match="GPU"):
+            call()

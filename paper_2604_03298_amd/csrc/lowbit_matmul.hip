@@ -35,7 +35,7 @@ __device__ __forceinline__ f32x4 mfma_mx4(int s, const u32x4 &a, const u32x4 &b,
            : s == 2 ? mfma_mx4_byte<2>(a, b, c, sa, sb)
                     : mfma_mx4_byte<3>(a, b, c, sa, sb);
 }
-// eight codes as bf16 values: at most two significant bits and the scale's power of two, so exact
+// eight codes as bf16 values: at most two significant bits and the scale's power of two, so exact; a scale of infinity makes each NaN
 __device__ __forceinline__ bf16x8 values_of(uint32_t codes, float scale)
 {
     const bf16x2 a = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 0), b = __builtin_amdgcn_cvt_scalef32_pk_bf16_fp4(codes, scale, 1);

@@ -603,3 +603,41 @@ def test_places_that_the_binding_refuses_and_pinned_memory(lowbit):
     assert call(**good | pinned) == lowbit.OK
     torch.cuda.synchronize()
     assert torch.equal(good["out"], want) and pinned["status"].item() == 0
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("dim", [128, 256])
+@pytest.mark.parametrize("counts,lengths", [([1, 1], [300, 0]), ([90], [200]), ([40, 60], [5000, 60])])
+def test_infinite_and_undefined_scores_of_wide_heads(lowbit, dim, counts, lengths, dtype):
+    """As test_infinite_and_undefined_scores, of three heads the middle one; the others' rows are those of the definition."""
+    c = Both(lowbit, lengths, 64, 1, dim, 42)
+    n = sum(lengths)
+    k, v = c.values(n, dtype), c.values(n, dtype)
+    k[0][:, :, 7] = 1.0
+    c.write(lengths, lengths, (k[0], k[0].cuda()), v)
+    for what in (float("-inf"), float("inf"), float("nan")):
+        q = torch.from_numpy(c.rng.standard_normal((sum(counts), 3, dim)).astype(np.float32)).to(dtype)
+        q[:, 1] = 0
+        q[:, 1, 7] = what
+        out = attend(c, q, counts, lengths)
+        at = 0
+        for count, length in zip(counts, lengths):
+            for i in range(count):
+                sees = length - count + i + 1 > 0
+                assert torch.isnan(out[at, 1]).all() if sees else (out[at] == 0).all(), (what, count, length, i)
+                at += 1
+        check_attention(c, out[:, ::2], q[:, ::2].contiguous(), counts, lengths)
+
+
+@pytest.mark.parametrize("dtype", HALF)
+@pytest.mark.parametrize("dim", [128, 256])
+@pytest.mark.parametrize("layout", [1, 2])
+def test_strides_of_wide_heads(lowbit, layout, dim, dtype):
+    counts, lengths = [1, 9, 60], [900, 9, 164]
+    c = Both(lowbit, lengths, 32, 2, dim, seed=43 + layout)
+    c.fill(lengths, dtype, layout)
+    q = torch.from_numpy(c.rng.standard_normal((70, 6, dim)).astype(np.float32)).to(dtype)
+    for new, most in ((None, None), (100, 100000)):
+        check_attention(c, attend(c, q, counts, lengths, 0.2, layout, new, most), q, counts, lengths, 0.2)
+    few = [1, 0, 5]
+    check_attention(c, attend(c, q[:6], few, lengths, None, layout), q[:6], few, lengths)

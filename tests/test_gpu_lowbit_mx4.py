@@ -343,3 +343,63 @@ def test_least_and_largest_activations(lowbit, m, dtype):
     fits = np.abs(want) < 60000 if dtype == torch.float16 else np.isfinite(want)
     off = np.abs(got - want) - plain.product_bound(xx, w, want, dtype)
     assert fits.mean() > 0.4 and (off[fits] <= 0).all()
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("m,n,k", [(1, 70, 300), (20, 70, 300), (50, 70, 300), (150, 70, 300), (300, 600, 300), (3, 20, 8100), (600, 1030, 256)])
+def test_blocks_without_values_make_their_row_of_weights_nan(lowbit, m, n, k, dtype):
+    """A scale byte of 255, whatever the codes: of the first block and of the last, of one row and of a tile's all; and only those rows."""
+    codes, scales = weights(n, k, 4)
+    blocks = -(-k // 32)
+    bad = [5, n - 1] + list(range(16, min(32, n)))
+    scales[5, 0] = scales[n - 1, blocks - 1] = 255
+    scales[16:32, blocks // 2] = 255
+    x = (torch.randn(m, k, generator=torch.Generator().manual_seed(5)).abs() + 0.1).to(dtype)
+    want = x.double().numpy() @ plain.mx4_decode(np.where(scales.repeat(16, 1) == 255, 0, codes).astype(np.uint8), np.where(scales == 255, 0, scales).astype(np.uint8), k).T
+    bound = plain.product_bound(x.double().numpy(), np.abs(plain.mx4_decode(codes, np.where(scales == 255, 0, scales).astype(np.uint8), k)), want, dtype)
+    ok = np.ones(n, dtype=bool)
+    ok[bad] = False
+    for fill in (0x00, 0x22, 0x77, 0xAA, 0xF2, None):      # zeros, ones, sixes, minus ones, mixed signs, any
+        held = codes if fill is None else np.where(scales.repeat(16, 1) == 255, fill, codes).astype(np.uint8)
+        out = torch.empty(m, n, dtype=dtype, device="cuda")
+        ws = space(lowbit.mx4_linear_workspace(m, n, k))
+        assert lowbit.mx4_linear(x.cuda(), torch.from_numpy(held).cuda(), torch.from_numpy(scales).cuda(), out, ws) == lowbit.OK
+        got = out.double().cpu().numpy()
+        assert np.isnan(got[:, ~ok]).all(), (fill, np.isnan(got[:, ~ok]).mean())
+        assert np.isfinite(got[:, ok]).all() and (np.abs(got - want)[:, ok] <= bound[:, ok]).all(), fill
+
+
+@pytest.mark.parametrize("dtype", [torch.bfloat16, torch.float16])
+@pytest.mark.parametrize("m", [1, 20, 50, 150, 600])
+def test_activations_that_are_not_finite_reach_their_own_row_only(lowbit, m, dtype):
+    n, k = 1030, 300
+    codes, scales = weights(n, k, 14)
+    codes[7] = 0                                           # infinity times zero
+    x = torch.randn(m, k, generator=torch.Generator().manual_seed(15)).to(dtype)
+    x[m // 2, 7] = float("inf")
+    if m > 1:
+        x[0, 299], x[m - 1, 0] = float("nan"), float("-inf")
+    out = torch.empty(m, n, dtype=dtype, device="cuda")
+    ws = space(lowbit.mx4_linear_workspace(m, n, k))
+    assert lowbit.mx4_linear(x.cuda(), torch.from_numpy(codes).cuda(), torch.from_numpy(scales).cuda(), out, ws) == lowbit.OK
+    with np.errstate(invalid="ignore"):
+        want = torch.from_numpy(x.double().numpy() @ plain.mx4_decode(codes, scales, k).T)
+    got = out.double().cpu()
+    assert torch.equal(torch.isnan(got), torch.isnan(want)) and torch.equal(torch.isinf(got), torch.isinf(want))
+    assert torch.equal(got[torch.isinf(want)], want[torch.isinf(want)])
+
+
+@pytest.mark.parametrize("m", [1, 20, 150, 600])
+def test_blocks_without_values_on_either_side_of_a_4_bit_product(lowbit, m):
+    n, k = 600, 300
+    codes, scales = weights(n, k, 4)
+    x_codes, x_scales = weights(m, k, 6)
+    scales[5, 0] = scales[n - 1, 9] = x_scales[m // 2, 1] = 255
+    bad = np.zeros((m, n), dtype=bool)
+    bad[m // 2], bad[:, 5], bad[:, n - 1] = True, True, True
+    for fill in (0x00, 0x22, 0xF2):
+        held, x_held = (np.where(s.repeat(16, 1) == 255, fill, c).astype(np.uint8) for c, s in ((codes, scales), (x_codes, x_scales)))
+        out = torch.empty(m, n, device="cuda")
+        ws = space(lowbit.mx4_matmul_workspace(m, n, k))
+        assert lowbit.mx4_matmul(*[torch.from_numpy(t).cuda() for t in (x_held, x_scales, held, scales)], out, ws) == lowbit.OK
+        assert np.array_equal(torch.isnan(out).cpu().numpy(), bad), fill

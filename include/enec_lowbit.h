@@ -122,11 +122,12 @@ int enec_cache_read(const enec_cache *cache, const enec_cache_batch *batch, void
  *   q_heads a multiple of kv_heads
  *   max_new, max_length  HOST: no sequence has more tokens in the call, or more in all (they shape the launch)
  *           ENEC_E_ARG from max_new (q_heads / kv_heads) = 2^21 or batch kv_heads = 2^23 on
- *   scale   above zero and finite, usually head_dim^-1/2
+ *   scale   above zero and at most 2^127, usually head_dim^-1/2
  *   workspace  DEVICE, 16-byte aligned, or NULL if workspace_bytes = enec_cache_attention_workspace(...) is 0.  What it says serves every
  *           call with no more sequences, tokens, max_new and max_length as well (n_tokens at most batch max_new, as in any call that leaves
  *           no sequence out); it is 35 MB at most then.
- * Scores, softmax and sums are held in 32 bits; for the product with v the probabilities are rounded to the sum of two bf16 numbers (16
+ * Scores, softmax and sums are held in 32 bits (queries from 2^110 on may leave their range: a score's sum is one over codes, which
+ * takes the page's scale last); for the product with v the probabilities are rounded to the sum of two bf16 numbers (16
  * significant bits). */
 size_t enec_cache_attention_workspace(const enec_cache *cache, uint32_t batch, uint32_t n_tokens, uint32_t q_heads, uint32_t max_new,
                                       uint32_t max_length);

@@ -2,8 +2,6 @@
 #include "enec_lowbit.h"
 #include "lowbit_pages.hpp"
 
-#include <cmath>
-
 namespace enec {
 namespace lowbit {
 
@@ -798,6 +796,7 @@ template <int DT> bool launch(const Attend &a, const Plan &p, hipStream_t s)
     return a.c.head_dim == 64 ? launch<DT, 64>(a, p, s) : a.c.head_dim == 128 ? launch<DT, 128>(a, p, s) : launch<DT, 256>(a, p, s);
 }
 
+constexpr float MAX_SCALE = 0x1p127f;              // times log2 e it is still finite
 constexpr uint32_t MAX_ROWS = 1u << 21, MAX_GROUPS = 1u << 23;      // what a launch holds: 65535 tiles of rows, 2^32 threads side by side
 
 // one call's arguments; 0 = none of its kernels can count with these
@@ -829,7 +828,7 @@ int enec_cache_attention(const enec_cache *cache, const enec_cache_batch *batch,
     if (const int rc = pages_of(cache, batch, a.c)) return rc;
     if (!shape_ok(cache, a.c.batch, a.c.n_tokens, q_heads, max_new, max_length)) return ENEC_E_ARG;
     if (a.c.batch == 0 || a.c.n_tokens == 0) return ENEC_OK;
-    if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 1) || max_new == 0 || !(scale > 0) || !std::isfinite(scale)) return ENEC_E_ARG;
+    if (!q || !out || (((uintptr_t)q | (uintptr_t)out) & 1) || max_new == 0 || !(scale > 0) || !(scale <= MAX_SCALE)) return ENEC_E_ARG;
     const uint32_t group = q_heads / a.c.heads;
     const Plan p = plan_of(a.c.batch, a.c.heads, group, a.c.head_dim, max_new, max_length);
     const size_t need = enec_cache_attention_workspace(cache, a.c.batch, a.c.n_tokens, q_heads, max_new, max_length);

@@ -261,3 +261,16 @@ def test_types_and_places_that_the_binding_refuses(lowbit):
                  lambda: lowbit.mx4_matmul(*x4, codes, scales, out)):
         with pytest.raises(ValueError, match="GPU"):
             call()
+
+
+def test_scales_that_leave_the_range_of_32_bits_are_refused(lowbit):
+    """The kernels have the scale times log2 e, which has to be finite too."""
+    L = lowbit.lib()
+    c, b = lowbit.CacheStruct(P, P, P, P, 10, 64, 4, 128), lowbit.BatchStruct(P, P, P, 8, 3, 5, None)
+    call = lambda scale, ws: L.enec_cache_attention(C.byref(c), C.byref(b), P, 1024, 128, P, 1024, 128, 0, 8, 1, 1 << 20, scale, ws, 1 << 40, None)  # noqa: E731
+    for scale in (3e38, 2.0 ** 127 * 1.5, 2.4e38):
+        assert call(scale, P) == lowbit.E_ARG, scale
+    need = L.enec_cache_attention_workspace(C.byref(c), 3, 5, 8, 1, 1 << 20)
+    assert need > 0                                        # the next thing wrong with these is that there is no workspace
+    for scale in (2.0 ** 127, 1e-40, 0.1):
+        assert call(scale, None) == lowbit.E_CAPACITY, scale

@@ -39,7 +39,8 @@ __device__ __forceinline__ float share_of(const Attend &a, const Sequence &s, ui
 
 // The largest of four lanes sixteen apart.  The exchanges swap rows of lanes of two registers that hold the same; as instructions of their own, since the
 // compiler takes the two results for equal.
-// (`maximum` is one instruction for three operands; fmaxf passes each through an instruction of its own first.  It gives NaN where one of them is, which is the row's result.)
+// (`maximum` is one instruction for three operands; fmaxf passes each through an instruction of its own first.  It gives NaN where one of them is, which is the
+// row's result.)
 __device__ __forceinline__ float over_groups_max(float v)
 {
     float a = v, b = v;
@@ -331,8 +332,8 @@ template <int DT, int D, int NT, bool MANY> struct Rows {
             }
             high = over_groups_max(high) * by;
             // Weights are taken relative to a maximum that may lag behind by up to 2^LAG, which costs no bits of theirs, and most tiles need no change of
-            // what is summed already (two prompts of 4000 tokens over 5003, fp16: 457 us with a lag of 8, 480 with none; where time is the memory's it is the same).
-            // (A row goes by its own scores only, so that its bits do not depend on the other rows of the wave.)
+            // what is summed already (two prompts of 4000 tokens over 5003, fp16: 457 us with a lag of 8, 480 with none; where time is the memory's it is the
+            // same).  (A row goes by its own scores only, so that its bits do not depend on the other rows of the wave.)
             const bool moves = high > most[n] + LAG;
             if (__any(moves)) {
                 const float now = moves ? high : most[n], fade = moves ? exp2_of(most[n] - now) : 1.0f;
@@ -450,8 +451,9 @@ __device__ __forceinline__ Cached cached_of(const Attend &a, const Sequence &s, 
 // been multiplied, the next tile's are copied there while the weights are computed and the values multiplied, and the next values while the next keys are.
 // It waits for its own copies only: no barrier until the end.  Two waves to a SIMD (head_dim 256: one) did more than copies further ahead: a tile's
 // chain of steps leaves half of a wave's cycles idle (64 sequences of up to 8191 tokens: 4 waves with two tiles each 150 us).
-// Bound by HBM: 64 sequences of up to 8191 tokens, 8 heads of 128, bf16 134 us (4.9 TB/s); two of 131072, fp16, pages of 16,
-// 83 us and the join 4.5.  One sequence of 1000 tokens: 10 us, a chain of dependent reads.
+// Bound by the way of the cached codes into LDS: 64 sequences of up to 8191 tokens, 8 heads of 128, bf16 135 us (4.95 TB/s; reads alone reach 7.0 on this
+// card), of which the copies and their waits take 128 without any arithmetic; two of 131072, fp16, pages of 16, 84 to 88 us and the join 4.7.  One sequence of
+// 1000 tokens: 10.3 us, a chain of dependent reads (7.9 without the arithmetic).  Heads of 64 72 us, of 256 150 (16 over 4 heads).
 template <int DT, int D, int NT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kernel(Attend a)
 {
@@ -578,9 +580,11 @@ __global__ void __launch_bounds__(64 * WAVES, D == 256 ? 1 : 2) attend_few_kerne
 // 16 NT rows to each of four waves, which share the tiles: a wave has all of them, so nothing is joined in the end.  The memory unit copies the codes
 // of a tile into LDS while the one before is worked on.  Every wave makes 16-bit values of the codes by itself, where it needs them: a conversion makes two of
 // them in the time of any vector instruction, and NT tiles of rows use each.
-// Bound by the vector and the matrix unit together: two prompts of 4000 tokens over 5003, 32 heads of 128 457 us (650 TFLOP/s) in either format, 32 heads
-// of 64 306, 16 of 256 546.  Multiplying a tile's values while the next tile's weights are computed, instruction by instruction, did not help, nor did four
-// tiles of rows to a wave, which do not fit the registers.
+// Bound by the vector and the matrix unit together: two prompts of 4000 tokens over 5003, 32 heads of 128, 457 to 472 us (630 to 650 TFLOP/s) in either format;
+// matrix instructions take 45 % of the cycles, vector instructions 65 % (the issue of the former among them).  32 heads of 64 take 306 us, 16 of 256 541 to
+// 547.  Multiplying a tile's values while the next tile's weights are computed, instruction by instruction, did not help, nor did four tiles of rows to a wave,
+// which do not fit the registers.  Rows fill the tiles of 128 only where there are many: 5 new tokens of 8 heads a group, 40 rows, over 4000 cached of 32
+// sequences take 125 us, 8 tokens of one head a group, 8 rows of the kernel above, over four times the codes 144.
 template <int DT, int D, int NT>
 __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
 {
@@ -638,7 +642,7 @@ __global__ void __launch_bounds__(256, 2) attend_many_kernel(Attend a)
         f32x4 x[NT][4];
         r.scores(tiles[buffer], k, x);
         // (a wave between its products goes first: the other one of its SIMD has matrix instructions running meanwhile; 400 -> 378 us for two prompts of
-        // 4000 tokens over 5003)
+        // 4000 tokens over 5003, with one bf16 number a weight)
         __builtin_amdgcn_s_setprio(1);
         r.add(tiles[buffer], x, t0, s.length, whole, page, power_of(kb), a.scale, page >= 0 ? power_of(vb) : 1.0f, [] { __builtin_amdgcn_s_setprio(0); });
         page = next_page, whole = next_whole, kb = next_kb, vb = next_vb;
@@ -751,8 +755,8 @@ Plan plan_of(uint32_t batch, uint32_t kv_heads, uint32_t group, uint32_t head_di
     return p;
 }
 
-// The rows of parts, each of a token, that no call exceeds with at most so many of all these.  Smaller calls may be split more, but a kernel's splits, sequences, heads and
-// tiles of rows multiply to `slots` at most, a tile has the tokens of so many rows, and a split has `least` tokens.
+// The rows of parts, each of a token, that no call exceeds with at most so many of all these.  Smaller calls may be split more, but a kernel's splits,
+// sequences, heads and tiles of rows multiply to `slots` at most, a tile has the tokens of so many rows, and a split has `least` tokens.
 uint64_t most_parts(uint32_t n_tokens, uint32_t q_heads, uint32_t group, uint32_t head_dim, uint32_t max_new, uint32_t max_length)
 {
     const uint64_t rows = (uint64_t)max_new * group;

@@ -118,10 +118,13 @@ template <int ROW> __device__ __forceinline__ uint32_t turn(uint32_t r)
 // its own there, so that each lane's 16 bytes are an access by themselves to the vector cache, where four neighbouring lanes of a copy make one
 // (2048 tokens x 4096 x 16384: 125 million accesses and 272 us then; the cache takes about one in a cycle).
 // As left operand a lane has row lane mod 16, and of a stage's blocks of 32 columns block lane / 16 (or 4 s + lane / 16 at step s).
-// Few tokens: bound by the weights' way from memory; 4096 x 11008 bf16 with one token 7.3 us a call (3.3 TB/s), 32 tokens 10, 8192 x 28672 with one token
-// 22 (5.7 TB/s).
-// Many: by the matrix unit and LDS; 4096 tokens x 8192 x 28672 bf16 1400 us (1375 TFLOP/s, what a large library product of bf16 reaches on this card),
-// fp16 255 us for 2048 x 4096 x 11008 (725 TFLOP/s), 4-bit activations 500 us for 4096 x 8192 x 28672 (3850 TFLOP/s; LDS is asked for nearly all it can give).
+// Few tokens: bound by the weights' way from memory, of which too little is asked for at a time: a stage is 2 KB of weights for 32 rows and 4 KB of
+// activations, mostly of tokens that are not there.  4096 x 11008 bf16 with one token 7.3 us a call (3.3 TB/s; 7.0 to 8.2 the kernel, 6.4 to 6.6 with 4-bit
+// activations, whose stages are twice as long), 32 tokens 8.0, 8192 x 28672 with one token 22 (5.7 TB/s).
+// Many: by the matrix unit and the waits of two stages, at whose ends all copies have to be in LDS and all waves meet: matrix instructions take 48 % of the
+// cycles (bf16) and 44 (4 bits), waits 28 and 32 % of the waves' time.  4096 tokens x 8192 x 28672 bf16 1420 to 1440 us (1340 TFLOP/s; a large library product of bf16 reaches 1378 on this card), fp16 238 to 268 us
+// for 2048 x 4096 x 11008 (690 to 775 TFLOP/s; five vector instructions scale each block's sum), 4-bit activations 490 to 527 us for 4096 x 8192 x 28672 (3650
+// to 3930 TFLOP/s).
 template <int ACT, int RT, int MT, int WN, int WM, int KG, int BUFFERS>
 __global__ void __launch_bounds__(64 * WN * WM * KG, RT * MT > 32 ? 1 : 2) product_tile_kernel(Product a)
 {
@@ -424,7 +427,8 @@ using namespace enec::lowbit;
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 // The tiles there are.  `resident` workgroups of one fit a compute unit (by LDS), and with all of them there a round of stages, `stages` of them, takes
-// `us` (measured: 1 to 4096 tokens with matrices of 4096 x 1024 to 8192 x 28672).
+// `us` (fitted to times of 1 to 4096 tokens with matrices of 4096 x 1024 to 8192 x 28672, as are the constants of plan_of; of 104 products over 12 us, with
+// every tile and split forced, the choice is within 5 % of the best for 82, within 10 % for 93, and a third off for the worst).
 struct Shape {
     uint32_t rows, tokens, resident, stages;
     double us;
@@ -467,8 +471,8 @@ Plan plan_of(uint32_t m, uint32_t n, uint32_t k, int act)
         for (uint32_t splits = 1; splits == 1 || (splittable && splits <= MOST_SPLITS && splits * UNIT <= stages && tiles * (splits / 2) < full); splits *= 2) {
             const uint32_t each = up(up(stages, splits), UNIT) * UNIT, count = up(stages, each);
             // The busiest compute unit has `most` workgroups.  Fewer than fit take their share of the time and some more; where one fits and not all
-            // units have one, memory has less to do; past that the units drift apart, and half of the last round's waste goes.  A workgroup's start and end are 3 us,
-            // and joining is a launch, the sums' way out and back.
+            // units have one, memory has less to do; past that the units drift apart, and half of the last round's waste goes.  A workgroup's start and end are
+            // 3 us, and joining is a launch, the sums' way out and back.
             const uint64_t all = tiles * count, most = (all + UNITS - 1) / UNITS, left = most % s.resident;
             double turns = (double)(most / s.resident) + (left ? (double)left / s.resident + (s.resident - left) * THIN[mx4 ? 2 : act] : 0);
             if (s.resident == 1 && all * 4 < most * UNITS * 3) turns *= 0.88;

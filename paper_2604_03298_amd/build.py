@@ -7,7 +7,8 @@ The host code (csrc/enec_api.hip, csrc/enec_pipeline.hip), the compression kerne
 (csrc/enec_per_block.hip, its fp32 kernels with deferred stores apart) and for tensors of one block (csrc/enec_single.hip), the
 decompression kernels (csrc/enec_decompress.hip, those for one stream apart) and the eighteen tables of compression kernels
 (csrc/enec_kernels.hip, once per element format, group length and kind of block size) are compiled side by side into
-_build/*.o and linked into libenec.so, and so are the low-bit kernels with their host code (csrc/lowbit_*.hip).
+_build/*.o and linked into libenec.so, and so are the low-bit kernels with their host code (csrc/lowbit_*.hip) and the draw of
+tokens (csrc/sampling.hip).
 """
 from __future__ import annotations
 
@@ -24,11 +25,13 @@ OBJ = os.path.join(HERE, "_build")
 SOURCES = [os.path.join(CSRC, "enec_api.hip"), os.path.join(CSRC, "enec_kernels.hip"),
            os.path.join(CSRC, "enec_per_block.hip"), os.path.join(CSRC, "enec_pipeline.hip"),
            os.path.join(CSRC, "enec_decompress.hip"), os.path.join(CSRC, "enec_single.hip")]
-LOWBIT = [os.path.join(CSRC, f"lowbit_{name}.hip") for name in ("mx4", "matmul", "cache", "attention")]
+LOWBIT = [os.path.join(CSRC, f"lowbit_{name}.hip") for name in ("mx4", "matmul", "cache", "attention", "fp8", "fp8_matmul")]
+SAMPLING = os.path.join(CSRC, "sampling.hip")
 HEADERS = [os.path.join(CSRC, "enec_device.hpp"), os.path.join(CSRC, "enec_kernels.hpp"),
            os.path.join(CSRC, "enec_per_block.hpp"), os.path.join(CSRC, "enec_decompress.hpp"),
            os.path.join(CSRC, "enec_single.hpp"), os.path.join(CSRC, "lowbit.hpp"), os.path.join(CSRC, "lowbit_pages.hpp"),
-           os.path.join(ROOT, "include", "enec_lowbit.h"),
+           os.path.join(CSRC, "lowbit_product.hpp"), os.path.join(CSRC, "lowbit_fp8.hpp"),
+           os.path.join(ROOT, "include", "enec_lowbit.h"), os.path.join(ROOT, "include", "enec_sampling.h"),
            os.path.join(ROOT, "include", "enec.h")]
 FLAGS = ["-O3", "-std=c++17", "--offload-arch=gfx950",
          "-Xclang", "-target-feature", "-Xclang", "-packed-fp32-ops", "-ffp-contract=off",
@@ -43,7 +46,7 @@ def _units():
              ("enec_per_block_fp32.o", ["-DENEC_FP32=1", SOURCES[2]]),
              ("enec_pipeline.o", [SOURCES[3]]), ("enec_single.o", [SOURCES[5]]),
              ("enec_decompress.o", ["-DENEC_ONE=0", SOURCES[4]]), ("enec_decompress_one.o", ["-DENEC_ONE=1", SOURCES[4]])]
-    units += [(os.path.basename(path)[:-4] + ".o", [path]) for path in LOWBIT]
+    units += [(os.path.basename(path)[:-4] + ".o", [path]) for path in LOWBIT + [SAMPLING]]
     for lpg in (2, 1, 4):           # lanes per group: group lengths 16, 8, 32
         for dt in (0, 2, 1):
             for logb in (14, 0):    # block size: the default one as a constant, any as an argument
@@ -84,7 +87,7 @@ def stale() -> bool:
     if not os.path.exists(LIB):
         return True
     t = os.path.getmtime(LIB)
-    return any(os.path.getmtime(p) > t for p in SOURCES + LOWBIT + HEADERS)
+    return any(os.path.getmtime(p) > t for p in SOURCES + LOWBIT + [SAMPLING] + HEADERS)
 
 
 if __name__ == "__main__":

@@ -92,6 +92,14 @@ __device__ __forceinline__ float power_of(uint32_t byte)
     return f32_of_bits(byte == 255 ? 0x7FC00000u : byte == 0 ? 1u << 22 : byte << 23);
 }
 
+// E4M3 codes: the byte of the smallest power of two 2^e with a <= 448 2^e, a given by its bits, 448 = 1.75 * 2^8: one exponent more where the mantissa is over 1.75.
+// Below 2^-126 the exponent field says 0 where the exponent is smaller still; both give the least scale.
+__device__ __forceinline__ uint32_t scale_byte(uint32_t a)
+{
+    const int32_t e = (int32_t)(a >> 23) - 8 + ((a & 0x7FFFFFu) > 0x600000u ? 1 : 0);
+    return e > 0 ? (uint32_t)e : 0;
+}
+
 // v / d for v < 2^31: (v * mul) >> shift with mul = ceil(2^(31 + s) / d), s = ceil(log2 d); exact, as the error of mul is below d <= 2^s
 struct Divide {
     uint32_t mul, shift, by;

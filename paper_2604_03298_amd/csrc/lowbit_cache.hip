@@ -43,14 +43,6 @@ __device__ __forceinline__ uint32_t finite_bits(float v)
     const uint32_t b = bits_of(v) & 0x7FFFFFFFu;
     return b < 0x7F800000u ? b : 0;
 }
-// the byte of the smallest power of two 2^e with a <= 448 2^e, 448 = 1.75 * 2^8: one exponent more where the mantissa is over 1.75.
-// Below 2^-126 the exponent field says 0 where the exponent is smaller still; both give the least scale.
-__device__ __forceinline__ uint32_t scale_byte(uint32_t a)
-{
-    const int32_t e = (int32_t)(a >> 23) - 8 + ((a & 0x7FFFFFu) > 0x600000u ? 1 : 0);
-    return e > 0 ? (uint32_t)e : 0;
-}
-
 // what an item's workgroup knows of its page
 struct Page {
     uint32_t first, end;        // slots of the page that the call's tokens have
@@ -59,13 +51,13 @@ struct Page {
     const int32_t *entry;       // where its number is; null: it has none
     bool good;
 };
-__device__ __forceinline__ Page page_of_item(const Pages &c, uint32_t item)
+__device__ __forceinline__ Page page_of_item(const Pages &c, uint32_t item, int32_t most = MAX_SEQUENCE)
 {
     const Found f = sequence_of_item(c, item);
     const Sequence &s = f.s;
     Page p{};
     if (f.b < 0) return p;
-    if (!s.good) {
+    if (!s.good || s.length > most) {
         complain(c);
         return p;
     }
@@ -92,6 +84,60 @@ __device__ __forceinline__ int32_t number_of(const Pages &c, const Page &p)
     return -1;
 }
 
+// Rotation by positions: pairs (j, half + j), or neighbours (2 j, 2 j + 1), of a head's first 2 half values.
+enum { STAY = 0, HALVES = 1, NEIGHBOURS = 2 };
+using f32x4_a8 = f32x4 __attribute__((aligned(8)));
+struct Turns {
+    const float *table;         // positions x half pairs
+    uint32_t half;
+    int32_t positions;
+};
+// cosines and sines of eight pairs from pair j on
+__device__ __forceinline__ void load_turns(const Turns &t, int32_t position, uint32_t j, float (&c)[8], float (&s)[8])
+{
+    const f32x4_a8 *p = reinterpret_cast<const f32x4_a8 *>(t.table + ((size_t)(uint32_t)position * t.half + j) * 2);
+#pragma unroll
+    for (int i = 0; i < 4; ++i) {
+        const f32x4 v = p[i];
+        c[2 * i] = v[0], s[2 * i] = v[1], c[2 * i + 1] = v[2], s[2 * i + 1] = v[3];
+    }
+}
+// eight neighbours: four pairs from pair j on
+__device__ __forceinline__ void turn_neighbours(const Turns &t, int32_t position, uint32_t j, float (&x)[8])
+{
+    const f32x4_a8 *p = reinterpret_cast<const f32x4_a8 *>(t.table + ((size_t)(uint32_t)position * t.half + j) * 2);
+#pragma unroll
+    for (int i = 0; i < 2; ++i) {
+        const f32x4 v = p[i];
+#pragma unroll
+        for (int k = 0; k < 2; ++k) {
+            float &a = x[4 * i + 2 * k], &b = x[4 * i + 2 * k + 1];
+            const float c = v[2 * k], s = v[2 * k + 1], first = a * c - b * s;
+            b = b * c + a * s, a = first;
+        }
+    }
+}
+// the eight values from element i + dim on, of a head that begins at element i
+template <int DT, int ROTATION>
+__device__ __forceinline__ void load8_turned(const void *in, size_t i, uint32_t dim, int32_t position, const Turns &t, float (&x)[8])
+{
+    load8<DT>(in, i + dim, x);
+    if (dim >= 2 * t.half) return;
+    if constexpr (ROTATION == NEIGHBOURS) {
+        turn_neighbours(t, position, dim / 2, x);
+    } else {
+        const bool second = dim >= t.half;
+        float y[8], c[8], s[8];
+        load8<DT>(in, second ? i + dim - t.half : i + dim + t.half, y);
+        load_turns(t, position, second ? dim - t.half : dim, c, s);
+#pragma unroll
+        for (int k = 0; k < 8; ++k) {
+            const float own = x[k] * c[k], other = y[k] * s[k];
+            x[k] = second ? own + other : own - other;
+        }
+    }
+}
+
 // A workgroup has one page of one head, keys or values: it alone knows all tokens that the scale depends on, and nothing is
 // shared between workgroups.  Tiles of 32 values: keys 2 tokens x 16 dimensions, values 16 tokens x 2 dimensions, so that
 // both ways a thread's codes are two runs of 16 bytes; consecutive threads have consecutive dimensions, so that the loads of a
@@ -101,7 +147,7 @@ __device__ __forceinline__ int32_t number_of(const Pages &c, const Page &p)
 // beside the new values, old scale, old codes.  (The last two need not wait for one another: asked for together they would shorten it; before the new values
 // they cost prompts 19 -> 25 us.)  A workgroup has a thread for each tile, 64 to 256.
 // Eight prompts of up to 2047 tokens, 8 heads of 128, fp16, pages of 16: 18.7 us, 14.5 back.  One token for each of 32 sequences, pages of 64: 7.9 us.
-template <int DT, bool V> struct Tile {
+template <int DT, bool V, int ROTATION = STAY> struct Tile {
     uint32_t slot, dim;         // first slot and dimension
     float x[32];
     static constexpr int SLOTS = V ? 16 : 2, DIMS = V ? 2 : 16;
@@ -110,7 +156,7 @@ template <int DT, bool V> struct Tile {
         dim = (t & ((1u << log_dims) - 1)) * DIMS;
         slot = (t >> log_dims) * SLOTS;
     }
-    __device__ __forceinline__ void load(const void *in, size_t token_stride, size_t head, const Page &p)
+    __device__ __forceinline__ void load(const void *in, size_t token_stride, size_t head, const Page &p, const Turns &turns)
     {
 #pragma unroll
         for (int s = 0; s < SLOTS; ++s) {
@@ -123,8 +169,12 @@ template <int DT, bool V> struct Tile {
             } else {
                 float u[16] = {};
                 if (has) {
-                    load8<DT>(in, i, *reinterpret_cast<float(*)[8]>(u));
-                    load8<DT>(in, i + 8, *reinterpret_cast<float(*)[8]>(u + 8));
+#pragma unroll
+                    for (int r = 0; r < 16; r += 8) {
+                        float(&v)[8] = *reinterpret_cast<float(*)[8]>(u + r);
+                        if constexpr (ROTATION == STAY) load8<DT>(in, i + r, v);
+                        else load8_turned<DT, ROTATION>(in, i - dim, dim + r, p.position + (int32_t)(slot + s), turns, v);
+                    }
                 }
 #pragma unroll
                 for (int j = 0; j < 16; ++j) x[16 * s + j] = u[j];
@@ -178,18 +228,18 @@ template <int DT, bool V> struct Tile {
     }
 };
 
-template <int DT, bool V>
+template <int DT, bool V, int ROTATION = STAY>
 __device__ __forceinline__ void write_page(const Pages &c, const Page &p, uint32_t head, const void *in, size_t token_stride, size_t head_stride,
-                                           uint32_t *shared)
+                                           uint32_t *shared, const Turns &turns = Turns{})
 {
     const size_t values = (size_t)c.head_dim << c.log_page;
     const uint32_t log_dims = (uint32_t)__builtin_ctz(c.head_dim / (V ? 2u : 16u)), tiles = (uint32_t)(values / 32);
-    Tile<DT, V> t;
+    Tile<DT, V, ROTATION> t;
     uint32_t a = 0;
     const int32_t number = number_of(c, p);
     for (uint32_t i = threadIdx.x; i < tiles; i += blockDim.x) {
         t.at(i, log_dims);
-        t.load(in, token_stride, head * head_stride, p);
+        if (ROTATION == STAY || p.position >= 0) t.load(in, token_stride, head * head_stride, p, turns);
         const uint32_t b = t.largest();
         a = a > b ? a : b;
     }
@@ -212,7 +262,7 @@ __device__ __forceinline__ void write_page(const Pages &c, const Page &p, uint32
     for (uint32_t i = threadIdx.x; i < tiles; i += blockDim.x) {
         if (tiles > blockDim.x) {
             t.at(i, log_dims);
-            t.load(in, token_stride, head * head_stride, p);
+            t.load(in, token_stride, head * head_stride, p, turns);
         }
         t.store(codes, c.log_page, c.head_dim, p, inverse, move, by);
     }
@@ -231,6 +281,71 @@ __global__ void __launch_bounds__(256) cache_write_kernel(Pages c, NewTokens n)
     if (!p.good) return;
     if (blockIdx.z == 0) write_page<DT, false>(c, p, blockIdx.y, n.k, n.k_token, n.k_head, shared);
     else write_page<DT, true>(c, p, blockIdx.y, n.v, n.v_token, n.v_head, shared);
+}
+
+// Queries of a page's tokens, a few heads to a workgroup.  A thread has a unit: both ends of eight pairs, so that a call may write where it reads, or eight
+// values that stay; or, of neighbours, eight values.
+struct Queries {
+    const void *in;
+    void *out;
+    size_t in_token, in_head, out_token, out_head;
+    uint32_t heads, per_group;              // all, and of those that share a key
+    Divide units;                           // of a head
+};
+constexpr uint32_t QUERY_HEADS = 4;         // of a workgroup
+template <int DT, int ROTATION>
+__device__ __forceinline__ void turn_queries(const Pages &c, const Page &p, const Queries &q, const Turns &turns, uint32_t head, uint32_t heads)
+{
+    const uint32_t count = (p.end - p.first) * q.units.by * heads;
+    for (uint32_t i = threadIdx.x; i < count; i += blockDim.x) {
+        const uint32_t rest = quotient(i, q.units), unit = i - rest * q.units.by;
+        const uint32_t token = rest / heads, h = head + rest - token * heads;
+        const int32_t position = p.position + (int32_t)(p.first + token);
+        const size_t from = (size_t)(p.token + p.first + token) * q.in_token + h * q.in_head, to = (size_t)(p.token + p.first + token) * q.out_token + h * q.out_head;
+        float x[8] = {}, y[8] = {};
+        if constexpr (ROTATION == NEIGHBOURS) {
+            if (position >= 0) {
+                load8<DT>(q.in, from + 8 * unit, x);
+                if (8 * unit < 2 * turns.half) turn_neighbours(turns, position, 4 * unit, x);
+            }
+            store8<DT>(q.out, to + 8 * unit, x);
+        } else {
+            const bool pair = 8 * unit < turns.half;
+            const uint32_t dim = pair ? 8 * unit : 8 * unit + turns.half;
+            if (position >= 0) {
+                load8<DT>(q.in, from + dim, x);
+                if (pair) {
+                    float co[8], si[8];
+                    load8<DT>(q.in, from + dim + turns.half, y);
+                    load_turns(turns, position, dim, co, si);
+#pragma unroll
+                    for (int k = 0; k < 8; ++k) {
+                        const float a = x[k], b = y[k];
+                        x[k] = a * co[k] - b * si[k], y[k] = b * co[k] + a * si[k];
+                    }
+                }
+            }
+            store8<DT>(q.out, to + dim, x);
+            if (pair) store8<DT>(q.out, to + dim + turns.half, y);
+        }
+    }
+}
+
+// Keys, values and queries side by side in one launch: blockIdx.z is 0, 1, or a few of the heads that share key head blockIdx.y.
+template <int DT, int ROTATION>
+__global__ void __launch_bounds__(256) cache_write_rotated_kernel(Pages c, NewTokens n, Queries q, Turns turns)
+{
+    __shared__ uint32_t shared[4];
+    const Page p = page_of_item(c, blockIdx.x, turns.positions);
+    if (!p.good) return;
+    if (blockIdx.z == 0) {
+        write_page<DT, false, ROTATION>(c, p, blockIdx.y, n.k, n.k_token, n.k_head, shared, turns);
+    } else if (blockIdx.z == 1) {
+        write_page<DT, true>(c, p, blockIdx.y, n.v, n.v_token, n.v_head, shared);
+    } else {
+        const uint32_t first = (blockIdx.z - 2) * QUERY_HEADS, left = q.per_group - first;
+        turn_queries<DT, ROTATION>(c, p, q, turns, blockIdx.y * q.per_group + first, left < QUERY_HEADS ? left : QUERY_HEADS);
+    }
 }
 
 // The way back, with the same tiles: two runs of 16 codes in, 32 values out, those of a token side by side over the threads.
@@ -342,6 +457,32 @@ int enec_cache_write(const enec_cache *cache, const enec_cache_batch *batch, con
     const dim3 grid((p.n_tokens >> p.log_page) + 2 * p.batch, p.heads, 2);
     auto kernel = dtype == ENEC_BF16 ? cache_write_kernel<BF16> : cache_write_kernel<FP16>;
     kernel<<<grid, threads_of(p), 0, (hipStream_t)stream>>>(p, NewTokens{k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride});
+    return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
+}
+
+int enec_cache_write_rotated(const enec_cache *cache, const enec_cache_batch *batch, const void *k, size_t k_token_stride, size_t k_head_stride,
+                             const void *v, size_t v_token_stride, size_t v_head_stride, const void *q, size_t q_token_stride, size_t q_head_stride,
+                             void *q_out, size_t q_out_token_stride, size_t q_out_head_stride, uint32_t q_heads, int dtype, const void *turns,
+                             uint32_t positions, uint32_t rotary, int interleaved, void *stream)
+{
+    if (dtype != ENEC_BF16 && dtype != ENEC_FP16) return ENEC_E_DTYPE;
+    Pages p;
+    if (const int rc = pages_of(cache, batch, p)) return rc;
+    if (rotary == 0 || rotary % 16 || rotary > p.head_dim) return ENEC_E_ARG;
+    if (q_heads % p.heads || q_heads / p.heads > 65533 * QUERY_HEADS || (q_heads != 0) != (q != nullptr) || (q_heads != 0) != (q_out != nullptr)) return ENEC_E_ARG;
+    if (q_heads && (((uintptr_t)q | (uintptr_t)q_out) & 1)) return ENEC_E_ARG;
+    // in place a unit's thread has read what it writes; with other strides it would write what another reads
+    if (q_heads && q == q_out && (q_token_stride != q_out_token_stride || q_head_stride != q_out_head_stride)) return ENEC_E_ARG;
+    if (p.batch == 0 || p.n_tokens == 0) return ENEC_OK;
+    if (!k || !v || !turns || (((uintptr_t)k | (uintptr_t)v) & 1) || ((uintptr_t)turns & 7)) return ENEC_E_ARG;
+    const uint32_t group = q_heads / p.heads, units = interleaved ? p.head_dim / 8 : (p.head_dim - rotary / 2) / 8;
+    const dim3 grid((p.n_tokens >> p.log_page) + 2 * p.batch, p.heads, 2 + (group + QUERY_HEADS - 1) / QUERY_HEADS);
+    auto kernel = dtype == ENEC_BF16 ? (interleaved ? cache_write_rotated_kernel<BF16, NEIGHBOURS> : cache_write_rotated_kernel<BF16, HALVES>)
+                                     : (interleaved ? cache_write_rotated_kernel<FP16, NEIGHBOURS> : cache_write_rotated_kernel<FP16, HALVES>);
+    kernel<<<grid, threads_of(p), 0, (hipStream_t)stream>>>(
+        p, NewTokens{k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride},
+        Queries{q, q_out, q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride, q_heads, group, divide_by(units)},
+        Turns{static_cast<const float *>(turns), rotary / 2, positions < (uint32_t)MAX_SEQUENCE ? (int32_t)positions : MAX_SEQUENCE});
     return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
 }
 

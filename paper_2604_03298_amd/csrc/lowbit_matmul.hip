@@ -1,6 +1,6 @@
 // Products with weights in microscaled 4-bit floating point.  The definitions stand in include/enec_lowbit.h.
 #include "enec_lowbit.h"
-#include "lowbit.hpp"
+#include "lowbit_product.hpp"
 
 #include <atomic>
 
@@ -66,38 +66,6 @@ __device__ __forceinline__ float scale_of(uint32_t bytes, int j)
     const uint32_t e = (j < 3 ? bytes << (23 - 8 * j) : bytes >> 1) & 0x7F800000u;
     return f32_of_bits(e > 0x00400000u ? e : 0x00400000u);
 }
-__device__ __forceinline__ void store4(void *y, int dtype, size_t at, uint32_t valid, const f32x4 &v)
-{
-    if (dtype == FP32) {
-        for (uint32_t i = 0; i < 4; ++i)
-            if (i < valid) static_cast<float *>(y)[at + i] = v[i];
-        return;
-    }
-    const u32x2 w = dtype == BF16 ? u32x2{pack2<BF16>(v[0], v[1]), pack2<BF16>(v[2], v[3])} : u32x2{pack2<FP16>(v[0], v[1]), pack2<FP16>(v[2], v[3])};
-    uint16_t *p = static_cast<uint16_t *>(y) + at;
-    if (valid >= 4) {
-        *reinterpret_cast<u32x2_a2 *>(p) = w;
-    } else {
-        for (uint32_t i = 0; i < 4; ++i)
-            if (i < valid) p[i] = (uint16_t)(w[i >> 1] >> (16 * (i & 1)));
-    }
-}
-
-// Memory through a descriptor, whose range the memory unit checks: rows behind a matrix's last one need no branch.  Offsets are 32 bits wide,
-// from a tile's first row.
-using Range = __amdgpu_buffer_rsrc_t;
-__device__ __forceinline__ Range range_of(const void *p, uint32_t bytes)
-{
-    return __builtin_amdgcn_make_buffer_rsrc(const_cast<void *>(p), 0, (int)bytes, 0x00020000);
-}
-// 16 or 4 bytes a lane into LDS, the lanes' side by side
-template <int BYTES> __device__ __forceinline__ void copy_to_lds(Range r, uint32_t at, uint8_t *to)
-{
-    const auto lds = (__attribute__((address_space(3))) void *)to;
-    if constexpr (BYTES == 16) __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds, 16, (int)at, 0, 0, 0);
-    else __builtin_amdgcn_raw_ptr_buffer_load_lds(r, lds, 4, (int)at, 0, 0, 0);
-}
-
 // How a stage lies in LDS.  A row (of weights, or a token's) is a run of chunks of 16 bytes, chunk i at place i ^ turn(row).  A wave reads 16 bytes a lane
 // in four goes of sixteen lanes, lanes {0-3, 12-15, 20-27} the first: rows {0-3, 12-15} of one lane group and rows {4-11} of its neighbour.  Each
 // turn puts such sixteen chunks into the sixteen different places of 256 bytes, so that no bank is asked twice:
@@ -405,18 +373,6 @@ __global__ void __launch_bounds__(256) lay_out_kernel(const uint16_t *__restrict
     out[at] = v;
 }
 
-// The sums of the splits, in their order (none, where there are no columns: zeros).
-__global__ void __launch_bounds__(256) join_kernel(const float *__restrict__ parts, uint32_t splits, uint32_t m, uint32_t n, size_t part_row, Divide per_row,
-                                                   void *y, size_t y_stride, int y_dtype)
-{
-    const uint32_t at = blockIdx.x * 256u + threadIdx.x, token = quotient(at, per_row), r = (at - token * per_row.by) * 4u;
-    if (token >= m) return;
-    const float *p = parts + (size_t)token * part_row + r;
-    f32x4 v = {};
-    for (uint32_t i = 0; i < splits; ++i) v += *reinterpret_cast<const f32x4 *>(p + i * (m * part_row));
-    store4(y, y_dtype, (size_t)token * y_stride + r, n - r, v);
-}
-
 }  // namespace lowbit
 }  // namespace enec
 
@@ -453,8 +409,6 @@ struct Plan {
 };
 constexpr uint32_t MOST_SPLITS = 16, UNIT = 4;      // a split is whole blocks of scales and whole rounds: so many stages, or a multiple
 
-inline uint32_t up(uint32_t v, uint32_t by) { return (v + by - 1) / by; }
-inline size_t part_row(uint32_t n) { return ((size_t)n + 15) / 16 * 16; }
 inline uint32_t stages_of(uint32_t k, int act) { return act == MX4 ? up(up(k, 128), 2) : up(k, 128); }
 
 Plan plan_of(uint32_t m, uint32_t n, uint32_t k, int act)

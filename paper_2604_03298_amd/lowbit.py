@@ -1,7 +1,7 @@
 """Thin Python binding of the low-bit part of libenec's C ABI (include/enec_lowbit.h).
 
-Matrices in microscaled 4-bit floating point with the products that read them, and a paged 8-bit cache with its
-attention.  As in enec.py: argument marshalling only, PyTorch for device memory and streams, status codes returned, no CPU
+Matrices in microscaled 4-bit or blockwise 8-bit floating point with the products that read them, and a paged 8-bit cache with its
+attention and the rotation of positions.  As in enec.py: argument marshalling only, PyTorch for device memory and streams, status codes returned, no CPU
 fallback.  The tensors' shapes, integer types and places are checked here, where C sees pointers only; a wrong one raises ValueError.
 """
 from __future__ import annotations
@@ -13,8 +13,9 @@ from . import enec
 from .enec import BF16, E_ARG, E_BLOCK, E_CAPACITY, E_DTYPE, FP16, FP32, OK, strerror  # noqa: F401
 
 EXPORTS = ["enec_mx4_bytes", "enec_mx4_quantize", "enec_mx4_dequantize", "enec_mx4_linear_workspace", "enec_mx4_linear",
-           "enec_mx4_matmul_workspace", "enec_mx4_matmul", "enec_cache_write", "enec_cache_read", "enec_cache_attention_workspace",
-           "enec_cache_attention"]
+           "enec_mx4_matmul_workspace", "enec_mx4_matmul", "enec_fp8_bytes", "enec_fp8_quantize", "enec_fp8_dequantize",
+           "enec_fp8_linear_workspace", "enec_fp8_linear", "enec_fp8_matmul_workspace", "enec_fp8_matmul", "enec_cache_write",
+           "enec_cache_write_rotated", "enec_cache_read", "enec_cache_attention_workspace", "enec_cache_attention"]
 
 
 class CacheStruct(C.Structure):
@@ -45,7 +46,15 @@ def lib():
                 ("enec_mx4_linear", i, [vp, sz, sz, i, vp, vp, sz, sz, vp, sz, vp, sz, vp]),
                 ("enec_mx4_matmul_workspace", sz, [sz, sz, sz]),
                 ("enec_mx4_matmul", i, [vp, vp, sz, vp, vp, sz, sz, vp, sz, i, vp, sz, vp]),
+                ("enec_fp8_bytes", i, [sz, sz, C.POINTER(sz), C.POINTER(sz)]),
+                ("enec_fp8_quantize", i, [vp, sz, sz, sz, i, vp, vp, vp]),
+                ("enec_fp8_dequantize", i, [vp, vp, sz, sz, vp, sz, i, vp]),
+                ("enec_fp8_linear_workspace", sz, [sz, sz, sz]),
+                ("enec_fp8_linear", i, [vp, sz, sz, i, vp, vp, sz, sz, vp, sz, vp, sz, vp]),
+                ("enec_fp8_matmul_workspace", sz, [sz, sz, sz]),
+                ("enec_fp8_matmul", i, [vp, vp, sz, vp, vp, sz, sz, vp, sz, i, vp, sz, vp]),
                 ("enec_cache_write", i, [cache, batch, vp, sz, sz, vp, sz, sz, i, vp]),
+                ("enec_cache_write_rotated", i, [cache, batch, vp, sz, sz, vp, sz, sz, vp, sz, sz, vp, sz, sz, u32, i, vp, u32, u32, i, vp]),
                 ("enec_cache_read", i, [cache, batch, vp, sz, sz, vp, sz, sz, i, vp]),
                 ("enec_cache_attention_workspace", sz, [cache, u32, u32, u32, u32, u32]),
                 ("enec_cache_attention", i, [cache, batch, vp, sz, sz, vp, sz, sz, i, u32, u32, u32, C.c_float, vp, sz, vp])):
@@ -191,6 +200,97 @@ def mx4_matmul(x_codes, x_scales, codes, scales, out, workspace=None, stream=Non
                                  y_stride, _dtype(out), ws, size, enec._stream_handle(stream))
 
 
+# ---- matrices in 8 bits -------------------------------------------------------------
+def fp8_bytes(rows: int, cols: int) -> tuple:
+    """(bytes of the codes, bytes of the scales) of a rows x cols matrix."""
+    codes, scales = C.c_size_t(0), C.c_size_t(0)
+    enec._check(lib().enec_fp8_bytes(rows, cols, C.byref(codes), C.byref(scales)), "enec_fp8_bytes")
+    return codes.value, scales.value
+
+
+def fp8_empty(rows: int, cols: int, device="cuda") -> tuple:
+    """Tensors for a rows x cols matrix: codes (rows, padded) and scales (rows, padded / 128 up to a multiple of 4), padded = cols up to a
+    multiple of 128."""
+    import torch
+    padded = -(-cols // 128) * 128
+    return (torch.empty(rows, padded, dtype=torch.uint8, device=device), torch.empty(rows, -(-padded // 512) * 4, dtype=torch.uint8, device=device))
+
+
+def _fp8(codes, scales, what):
+    """(rows, padded columns) of a matrix in 8 bits."""
+    rows, padded = codes.shape
+    n, blocks = scales.shape
+    if padded & 127 or blocks != (padded + 511) // 512 * 4 or n != rows or codes.itemsize != 1 or scales.itemsize != 1 \
+            or not codes.is_contiguous() or not scales.is_contiguous():
+        raise ValueError(f"{what}: codes (rows, padded) and scales (rows, padded / 128 up to a multiple of 4) of bytes without gaps are wanted, "
+                         "padded a multiple of 128")
+    return rows, padded
+
+
+def fp8_quantize(src, codes, scales, stream=None) -> int:
+    """Enqueues enec_fp8_quantize.  src: (rows, cols) of bf16, fp16 or fp32; codes, scales: see fp8_empty."""
+    rows, cols, stride = _rows(src, "src")
+    n, padded = _fp8(codes, scales, "codes")
+    _same_padding(padded, cols)
+    if n != rows:
+        raise ValueError("src and codes differ in their rows")
+    if not src.get_device() == codes.get_device() == scales.get_device() >= 0:
+        _on_gpu(src, codes, scales)
+    return lib().enec_fp8_quantize(src.data_ptr(), rows, cols, stride, _dtype(src), codes.data_ptr(), scales.data_ptr(),
+                                   enec._stream_handle(stream))
+
+
+def fp8_dequantize(codes, scales, out, stream=None) -> int:
+    """Enqueues enec_fp8_dequantize.  out: (rows, cols) of bf16, fp16 or fp32."""
+    rows, cols, stride = _rows(out, "out")
+    n, padded = _fp8(codes, scales, "codes")
+    _same_padding(padded, cols)
+    if n != rows:
+        raise ValueError("out and codes differ in their rows")
+    if not codes.get_device() == scales.get_device() == out.get_device() >= 0:
+        _on_gpu(codes, scales, out)
+    return lib().enec_fp8_dequantize(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), stride, _dtype(out),
+                                     enec._stream_handle(stream))
+
+
+def fp8_linear_workspace(m: int, n: int, k: int) -> int:
+    return int(lib().enec_fp8_linear_workspace(m, n, k))
+
+
+def fp8_linear(x, codes, scales, out, workspace=None, stream=None) -> int:
+    """Enqueues enec_fp8_linear: out (m, n) = x (m, k) w^T, x and out bf16 or fp16, x brought into 8 bits, w (n, k) in 8 bits."""
+    m, k, x_stride = _rows(x, "x")
+    n, padded = _fp8(codes, scales, "codes")
+    _same_padding(padded, k)
+    rows, cols, y_stride = _rows(out, "out")
+    if (rows, cols) != (m, n) or out.dtype != x.dtype:
+        raise ValueError(f"out: ({m}, {n}) of x's format is wanted")
+    if not x.get_device() == codes.get_device() == scales.get_device() == out.get_device() == (x if workspace is None else workspace).get_device() >= 0:
+        _on_gpu(x, codes, scales, out, workspace)
+    ws, size = _space(workspace)
+    return lib().enec_fp8_linear(x.data_ptr(), m, x_stride, _dtype(x), codes.data_ptr(), scales.data_ptr(), n, k, out.data_ptr(), y_stride,
+                                 ws, size, enec._stream_handle(stream))
+
+
+def fp8_matmul_workspace(m: int, n: int, k: int) -> int:
+    return int(lib().enec_fp8_matmul_workspace(m, n, k))
+
+
+def fp8_matmul(x_codes, x_scales, codes, scales, out, workspace=None, stream=None) -> int:
+    """Enqueues enec_fp8_matmul: out (m, n) = x w^T with both in 8 bits; out bf16, fp16 or fp32."""
+    m, padded = _fp8(x_codes, x_scales, "x_codes")
+    n, other = _fp8(codes, scales, "codes")
+    rows, cols, y_stride = _rows(out, "out")
+    if padded != other or (rows, cols) != (m, n):
+        raise ValueError(f"matrices of as many columns and out ({m}, {n}) are wanted")
+    if not x_codes.get_device() == x_scales.get_device() == codes.get_device() == scales.get_device() == out.get_device() \
+            == (out if workspace is None else workspace).get_device() >= 0:
+        _on_gpu(x_codes, x_scales, codes, scales, out, workspace)
+    ws, size = _space(workspace)
+    return lib().enec_fp8_matmul(x_codes.data_ptr(), x_scales.data_ptr(), m, codes.data_ptr(), scales.data_ptr(), n, padded, out.data_ptr(),
+                                 y_stride, _dtype(out), ws, size, enec._stream_handle(stream))
+
+
 # ---- the cache ----------------------------------------------------------------------
 class Cache:
     """Device tensors of a paged cache: k_codes (pages, heads, page_tokens, head_dim) and v_codes (pages, heads, head_dim, page_tokens) of
@@ -267,6 +367,31 @@ def cache_write(cache, k, v, table, starts, lengths, status=None, stream=None) -
     tokens, kt, kh, vt, vh = _tokens(k, v, cache.heads, cache.head_dim, "k and v")
     b = _batch(cache, k, v, table, starts, lengths, tokens, status)
     return lib().enec_cache_write(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, _dtype(k), enec._stream_handle(stream))
+
+
+def cache_write_rotated(cache, k, v, q, q_out, turns, table, starts, lengths, interleaved: bool = False, status=None, stream=None) -> int:
+    """Enqueues enec_cache_write_rotated: cache_write with keys rotated by their positions, and q (tokens, q_heads, head_dim) into q_out.  q and
+    q_out may be one tensor, or None: keys only.  turns: (positions, rotary / 2, 2) of fp32, cosines and sines."""
+    import torch
+    tokens, kt, kh, vt, vh = _tokens(k, v, cache.heads, cache.head_dim, "k and v")
+    if len(turns.shape) != 3 or turns.shape[2] != 2 or turns.dtype is not torch.float32 or not turns.is_contiguous():
+        raise ValueError("turns: (positions, rotary / 2, 2) of fp32 without gaps are wanted")
+    if (q is None) != (q_out is None):
+        raise ValueError("q and q_out, or neither, are wanted")
+    heads, queries = 0, (None, 0, 0, None, 0, 0)
+    if q is not None:
+        if len(q.shape) != 3 or q.shape[0] != tokens or q.dtype != k.dtype:
+            raise ValueError("q: as many tokens as k has, of its format, are wanted")
+        heads = q.shape[1]
+        _, qt, qh, ot, oh = _tokens(q, q_out, heads, cache.head_dim, "q and q_out")
+        queries = (q.data_ptr(), qt, qh, q_out.data_ptr(), ot, oh)
+        if not q.get_device() == q_out.get_device() == cache.device:
+            _on_gpu(cache.tensors[0], q, q_out)
+    if turns.get_device() != cache.device:
+        _on_gpu(cache.tensors[0], turns)
+    b = _batch(cache, k, v, table, starts, lengths, tokens, status)
+    return lib().enec_cache_write_rotated(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, *queries, heads, _dtype(k), turns.data_ptr(),
+                                          turns.shape[0], 2 * turns.shape[1], int(interleaved), enec._stream_handle(stream))
 
 
 def cache_read(cache, k, v, table, starts, lengths, status=None, stream=None) -> int:

@@ -7,18 +7,55 @@ namespace sampling {
 
 using namespace lowbit;
 
-constexpr uint32_t THREADS = 1024, WAVES = THREADS / 64, VEC = 8, CHUNK = THREADS * VEC;
-constexpr uint32_t MAX_VOCAB = 1u << 22;
-constexpr uint32_t BINS = 2048;
+// The order of a row is never made.  Three launches, the first two with a workgroup for each part of a row, the last with one for each row:
+//   1. survey: each part's largest logit, and a histogram of its logits in bins that ascend with them.  Logits well over the others are counted all, of the
+//      others one in four, as atomics on LDS are what this launch would spend its time on;
+//   2. weigh: the histogram says about where a cut lies, and how far off that may be.  Weights of logits above are summed in 64 bits and their tokens counted, and
+//      the tokens in between, some hundred, are listed;
+//   3. draw: the cuts are picked from the list; then the token is drawn by the kept weights of each run of logits, and of one run's.
+// Where a cut turns out to lie outside the list, or the list is too short (many ties, scales without sense), the third launch finds the cut's key from its highest
+// bits down instead, which takes up to three passes over the row a cut and is always right.
+constexpr uint32_t PART_THREADS = 512, PART_WAVES = PART_THREADS / 64, DRAW_THREADS = 1024, DRAW_WAVES = DRAW_THREADS / 64;
+constexpr uint32_t VEC = 8, PIECE = 64 * VEC, CHUNK = DRAW_THREADS * VEC;
+constexpr uint32_t MAX_VOCAB = 1u << 22, MAX_PARTS = 16, WORKGROUPS = 512;
+constexpr uint32_t FULLY_COUNTED = 16384;               // a vocabulary up to that
+constexpr uint32_t BINS = 4096, DIGITS = 2048, EACH_LISTED = 8, LISTED = EACH_LISTED * DRAW_THREADS, PART_LISTED = 4096;
+
+struct Part {
+    uint32_t key, first;                // its largest logit's, and that logit's index
+    int32_t base;                       // the grid's bin that its histogram begins with; it goes down from there
+    float width;                        // of the row's bins
+    float counted;                      // from this logit on all are counted
+    uint32_t over;                      // tokens over top_k's listed ones
+    uint32_t unused[2];
+    uint64_t low, middle;               // weights over top_p's listed ones, and between those and top_k's
+    uint64_t kept[PART_WAVES];          // of what lies over the list what min_p keeps, of each wave's run
+};
+struct Row {
+    uint32_t listed;
+    float p_high, p_low, k_high, k_low;             // top_p's listed logits, from p_low to below p_high, and top_k's
+    uint32_t unused[3];
+};
+struct Listed {
+    uint32_t key, index;
+};
 
 struct Rows {
     const void *logits;
     size_t stride;
     uint32_t vocab, log_unit;           // weights are multiples of 2^-log_unit
-    enec_sampling how;
+    uint32_t parts, run;                // of a row; logits of a wave's run
+    const float *temperature, *top_p, *min_p, *uniform;
+    const int32_t *top_k;
+    uint32_t has;                       // which of them are there (the others point somewhere that may be read)
     int32_t *tokens;
     float *log_probs;
+    Part *part;
+    Row *rows;
+    Listed *list;
+    uint32_t *bins;
 };
+enum { HAS_TEMPERATURE = 1, HAS_TOP_K = 2, HAS_TOP_P = 4, HAS_MIN_P = 8 };
 
 // Floats order as these whole numbers do; 0 and -0 are one.  No float has 0.
 __device__ __forceinline__ uint32_t key_of(float v)
@@ -30,33 +67,77 @@ __device__ __forceinline__ float value_of(uint32_t key) { return f32_of_bits(key
 constexpr uint32_t LEAST_KEY = 0x007FFFFFu;             // minus infinity's
 constexpr uint32_t INFINITY_KEY = 0xFF800000u;
 
-// this thread's eight logits of a chunk, as keys; 0 behind the row's end
-template <int DT> __device__ __forceinline__ void load_keys(const Rows &a, size_t row, uint32_t chunk, uint32_t (&k)[VEC])
-{
-    const uint32_t first = chunk * CHUNK + threadIdx.x * VEC;
-    const size_t i = row * a.stride + first;
-    if (first + VEC <= a.vocab) {
-        float v[VEC];
-        load8<DT>(a.logits, i, v);
-#pragma unroll
-        for (uint32_t j = 0; j < VEC; ++j) k[j] = key_of(v[j]);
-    } else {
-#pragma unroll
-        for (uint32_t j = 0; j < VEC; ++j) k[j] = first + j < a.vocab ? key_of(load1<DT>(a.logits, i + j)) : 0;
-    }
-}
-
-// Weights as whole numbers: adding 2^(52 - log_unit) to a number up to one leaves its multiple of 2^-log_unit in the low bits, rounded to nearest.
-struct Weights {
-    double largest, inverse, magic;     // the largest logit, 1 / T
-    bool infinite;                      // the largest is
-    __device__ __forceinline__ double value(uint32_t key) const
+// What a row is drawn with.
+struct How {
+    float temperature, top_p, min_p, uniform;
+    uint32_t top_k;                     // 0: all
+    bool good, by_mass;
+    __device__ __forceinline__ How(const Rows &a, size_t row)
     {
-        const double d = ((double)value_of(key) - largest) * inverse;
-        const double w = exp(d < -800.0 ? -800.0 : d);
-        return infinite ? (key == INFINITY_KEY ? 1.0 : 0.0) : key <= LEAST_KEY ? 0.0 : w;
+        const float t = a.temperature[row], p = a.top_p[row], m = a.min_p[row];
+        const int32_t k = a.top_k[row];
+        uniform = a.uniform[row];
+        temperature = a.has & HAS_TEMPERATURE ? t : 1.0f, top_p = a.has & HAS_TOP_P ? p : 1.0f, min_p = a.has & HAS_MIN_P ? m : 0.0f;
+        top_k = a.has & HAS_TOP_K && k > 0 && (uint32_t)k < a.vocab ? (uint32_t)k : 0;
+        good = temperature >= 0.0f && temperature <= 3.4028234663852886e38f && uniform >= 0.0f && uniform < 1.0f && top_p == top_p && min_p == min_p;
+        by_mass = top_p < 1.0f;
     }
-    __device__ __forceinline__ uint64_t whole(double w) const { return __builtin_bit_cast(uint64_t, w + magic) - __builtin_bit_cast(uint64_t, magic); }
+    __device__ __forceinline__ bool greedy() const { return temperature == 0.0f; }
+    __device__ __forceinline__ bool cuts() const { return good && !greedy() && (top_k || by_mass); }
+    __device__ __forceinline__ bool wants_first() const { return greedy() || min_p > 1.0f; }
+};
+
+// A grid of bins over all numbers, ascending with them, of which a row's are those from `base` down.
+struct Grid {
+    float each;                         // 1 / width
+    int32_t base;
+    // the lower end of bin b
+    __device__ __forceinline__ float end(uint32_t b, float width) const { return (float)(((double)base - (double)b) * (double)width); }
+    __device__ __forceinline__ int32_t of(float v) const
+    {
+        return (int32_t)__builtin_amdgcn_fmed3f(__builtin_floorf(v * each), -2147483648.0f, 2147483520.0f);
+    }
+    __device__ __forceinline__ uint32_t bin(float v) const
+    {
+        const uint32_t b = (uint32_t)base - (uint32_t)of(v);
+        return b < BINS - 1 ? b : BINS - 1;
+    }
+};
+
+// exp(d / T) for d <= 0, as 2^n 2^r with |r| <= 1/2, the second by its series, whose twelfth term is below 2^-47.  Adding 1.5 2^52 rounds to a whole number,
+// which then stands in the low bits.  Weights are whole numbers: adding 2^(52 - log_unit) to a number up to one leaves its multiple of 2^-log_unit in
+// the low bits, rounded to nearest.
+constexpr double LN2 = 0.693147180559945309417;
+template <int K> constexpr double TERM = TERM<K - 1> * LN2 / K;
+template <> constexpr double TERM<0> = 1.0;
+template <int K> __device__ __forceinline__ double series(double p, double r)
+{
+    if constexpr (K < 0) return p;
+    else return series<K - 1>(__builtin_fma(p, r, TERM<K>), r);
+}
+struct Weights {
+    double top, scale, magic;           // the largest logit, 1 / (T ln 2)
+    bool infinite;                      // the largest is
+    __device__ __forceinline__ Weights(const Rows &a, const How &how, uint32_t most)
+    {
+        infinite = most == INFINITY_KEY;
+        top = (double)value_of(infinite ? INFINITY_KEY - 1 : most), scale = 1.0 / LN2 / (double)how.temperature;
+        magic = __builtin_bit_cast(double, (uint64_t)(1023 + 52 - a.log_unit) << 52);
+    }
+    __device__ __forceinline__ double value(float v) const
+    {
+        constexpr double WHOLE = 6755399441055744.0, NOTHING = -60.0;          // (2^-60 is rounded to nothing)
+        double t = __builtin_fmax(((double)v - top) * scale, NOTHING);
+        if (infinite) t = v == __builtin_inff() ? 0.0 : NOTHING;
+        const double shifted = t + WHOLE, r = t - (shifted - WHOLE);
+        const double p = series<10>(TERM<11>, r);
+        const uint64_t bits = __builtin_bit_cast(uint64_t, p);
+        const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, shifted) << 20;
+        return __builtin_bit_cast(double, (uint64_t)((uint32_t)(bits >> 32) + n) << 32 | (uint32_t)bits);
+    }
+    // as a whole number, and that on top of a constant, which sums take off in one go
+    __device__ __forceinline__ uint64_t raised(double w) const { return __builtin_bit_cast(uint64_t, w + magic); }
+    __device__ __forceinline__ uint64_t whole(double w) const { return raised(w) - __builtin_bit_cast(uint64_t, magic); }
 };
 
 // The order's elements up to one: keys above `key`, and `key` itself up to index `last`.
@@ -64,68 +145,499 @@ struct Cut {
     uint32_t key, last;
     __device__ __forceinline__ bool keeps(uint32_t k, uint32_t i) const { return k > key || (k == key && i <= last); }
 };
-
-struct Shared {
-    uint64_t mass[BINS];
-    uint32_t count[BINS];
-    uint64_t wave_mass[WAVES];
-    uint32_t wave_a[WAVES], wave_b[WAVES];
-    uint64_t found_mass, found_before;
-    uint32_t found, found_count;
+// min_p's: the first token is kept whatever it says (up to one it keeps all of the largest logit)
+struct Least {
+    double min_p;
+    uint32_t first;
+    __device__ __forceinline__ bool keeps(double w, uint32_t i) const { return w >= min_p || i == first; }
 };
 
-template <class T> __device__ __forceinline__ T wave_sum(T v)
+// eight logits from index `first` on; n of them are there, the others zeros
+template <int DT> __device__ __forceinline__ uint32_t load_chunk(const Rows &a, size_t row, uint32_t first, uint32_t end, float (&v)[VEC])
 {
+    const size_t i = row * a.stride + first;
 #pragma unroll
-    for (int k = 1; k < 64; k *= 2) v += __shfl_xor(v, k);
-    return v;
-}
-// sum over the lanes before this one
-template <class T> __device__ __forceinline__ T wave_before(T v)
-{
-    const uint32_t lane = threadIdx.x & 63;
-    T s = v;
-#pragma unroll
-    for (int k = 1; k < 64; k *= 2) {
-        const T o = __shfl_up(s, k);
-        s += lane >= (uint32_t)k ? o : 0;
+    for (uint32_t j = 0; j < VEC; ++j) v[j] = 0;
+    if (first + VEC <= end) {
+        load8<DT>(a.logits, i, v);
+        return VEC;
     }
-    return s - v;
-}
-// sum over the threads before this one, and over all
-template <class T> __device__ __forceinline__ T block_before(T v, T *waves, T &total)
-{
-    const uint32_t wave = threadIdx.x >> 6;
-    const T before = wave_before(v);
-    __syncthreads();
-    if ((threadIdx.x & 63) == 63) waves[wave] = before + v;
-    __syncthreads();
-    T sum = 0, mine = 0;
+    if (first >= end) return 0;
 #pragma unroll
-    for (uint32_t i = 0; i < WAVES; ++i) {
-        mine = i == wave ? sum : mine;
-        sum += waves[i];
-    }
-    total = sum;
-    return mine + before;
+    for (uint32_t j = 0; j + 1 < VEC; ++j)
+        if (first + j < end) v[j] = load1<DT>(a.logits, i + j);
+    return end - first;
 }
 
-// The index of the `nth` (from 1) token with this key, in ascending order; all of them: the last index.
-template <int DT> __device__ uint32_t index_of_tie(const Rows &a, size_t row, uint32_t key, uint32_t nth, Shared &s)
+// A wave's run of a row: pieces of eight logits a lane, and, in the last run, up to seven that are one a lane.
+template <int DT> struct Run {
+    const Rows &a;
+    size_t row;
+    uint32_t begin, end, rest;
+    bool has_rest;
+    float v0[VEC], rest_value;                              // the first piece
+    __device__ __forceinline__ Run(const Rows &rows, size_t r, uint32_t run) : a(rows), row(r), v0{}, rest_value(0)
+    {
+        const uint32_t lane = threadIdx.x & 63, whole = a.vocab / VEC * VEC;
+        begin = run * a.run, end = begin + a.run < whole ? begin + a.run : whole;
+        if (begin + lane * VEC < end) load8<DT>(a.logits, row * a.stride + begin + lane * VEC, v0);
+        rest = whole + lane;
+        has_rest = run == whole / a.run && rest < a.vocab;
+        if (has_rest) rest_value = load1<DT>(a.logits, row * a.stride + rest);
+    }
+    // f(eight logits, index of the first) for every piece; its logits are asked for before those of the piece before are used
+    template <class F> __device__ __forceinline__ void pieces(F &&f) const
+    {
+        float v[VEC], next[VEC];
+#pragma unroll
+        for (uint32_t j = 0; j < VEC; ++j) v[j] = next[j] = v0[j];
+#pragma unroll 1
+        for (uint32_t first = begin + (threadIdx.x & 63) * VEC; first < end; first += PIECE) {
+            if (first + PIECE < end) load8<DT>(a.logits, row * a.stride + first + PIECE, next);
+            f(v, first);
+#pragma unroll
+            for (uint32_t j = 0; j < VEC; ++j) v[j] = next[j];
+        }
+    }
+    // f(logit, index, number in its piece) for every token.  Says how many a lane had.
+    template <class F> __device__ __forceinline__ uint32_t each(F &&f) const
+    {
+        uint32_t n = has_rest ? 1 : 0;
+        pieces([&](const float (&v)[VEC], uint32_t first) {
+#pragma unroll
+            for (uint32_t j = 0; j < VEC; ++j) f(v[j], first + j, j);
+            n += VEC;
+        });
+        if (has_rest) f(rest_value, rest, 1u);
+        return n;
+    }
+};
+
+// A value of another lane: 32 or 64 bits by lane moves.  Lanes that have no such neighbour, or whose rows are not in ROWS, get `none`.
+template <int CONTROL, int ROWS, class T> __device__ __forceinline__ T moved(T v, T none)
 {
-    const uint32_t chunks = (a.vocab + CHUNK - 1) / CHUNK;
-    for (uint32_t c = 0; c < chunks; ++c) {
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_update_dpp(__builtin_bit_cast(int, none), __builtin_bit_cast(int, v), CONTROL, ROWS, 15, false));
+    } else {
+        const uint64_t a = __builtin_bit_cast(uint64_t, v), b = __builtin_bit_cast(uint64_t, none);
+        const uint32_t low = moved<CONTROL, ROWS>((uint32_t)a, (uint32_t)b), high = moved<CONTROL, ROWS>((uint32_t)(a >> 32), (uint32_t)(b >> 32));
+        return __builtin_bit_cast(T, (uint64_t)high << 32 | low);
+    }
+}
+template <class T> __device__ __forceinline__ T of_lane(T v, uint32_t lane)
+{
+    if constexpr (sizeof(T) == 4) {
+        return __builtin_bit_cast(T, __builtin_amdgcn_readlane(__builtin_bit_cast(int, v), (int)lane));
+    } else {
+        const uint64_t a = __builtin_bit_cast(uint64_t, v);
+        return __builtin_bit_cast(T, (uint64_t)of_lane((uint32_t)(a >> 32), lane) << 32 | of_lane((uint32_t)a, lane));
+    }
+}
+// f over the lanes up to this one, in six steps: 1, 2, 4 and 8 to the right in each row of sixteen, a row's last to the next row, the second row's last to the upper half
+template <class T, class F> __device__ __forceinline__ T wave_scan(T v, T none, F &&f)
+{
+    v = f(v, moved<0x111, 15>(v, none));
+    v = f(v, moved<0x112, 15>(v, none));
+    v = f(v, moved<0x114, 15>(v, none));
+    v = f(v, moved<0x118, 15>(v, none));
+    v = f(v, moved<0x142, 10>(v, none));
+    return f(v, moved<0x143, 12>(v, none));
+}
+template <class T> __device__ __forceinline__ T wave_up_to(T v)
+{
+    return wave_scan(v, (T)0, [](T x, T y) { return x + y; });
+}
+template <class T> __device__ __forceinline__ T wave_sum(T v) { return of_lane(wave_up_to(v), 63); }
+template <class T> __device__ __forceinline__ T wave_max(T v, T none)
+{
+    return of_lane(wave_scan(v, none, [](T x, T y) { return x > y ? x : y; }), 63);
+}
+template <class T> __device__ __forceinline__ T wave_min(T v, T none)
+{
+    return of_lane(wave_scan(v, none, [](T x, T y) { return x < y ? x : y; }), 63);
+}
+// sum over the threads before this one, and over all; `waves` has sixteen entries
+template <uint32_t WAVES, class T> __device__ __forceinline__ T block_before(T v, T *waves, T &total)
+{
+    static_assert(WAVES <= 16, "a row of lanes");
+    const uint32_t wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), lane = threadIdx.x & 63;
+    const T up_to = wave_up_to(v);
+    __syncthreads();
+    if (lane == 63) waves[wave] = up_to;
+    __syncthreads();
+    const T sums = wave_up_to(lane < WAVES ? waves[lane & 15] : (T)0);
+    total = of_lane(sums, WAVES - 1);
+    return (wave ? of_lane(sums, wave - 1) : (T)0) + (up_to - v);
+}
+__device__ __forceinline__ void add(uint64_t &to, uint64_t v) { atomicAdd(reinterpret_cast<unsigned long long *>(&to), (unsigned long long)v); }
+
+// The grid's bins that histograms begin with are whole numbers of a thread's bins, so that one part's are another's moved by whole threads.
+__device__ __forceinline__ int32_t base_over(int32_t bin, int32_t free)
+{
+    const int64_t b = ((int64_t)bin + free + 7) & ~(int64_t)7;
+    return (int32_t)(b < 2147483640 ? b : 2147483640);
+}
+
+// ---- 1 ------------------------------------------------------------------------------
+
+template <int DT> __global__ void __launch_bounds__(PART_THREADS) survey_kernel(Rows a)
+{
+    __shared__ uint32_t count[BINS], first[PART_WAVES];
+    __shared__ float high[PART_WAVES], low[PART_WAVES], begins[PART_WAVES];
+    __shared__ bool nans;
+    const size_t row = blockIdx.x / a.parts;
+    const uint32_t part = blockIdx.x % a.parts, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Run<DT> run(a, row, part * PART_WAVES + wave);
+    const uint32_t sample = a.vocab < PART_THREADS ? threadIdx.x : (uint32_t)((uint64_t)threadIdx.x * a.vocab / PART_THREADS);
+    float some = sample < a.vocab ? load1<DT>(a.logits, row * a.stride + sample) : __builtin_nanf("");
+    const How how(a, row);
+    const bool cuts = how.cuts();
+    constexpr float INF = __builtin_inff();
+    Grid grid{1.0f, 0};
+    float width = 1.0f, counted = -INF;
+    if (threadIdx.x == 0) nans = false;
+    if (cuts) {
+        // The bins' width by the spread of 512 logits of the row: twice that down from the largest, or 24 T, beyond which weights are below 2^-34.  And the largest of
+        // the waves' first pieces, over which a tenth of the bins are left free.
+        some = some > -INF && some < INF ? some : __builtin_nanf("");
+        float h = some, l = some, b = -INF;
+#pragma unroll
+        for (uint32_t j = 0; j < VEC; ++j)
+            if (run.begin + lane * VEC < run.end) b = fmaxf(b, run.v0[j]);
+        if (run.has_rest) b = fmaxf(b, run.rest_value);
+        h = wave_max(h == h ? h : -INF, -INF), l = wave_min(l == l ? l : INF, INF), b = wave_max(b, -INF);
+        if (lane == 0) high[wave] = h, low[wave] = l, begins[wave] = b;
+        for (uint32_t i = threadIdx.x; i < BINS; i += PART_THREADS) count[i] = 0;
+        __syncthreads();
+#pragma unroll
+        for (uint32_t i = 0; i < PART_WAVES; ++i) h = fmaxf(h, high[i]), l = fminf(l, low[i]), b = fmaxf(b, begins[i]);
+        const float spread = h - l > 0.0f ? 2.0f * (h - l) : 16.0f, reach = 24.0f * how.temperature;
+        width = (how.top_k || spread < reach ? spread : reach) / BINS;
+        width = width > 1e-30f ? width < 1e30f ? width : 1e30f : 1e-30f;
+        counted = a.vocab > FULLY_COUNTED ? h - 0.25f * (h - l) : -INF;
+        grid.each = 1.0f / width;
+        grid.base = base_over(grid.of(b), BINS / 10);
+    }
+    float most = -INF;
+    bool nan = false;
+    auto count_one = [&](float v, uint32_t, uint32_t j) {
+        const bool one = v >= counted;
+        // (what lies over the free bins is put right below)
+        if (one || j % 4 == 0) atomicAdd(&count[grid.bin(v)], one ? 1u : 4u);
+    };
+    if (cuts) run.each([&](float v, uint32_t i, uint32_t j) { most = fmaxf(most, v), nan |= v != v, count_one(v, i, j); });
+    else run.each([&](float v, uint32_t, uint32_t) { most = fmaxf(most, v), nan |= v != v; });
+    most = wave_max(most, -INF);
+    __syncthreads();
+    if (lane == 0) high[wave] = most;
+    if (nan) nans = true;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t i = 0; i < PART_WAVES; ++i) most = fmaxf(most, high[i]);
+    if (cuts && grid.of(most) > grid.base) {                // once more, from the largest down
+        grid.base = base_over(grid.of(most), 0);
+        for (uint32_t i = threadIdx.x; i < BINS; i += PART_THREADS) count[i] = 0;
+        __syncthreads();
+        run.each(count_one);
+    }
+    uint32_t at = 0xFFFFFFFFu;
+    if (how.wants_first()) {
+        run.each([&](float v, uint32_t i, uint32_t) { at = v == most && i < at ? i : at; });
+        at = wave_min(at, 0xFFFFFFFFu);
+        if (lane == 0) first[wave] = at;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        if (how.wants_first())
+            for (uint32_t i = 1; i < PART_WAVES; ++i) at = first[i] < at ? first[i] : at;
+        Part &p = a.part[blockIdx.x];
+        p.key = nans ? 0xFFFFFFFFu : key_of(most), p.first = at, p.base = grid.base, p.width = width, p.counted = counted;
+        if (part == 0) a.rows[row].listed = 0;
+    }
+    if (cuts) {
+        u32x4 *to = reinterpret_cast<u32x4 *>(a.bins + (size_t)blockIdx.x * BINS);
+        for (uint32_t i = threadIdx.x; i < BINS / 4; i += PART_THREADS) to[i] = reinterpret_cast<const u32x4 *>(count)[i];
+    }
+}
+
+// What a row's parts say together: the largest logit, its key and its first token, and the row's bins.  Lane p of a wave has part p's.
+struct Top {
+    uint32_t key, first;
+    Grid grid;
+    float width;
+    int32_t base;                       // this lane's part's
+    __device__ __forceinline__ Top(const Rows &a, size_t row)
+    {
+        const uint32_t lane = threadIdx.x & 63;
+        const u32x4 v = *reinterpret_cast<const u32x4 *>(a.part + row * a.parts + (lane < a.parts ? lane : 0));
+        key = v[0], first = v[1], base = (int32_t)v[2];
+        int32_t most = base;
+#pragma unroll
+        for (uint32_t k = 1; k < MAX_PARTS; k *= 2) {
+            const uint32_t o = __shfl_xor(key, k), i = __shfl_xor(first, k);
+            const int32_t b = __shfl_xor(most, k);
+            first = o > key || (o == key && i < first) ? i : first, key = o > key ? o : key, most = b > most ? b : most;
+        }
+        key = __builtin_amdgcn_readfirstlane(key), first = __builtin_amdgcn_readfirstlane(first);
+        width = __builtin_bit_cast(float, __builtin_amdgcn_readfirstlane(v[3]));
+        grid = Grid{1.0f / width, __builtin_amdgcn_readfirstlane(most)};
+    }
+    __device__ __forceinline__ bool good() const { return key > LEAST_KEY && key <= INFINITY_KEY; }
+};
+
+// ---- 2 ------------------------------------------------------------------------------
+
+template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(Rows a)
+{
+    __shared__ uint32_t waves[16], n_listed, reserved, over_sum;
+    __shared__ float waves_f[16], k_mass, k_off;
+    __shared__ uint64_t low_sum, middle_sum;
+    __shared__ uint32_t k_first, k_last, p_first, p_last, p_wide, few;
+    __shared__ Listed list[PART_LISTED];
+    const size_t row = blockIdx.x / a.parts;
+    const uint32_t part = blockIdx.x % a.parts, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
+    const Run<DT> run(a, row, part * PART_WAVES + wave);
+    const Top top(a, row);
+    const float counted = a.part[row * a.parts].counted;
+    const How how(a, row);
+    if (!how.good || how.greedy() || !top.good()) return;
+    const Weights w(a, how, top.key);
+    const Least least{(double)how.min_p, how.min_p > 1.0f ? top.first : 0xFFFFFFFFu};
+    const uint64_t magic = __builtin_bit_cast(uint64_t, w.magic);
+    Part &mine = a.part[blockIdx.x];
+    if (!how.cuts()) {
+        uint64_t kept = 0;
+        uint32_t n;
+        if (how.min_p > 0.0f) {
+            n = run.each([&](float v, uint32_t i, uint32_t) {
+                const double x = w.value(v);
+                kept += w.raised(least.keeps(x, i) ? x : 0.0);
+            });
+        } else {
+            n = run.each([&](float v, uint32_t, uint32_t) { kept += w.raised(w.value(v)); });
+        }
+        kept = wave_sum(kept - n * magic);
+        if (lane == 0) mine.kept[wave] = kept;
+        return;
+    }
+    // Eight bins a thread: the parts' histograms, each as far below this row's as its base; what is below all bins is in the last.
+    constexpr uint32_t EACH = BINS / PART_THREADS;
+    static_assert(EACH == 8, "two vectors of four");
+    uint32_t n[EACH] = {};
+    const uint32_t b0 = threadIdx.x * EACH;
+#pragma unroll 1
+    for (uint32_t p = 0; p < a.parts; p += 4) {
+        u32x4 v[4], u[4];
+        uint32_t shift[4];
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q) {                      // (loads that do not wait for one another)
+            const uint32_t o = p + q < a.parts ? p + q : p;
+            shift[q] = (uint32_t)top.grid.base - (uint32_t)of_lane(top.base, o);
+            const u32x4 *from = reinterpret_cast<const u32x4 *>(a.bins + (row * a.parts + o) * BINS + (shift[q] <= b0 ? b0 - shift[q] : 0));
+            v[q] = from[0], u[q] = from[1];
+            shift[q] = p + q < a.parts ? shift[q] : 0xFFFFFFFFu;
+        }
+#pragma unroll
+        for (uint32_t q = 0; q < 4; ++q)
+#pragma unroll
+            for (uint32_t j = 0; j < 4; ++j) n[j] += shift[q] <= b0 ? v[q][j] : 0, n[4 + j] += shift[q] <= b0 ? u[q][j] : 0;
+    }
+    // Tokens and weights up to each bin, the latter by the bins' middles, and the variance of what one in four was counted of (the last bin has no weight to speak of).
+    const uint32_t exact = a.vocab > FULLY_COUNTED ? top.grid.bin(counted) : BINS;
+    const float cold = 1.0f / how.temperature, step = top.width * cold;
+    const float middle_of_0 = (float)((((double)top.grid.base + 0.5) * (double)top.width - (double)value_of(top.key)) * (double)cold);
+    float e[EACH], e_sum = 0, e_all, v_sum = 0, v_before, v_all, c_sum = 0, c_all;
+    uint32_t n_sum = 0, n_all;
+#pragma unroll
+    for (uint32_t j = 0; j < EACH; ++j) {
+        const float d = middle_of_0 - (float)(b0 + j) * step, each = b0 + j == BINS - 1 ? 0.0f : d > 0.0f ? 1.0f : __expf(d);
+        e[j] = (float)n[j] * each;
+        n_sum += n[j], e_sum += e[j];
+        if (b0 + j >= exact) v_sum += 3.0f * e[j] * each, c_sum += 3.0f * (float)n[j];
+    }
+    if (threadIdx.x == 0) {
+        k_first = k_last = p_first = p_last = p_wide = BINS - 1, few = 0xFFFFFFFFu;
+        n_listed = 0, over_sum = 0, low_sum = middle_sum = 0, k_mass = k_off = 0;
+    }
+    const uint32_t n_before = block_before<PART_WAVES>(n_sum, waves, n_all);
+    const float e_before = block_before<PART_WAVES>(e_sum, waves_f, e_all);
+    if (how.top_k) {
+        // the bins that the cut may lie in: four standard deviations around where it seems to
+        const float wanted = (float)how.top_k, c_before = block_before<PART_WAVES>(c_sum, waves_f, c_all);
+        uint32_t before = n_before;
+        float at = e_before, c = c_before;
+#pragma unroll
+        for (uint32_t j = 0; j < EACH; ++j) {
+            c += b0 + j >= exact ? 3.0f * (float)n[j] : 0.0f;
+            if (before < how.top_k && how.top_k <= before + n[j])
+                k_mass = at + e[j] * ((wanted - (float)before) / (float)n[j]), k_off = 4.0f * __builtin_sqrtf(c);
+            before += n[j], at += e[j];
+        }
+        __syncthreads();
+        const float off = k_off;
+        float sum = (float)n_before;
+#pragma unroll
+        for (uint32_t j = 0; j < EACH; ++j) {
+            const float next = sum + (float)n[j];
+            if (sum < wanted - off && wanted - off <= next) k_first = b0 + j;
+            if (sum < wanted + off && wanted + off <= next) k_last = b0 + j;
+            sum = next;
+        }
+        if (threadIdx.x == 0 && wanted - off <= 0.0f) k_first = 0;
+        e_all = k_mass > 0.0f ? k_mass : e_all;
+    }
+    if (how.by_mass) {
+        // The same.  A share p of the sum of all is passed as early as what lies above is estimated too high and what lies below too low: p^2 and (1 - p)^2 of
+        // their variances.  And half a bin's width for the estimate by middles, by far less where many tokens share in it.
+        v_before = block_before<PART_WAVES>(v_sum, waves_f, v_all);
+        const float p = how.top_p > 1e-6f ? how.top_p : 1e-6f, target = p * e_all;
+        if (e_before < target && target <= e_before + e_sum) k_off = v_before + v_sum;
+        __syncthreads();
+        const float off = 4.0f * __builtin_sqrtf((1.0f - p) * (1.0f - p) * k_off + p * p * (v_all - k_off > 0.0f ? v_all - k_off : 0.0f)), width = target * step;
+        float at = e_before;
+#pragma unroll
+        for (uint32_t j = 0; j < EACH; ++j) {
+            const float next = j + 1 < EACH ? at + e[j] : e_before + e_sum;
+            if (at < target + off + width && target + off + width <= next) p_wide = b0 + j;
+            if (at < target - off - width / 16 && target - off - width / 16 <= next) p_first = b0 + j;
+            if (at < target + off + width / 16 && target + off + width / 16 <= next) p_last = b0 + j;
+            at = next;
+        }
+        if (threadIdx.x == 0 && target - off - width / 16 <= 0.0f) p_first = 0;
+    }
+    __syncthreads();
+    // The listed logits: all down to the cut where those are few; else what lies around the cuts.
+    const float INF = __builtin_inff();
+    const uint32_t down_to = how.top_k ? k_last : p_wide;
+    uint32_t before = n_before;
+#pragma unroll
+    for (uint32_t j = 0; j < EACH; ++j) {
+        before += n[j];
+        if (b0 + j == (down_to + 1 < BINS ? down_to + 1 : down_to)) few = before;
+    }
+    __syncthreads();
+    const bool all = few <= LISTED - LISTED / 8;
+    auto high_end = [&](uint32_t b) { return b < 2 ? INF : top.grid.end(b - 2, top.width); };
+    auto low_end = [&](uint32_t b) { return b + 2 < BINS ? top.grid.end(b + 1, top.width) : -INF; };
+    const float k_low = how.top_k ? low_end(k_last) : -INF, k_high = !how.top_k ? -INF : all ? INF : high_end(k_first);
+    const float p_low = !how.by_mass ? INF : all ? (how.top_k ? k_low : low_end(p_wide)) : low_end(p_last);
+    // (no lower than top_k's, so that all listed logits are below what is weighed)
+    const float p_high = all ? INF : how.by_mass ? fmaxf(high_end(p_first), k_high) : k_high;
+    // What is over top_p's list is weighed, and so is what lies between it and top_k's; without top_p, what is over top_k's.
+    uint64_t low = 0, kept = 0, all_weights = 0;
+    uint32_t over = 0, weighed = 0;
+    const bool some_kept = how.min_p > 0.0f;
+    auto listed = [&](float v) { return v >= k_low && ((v >= p_low && v < p_high) || (how.top_k && v < k_high)); };
+    auto weigh = [&](float v, uint32_t i, bool there) {
+        const double x = there ? w.value(v) : 0.0, first = v >= p_high ? x : 0.0;
+        all_weights += w.raised(x), low += w.raised(first);
+        if (some_kept) kept += w.raised(least.keeps(first, i) ? first : 0.0);
+        if (how.top_k) over += v >= k_high;
+    };
+    run.pieces([&](const float (&v)[VEC], uint32_t first) {
+        uint32_t in = 0;
+        bool any = false;
+#pragma unroll
+        for (uint32_t j = 0; j < VEC; ++j) any |= v[j] >= k_low;
+        if (!__any(any)) return;                            // (a wave of tokens behind top_k's cut)
+        weighed += VEC;
+#pragma unroll
+        for (uint32_t j = 0; j < VEC; ++j) {
+            const bool here = listed(v[j]);
+            in |= here ? 1u << j : 0;
+            weigh(v[j], first + j, !here && v[j] >= k_low);
+        }
+        if (__any(in != 0)) {
+            // one addition a wave; the lanes' places by the bits of their counts
+            const uint32_t n = (uint32_t)__builtin_popcount(in);
+            uint32_t at = 0, sum = 0;
+#pragma unroll
+            for (uint32_t k = 0; k < 4; ++k) {
+                const uint64_t set = __ballot(n >> k & 1);
+                at += (uint32_t)__builtin_amdgcn_mbcnt_hi((uint32_t)(set >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)set, 0)) << k;
+                sum += (uint32_t)__builtin_popcountll(set) << k;
+            }
+            const uint32_t leader = (uint32_t)__builtin_ctzll(__ballot(1));
+            uint32_t base = 0;
+            if (lane == leader) base = atomicAdd(&n_listed, sum);
+            at += __builtin_amdgcn_readlane(base, leader);
+#pragma unroll
+            for (uint32_t j = 0; j < VEC; ++j) {
+                if (in >> j & 1) {
+                    if (at < PART_LISTED) list[at] = Listed{key_of(v[j]), first + j};
+                    ++at;
+                }
+            }
+        }
+    });
+    if (run.has_rest) {
+        if (listed(run.rest_value)) {
+            const uint32_t at = atomicAdd(&n_listed, 1u);
+            if (at < PART_LISTED) list[at] = Listed{key_of(run.rest_value), run.rest};
+        } else {
+            weigh(run.rest_value, run.rest, run.rest_value >= k_low), ++weighed;
+        }
+    }
+    low -= weighed * magic, all_weights -= weighed * magic, kept -= weighed * magic;
+    kept = wave_sum(some_kept ? kept : low);
+    if (lane == 0) mine.kept[wave] = kept;
+    if (how.by_mass) {
+        low = wave_sum(low);
+        const uint64_t middle = wave_sum(all_weights) - low;
+        if (lane == 0) add(low_sum, low), add(middle_sum, middle);
+    }
+    if (how.top_k) {
+        over = wave_sum(over);
+        if (lane == 0) atomicAdd(&over_sum, over);
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) {
+        mine.low = low_sum, mine.middle = middle_sum, mine.over = over_sum;
+        // (a part whose list is too short makes the row's too long)
+        reserved = n_listed ? atomicAdd(&a.rows[row].listed, n_listed <= PART_LISTED ? n_listed : LISTED + 1) : 0;
+        if (part == 0) {
+            Row &r = a.rows[row];
+            r.p_high = p_high, r.p_low = p_low, r.k_high = k_high, r.k_low = k_low;
+        }
+    }
+    __syncthreads();
+    const uint32_t many = n_listed < PART_LISTED ? n_listed : PART_LISTED;
+    for (uint32_t i = threadIdx.x; i < many; i += PART_THREADS)
+        if (reserved + i < LISTED) a.list[row * LISTED + reserved + i] = list[i];
+}
+
+// ---- 3 ------------------------------------------------------------------------------
+
+constexpr uint32_t FEW = 64;
+struct Shared {
+    uint64_t mass[DIGITS];
+    uint32_t count[DIGITS];
+    uint64_t wave_mass[16], wave_most[DRAW_WAVES], wave_least[DRAW_WAVES];
+    uint32_t wave_count[16];
+    uint64_t run_mass[MAX_PARTS * PART_WAVES];      // kept weights of each wave's run
+    uint64_t few[FEW], few_weight[FEW];
+    uint64_t found_before, found_place;
+    uint32_t found, found_count, n_few;
+};
+
+// The index of the `nth` (from 1) token with this key, in ascending order; all of them: the last index.
+template <int DT> __device__ __forceinline__ uint32_t index_of_tie(const Rows &a, size_t row, uint32_t key, uint32_t nth, Shared &s)
+{
+    for (uint32_t c = 0; c < a.vocab; c += CHUNK) {
+        float v[VEC];
         uint32_t k[VEC], n = 0, total;
-        load_keys<DT>(a, row, c, k);
+        const uint32_t there = load_chunk<DT>(a, row, c + threadIdx.x * VEC, a.vocab, v);
+#pragma unroll
+        for (uint32_t j = 0; j < VEC; ++j) k[j] = j < there ? key_of(v[j]) : 0;
 #pragma unroll
         for (uint32_t j = 0; j < VEC; ++j) n += k[j] == key;
-        const uint32_t before = block_before(n, s.wave_a, total);
+        const uint32_t before = block_before<DRAW_WAVES>(n, s.wave_count, total);
         if (before < nth && nth <= before + n) {
             uint32_t seen = before;
 #pragma unroll
             for (uint32_t j = 0; j < VEC; ++j) {
                 seen += k[j] == key;
-                if (k[j] == key && seen == nth) s.found = c * CHUNK + threadIdx.x * VEC + j;
+                if (k[j] == key && seen == nth) s.found = c + threadIdx.x * VEC + j;
             }
         }
         __syncthreads();
@@ -137,148 +649,260 @@ template <int DT> __device__ uint32_t index_of_tie(const Rows &a, size_t row, ui
 
 // Where the order is cut by a number of tokens (MASS: by a sum of weights): the last token before which there are fewer than `target`, among those that `within` keeps.
 // The key's bits are found from the top, 11 at a time.
-template <int DT, bool MASS> __device__ Cut select(const Rows &a, size_t row, const Weights &w, const Cut &within, uint64_t target, Shared &s)
+template <int DT, bool MASS> __device__ __forceinline__ Cut select(const Rows &a, size_t row, const Weights &w, const Cut &within, uint64_t target, Shared &s)
 {
-    const uint32_t chunks = (a.vocab + CHUNK - 1) / CHUNK;
     uint32_t prefix = 0;
+#pragma unroll 1
     for (int shift = 21; shift >= -1; shift -= 11) {
         const int low = shift < 0 ? 0 : shift, bits = shift < 0 ? 10 : 11;
-        for (uint32_t i = threadIdx.x; i < BINS; i += THREADS) s.count[i] = 0, s.mass[i] = 0;
         __syncthreads();
-        for (uint32_t c = 0; c < chunks; ++c) {
-            uint32_t k[VEC];
-            load_keys<DT>(a, row, c, k);
+        for (uint32_t i = threadIdx.x; i < DIGITS; i += DRAW_THREADS) s.count[i] = 0, s.mass[i] = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (uint32_t c = 0; c < a.vocab; c += CHUNK) {
+            float v[VEC];
+            const uint32_t there = load_chunk<DT>(a, row, c + threadIdx.x * VEC, a.vocab, v);
 #pragma unroll
             for (uint32_t j = 0; j < VEC; ++j) {
-                if (k[j] == 0 || (shift != 21 && (k[j] ^ prefix) >> (low + bits) != 0)) continue;
-                const uint32_t digit = k[j] >> low & ((1u << bits) - 1);
+                const uint32_t k = key_of(v[j]);
+                if (j >= there || (shift != 21 && (k ^ prefix) >> (low + bits) != 0)) continue;
+                const uint32_t digit = k >> low & ((1u << bits) - 1);
                 if constexpr (MASS) {
-                    if (!within.keeps(k[j], c * CHUNK + threadIdx.x * VEC + j)) continue;
-                    atomicAdd(reinterpret_cast<unsigned long long *>(&s.mass[digit]), (unsigned long long)w.whole(w.value(k[j])));
+                    if (!within.keeps(k, c + threadIdx.x * VEC + j)) continue;
+                    add(s.mass[digit], w.whole(w.value(v[j])));
                 }
                 atomicAdd(&s.count[digit], 1u);
             }
         }
         __syncthreads();
-        // two bins a thread, in descending order
+        // two digits a thread, in descending order
         uint64_t m[2], total;
-        uint32_t bin[2];
+        uint32_t digit[2];
         for (uint32_t j = 0; j < 2; ++j) {
-            bin[j] = BINS - 1 - (2 * threadIdx.x + j);
-            m[j] = MASS ? s.mass[bin[j]] : s.count[bin[j]];
+            digit[j] = DIGITS - 1 - (2 * threadIdx.x + j);
+            m[j] = MASS ? s.mass[digit[j]] : s.count[digit[j]];
         }
-        uint64_t before = block_before<uint64_t>(m[0] + m[1], s.wave_mass, total);
+        uint64_t before = block_before<DRAW_WAVES>(m[0] + m[1], s.wave_mass, total);
         for (uint32_t j = 0; j < 2; ++j) {
-            if (before < target && target <= before + m[j]) s.found = bin[j], s.found_before = before, s.found_count = s.count[bin[j]];
+            if (before < target && target <= before + m[j]) s.found = digit[j], s.found_before = before, s.found_count = s.count[digit[j]];
             before += m[j];
         }
         __syncthreads();
         prefix |= s.found << low;
         target -= s.found_before;
-        __syncthreads();
     }
-    const uint64_t each = MASS ? w.whole(w.value(prefix)) : 1, nth = (target + each - 1) / each;
+    const uint64_t each = MASS ? w.whole(w.value(value_of(prefix))) : 1, nth = (target + each - 1) / each;
     const uint32_t ties = s.found_count;
     __syncthreads();
     return {prefix, nth >= ties ? within.key == prefix ? within.last : a.vocab - 1 : index_of_tie<DT>(a, row, prefix, (uint32_t)nth, s)};
 }
 
-template <int DT> __global__ void __launch_bounds__(THREADS) sample_kernel(Rows a)
+// A token's place in the order as one number, the first of the order having the largest.
+__device__ __forceinline__ uint64_t place_of(uint32_t key, uint32_t index) { return (uint64_t)key << 32 | (0xFFFFFFFFu - index); }
+
+// The same among the listed tokens, EACH_LISTED a thread, of which `target` is at most the sum of the weights (0: not to be cut): bins of the places between the first
+// and the last of them; those of the bin that the cut lies in again, until few are left, which are compared with one another.
+__device__ __forceinline__ Cut select_listed(const uint64_t (&place)[EACH_LISTED], uint64_t (&weight)[EACH_LISTED], uint64_t target, Shared &s)
+{
+    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
+    constexpr uint64_t ALL = ~(uint64_t)0;
+    for (;;) {
+        uint64_t most = 0, least = ALL;
+        uint32_t n = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < EACH_LISTED; ++j) {
+            if (weight[j] == 0) continue;
+            most = place[j] > most ? place[j] : most, least = place[j] < least ? place[j] : least, ++n;
+        }
+        most = wave_max(most, (uint64_t)0), least = wave_min(least, ALL), n = wave_sum(n);
+        __syncthreads();
+        s.mass[threadIdx.x] = 0;
+        if (lane == 0) s.wave_most[wave] = most, s.wave_least[wave] = least, s.wave_count[wave] = n;
+        __syncthreads();
+        const bool there = lane < DRAW_WAVES;
+        most = wave_max(there ? s.wave_most[lane & 15] : 0, (uint64_t)0), least = wave_min(there ? s.wave_least[lane & 15] : ALL, ALL);
+        if (wave_sum(there ? s.wave_count[lane & 15] : 0) <= FEW) break;
+        const uint64_t spread = most - least;
+        const int shift = spread < DRAW_THREADS ? 0 : 54 - __builtin_clzll(spread);         // spread >> shift is below 1024
+#pragma unroll
+        for (uint32_t j = 0; j < EACH_LISTED; ++j)
+            if (weight[j]) add(s.mass[(most - place[j]) >> shift], weight[j]);
+        __syncthreads();
+        uint64_t total;
+        const uint64_t m = s.mass[threadIdx.x], before = block_before<DRAW_WAVES>(m, s.wave_mass, total);
+        if (before < target && target <= before + m) s.found = threadIdx.x, s.found_before = before;
+        __syncthreads();
+        const uint32_t found = s.found;
+        target -= s.found_before;
+#pragma unroll
+        for (uint32_t j = 0; j < EACH_LISTED; ++j) weight[j] = (most - place[j]) >> shift == found ? weight[j] : 0;
+    }
+    __syncthreads();
+    if (threadIdx.x == 0) s.n_few = 0;
+    __syncthreads();
+#pragma unroll
+    for (uint32_t j = 0; j < EACH_LISTED; ++j) {
+        if (weight[j] == 0) continue;
+        const uint32_t at = atomicAdd(&s.n_few, 1u);
+        s.few[at] = place[j], s.few_weight[at] = weight[j];
+    }
+    __syncthreads();
+    if (threadIdx.x < s.n_few) {
+        const uint64_t mine = s.few[threadIdx.x], own = s.few_weight[threadIdx.x];
+        uint64_t sum = 0;
+        for (uint32_t i = 0; i < s.n_few; ++i) sum += s.few[i] > mine ? s.few_weight[i] : 0;
+        if (sum < target && target <= sum + own) s.found_place = mine;
+    }
+    __syncthreads();
+    return {(uint32_t)(s.found_place >> 32), 0xFFFFFFFFu - (uint32_t)s.found_place};
+}
+
+template <int DT> __global__ void __launch_bounds__(DRAW_THREADS) draw_kernel(Rows a)
 {
     __shared__ Shared s;
-    __shared__ uint64_t chunk_mass[MAX_VOCAB / CHUNK];
     const size_t row = blockIdx.x;
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6, chunks = (a.vocab + CHUNK - 1) / CHUNK;
-    const float temperature = a.how.temperature ? a.how.temperature[row] : 1.0f, u = a.how.uniform[row];
-    const float top_p = a.how.top_p ? a.how.top_p[row] : 1.0f, min_p = a.how.min_p ? a.how.min_p[row] : 0.0f;
-    const int32_t top_k = a.how.top_k ? a.how.top_k[row] : 0;
-
-    // the first of the order; a NaN's key lies above infinity's, or below minus infinity's
-    uint32_t best = 0, at = 0;
-    bool nan = false;
-    for (uint32_t c = 0; c < chunks; ++c) {
-        uint32_t k[VEC];
-        load_keys<DT>(a, row, c, k);
-#pragma unroll
-        for (uint32_t j = 0; j < VEC; ++j) {
-            if (k[j] > best) best = k[j], at = c * CHUNK + threadIdx.x * VEC + j;
-            nan |= k[j] > INFINITY_KEY || (k[j] != 0 && k[j] < LEAST_KEY);
-        }
-    }
-    if (nan) best = 0xFFFFFFFFu;
-#pragma unroll
-    for (int k = 1; k < 64; k *= 2) {
-        const uint32_t b = __shfl_xor(best, k), i = __shfl_xor(at, k);
-        if (b > best || (b == best && i < at)) best = b, at = i;
-    }
-    if (lane == 0) s.wave_a[wave] = best, s.wave_b[wave] = at;
-    __syncthreads();
-    for (uint32_t i = 0; i < WAVES; ++i)
-        if (s.wave_a[i] > best || (s.wave_a[i] == best && s.wave_b[i] < at)) best = s.wave_a[i], at = s.wave_b[i];
-    __syncthreads();
-    const bool good = best > LEAST_KEY && best <= INFINITY_KEY && temperature >= 0.0f && temperature <= 3.4028234663852886e38f && u >= 0.0f && u < 1.0f && top_p == top_p &&
-                      min_p == min_p;
-    if (!good || temperature == 0.0f) {
+    const uint32_t runs = a.parts * PART_WAVES;
+    const Top top(a, row);
+    const uint64_t kept = threadIdx.x < runs ? a.part[row * a.parts + threadIdx.x / PART_WAVES].kept[threadIdx.x % PART_WAVES] : 0;
+    const Part &part = a.part[row * a.parts + ((threadIdx.x & 63) < a.parts ? threadIdx.x & 63 : 0)];
+    const bool a_part = (threadIdx.x & 63) < a.parts;         // (lanes behind the parts add nothing)
+    uint64_t low = a_part ? part.low : 0, middle = a_part ? part.middle : 0;
+    uint32_t over = a_part ? part.over : 0;
+    const Row r = a.rows[row];
+    const How how(a, row);
+    const bool good = how.good && top.good();
+    if (!good || how.greedy()) {
         if (threadIdx.x == 0) {
-            a.tokens[row] = good ? (int32_t)at : -1;
+            a.tokens[row] = good ? (int32_t)top.first : -1;
             if (a.log_probs) a.log_probs[row] = good ? 0.0f : __builtin_nanf("");
         }
         return;
     }
-    const Weights w{(double)value_of(best), 1.0 / (double)temperature, __builtin_bit_cast(double, (uint64_t)(1023 + 52 - a.log_unit) << 52), best == INFINITY_KEY};
+    const Weights w(a, how, top.key);
+    const Least least{(double)how.min_p, how.min_p > 1.0f ? top.first : 0xFFFFFFFFu};
+    if (threadIdx.x < runs) s.run_mass[threadIdx.x] = kept;
+    __syncthreads();
     Cut cut{0, a.vocab - 1};
-    if (top_k > 0 && (uint32_t)top_k < a.vocab) cut = select<DT, false>(a, row, w, cut, (uint64_t)top_k, s);
-
-    // the kept weights of each chunk; with top_p first all that top_k leaves
-    uint64_t total = 0;
-    for (int round = top_p < 1.0f ? 0 : 1; round < 2; ++round) {
-        for (uint32_t c = threadIdx.x; c < chunks; c += THREADS) chunk_mass[c] = 0;
-        __syncthreads();
-        for (uint32_t c = 0; c < chunks; ++c) {
-            uint32_t k[VEC];
-            uint64_t m = 0;
-            load_keys<DT>(a, row, c, k);
+    if (how.cuts()) {
+        bool done = r.listed <= LISTED;
+        if (done) {
+            uint64_t place[EACH_LISTED], weight[EACH_LISTED], m[EACH_LISTED];
+            uint32_t kept_too = 0;
+            auto value_at = [&](uint32_t j) { return value_of((uint32_t)(place[j] >> 32)); };
+            auto mine = [&](uint32_t j) { return j * DRAW_THREADS + threadIdx.x < r.listed; };
 #pragma unroll
-            for (uint32_t j = 0; j < VEC; ++j) {
-                const uint32_t i = c * CHUNK + threadIdx.x * VEC + j;
-                if (!cut.keeps(k[j], i)) continue;
-                const double v = w.value(k[j]);
-                if (round == 0 || v >= (double)min_p || i == at) m += w.whole(v);
+            for (uint32_t j = 0; j < EACH_LISTED; ++j) {
+                const uint32_t i = j * DRAW_THREADS + threadIdx.x;
+                const Listed l = i < r.listed ? a.list[row * LISTED + i] : Listed{LEAST_KEY, 0};
+                place[j] = place_of(l.key, l.index), m[j] = 0;
+                if (j * DRAW_THREADS < r.listed) {
+                    const double x = w.value(value_of(l.key));
+                    m[j] = mine(j) ? w.whole(x) : 0, kept_too |= mine(j) && least.keeps(x, l.index) ? 1u << j : 0;
+                }
             }
-            m = wave_sum(m);
-            if (lane == 0 && m) atomicAdd(reinterpret_cast<unsigned long long *>(&chunk_mass[c]), (unsigned long long)m);
+            low = wave_sum(low), middle = wave_sum(middle), over = wave_sum(over);
+            auto keeps = [&](uint32_t j) { return cut.keeps((uint32_t)(place[j] >> 32), 0xFFFFFFFFu - (uint32_t)place[j]); };
+            if (how.top_k) {
+                uint32_t in = 0, all;
+#pragma unroll
+                for (uint32_t j = 0; j < EACH_LISTED; ++j) weight[j] = mine(j) && value_at(j) >= r.k_low && value_at(j) < r.k_high, in += (uint32_t)weight[j];
+                // (a plus infinity is no less than any border: it is over the list, and has been counted there)
+                block_before<DRAW_WAVES>(in, s.wave_count, all);
+                done = over < how.top_k && how.top_k - over <= all;
+                if (done) cut = select_listed(place, weight, how.top_k - over, s);
+            }
+            if (how.by_mass && done) {
+                uint64_t in = 0, others = 0, sum, rest;
+#pragma unroll
+                for (uint32_t j = 0; j < EACH_LISTED; ++j) {
+                    const bool here = value_at(j) >= r.p_low && value_at(j) < r.p_high;
+                    weight[j] = here && keeps(j) ? m[j] : 0;
+                    in += weight[j], others += !here && keeps(j) ? m[j] : 0;
+                }
+                block_before<DRAW_WAVES>(in, s.wave_mass, sum);
+                block_before<DRAW_WAVES>(others, s.wave_mass, rest);
+                const double wanted = __builtin_ceil((double)how.top_p * (double)(low + middle + sum + rest));
+                const uint64_t target = wanted < 1.0 ? 1 : (uint64_t)wanted;
+                done = target > low && target <= low + sum;
+                if (done) cut = select_listed(place, weight, target - low, s);
+            }
+            if (done) {
+#pragma unroll
+                for (uint32_t j = 0; j < EACH_LISTED; ++j)
+                    if (kept_too >> j & 1 && keeps(j)) add(s.run_mass[(0xFFFFFFFFu - (uint32_t)place[j]) / a.run], m[j]);
+            }
         }
-        __syncthreads();
-        total = 0;
-        for (uint32_t c = 0; c < chunks; ++c) total += chunk_mass[c];
-        __syncthreads();
-        if (round == 0) {
-            const double wanted = __builtin_ceil((double)top_p * (double)total);
-            cut = select<DT, true>(a, row, w, cut, wanted < 1.0 ? 1 : (uint64_t)wanted, s);
+        if (__builtin_expect(!done, 0)) {
+            cut = Cut{0, a.vocab - 1};
+            if (how.top_k) cut = select<DT, false>(a, row, w, cut, how.top_k, s);
+            // the kept weights, twice if the second cut needs the first one's
+#pragma unroll 1
+            for (int round = how.by_mass ? 0 : 1; round < 2; ++round) {
+                uint64_t all = 0, total;
+                __syncthreads();
+                if (threadIdx.x < runs) s.run_mass[threadIdx.x] = 0;
+                __syncthreads();
+#pragma unroll 1
+                for (uint32_t c = 0; c < a.vocab; c += CHUNK) {
+                    float v[VEC];
+                    uint64_t sum = 0;
+                    const uint32_t first = c + threadIdx.x * VEC;       // (a wave's 512 logits are of one run)
+                    const uint32_t there = load_chunk<DT>(a, row, first, a.vocab, v);
+#pragma unroll
+                    for (uint32_t j = 0; j < VEC; ++j) {
+                        const double x = w.value(v[j]);
+                        sum += j < there && cut.keeps(key_of(v[j]), first + j) && (round == 0 || least.keeps(x, first + j)) ? w.whole(x) : 0;
+                    }
+                    all += sum;
+                    if (round == 1 && sum) add(s.run_mass[first / a.run], sum);
+                }
+                if (round == 0) {
+                    block_before<DRAW_WAVES>(all, s.wave_mass, total);
+                    const double wanted = __builtin_ceil((double)how.top_p * (double)total);
+                    cut = select<DT, true>(a, row, w, cut, wanted < 1.0 ? 1 : (uint64_t)wanted, s);
+                }
+            }
         }
     }
-    uint64_t left = (uint64_t)((double)u * (double)total);
+    __syncthreads();
+    uint64_t total, all;
+    const uint64_t run_mass = threadIdx.x < runs ? s.run_mass[threadIdx.x] : 0, run_before = block_before<DRAW_WAVES>(run_mass, s.wave_mass, total);
+    uint64_t left = (uint64_t)((double)how.uniform * (double)total);
     left = left < total ? left : total - 1;
-    uint32_t c = 0;
-    while (chunk_mass[c] <= left) left -= chunk_mass[c++];
-    uint32_t k[VEC];
-    uint64_t m[VEC], sum = 0, all;
-    load_keys<DT>(a, row, c, k);
+    if (run_before <= left && left < run_before + run_mass) s.found = threadIdx.x, s.found_before = run_before;
+    __syncthreads();
+    left -= s.found_before;
+    const uint32_t begin = s.found * a.run, end = begin + a.run < a.vocab ? begin + a.run : a.vocab;
+#pragma unroll 1
+    for (uint32_t c = begin; c < end; c += CHUNK) {
+        float v[VEC];
+        uint64_t m[VEC], sum = 0;
+        const uint32_t first = c + threadIdx.x * VEC;
+        const uint32_t there = load_chunk<DT>(a, row, first, end, v);
 #pragma unroll
-    for (uint32_t j = 0; j < VEC; ++j) {
-        const uint32_t i = c * CHUNK + threadIdx.x * VEC + j;
-        const double v = w.value(k[j]);
-        m[j] = cut.keeps(k[j], i) && (v >= (double)min_p || i == at) ? w.whole(v) : 0;
-        sum += m[j];
-    }
-    uint64_t before = block_before<uint64_t>(sum, s.wave_mass, all);
-#pragma unroll
-    for (uint32_t j = 0; j < VEC; ++j) {
-        if (before <= left && left < before + m[j]) {
-            a.tokens[row] = (int32_t)(c * CHUNK + threadIdx.x * VEC + j);
-            if (a.log_probs) a.log_probs[row] = (float)-log1p((double)(total - m[j]) / (double)m[j]);
+        for (uint32_t j = 0; j < VEC; ++j) {
+            const double x = w.value(v[j]);
+            m[j] = j < there && cut.keeps(key_of(v[j]), first + j) && least.keeps(x, first + j) ? w.whole(x) : 0;
+            sum += m[j];
         }
-        before += m[j];
+        uint64_t before = block_before<DRAW_WAVES>(sum, s.wave_mass, all);
+        if (all <= left) {
+            left -= all;
+            continue;
+        }
+        uint64_t mine = 0;
+        uint32_t token = 0;
+#pragma unroll
+        for (uint32_t j = 0; j < VEC; ++j) {
+            const bool here = before <= left && left < before + m[j];
+            mine = here ? m[j] : mine, token = here ? first + j : token;
+            before += m[j];
+        }
+        if (mine) {
+            a.tokens[row] = (int32_t)token;
+            if (a.log_probs) a.log_probs[row] = (float)-log1p((double)(total - mine) / (double)mine);
+        }
+        return;
     }
 }
 
@@ -287,34 +911,65 @@ template <int DT> __global__ void __launch_bounds__(THREADS) sample_kernel(Rows 
 
 using namespace enec::sampling;
 
-static inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+namespace {
+
+inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
+inline bool sizes_ok(size_t rows, size_t vocab) { return vocab != 0 && vocab <= MAX_VOCAB && rows <= (1u << 24); }
+// parts of a row, whole pieces for each wave: enough for the card, and no more than that many beyond one a row
+inline uint32_t part_of(size_t rows, size_t vocab)
+{
+    size_t parts = rows ? WORKGROUPS / rows : 1;
+    parts = parts < 1 ? 1 : parts > MAX_PARTS ? MAX_PARTS : parts;
+    const size_t pieces = (vocab + parts * PART_WAVES * PIECE - 1) / (parts * PART_WAVES * PIECE);
+    return (uint32_t)(pieces * PART_WAVES * PIECE);
+}
+inline size_t most_parts(size_t rows) { return rows * MAX_PARTS < rows + WORKGROUPS ? rows * MAX_PARTS : rows + WORKGROUPS; }
+constexpr size_t PART_BYTES = sizeof(Part) + BINS * 4, ROW_BYTES = sizeof(Row) + LISTED * sizeof(Listed);
+static_assert(sizeof(Part) % 16 == 0 && sizeof(Row) % 16 == 0, "what follows is aligned");
+
+}  // namespace
 
 extern "C" {
 
 size_t enec_sample_workspace(size_t rows, size_t vocab)
 {
-    (void)rows, (void)vocab;
-    return 0;
+    if (!sizes_ok(rows, vocab) || rows == 0) return 0;
+    return most_parts(rows) * PART_BYTES + rows * ROW_BYTES;
 }
 
 int enec_sample(const void *logits, size_t rows, size_t vocab, size_t row_stride, int dtype, const enec_sampling *how, int32_t *tokens, float *log_probs,
                 void *workspace, size_t workspace_bytes, void *stream)
 {
     if (dtype != ENEC_BF16 && dtype != ENEC_FP16 && dtype != ENEC_FP32) return ENEC_E_DTYPE;
-    if (vocab == 0 || vocab > MAX_VOCAB || rows > (1u << 24) || !how) return ENEC_E_ARG;
+    if (!sizes_ok(rows, vocab) || !how) return ENEC_E_ARG;
     if (rows == 0) return ENEC_OK;
     if (!logits || !aligned(logits, dtype == ENEC_FP32 ? 4 : 2) || row_stride < vocab || !tokens || !how->uniform) return ENEC_E_ARG;
     for (const void *p : {(const void *)tokens, (const void *)log_probs, (const void *)how->temperature, (const void *)how->top_k, (const void *)how->top_p,
                           (const void *)how->min_p, (const void *)how->uniform})
         if (!aligned(p, 4)) return ENEC_E_ARG;
     const size_t need = enec_sample_workspace(rows, vocab);
-    if (workspace_bytes < need || (need && !workspace)) return ENEC_E_CAPACITY;
-    if (need && !aligned(workspace, 16)) return ENEC_E_ARG;
+    if (workspace_bytes < need || !workspace) return ENEC_E_CAPACITY;
+    if (!aligned(workspace, 16)) return ENEC_E_ARG;
     uint32_t log_vocab = 0;
     while (((size_t)1 << log_vocab) < vocab) ++log_vocab;
-    const Rows a{logits, row_stride, (uint32_t)vocab, log_vocab > 16 ? 62 - log_vocab : 46, *how, tokens, log_probs};
-    auto kernel = dtype == ENEC_BF16 ? sample_kernel<BF16> : dtype == ENEC_FP16 ? sample_kernel<FP16> : sample_kernel<FP32>;
-    kernel<<<dim3((unsigned)rows), THREADS, 0, (hipStream_t)stream>>>(a);
+    const uint32_t part = part_of(rows, vocab), parts = (uint32_t)((vocab + part - 1) / part);
+    Part *part_at = static_cast<Part *>(workspace);
+    uint32_t *bins = reinterpret_cast<uint32_t *>(part_at + rows * parts);
+    Row *rows_at = reinterpret_cast<Row *>(bins + rows * parts * BINS);
+    const auto there = [&](const void *p) { return p ? p : how->uniform; };
+    const Rows a{logits, row_stride, (uint32_t)vocab, log_vocab > 16 ? 62 - log_vocab : 46, parts, part / PART_WAVES, static_cast<const float *>(there(how->temperature)),
+                 static_cast<const float *>(there(how->top_p)), static_cast<const float *>(there(how->min_p)), how->uniform,
+                 static_cast<const int32_t *>(there(how->top_k)),
+                 (how->temperature ? HAS_TEMPERATURE : 0u) | (how->top_k ? HAS_TOP_K : 0u) | (how->top_p ? HAS_TOP_P : 0u) | (how->min_p ? HAS_MIN_P : 0u), tokens, log_probs,
+                 part_at, rows_at, reinterpret_cast<Listed *>(rows_at + rows), bins};
+    const dim3 all((unsigned)(rows * parts));
+    hipStream_t s = (hipStream_t)stream;
+    auto survey = dtype == ENEC_BF16 ? survey_kernel<BF16> : dtype == ENEC_FP16 ? survey_kernel<FP16> : survey_kernel<FP32>;
+    auto weigh = dtype == ENEC_BF16 ? weigh_kernel<BF16> : dtype == ENEC_FP16 ? weigh_kernel<FP16> : weigh_kernel<FP32>;
+    auto draw = dtype == ENEC_BF16 ? draw_kernel<BF16> : dtype == ENEC_FP16 ? draw_kernel<FP16> : draw_kernel<FP32>;
+    survey<<<all, PART_THREADS, 0, s>>>(a);
+    weigh<<<all, PART_THREADS, 0, s>>>(a);
+    draw<<<dim3((unsigned)rows), DRAW_THREADS, 0, s>>>(a);
     return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
 }
 

@@ -8,12 +8,14 @@
 namespace enec {
 namespace lowbit {
 
+using f32x4_a4 = f32x4 __attribute__((aligned(4)));
+
 struct Product8 {
-    const uint8_t *x, *x_scales, *w, *w_scales;
+    const uint8_t *x, *x_scales, *w, *w_scales;         // (x: 16-bit values, where the kernel brings them into 8 bits)
     void *y;
-    size_t y_stride, part_row;
+    size_t x_stride, y_stride, part_row;                // elements
     float *parts;
-    uint32_t m, n, groups, scale_row;   // groups of 128 columns; bytes between rows of scales
+    uint32_t m, n, k, groups, scale_row;                // groups of 128 columns; bytes between rows of scales
     uint32_t n_tiles, m_tiles, split_stages;
     int y_dtype;
 };
@@ -46,14 +48,14 @@ __device__ __forceinline__ bf16x8 eight_values(const i32x8 &v, int q, int byte)
 // sixteen different places of 256 bytes.  A wave reads the next half stage into registers while it multiplies this one; the only barrier of a stage is between
 // its halves, when all waves have the second half in registers: the stage's buffer is free then, and the next stage has landed.
 template <bool EXACT, int RA, int RB, int WA, int WB, int BUFFERS>
-__global__ void __launch_bounds__(64 * WA * WB, RA * RB > 8 ? 1 : 2) fp8_tile_kernel(Product8 a)
+__global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_kernel(Product8 a)
 {
     constexpr uint32_t THREADS = 64 * WA * WB, ROWS = 32 * RA * WA, TOKENS = 32 * RB * WB, ALL = ROWS + TOKENS, STAGE = ALL * 128;
-    constexpr uint32_t W_COPIES = ROWS * 8 / THREADS, COPIES = ALL * 8 / THREADS;
+    constexpr uint32_t W_COPIES = ROWS * 8 / THREADS, COPIES = ALL * 8 / THREADS, SCALES = (ALL + 63) / 64 * 256;      // (copied by 64)
     static_assert(ROWS * 8 % THREADS == 0 && TOKENS * 8 % THREADS == 0 && THREADS % 128 == 0 && ROWS % 64 == 0, "whole copies of a wave");
-    static_assert(BUFFERS >= 2 && BUFFERS <= 5, "scales land within three stages");
+    static_assert(BUFFERS >= 2 && BUFFERS <= 9, "scales land within seven stages");
     extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
-    uint8_t *scale_bytes = shared + BUFFERS * STAGE;        // of four stages, two in turn: four bytes of each row, then of each token
+    uint8_t *scale_bytes = shared + BUFFERS * STAGE;        // of four stages, three in turn: four bytes of each row, then of each token
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, c = lane & 31;
     const uint32_t wa = wave % WA, wb = wave / WA;
     // Workgroups are dealt out to the eight dies one by one: each die takes a run of tiles, in bands of tiles of tokens (see product_tile_kernel).
@@ -80,7 +82,7 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB > 8 ? 1 : 2) fp8_tile_ke
         for (uint32_t r = 0; r < COPIES; ++r) fetch_one(stage, slot, r);
     };
     auto fetch_scales = [&](uint32_t block) {
-        uint8_t *to = scale_bytes + (block & 1) * (ALL * 4);
+        uint8_t *to = scale_bytes + block % 3 * SCALES;
 #pragma unroll
         for (uint32_t r = 0; r < ALL; r += THREADS) {
             const uint32_t begin = r + wave * 64, row = begin + lane;
@@ -88,6 +90,19 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB > 8 ? 1 : 2) fp8_tile_ke
             if (begin < ROWS) copy_to_lds<4>(w_scales, row * a.scale_row + block * 4, to + begin * 4);
             else copy_to_lds<4>(x_scales, (row - ROWS) * a.scale_row + block * 4, to + begin * 4);
         }
+    };
+
+    // Large tiles have room for one or two stages ahead, which is less than the way from memory takes: a stage's lines are asked for TOUCH stages before its copies, four
+    // bytes each, into LDS that nobody reads, so that the copies find them in the die's cache.  A wave touches 64 rows, a workgroup half of the tile's weights and half of its
+    // tokens; its neighbours, which work on the same rows, touch the others.
+    constexpr uint32_t TOUCH = RA * RB > 8 ? 2 : 0;
+    uint8_t *junk = scale_bytes + 3 * SCALES + wave * 256;
+    const bool alone = band < 2;
+    const uint32_t touched = (alone ? wave * 64 : (wave & 1) * 64 + (wave < 2 ? within % band : within / band) % 2 * 128) + lane;
+    auto touch = [&](uint32_t stage) {
+        const uint32_t there = stage < end ? pitch : 0;
+        const Range of = alone || wave < 2 ? range_of(w, rows * there) : range_of(x, tokens * there);
+        copy_to_lds<4>(of, touched * pitch + stage * 128, junk);
     };
 
     // where this lane's chunks lie: of rows c, 32 + c, ..., half a stage has two of them for a lane
@@ -112,7 +127,7 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB > 8 ? 1 : 2) fp8_tile_ke
         }
     };
     auto read_scales = [&](uint32_t stage, int parity) {
-        const uint8_t *t = scale_bytes + (stage >> 2 & 1) * (ALL * 4) + (stage & 3);
+        const uint8_t *t = scale_bytes + (stage >> 2) % 3 * SCALES + (stage & 3);
 #pragma unroll
         for (int i = 0; i < RA; ++i) ws[parity][i] = t[ws_at + i * 128];
 #pragma unroll
@@ -120,7 +135,7 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB > 8 ? 1 : 2) fp8_tile_ke
     };
     // A wave's copies are counted, and done in the order in which they were issued: with at most AHEAD left, those of the next stage are in LDS.  Then all
     // waves' are, and this stage's second half is in everybody's registers.
-    constexpr int AHEAD = (BUFFERS - 2) * COPIES;
+    constexpr int AHEAD = (BUFFERS - 2) * COPIES + (TOUCH ? BUFFERS - 1 : 0);
     auto meet = [&] {
         __builtin_amdgcn_sched_barrier(0);
         asm volatile("s_waitcnt vmcnt(%0) lgkmcnt(0)\n\ts_barrier" ::"n"(AHEAD) : "memory");
@@ -128,11 +143,14 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB > 8 ? 1 : 2) fp8_tile_ke
     };
 
     f32x16 acc[RA][RB] = {};
-    fetch_scales(first / 4);                                // (a split begins with such a block)
+    fetch_scales(first / 4), fetch_scales(first / 4 + 1);   // (a split begins with such a block)
 #pragma unroll
-    for (int b = 0; b < BUFFERS; ++b) fetch(first + b, b);
+    for (int b = 0; b < BUFFERS; ++b) {
+        fetch(first + b, b);
+        if constexpr (TOUCH != 0) touch(first + BUFFERS + b);
+    }
     __builtin_amdgcn_sched_barrier(0);
-    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((BUFFERS - 1) * COPIES) : "memory");
+    asm volatile("s_waitcnt vmcnt(%0)\n\ts_barrier" ::"n"((BUFFERS - 1) * COPIES + (TOUCH ? BUFFERS : 0)) : "memory");
     __builtin_amdgcn_sched_barrier(0);
 #pragma unroll
     for (int i = 0; i < RA + RB; ++i) read(i, 0, 0);
@@ -145,7 +163,7 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB > 8 ? 1 : 2) fp8_tile_ke
         for (int half = 0; half < 2; ++half) {
             if (half == 1) {
                 meet();
-                if ((s & 3) == 0) fetch_scales(s / 4 + 1);
+                if ((s & 3) == 0) fetch_scales(s / 4 + 2);
                 if constexpr (EXACT) fetch(s + BUFFERS, slot);
                 read_scales(s + 1, parity ^ 1);
             }
@@ -178,6 +196,7 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB > 8 ? 1 : 2) fp8_tile_ke
                     }
                     const int t = i / RB, u = i % RB;
                     acc[t][u] = __builtin_amdgcn_mfma_scale_f32_32x32x64_f8f6f4(wv[half][t], xv[half][u], acc[t][u], 0, 0, 0, ws[parity][t], 0, xs[parity][u]);
+                    if (TOUCH != 0 && half == 1 && i == TILES - 1) touch(s + BUFFERS + TOUCH);
                     __builtin_amdgcn_sched_barrier(0);
                 }
             }
@@ -190,7 +209,42 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB > 8 ? 1 : 2) fp8_tile_ke
         step(s + 1, 1);
     }
     if (s < end) step(s, 0);
-    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (no copy may come after the workgroup)
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (no copy may come after the workgroup, nor into what follows)
+    if (!EXACT && !a.parts) {
+        // 16-bit values by way of LDS, a token's rows side by side there: a lane's four rows of a token would be stores of 8 bytes, 32 tokens apart
+        constexpr uint32_t PITCH = ROWS * 2 + 16, CHUNKS = ROWS / 8;
+        __syncthreads();
+#pragma unroll
+        for (int u = 0; u < RB; ++u)
+#pragma unroll
+            for (int t = 0; t < RA; ++t)
+#pragma unroll
+                for (int e = 0; e < 4; ++e) {
+                    const f32x16 &v = acc[t][u];
+                    const u32x2 w = a.y_dtype == BF16 ? u32x2{pack2<BF16>(v[4 * e], v[4 * e + 1]), pack2<BF16>(v[4 * e + 2], v[4 * e + 3])}
+                                                      : u32x2{pack2<FP16>(v[4 * e], v[4 * e + 1]), pack2<FP16>(v[4 * e + 2], v[4 * e + 3])};
+                    *reinterpret_cast<u32x2 *>(shared + (wb * (32 * RB) + 32 * u + c) * PITCH + (wa * (32 * RA) + 32 * t + 8 * e + 4 * g) * 2) = w;
+                }
+        __syncthreads();
+#pragma unroll 4
+        for (uint32_t i = threadIdx.x; i < TOKENS * CHUNKS; i += THREADS) {
+            const uint32_t token = i / CHUNKS, r = i % CHUNKS * 8;
+            if (token >= tokens || r >= rows) continue;
+            const u32x4 v = *reinterpret_cast<const u32x4 *>(shared + token * PITCH + r * 2);
+            uint16_t *to = static_cast<uint16_t *>(a.y) + (size_t)(m0 + token) * a.y_stride + n0 + r;
+            if (r + 8 <= rows) {
+                *reinterpret_cast<u32x4_a2 *>(to) = v;
+            } else {
+#pragma unroll
+                for (uint32_t j = 0; j < 7; ++j)
+                    if (r + j < rows) to[j] = (uint16_t)(v[j >> 1] >> (16 * (j & 1)));
+            }
+        }
+        return;
+    }
+    // 32-bit values: four rows of a token are 16 bytes
+    float *to = a.parts ? a.parts + (size_t)blockIdx.y * a.m * a.part_row : static_cast<float *>(a.y);
+    const size_t stride = a.parts ? a.part_row : a.y_stride;
 #pragma unroll
     for (int u = 0; u < RB; ++u) {
         const uint32_t token = m0 + wb * (32 * RB) + 32 * u + c;
@@ -200,72 +254,167 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB > 8 ? 1 : 2) fp8_tile_ke
 #pragma unroll
             for (int e = 0; e < 4; ++e) {
                 const uint32_t r = n0 + wa * (32 * RA) + 32 * t + 8 * e + 4 * g;
-                if (r >= a.n) continue;
                 const f32x4 v = {acc[t][u][4 * e], acc[t][u][4 * e + 1], acc[t][u][4 * e + 2], acc[t][u][4 * e + 3]};
-                if (a.parts) *reinterpret_cast<f32x4 *>(a.parts + ((size_t)blockIdx.y * a.m + token) * a.part_row + r) = v;
-                else store4(a.y, a.y_dtype, (size_t)token * a.y_stride + r, a.n - r, v);
+                if (r + 4 <= a.n) {
+                    *reinterpret_cast<f32x4_a4 *>(to + (size_t)token * stride + r) = v;
+                } else {
+#pragma unroll
+                    for (uint32_t j = 0; j < 3; ++j)
+                        if (r + j < a.n) to[(size_t)token * stride + r + j] = v[j];
+                }
             }
         }
     }
 }
 
-// Up to sixteen tokens: bound by the weights' way from memory.  A workgroup has sixteen rows of weights, and its waves take units of 512 columns in turn, straight
-// into registers, the next unit asked for before this one is multiplied; the waves' sums meet in LDS, in their order.
-template <bool EXACT, int WAVES>
-__global__ void __launch_bounds__(64 * WAVES) fp8_thin_kernel(Product8 a)
+// Up to 16 XT tokens: bound by the weights' way from memory.  A workgroup has sixteen rows of weights; its waves take units of four blocks of 128 columns in turn,
+// each through a ring of its own in LDS that the memory unit fills, so that no wave waits for another one before their sums meet.  The instruction here
+// multiplies sixteen rows and sixteen tokens over a whole block: a lane has row (or token) lane mod 16 and chunks 2 g and 2 g + 1 of its eight, g = lane div 16.
+// Chunk i lies at place i ^ turn(row): the sixteen lanes of a read's quarter are rows {0-3, 12-15} of one g and {4-11} of the next, and find sixteen places.
+// With X_INSIDE the workgroup brings the few tokens' 16-bit values into 8 bits itself, while its first weights are on their way.
+__device__ __forceinline__ uint32_t thin_turn(uint32_t r) { return (r >> 1 & 1) | (r >> 1 & 4); }
+template <bool EXACT, int X_INSIDE, int XT, int WAVES>
+__global__ void __launch_bounds__(64 * WAVES, 2) fp8_thin_kernel(Product8 a)
 {
-    __shared__ f32x4 sums[WAVES][64];
+    constexpr uint32_t W_SIZE = 16 * 128, STAGE = X_INSIDE ? W_SIZE : (1 + XT) * W_SIZE, COPIES = STAGE / 1024;
+    static_assert(!X_INSIDE || XT == 1, "few tokens");
+    extern __shared__ __attribute__((aligned(16))) uint8_t shared[];
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 4, c = lane & 15;
-    const uint32_t n0 = blockIdx.x * 16, pitch = a.groups * 128;
-    // rows and tokens that are not there read the last one's, and their sums go nowhere
-    const uint32_t row = n0 + c < a.n ? n0 + c : a.n - 1, token = c < a.m ? c : a.m - 1;
-    const uint8_t *w = a.w + (size_t)row * pitch + 32 * g, *x = a.x + (size_t)token * pitch + 32 * g;
-    const uint32_t *w_scales = reinterpret_cast<const uint32_t *>(a.w_scales + (size_t)row * a.scale_row);
-    const uint32_t *x_scales = reinterpret_cast<const uint32_t *>(a.x_scales + (size_t)token * a.scale_row);
+    uint8_t *ring = shared + wave * (4 * STAGE), *x_codes = shared + WAVES * (4 * STAGE), *x_bytes = x_codes + a.m * a.groups * 128;
+    const uint32_t n0 = blockIdx.x * 16, pitch = a.groups * 128, rows = a.n - n0 < 16 ? a.n - n0 : 16;
+    const uint8_t *w = a.w + (size_t)n0 * pitch;
+    // rows and tokens that are not there take the last one's scale, and their sums go nowhere
+    uint32_t token[XT];
+#pragma unroll
+    for (uint32_t u = 0; u < XT; ++u) token[u] = 16 * u + c < a.m ? 16 * u + c : a.m - 1;
+    const uint32_t *w_scales = reinterpret_cast<const uint32_t *>(a.w_scales + (size_t)(n0 + (c < rows ? c : rows - 1)) * a.scale_row);
     const uint32_t units = (a.groups + 3) / 4;
-    struct Unit {
-        u32x4 w[8], x[8];
-        uint32_t ws, xs;
-    };
-    auto load = [&](uint32_t i, Unit &v) {
-        v.ws = w_scales[i], v.xs = x_scales[i];
+    const uint32_t from = lane / 8 * pitch + 16 * ((lane & 7) ^ thin_turn(lane / 8)), from8 = (8 + lane / 8) * pitch + 16 * ((lane & 7) ^ thin_turn(8 + lane / 8));
+    auto fetch = [&](uint32_t stage, uint32_t slot) {       // (behind the end: nothing is read, but as many copies are counted)
+        const uint32_t there = stage < a.groups ? pitch : 0;
+        const Range wr = range_of(w, rows * there);
+        copy_to_lds<16>(wr, from + stage * 128, ring + slot * STAGE);
+        copy_to_lds<16>(wr, from8 + stage * 128, ring + slot * STAGE + 1024);
+        if constexpr (!X_INSIDE) {
+            const Range xr = range_of(a.x, a.m * there);
 #pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-            if (4 * i + j >= a.groups) continue;
-            const u32x4 *p = reinterpret_cast<const u32x4 *>(w + (size_t)(4 * i + j) * 128), *q = reinterpret_cast<const u32x4 *>(x + (size_t)(4 * i + j) * 128);
-            v.w[2 * j] = __builtin_nontemporal_load(p), v.w[2 * j + 1] = __builtin_nontemporal_load(p + 1);
-            v.x[2 * j] = q[0], v.x[2 * j + 1] = q[1];
-        }
-    };
-    f32x4 acc = {};
-    Unit v[2];
-    if (wave < units) load(wave, v[0]);
-    auto step = [&](uint32_t i, const Unit &now, Unit &next) {
-        if (i + WAVES < units) load(i + WAVES, next);
-#pragma unroll
-        for (uint32_t j = 0; j < 4; ++j) {
-            if (4 * i + j >= a.groups) continue;
-            const i32x8 wv = halves(now.w[2 * j], now.w[2 * j + 1]), xv = halves(now.x[2 * j], now.x[2 * j + 1]);
-            const int ws = (int)(now.ws >> (8 * j)), xs = (int)(now.xs >> (8 * j));
-            if constexpr (EXACT) {
-#pragma unroll
-                for (int q = 0; q < 4; ++q) acc = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_values(wv, q, ws & 255), eight_values(xv, q, xs & 255), acc, 0, 0, 0);
-            } else {
-                acc = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv, acc, 0, 0, 0, ws, 0, xs);
+            for (uint32_t u = 0; u < XT; ++u) {
+                copy_to_lds<16>(xr, from + 16 * u * pitch + stage * 128, ring + slot * STAGE + (1 + u) * W_SIZE);
+                copy_to_lds<16>(xr, from8 + 16 * u * pitch + stage * 128, ring + slot * STAGE + (1 + u) * W_SIZE + 1024);
             }
         }
     };
-    for (uint32_t i = wave; i < units; i += 2 * WAVES) {
-        step(i, v[0], v[1]);
-        if (i + WAVES < units) step(i + WAVES, v[1], v[0]);
+    auto scale_at = [&](const uint32_t *p, uint32_t i) { return p[i < units ? i : units - 1]; };
+    auto x_scale_at = [&](uint32_t u, uint32_t i) {
+        return X_INSIDE ? 0 : scale_at(reinterpret_cast<const uint32_t *>(a.x_scales + (size_t)token[u] * a.scale_row), i);
+    };
+    uint32_t ws = scale_at(w_scales, wave), xs[XT], next_xs[XT];
+#pragma unroll
+    for (uint32_t u = 0; u < XT; ++u) xs[u] = x_scale_at(u, wave);
+    // The tokens' values: sixteen threads a block, eight values each, the first ones asked for before any weights.
+    constexpr int DT = X_INSIDE ? X_INSIDE - 1 : 0, AHEAD = 4;
+    const uint32_t per_row = a.groups * 16, all = X_INSIDE ? a.m * per_row : 0;
+    auto load_x = [&](uint32_t i, float (&v)[8]) {
+        const uint32_t r = i / per_row, col = (i - r * per_row) * 8;
+        const size_t at = (size_t)r * a.x_stride + col;
+#pragma unroll
+        for (uint32_t j = 0; j < 8; ++j) v[j] = 0.0f;
+        if (i >= all) return;
+        if (col + 8 <= a.k) {
+            load8<DT>(a.x, at, v);
+        } else if (col < a.k) {                             // (loads that do not wait for one another)
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) v[j] = load1<DT>(a.x, at + (col + j < a.k ? j : a.k - 1 - col));
+#pragma unroll
+            for (uint32_t j = 0; j < 8; ++j) v[j] = col + j < a.k ? v[j] : 0.0f;
+        }
+    };
+    auto store_x = [&](uint32_t i, const float (&v)[8]) {
+        if (i >= all) return;
+        const uint32_t r = i / per_row, col = (i - r * per_row) * 8, byte = block_byte(v);
+        // (a block's chunks turned by its row, as the ring's)
+        *reinterpret_cast<u32x2 *>(x_codes + r * pitch + (col & ~127u) + ((col >> 4 & 7) ^ thin_turn(r)) * 16 + (col & 8)) = fp8_codes(v, byte);
+        if ((i & 15) == 0) x_bytes[r * a.groups + (col >> 7)] = (uint8_t)byte;
+    };
+    float first_x[AHEAD][8];
+    if constexpr (X_INSIDE != 0) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) load_x(threadIdx.x + u * 64 * WAVES, first_x[u]);
+        __builtin_amdgcn_sched_barrier(0);
     }
-    if (wave != 0) sums[wave][lane] = acc;
+#pragma unroll
+    for (uint32_t j = 0; j < 4; ++j) fetch(4 * wave + j, j);
+    if constexpr (X_INSIDE != 0) {
+#pragma unroll
+        for (int u = 0; u < AHEAD; ++u) store_x(threadIdx.x + u * 64 * WAVES, first_x[u]);
+        for (uint32_t i = threadIdx.x + AHEAD * 64 * WAVES; i < all; i += 64 * WAVES) {
+            float v[8];
+            load_x(i, v), store_x(i, v);
+        }
+        asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
+    }
+    const uint32_t low = ((2 * g) ^ thin_turn(c)) * 16, high = ((2 * g + 1) ^ thin_turn(c)) * 16;
+    f32x4 acc[XT] = {};
+    for (uint32_t i = wave; i < units; i += WAVES) {
+        const uint32_t next_ws = scale_at(w_scales, i + WAVES);
+#pragma unroll
+        for (uint32_t u = 0; u < XT; ++u) next_xs[u] = x_scale_at(u, i + WAVES);
+#pragma unroll
+        for (uint32_t j = 0; j < 4; ++j) {
+            const uint32_t stage = 4 * i + j < a.groups ? 4 * i + j : a.groups - 1;
+            // A wave's copies are done in the order in which they were issued: three stages' may be left
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("s_waitcnt vmcnt(%0)" ::"n"(3 * COPIES) : "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            const uint8_t *t = ring + j * STAGE + c * 128;
+            const i32x8 wv = halves(*reinterpret_cast<const u32x4 *>(t + low), *reinterpret_cast<const u32x4 *>(t + high));
+            i32x8 xv[XT];
+            uint32_t xb[XT];
+#pragma unroll
+            for (uint32_t u = 0; u < XT; ++u) {
+                // (a token that is not there: the last one's codes, of its tile in the ring; turns go by the row within a tile)
+                const uint32_t r = X_INSIDE ? token[u] : token[u] & 15;
+                const uint8_t *x = X_INSIDE ? x_codes + r * pitch + stage * 128 : ring + j * STAGE + (1 + (token[u] >> 4)) * W_SIZE + r * 128;
+                xv[u] = halves(*reinterpret_cast<const u32x4 *>(x + ((2 * g) ^ thin_turn(r)) * 16), *reinterpret_cast<const u32x4 *>(x + ((2 * g + 1) ^ thin_turn(r)) * 16));
+                xb[u] = X_INSIDE ? x_bytes[r * a.groups + stage] : xs[u] >> (8 * j) & 255;
+            }
+            __builtin_amdgcn_sched_barrier(0);
+            asm volatile("s_waitcnt lgkmcnt(0)" ::: "memory");
+            __builtin_amdgcn_sched_barrier(0);
+            fetch(4 * (i + WAVES) + j, j);
+            if (4 * i + j >= a.groups) continue;
+            const int wb = (int)(ws >> (8 * j) & 255);
+#pragma unroll
+            for (uint32_t u = 0; u < XT; ++u) {
+                if constexpr (EXACT) {
+#pragma unroll
+                    for (int q = 0; q < 4; ++q)
+                        acc[u] = __builtin_amdgcn_mfma_f32_16x16x32_bf16(eight_values(wv, q, wb), eight_values(xv[u], q, (int)xb[u]), acc[u], 0, 0, 0);
+                } else {
+                    acc[u] = __builtin_amdgcn_mfma_scale_f32_16x16x128_f8f6f4(wv, xv[u], acc[u], 0, 0, 0, wb, 0, (int)xb[u]);
+                }
+            }
+        }
+        ws = next_ws;
+#pragma unroll
+        for (uint32_t u = 0; u < XT; ++u) xs[u] = next_xs[u];
+    }
+    asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (no copy may come into what the sums take)
+    __syncthreads();
+    f32x4 *sums = reinterpret_cast<f32x4 *>(shared);
+    if (wave != 0) {
+#pragma unroll
+        for (uint32_t u = 0; u < XT; ++u) sums[(wave * XT + u) * 64 + lane] = acc[u];
+    }
     __syncthreads();
     if (wave != 0) return;
-#pragma unroll
-    for (int k = 1; k < WAVES; ++k) acc += sums[k][lane];
     const uint32_t r = n0 + 4 * g;
-    if (c < a.m && r < a.n) store4(a.y, a.y_dtype, (size_t)c * a.y_stride + r, a.n - r, acc);
+#pragma unroll
+    for (uint32_t u = 0; u < XT; ++u) {
+#pragma unroll
+        for (int k = 1; k < WAVES; ++k) acc[u] += sums[(k * XT + u) * 64 + lane];
+        if (16 * u + c < a.m && r < a.n) store4(a.y, a.y_dtype, (size_t)(16 * u + c) * a.y_stride + r, a.n - r, acc[u]);
+    }
 }
 
 }  // namespace lowbit
@@ -277,21 +426,73 @@ using namespace enec::lowbit;
 
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
+// The tiles there are; with one on every compute unit a stage takes `us`, for y in 16 and in 32 bits (fitted, as are plan_of's constants, to times of products of 1 to
+// 4096 tokens with matrices of 1024 x 4096 to 28672 x 8192, every tile and split forced).
 struct Shape {
     uint32_t rows, tokens;
+    double us, us_exact;
 };
-constexpr Shape SHAPES[] = {{256, 256}, {128, 128}, {64, 64}};
-constexpr uint32_t THIN = 16;                       // tokens at most
+constexpr int SHAPES = 7, FIRST_EXACT = 3;
+constexpr Shape SHAPE[SHAPES] = {{256, 256, 1.52, 0}, {256, 192, 1.22, 0}, {256, 128, 0.88, 0}, {128, 128, 0.60, 1.08}, {128, 64, 0.36, 0.58}, {64, 64, 0.25, 0.37}, {64, 32, 0.225, 0.36}};
+constexpr uint32_t THIN = 64;                       // tokens at most of the kernel for few
+constexpr uint32_t UNITS = 256;                     // compute units
+constexpr uint32_t MOST_SPLITS = 16, UNIT = 4;      // a split is whole blocks of scales: so many stages, or a multiple
+constexpr uint32_t MOST_SPLIT_TILES = 320;          // tiles and splits together, where there are splits
 
-int shape_of(uint32_t m, uint32_t n)
+// How a product is cut up: the tile (-1: the kernel for few tokens), and the splits of the columns where tiles alone leave the card empty.
+struct Plan {
+    int shape;
+    uint32_t splits, split_stages;
+};
+inline bool too_large(const Shape &s, uint32_t m) { return s.tokens > 32 && s.tokens >= 2 * up(m, 16) * 16; }      // half of the tile or more would be empty
+
+Plan plan_of(uint32_t m, uint32_t n, uint32_t groups, bool exact)
 {
-    if (m > 128 && n > 128) return 0;
-    return m > 64 ? 1 : 2;
+    Plan p{-1, 1, up(groups, UNIT) * UNIT};
+    const double matrix = (double)n * groups * 128, from_memory = matrix / 5.0e6 + 4;
+    double best = 1e300;
+    if (m <= THIN) {
+        // every sixteen rows read all tokens again, at what the dies' caches give
+        const uint32_t tiles = m <= 16 ? 1 : m <= 32 ? 2 : 4;
+        const double cached = 3 + matrix * (1 + tiles) / 12.5e6;
+        best = cached > from_memory ? cached : from_memory;
+    }
+    for (int i = exact ? FIRST_EXACT : 0; i < SHAPES; ++i) {
+        const Shape &s = SHAPE[i];
+        if (too_large(s, m)) continue;
+        const uint64_t tiles = (uint64_t)up(n, s.rows) * up(m, s.tokens);
+        const bool splittable = i >= FIRST_EXACT && (uint64_t)m * up(n, 4) < 1u << 31;
+        for (uint32_t splits = 1; splits == 1 || (splittable && splits <= MOST_SPLITS && splits * UNIT <= groups && tiles * splits <= MOST_SPLIT_TILES); ++splits) {
+            const uint32_t each = up(up(groups, splits), UNIT) * UNIT, count = up(groups, each);
+            const uint64_t all = tiles * count, rounds = (all + UNITS - 1) / UNITS;
+            // a workgroup's start and end are 3 us; units that have none leave the others more of the memory; joining is a launch, the sums' way out and back
+            const double stage = (exact ? s.us_exact : s.us) * (all <= 192 ? 0.87 : 1.0);
+            double us = (double)rounds * (each * stage + 3);
+            us = (us > from_memory ? us : from_memory) + (count > 1 ? 3 + (double)count * m * n * 8 / 4e6 : 0);
+            if (us < best) best = us, p.shape = i, p.splits = count, p.split_stages = each;
+        }
+    }
+    return p;
+}
+
+// Bytes for the sums of the splits: of no more than m tokens, however few, so that one piece serves products of any number of them (fewer may be split
+// more).  The number of splits and tiles is bounded, which bounds the splits' tokens by the tile's.
+size_t parts_of(uint32_t m, uint32_t n, uint32_t groups)
+{
+    const uint32_t by_columns = groups / UNIT < MOST_SPLITS ? groups / UNIT : MOST_SPLITS;
+    uint64_t most = 0;
+    for (int i = FIRST_EXACT; i < SHAPES && by_columns > 1; ++i) {
+        const Shape &s = SHAPE[i];
+        if (too_large(s, m)) continue;
+        const uint64_t by_tiles = (uint64_t)s.tokens * (MOST_SPLIT_TILES / up(n, s.rows)), by_splits = (uint64_t)by_columns * m, rows = by_tiles < by_splits ? by_tiles : by_splits;
+        most = most > rows ? most : rows;
+    }
+    return most * part_row(n) * sizeof(float);
 }
 
 template <bool EXACT, int RA, int RB, int WA, int WB, int BUFFERS> bool launch_tile(Product8 a, uint32_t splits, hipStream_t s)
 {
-    constexpr size_t ROWS = 32 * RA * WA, TOKENS = 32 * RB * WB, LDS = (ROWS + TOKENS) * (128 * BUFFERS + 8);
+    constexpr size_t ROWS = 32 * RA * WA, TOKENS = 32 * RB * WB, LDS = (ROWS + TOKENS) * 128 * BUFFERS + (ROWS + TOKENS + 63) / 64 * 768 + (RA * RB > 8 ? WA * WB * 256 : 0);
     static_assert(LDS <= 160 * 1024, "LDS of a compute unit");
     static std::atomic<uint64_t> allowed{0};
     const auto kernel = fp8_tile_kernel<EXACT, RA, RB, WA, WB, BUFFERS>;
@@ -301,25 +502,63 @@ template <bool EXACT, int RA, int RB, int WA, int WB, int BUFFERS> bool launch_t
     return true;
 }
 
-template <bool EXACT> int launch(Product8 a, hipStream_t s)
+template <bool EXACT> bool launch_shape(const Product8 &a, const Plan &p, hipStream_t s)
+{
+    if constexpr (!EXACT) {
+        switch (p.shape) {
+        case 0: return launch_tile<false, 4, 4, 2, 2, 2>(a, p.splits, s);
+        case 1: return launch_tile<false, 4, 3, 2, 2, 2>(a, p.splits, s);
+        case 2: return launch_tile<false, 4, 2, 2, 2, 3>(a, p.splits, s);
+        }
+    }
+    switch (p.shape) {
+    case 3: return launch_tile<EXACT, 2, 2, 2, 2, 4>(a, p.splits, s);
+    case 4: return launch_tile<EXACT, 2, 1, 2, 2, 3>(a, p.splits, s);
+    case 5: return launch_tile<EXACT, 1, 1, 2, 2, 4>(a, p.splits, s);
+    default: return launch_tile<EXACT, 1, 1, 2, 1, 5>(a, p.splits, s);
+    }
+}
+
+constexpr size_t X_INSIDE_BYTES = 32 * 1024;            // codes of the tokens that a workgroup makes itself
+inline bool x_inside(uint32_t m, uint32_t groups) { return m <= 16 && (size_t)m * groups * 128 <= X_INSIDE_BYTES; }
+
+template <bool EXACT, int X_INSIDE, int XT, int WAVES> bool launch_thin_of(const Product8 &a, hipStream_t s)
+{
+    static std::atomic<uint64_t> allowed{0};
+    constexpr size_t RINGS = WAVES * 4 * (X_INSIDE ? 2048 : 2048 * (1 + XT));
+    const size_t lds = RINGS + (X_INSIDE ? (size_t)a.m * a.groups * 129 : 0);
+    const auto kernel = fp8_thin_kernel<EXACT, X_INSIDE, XT, WAVES>;
+    if (lds > 65536 && !allow_lds((const void *)kernel, RINGS + (X_INSIDE ? X_INSIDE_BYTES * 129 / 128 : 0), allowed)) return false;
+    kernel<<<up(a.n, 16), 64 * WAVES, lds, s>>>(a);
+    return true;
+}
+template <bool EXACT, int X_INSIDE, int XT> bool launch_thin(const Product8 &a, hipStream_t s)
+{
+    const uint32_t units = up(a.groups, 4);
+    constexpr int MOST = XT > 2 ? 2 : XT > 1 ? 4 : 8;
+    if (units <= 8 || MOST == 2) return launch_thin_of<EXACT, X_INSIDE, XT, 2>(a, s);
+    if (units <= 16) return launch_thin_of<EXACT, X_INSIDE, XT, MOST < 4 ? MOST : 4>(a, s);
+    return launch_thin_of<EXACT, X_INSIDE, XT, MOST>(a, s);
+}
+
+template <bool EXACT> int launch(Product8 a, void *parts, hipStream_t s)
 {
     if (a.groups == 0) {
         const uint32_t per_row = up(a.n, 4);
         join_kernel<<<up(a.m * per_row, 256), 256, 0, s>>>(nullptr, 0, a.m, a.n, 0, divide_by(per_row), a.y, a.y_stride, a.y_dtype);
         return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
     }
-    a.split_stages = up(a.groups, 4) * 4;
     bool ok = true;
-    if (a.m <= THIN) {
-        fp8_thin_kernel<EXACT, 8><<<up(a.n, 16), 512, 0, s>>>(a);
+    const Plan p = plan_of(a.m, a.n, a.groups, EXACT);
+    if (p.shape < 0) {
+        ok = a.m <= 16 ? launch_thin<EXACT, 0, 1>(a, s) : a.m <= 32 ? launch_thin<EXACT, 0, 2>(a, s) : launch_thin<EXACT, 0, 4>(a, s);
     } else {
-        const int shape = shape_of(a.m, a.n);
-        if constexpr (EXACT) {
-            ok = shape < 2 ? launch_tile<true, 2, 2, 2, 2, 2>(a, 1, s) : launch_tile<true, 1, 1, 2, 2, 4>(a, 1, s);
-        } else {
-            ok = shape == 0   ? launch_tile<false, 4, 4, 2, 2, 2>(a, 1, s)
-                 : shape == 1 ? launch_tile<false, 2, 2, 2, 2, 2>(a, 1, s)
-                              : launch_tile<false, 1, 1, 2, 2, 4>(a, 1, s);
+        a.split_stages = p.split_stages;
+        if (p.splits > 1) a.parts = static_cast<float *>(parts), a.part_row = part_row(a.n);
+        ok = launch_shape<EXACT>(a, p, s);
+        if (ok && p.splits > 1) {
+            const uint32_t per_row = up(a.n, 4);
+            join_kernel<<<up(a.m * per_row, 256), 256, 0, s>>>(a.parts, p.splits, a.m, a.n, a.part_row, divide_by(per_row), a.y, a.y_stride, a.y_dtype);
         }
     }
     return ok && hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
@@ -343,12 +582,12 @@ extern "C" {
 size_t enec_fp8_linear_workspace(size_t m, size_t n, size_t k)
 {
     if (!sizes_ok(m, n, k) || m == 0 || n == 0 || k == 0) return 0;
-    return codes_space(m, k) + scales_space(m, k);
+    return codes_space(m, k) + scales_space(m, k) + enec_fp8_matmul_workspace(m, n, k);
 }
 size_t enec_fp8_matmul_workspace(size_t m, size_t n, size_t k)
 {
     if (!sizes_ok(m, n, k) || m == 0 || n == 0 || k == 0) return 0;
-    return 0;
+    return parts_of((uint32_t)m, (uint32_t)n, (uint32_t)((k + 127) / 128));
 }
 
 int enec_fp8_linear(const void *x, size_t m, size_t x_stride, int dtype, const void *codes, const void *scales, size_t n, size_t k, void *y, size_t y_stride,
@@ -362,12 +601,18 @@ int enec_fp8_linear(const void *x, size_t m, size_t x_stride, int dtype, const v
     const size_t need = enec_fp8_linear_workspace(m, n, k);
     if (workspace_bytes < need || (need && !workspace)) return ENEC_E_CAPACITY;
     if (need && !aligned(workspace, 16)) return ENEC_E_ARG;
-    uint8_t *x_codes = static_cast<uint8_t *>(workspace), *x_scales = x_codes + codes_space(m, k);
+    const hipStream_t s = (hipStream_t)stream;
+    uint8_t *x_codes = static_cast<uint8_t *>(workspace), *x_scales = x_codes + codes_space(m, k), *parts = x_scales + scales_space(m, k);
+    Product8 a{x_codes, x_scales, static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), y, x_stride, y_stride, 0, nullptr, (uint32_t)m, (uint32_t)n,
+               (uint32_t)k, (uint32_t)((k + 127) / 128), (uint32_t)fp8_scale_row(k), 0, 0, 0, dtype};
+    if (k != 0 && x_inside(a.m, a.groups)) {
+        a.x = static_cast<const uint8_t *>(x);
+        const bool ok = dtype == ENEC_BF16 ? launch_thin<false, BF16 + 1, 1>(a, s) : launch_thin<false, FP16 + 1, 1>(a, s);
+        return ok && hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
+    }
     if (k != 0)
-        if (const int rc = quantize_to_fp8(x, m, k, x_stride, dtype, x_codes, x_scales, (hipStream_t)stream)) return rc;
-    const Product8 a{x_codes, x_scales, static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), y, y_stride, 0, nullptr, (uint32_t)m, (uint32_t)n,
-                     (uint32_t)((k + 127) / 128), (uint32_t)fp8_scale_row(k), 0, 0, 0, dtype};
-    return launch<false>(a, (hipStream_t)stream);
+        if (const int rc = quantize_to_fp8(x, m, k, x_stride, dtype, x_codes, x_scales, s)) return rc;
+    return launch<false>(a, parts, s);
 }
 
 int enec_fp8_matmul(const void *x_codes, const void *x_scales, size_t m, const void *codes, const void *scales, size_t n, size_t k, void *y, size_t y_stride,
@@ -383,9 +628,10 @@ int enec_fp8_matmul(const void *x_codes, const void *x_scales, size_t m, const v
     if (workspace_bytes < need || (need && !workspace)) return ENEC_E_CAPACITY;
     if (need && !aligned(workspace, 16)) return ENEC_E_ARG;
     const Product8 a{static_cast<const uint8_t *>(x_codes), static_cast<const uint8_t *>(x_scales), static_cast<const uint8_t *>(codes),
-                     static_cast<const uint8_t *>(scales), y, y_stride, 0, nullptr, (uint32_t)m, (uint32_t)n, (uint32_t)((k + 127) / 128),
+                     static_cast<const uint8_t *>(scales), y, 0, y_stride, 0, nullptr, (uint32_t)m, (uint32_t)n, (uint32_t)k, (uint32_t)((k + 127) / 128),
                      (uint32_t)fp8_scale_row(k), 0, 0, 0, dtype};
-    return dtype == ENEC_FP32 ? launch<true>(a, (hipStream_t)stream) : launch<false>(a, (hipStream_t)stream);
+    const hipStream_t s = (hipStream_t)stream;
+    return dtype == ENEC_FP32 ? launch<true>(a, workspace, s) : launch<false>(a, workspace, s);
 }
 
 }  // extern "C"

@@ -165,7 +165,8 @@ int enec_cache_write(const enec_cache *cache, const enec_cache_batch *batch, con
  *   q_heads a multiple of kv_heads
  *   turns   DEVICE, fp32, positions x rotary / 2 pairs (cosine, sine), 8-byte aligned, without gaps
  *   rotary  a multiple of 16 from 16 to head_dim
- * A sequence whose length exceeds `positions` is left out, and told of like the others. */
+ * A sequence whose length exceeds `positions` is left out, and told of like the others.
+ * ENEC_E_ARG also if q_heads / kv_heads exceeds 65535, or (n_tokens div page_tokens + 2 batch) (2 kv_heads + q_heads) 2^30. */
 int enec_cache_write_rotated(const enec_cache *cache, const enec_cache_batch *batch, const void *k, size_t k_token_stride, size_t k_head_stride,
                              const void *v, size_t v_token_stride, size_t v_head_stride, const void *q, size_t q_token_stride, size_t q_head_stride,
                              void *q_out, size_t q_out_token_stride, size_t q_out_head_stride, uint32_t q_heads, int dtype, const void *turns,

@@ -92,29 +92,23 @@ struct Turns {
     uint32_t half;
     int32_t positions;
 };
-// cosines and sines of eight pairs from pair j on
-__device__ __forceinline__ void load_turns(const Turns &t, int32_t position, uint32_t j, float (&c)[8], float (&s)[8])
+// cosines and sines of N pairs from pair j on
+template <int N> __device__ __forceinline__ void load_turns(const Turns &t, int32_t position, uint32_t j, float (&c)[N], float (&s)[N])
 {
     const f32x4_a8 *p = reinterpret_cast<const f32x4_a8 *>(t.table + ((size_t)(uint32_t)position * t.half + j) * 2);
 #pragma unroll
-    for (int i = 0; i < 4; ++i) {
+    for (int i = 0; i < N / 2; ++i) {
         const f32x4 v = p[i];
         c[2 * i] = v[0], s[2 * i] = v[1], c[2 * i + 1] = v[2], s[2 * i + 1] = v[3];
     }
 }
-// eight neighbours: four pairs from pair j on
-__device__ __forceinline__ void turn_neighbours(const Turns &t, int32_t position, uint32_t j, float (&x)[8])
+// eight neighbours, four pairs
+__device__ __forceinline__ void turn_neighbours(const float (&c)[4], const float (&s)[4], float (&x)[8])
 {
-    const f32x4_a8 *p = reinterpret_cast<const f32x4_a8 *>(t.table + ((size_t)(uint32_t)position * t.half + j) * 2);
 #pragma unroll
-    for (int i = 0; i < 2; ++i) {
-        const f32x4 v = p[i];
-#pragma unroll
-        for (int k = 0; k < 2; ++k) {
-            float &a = x[4 * i + 2 * k], &b = x[4 * i + 2 * k + 1];
-            const float c = v[2 * k], s = v[2 * k + 1], first = a * c - b * s;
-            b = b * c + a * s, a = first;
-        }
+    for (int i = 0; i < 4; ++i) {
+        const float a = x[2 * i], b = x[2 * i + 1];
+        x[2 * i] = a * c[i] - b * s[i], x[2 * i + 1] = b * c[i] + a * s[i];
     }
 }
 // the eight values from element i + dim on, of a head that begins at element i
@@ -124,7 +118,9 @@ __device__ __forceinline__ void load8_turned(const void *in, size_t i, uint32_t 
     load8<DT>(in, i + dim, x);
     if (dim >= 2 * t.half) return;
     if constexpr (ROTATION == NEIGHBOURS) {
-        turn_neighbours(t, position, dim / 2, x);
+        float c[4], s[4];
+        load_turns(t, position, dim / 2, c, s);
+        turn_neighbours(c, s, x);
     } else {
         const bool second = dim >= t.half;
         float y[8], c[8], s[8];
@@ -293,58 +289,77 @@ struct Queries {
     Divide units;                           // of a head
 };
 constexpr uint32_t QUERY_HEADS = 4;         // of a workgroup
-template <int DT, int ROTATION>
+template <int DT, int ROTATION, int U>
 __device__ __forceinline__ void turn_queries(const Pages &c, const Page &p, const Queries &q, const Turns &turns, uint32_t head, uint32_t heads)
 {
-    const uint32_t count = (p.end - p.first) * q.units.by * heads;
-    for (uint32_t i = threadIdx.x; i < count; i += blockDim.x) {
-        const uint32_t rest = quotient(i, q.units), unit = i - rest * q.units.by;
-        const uint32_t token = rest / heads, h = head + rest - token * heads;
-        const int32_t position = p.position + (int32_t)(p.first + token);
-        const size_t from = (size_t)(p.token + p.first + token) * q.in_token + h * q.in_head, to = (size_t)(p.token + p.first + token) * q.out_token + h * q.out_head;
-        float x[8] = {}, y[8] = {};
-        if constexpr (ROTATION == NEIGHBOURS) {
-            if (position >= 0) {
-                load8<DT>(q.in, from + 8 * unit, x);
-                if (8 * unit < 2 * turns.half) turn_neighbours(turns, position, 4 * unit, x);
+    constexpr int PAIRS = ROTATION == HALVES ? 8 : 4;
+    const uint32_t count = (p.end - p.first) * q.units.by * heads, half = turns.half;
+    for (uint32_t first = threadIdx.x; first < count; first += U * blockDim.x) {
+        float x[U][8], y[U][8], co[U][PAIRS], si[U][PAIRS];
+        size_t to[U];
+        uint32_t dim[U];
+        bool turned[U];             // the unit is turned; of halves, both ends are the unit's
+        // (loads that do not wait for one another, turns among them: asked for behind the values they cost 10 us of 45)
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            const uint32_t i = first + u * blockDim.x < count ? first + u * blockDim.x : first, rest = quotient(i, q.units), unit = i - rest * q.units.by;
+            const uint32_t token = rest / heads, h = head + rest - token * heads;
+            const size_t from = (size_t)(p.token + p.first + token) * q.in_token + h * q.in_head;
+            const int32_t position = p.position + (int32_t)(p.first + token);
+            to[u] = (size_t)(p.token + p.first + token) * q.out_token + h * q.out_head;
+            turned[u] = 8 * unit < (ROTATION == HALVES ? half : 2 * half);
+            dim[u] = ROTATION == NEIGHBOURS || turned[u] ? 8 * unit : 8 * unit + half;
+#pragma unroll
+            for (int k = 0; k < 8; ++k) x[u][k] = y[u][k] = 0;
+#pragma unroll
+            for (int k = 0; k < PAIRS; ++k) co[u][k] = si[u][k] = 0;
+            if (position < 0) continue;                     // (zeros, turned or not)
+            load8<DT>(q.in, from + dim[u], x[u]);
+            if (turned[u]) {
+                if (ROTATION == HALVES) load8<DT>(q.in, from + dim[u] + half, y[u]);
+                load_turns(turns, position, ROTATION == HALVES ? dim[u] : dim[u] / 2, co[u], si[u]);
             }
-            store8<DT>(q.out, to + 8 * unit, x);
-        } else {
-            const bool pair = 8 * unit < turns.half;
-            const uint32_t dim = pair ? 8 * unit : 8 * unit + turns.half;
-            if (position >= 0) {
-                load8<DT>(q.in, from + dim, x);
-                if (pair) {
-                    float co[8], si[8];
-                    load8<DT>(q.in, from + dim + turns.half, y);
-                    load_turns(turns, position, dim, co, si);
+        }
+#pragma unroll
+        for (int u = 0; u < U; ++u) {
+            if (first + u * blockDim.x >= count) break;
+            if (turned[u]) {
+                if constexpr (ROTATION == NEIGHBOURS) {
+                    turn_neighbours(co[u], si[u], x[u]);
+                } else {
 #pragma unroll
                     for (int k = 0; k < 8; ++k) {
-                        const float a = x[k], b = y[k];
-                        x[k] = a * co[k] - b * si[k], y[k] = b * co[k] + a * si[k];
+                        const float a = x[u][k], b = y[u][k];
+                        x[u][k] = a * co[u][k] - b * si[u][k], y[u][k] = b * co[u][k] + a * si[u][k];
                     }
                 }
             }
-            store8<DT>(q.out, to + dim, x);
-            if (pair) store8<DT>(q.out, to + dim + turns.half, y);
+            store8<DT>(q.out, to[u] + dim[u], x[u]);
+            if (ROTATION == HALVES && turned[u]) store8<DT>(q.out, to[u] + dim[u] + half, y[u]);
         }
     }
 }
 
-// Keys, values and queries side by side in one launch: blockIdx.z is 0, 1, or a few of the heads that share key head blockIdx.y.
+// Keys, values and queries side by side in one launch: a page's heads follow one another, and for each of them its keys, its values, and the queries that share
+// it, a few heads to a workgroup; so workgroups that run together have neighbouring memory.
+struct Order {
+    Divide per_page, per_head;
+};
 template <int DT, int ROTATION>
-__global__ void __launch_bounds__(256) cache_write_rotated_kernel(Pages c, NewTokens n, Queries q, Turns turns)
+__global__ void __launch_bounds__(256) cache_write_rotated_kernel(Pages c, NewTokens n, Queries q, Turns turns, Order order)
 {
     __shared__ uint32_t shared[4];
-    const Page p = page_of_item(c, blockIdx.x, turns.positions);
+    const uint32_t item = quotient(blockIdx.x, order.per_page), within = blockIdx.x - item * order.per_page.by;
+    const uint32_t head = quotient(within, order.per_head), part = within - head * order.per_head.by;
+    const Page p = page_of_item(c, item, turns.positions);
     if (!p.good) return;
-    if (blockIdx.z == 0) {
-        write_page<DT, false, ROTATION>(c, p, blockIdx.y, n.k, n.k_token, n.k_head, shared, turns);
-    } else if (blockIdx.z == 1) {
-        write_page<DT, true>(c, p, blockIdx.y, n.v, n.v_token, n.v_head, shared);
+    if (part == 0) {
+        write_page<DT, false, ROTATION>(c, p, head, n.k, n.k_token, n.k_head, shared, turns);
+    } else if (part == 1) {
+        write_page<DT, true>(c, p, head, n.v, n.v_token, n.v_head, shared);
     } else {
-        const uint32_t first = (blockIdx.z - 2) * QUERY_HEADS, left = q.per_group - first;
-        turn_queries<DT, ROTATION>(c, p, q, turns, blockIdx.y * q.per_group + first, left < QUERY_HEADS ? left : QUERY_HEADS);
+        const uint32_t first = (part - 2) * QUERY_HEADS, left = q.per_group - first;
+        turn_queries<DT, ROTATION, 2>(c, p, q, turns, head * q.per_group + first, left < QUERY_HEADS ? left : QUERY_HEADS);
     }
 }
 
@@ -469,20 +484,23 @@ int enec_cache_write_rotated(const enec_cache *cache, const enec_cache_batch *ba
     Pages p;
     if (const int rc = pages_of(cache, batch, p)) return rc;
     if (rotary == 0 || rotary % 16 || rotary > p.head_dim) return ENEC_E_ARG;
-    if (q_heads % p.heads || q_heads / p.heads > 65533 * QUERY_HEADS || (q_heads != 0) != (q != nullptr) || (q_heads != 0) != (q_out != nullptr)) return ENEC_E_ARG;
+    if (q_heads % p.heads || q_heads / p.heads > 65535 || (q_heads != 0) != (q != nullptr) || (q_heads != 0) != (q_out != nullptr)) return ENEC_E_ARG;
     if (q_heads && (((uintptr_t)q | (uintptr_t)q_out) & 1)) return ENEC_E_ARG;
     // in place a unit's thread has read what it writes; with other strides it would write what another reads
     if (q_heads && q == q_out && (q_token_stride != q_out_token_stride || q_head_stride != q_out_head_stride)) return ENEC_E_ARG;
     if (p.batch == 0 || p.n_tokens == 0) return ENEC_OK;
     if (!k || !v || !turns || (((uintptr_t)k | (uintptr_t)v) & 1) || ((uintptr_t)turns & 7)) return ENEC_E_ARG;
     const uint32_t group = q_heads / p.heads, units = interleaved ? p.head_dim / 8 : (p.head_dim - rotary / 2) / 8;
-    const dim3 grid((p.n_tokens >> p.log_page) + 2 * p.batch, p.heads, 2 + (group + QUERY_HEADS - 1) / QUERY_HEADS);
+    const uint32_t parts = 2 + (group + QUERY_HEADS - 1) / QUERY_HEADS;
+    const uint64_t blocks = ((uint64_t)(p.n_tokens >> p.log_page) + 2 * p.batch) * p.heads * parts;
+    if (blocks >= (uint64_t)1 << 31) return ENEC_E_ARG;
     auto kernel = dtype == ENEC_BF16 ? (interleaved ? cache_write_rotated_kernel<BF16, NEIGHBOURS> : cache_write_rotated_kernel<BF16, HALVES>)
                                      : (interleaved ? cache_write_rotated_kernel<FP16, NEIGHBOURS> : cache_write_rotated_kernel<FP16, HALVES>);
-    kernel<<<grid, threads_of(p), 0, (hipStream_t)stream>>>(
+    kernel<<<dim3((unsigned)blocks), threads_of(p), 0, (hipStream_t)stream>>>(
         p, NewTokens{k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride},
         Queries{q, q_out, q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride, q_heads, group, divide_by(units)},
-        Turns{static_cast<const float *>(turns), rotary / 2, positions < (uint32_t)MAX_SEQUENCE ? (int32_t)positions : MAX_SEQUENCE});
+        Turns{static_cast<const float *>(turns), rotary / 2, positions < (uint32_t)MAX_SEQUENCE ? (int32_t)positions : MAX_SEQUENCE},
+        Order{divide_by(p.heads * parts), divide_by(parts)});
     return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
 }
 

@@ -9,7 +9,7 @@ using namespace lowbit;
 
 // The order of a row is never made.  Three launches, the first two with a workgroup for each part of a row, the last with one for each row:
 //   1. survey: each part's largest logit, and a histogram of its logits in bins that ascend with them.  Logits well over the others are counted all, of the
-//      others one in four, as atomics on LDS are what this launch would spend its time on;
+//      others one in eight, as atomics on LDS are what this launch would spend its time on;
 //   2. weigh: the histogram says about where a cut lies, and how far off that may be.  Weights of logits above are summed in 64 bits and their tokens counted, and
 //      the tokens in between, some hundred, are listed;
 //   3. draw: the cuts are picked from the list; then the token is drawn by the kept weights of each run of logits, and of one run's.
@@ -28,7 +28,7 @@ struct Part {
     float counted;                      // from this logit on all are counted
     uint32_t over;                      // tokens over top_k's listed ones
     uint32_t unused[2];
-    uint64_t low, middle;               // weights over top_p's listed ones, and between those and top_k's
+    uint64_t low, all;                  // weights over top_p's listed ones, and all down to the end of top_k's
     uint64_t kept[PART_WAVES];          // of what lies over the list what min_p keeps, of each wave's run
 };
 struct Row {
@@ -323,7 +323,7 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) survey_kernel(
     auto count_one = [&](float v, uint32_t, uint32_t j) {
         const bool one = v >= counted;
         // (what lies over the free bins is put right below)
-        if (one || j % 4 == 0) atomicAdd(&count[grid.bin(v)], one ? 1u : 4u);
+        if (one || j == 0) atomicAdd(&count[grid.bin(v)], one ? 1u : VEC);
     };
     if (cuts) run.each([&](float v, uint32_t i, uint32_t j) { most = fmaxf(most, v), nan |= v != v, count_one(v, i, j); });
     else run.each([&](float v, uint32_t, uint32_t) { most = fmaxf(most, v), nan |= v != v; });
@@ -391,7 +391,7 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
 {
     __shared__ uint32_t waves[16], n_listed, reserved, over_sum;
     __shared__ float waves_f[16], k_mass, k_off;
-    __shared__ uint64_t low_sum, middle_sum;
+    __shared__ uint64_t low_sum, all_sum;
     __shared__ uint32_t k_first, k_last, p_first, p_last, p_wide, few;
     __shared__ Listed list[PART_LISTED];
     const size_t row = blockIdx.x / a.parts;
@@ -442,7 +442,7 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
 #pragma unroll
             for (uint32_t j = 0; j < 4; ++j) n[j] += shift[q] <= b0 ? v[q][j] : 0, n[4 + j] += shift[q] <= b0 ? u[q][j] : 0;
     }
-    // Tokens and weights up to each bin, the latter by the bins' middles, and the variance of what one in four was counted of (the last bin has no weight to speak of).
+    // Tokens and weights up to each bin, the latter by the bins' middles, and the variance of what one in eight was counted of (the last bin has no weight to speak of).
     const uint32_t exact = a.vocab > FULLY_COUNTED ? top.grid.bin(counted) : BINS;
     const float cold = 1.0f / how.temperature, step = top.width * cold;
     const float middle_of_0 = (float)((((double)top.grid.base + 0.5) * (double)top.width - (double)value_of(top.key)) * (double)cold);
@@ -453,11 +453,11 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
         const float d = middle_of_0 - (float)(b0 + j) * step, each = b0 + j == BINS - 1 ? 0.0f : d > 0.0f ? 1.0f : __expf(d);
         e[j] = (float)n[j] * each;
         n_sum += n[j], e_sum += e[j];
-        if (b0 + j >= exact) v_sum += 3.0f * e[j] * each, c_sum += 3.0f * (float)n[j];
+        if (b0 + j >= exact) v_sum += (VEC - 1) * e[j] * each, c_sum += (VEC - 1) * (float)n[j];
     }
     if (threadIdx.x == 0) {
         k_first = k_last = p_first = p_last = p_wide = BINS - 1, few = 0xFFFFFFFFu;
-        n_listed = 0, over_sum = 0, low_sum = middle_sum = 0, k_mass = k_off = 0;
+        n_listed = 0, over_sum = 0, low_sum = all_sum = 0, k_mass = k_off = 0;
     }
     const uint32_t n_before = block_before<PART_WAVES>(n_sum, waves, n_all);
     const float e_before = block_before<PART_WAVES>(e_sum, waves_f, e_all);
@@ -468,7 +468,7 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
         float at = e_before, c = c_before;
 #pragma unroll
         for (uint32_t j = 0; j < EACH; ++j) {
-            c += b0 + j >= exact ? 3.0f * (float)n[j] : 0.0f;
+            c += b0 + j >= exact ? (VEC - 1) * (float)n[j] : 0.0f;
             if (before < how.top_k && how.top_k <= before + n[j])
                 k_mass = at + e[j] * ((wanted - (float)before) / (float)n[j]), k_off = 4.0f * __builtin_sqrtf(c);
             before += n[j], at += e[j];
@@ -526,26 +526,37 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
     // What is over top_p's list is weighed, and so is what lies between it and top_k's; without top_p, what is over top_k's.
     uint64_t low = 0, kept = 0, all_weights = 0;
     uint32_t over = 0, weighed = 0;
-    const bool some_kept = how.min_p > 0.0f;
-    auto listed = [&](float v) { return v >= k_low && ((v >= p_low && v < p_high) || (how.top_k && v < k_high)); };
-    auto weigh = [&](float v, uint32_t i, bool there) {
-        const double x = there ? w.value(v) : 0.0, first = v >= p_high ? x : 0.0;
+    const bool some_kept = how.min_p > 0.0f, by_count = how.top_k != 0;
+    auto listed = [&](float v) { return (v >= p_low && v < p_high) || (by_count && v >= k_low && v < k_high); };
+    // (what is listed is weighed too, the third launch takes it off again)
+    auto weigh = [&](float v, uint32_t i) {
+        const double x = by_count && !(v >= k_low) ? 0.0 : w.value(v), first = v >= p_high ? x : 0.0;
         all_weights += w.raised(x), low += w.raised(first);
         if (some_kept) kept += w.raised(least.keeps(first, i) ? first : 0.0);
-        if (how.top_k) over += v >= k_high;
+        if (by_count) over += v >= k_high;
     };
     run.pieces([&](const float (&v)[VEC], uint32_t first) {
+        if (by_count) {
+            bool any = false;
+#pragma unroll
+            for (uint32_t j = 0; j < VEC; ++j) any |= v[j] >= k_low;
+            if (!__any(any)) return;                        // (a wave of tokens behind top_k's cut)
+        }
         uint32_t in = 0;
-        bool any = false;
-#pragma unroll
-        for (uint32_t j = 0; j < VEC; ++j) any |= v[j] >= k_low;
-        if (!__any(any)) return;                            // (a wave of tokens behind top_k's cut)
         weighed += VEC;
+        if (by_count || some_kept) {
 #pragma unroll
-        for (uint32_t j = 0; j < VEC; ++j) {
-            const bool here = listed(v[j]);
-            in |= here ? 1u << j : 0;
-            weigh(v[j], first + j, !here && v[j] >= k_low);
+            for (uint32_t j = 0; j < VEC; ++j) {
+                in |= listed(v[j]) ? 1u << j : 0;
+                weigh(v[j], first + j);
+            }
+        } else {
+#pragma unroll
+            for (uint32_t j = 0; j < VEC; ++j) {
+                in |= v[j] >= p_low && v[j] < p_high ? 1u << j : 0;
+                const double x = w.value(v[j]);
+                all_weights += w.raised(x), low += w.raised(v[j] >= p_high ? x : 0.0);
+            }
         }
         if (__any(in != 0)) {
             // one addition a wave; the lanes' places by the bits of their counts
@@ -574,17 +585,15 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
         if (listed(run.rest_value)) {
             const uint32_t at = atomicAdd(&n_listed, 1u);
             if (at < PART_LISTED) list[at] = Listed{key_of(run.rest_value), run.rest};
-        } else {
-            weigh(run.rest_value, run.rest, run.rest_value >= k_low), ++weighed;
         }
+        weigh(run.rest_value, run.rest), ++weighed;
     }
     low -= weighed * magic, all_weights -= weighed * magic, kept -= weighed * magic;
     kept = wave_sum(some_kept ? kept : low);
     if (lane == 0) mine.kept[wave] = kept;
     if (how.by_mass) {
-        low = wave_sum(low);
-        const uint64_t middle = wave_sum(all_weights) - low;
-        if (lane == 0) add(low_sum, low), add(middle_sum, middle);
+        low = wave_sum(low), all_weights = wave_sum(all_weights);
+        if (lane == 0) add(low_sum, low), add(all_sum, all_weights);
     }
     if (how.top_k) {
         over = wave_sum(over);
@@ -592,7 +601,7 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
     }
     __syncthreads();
     if (threadIdx.x == 0) {
-        mine.low = low_sum, mine.middle = middle_sum, mine.over = over_sum;
+        mine.low = low_sum, mine.all = all_sum, mine.over = over_sum;
         // (a part whose list is too short makes the row's too long)
         reserved = n_listed ? atomicAdd(&a.rows[row].listed, n_listed <= PART_LISTED ? n_listed : LISTED + 1) : 0;
         if (part == 0) {
@@ -766,7 +775,7 @@ template <int DT> __global__ void __launch_bounds__(DRAW_THREADS) draw_kernel(Ro
     const uint64_t kept = threadIdx.x < runs ? a.part[row * a.parts + threadIdx.x / PART_WAVES].kept[threadIdx.x % PART_WAVES] : 0;
     const Part &part = a.part[row * a.parts + ((threadIdx.x & 63) < a.parts ? threadIdx.x & 63 : 0)];
     const bool a_part = (threadIdx.x & 63) < a.parts;         // (lanes behind the parts add nothing)
-    uint64_t low = a_part ? part.low : 0, middle = a_part ? part.middle : 0;
+    uint64_t low = a_part ? part.low : 0, weights = a_part ? part.all : 0;
     uint32_t over = a_part ? part.over : 0;
     const Row r = a.rows[row];
     const How how(a, row);
@@ -800,7 +809,7 @@ template <int DT> __global__ void __launch_bounds__(DRAW_THREADS) draw_kernel(Ro
                     m[j] = mine(j) ? w.whole(x) : 0, kept_too |= mine(j) && least.keeps(x, l.index) ? 1u << j : 0;
                 }
             }
-            low = wave_sum(low), middle = wave_sum(middle), over = wave_sum(over);
+            low = wave_sum(low), weights = wave_sum(weights), over = wave_sum(over);
             auto keeps = [&](uint32_t j) { return cut.keeps((uint32_t)(place[j] >> 32), 0xFFFFFFFFu - (uint32_t)place[j]); };
             if (how.top_k) {
                 uint32_t in = 0, all;
@@ -812,16 +821,17 @@ template <int DT> __global__ void __launch_bounds__(DRAW_THREADS) draw_kernel(Ro
                 if (done) cut = select_listed(place, weight, how.top_k - over, s);
             }
             if (how.by_mass && done) {
-                uint64_t in = 0, others = 0, sum, rest;
+                // (of all weights down to the end of top_k's list those are not kept that its cut leaves out)
+                uint64_t in = 0, out = 0, sum, left_out;
 #pragma unroll
                 for (uint32_t j = 0; j < EACH_LISTED; ++j) {
-                    const bool here = value_at(j) >= r.p_low && value_at(j) < r.p_high;
-                    weight[j] = here && keeps(j) ? m[j] : 0;
-                    in += weight[j], others += !here && keeps(j) ? m[j] : 0;
+                    const bool here = value_at(j) >= r.p_low && value_at(j) < r.p_high, stays = keeps(j);
+                    weight[j] = here && stays ? m[j] : 0;
+                    in += weight[j], out += stays ? 0 : m[j];
                 }
                 block_before<DRAW_WAVES>(in, s.wave_mass, sum);
-                block_before<DRAW_WAVES>(others, s.wave_mass, rest);
-                const double wanted = __builtin_ceil((double)how.top_p * (double)(low + middle + sum + rest));
+                block_before<DRAW_WAVES>(out, s.wave_mass, left_out);
+                const double wanted = __builtin_ceil((double)how.top_p * (double)(weights - left_out));
                 const uint64_t target = wanted < 1.0 ? 1 : (uint64_t)wanted;
                 done = target > low && target <= low + sum;
                 if (done) cut = select_listed(place, weight, target - low, s);

@@ -19,22 +19,20 @@ constexpr uint32_t PART_THREADS = 512, PART_WAVES = PART_THREADS / 64, DRAW_THRE
 constexpr uint32_t VEC = 8, PIECE = 64 * VEC, CHUNK = DRAW_THREADS * VEC;
 constexpr uint32_t MAX_VOCAB = 1u << 22, MAX_PARTS = 16, WORKGROUPS = 512;
 constexpr uint32_t FULLY_COUNTED = 16384;               // a vocabulary up to that
-constexpr uint32_t BINS = 4096, DIGITS = 2048, EACH_LISTED = 8, LISTED = EACH_LISTED * DRAW_THREADS, PART_LISTED = 4096;
+constexpr uint32_t BINS = 2048, DIGITS = 2048, EACH_LISTED = 8, LISTED = EACH_LISTED * DRAW_THREADS, PART_LISTED = 4096, SAMPLE = 128;
 
 struct Part {
     uint32_t key, first;                // its largest logit's, and that logit's index
     int32_t base;                       // the grid's bin that its histogram begins with; it goes down from there
     float width;                        // of the row's bins
     float counted;                      // from this logit on all are counted
-    uint32_t over;                      // tokens over top_k's listed ones
-    uint32_t unused[2];
+    uint32_t over, listed;              // tokens over top_k's listed ones, and how many are listed
+    uint32_t unused;
     uint64_t low, all;                  // weights over top_p's listed ones, and all down to the end of top_k's
     uint64_t kept[PART_WAVES];          // of what lies over the list what min_p keeps, of each wave's run
 };
 struct Row {
-    uint32_t listed;
     float p_high, p_low, k_high, k_low;             // top_p's listed logits, from p_low to below p_high, and top_k's
-    uint32_t unused[3];
 };
 struct Listed {
     uint32_t key, index;
@@ -274,7 +272,7 @@ __device__ __forceinline__ void add(uint64_t &to, uint64_t v) { atomicAdd(reinte
 // The grid's bins that histograms begin with are whole numbers of a thread's bins, so that one part's are another's moved by whole threads.
 __device__ __forceinline__ int32_t base_over(int32_t bin, int32_t free)
 {
-    const int64_t b = ((int64_t)bin + free + 7) & ~(int64_t)7;
+    const int64_t b = ((int64_t)bin + free + 3) & ~(int64_t)3;
     return (int32_t)(b < 2147483640 ? b : 2147483640);
 }
 
@@ -288,8 +286,8 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) survey_kernel(
     const size_t row = blockIdx.x / a.parts;
     const uint32_t part = blockIdx.x % a.parts, lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6);
     const Run<DT> run(a, row, part * PART_WAVES + wave);
-    const uint32_t sample = a.vocab < PART_THREADS ? threadIdx.x : (uint32_t)((uint64_t)threadIdx.x * a.vocab / PART_THREADS);
-    float some = sample < a.vocab ? load1<DT>(a.logits, row * a.stride + sample) : __builtin_nanf("");
+    const uint32_t sample = a.vocab < SAMPLE ? threadIdx.x : (uint32_t)((uint64_t)threadIdx.x * a.vocab / SAMPLE);
+    float some = threadIdx.x < SAMPLE && sample < a.vocab ? load1<DT>(a.logits, row * a.stride + sample) : __builtin_nanf("");
     const How how(a, row);
     const bool cuts = how.cuts();
     constexpr float INF = __builtin_inff();
@@ -297,7 +295,7 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) survey_kernel(
     float width = 1.0f, counted = -INF;
     if (threadIdx.x == 0) nans = false;
     if (cuts) {
-        // The bins' width by the spread of 512 logits of the row: twice that down from the largest, or 24 T, beyond which weights are below 2^-34.  And the largest of
+        // The bins' width by the spread of some logits of the row: twice that down from the largest, or 24 T, beyond which weights are below 2^-34.  And the largest of
         // the waves' first pieces, over which a tenth of the bins are left free.
         some = some > -INF && some < INF ? some : __builtin_nanf("");
         float h = some, l = some, b = -INF;
@@ -352,7 +350,6 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) survey_kernel(
             for (uint32_t i = 1; i < PART_WAVES; ++i) at = first[i] < at ? first[i] : at;
         Part &p = a.part[blockIdx.x];
         p.key = nans ? 0xFFFFFFFFu : key_of(most), p.first = at, p.base = grid.base, p.width = width, p.counted = counted;
-        if (part == 0) a.rows[row].listed = 0;
     }
     if (cuts) {
         u32x4 *to = reinterpret_cast<u32x4 *>(a.bins + (size_t)blockIdx.x * BINS);
@@ -389,9 +386,9 @@ struct Top {
 
 template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(Rows a)
 {
-    __shared__ uint32_t waves[16], n_listed, reserved, over_sum;
+    __shared__ uint32_t waves[16], n_listed, over_of[PART_WAVES];
     __shared__ float waves_f[16], k_mass, k_off;
-    __shared__ uint64_t low_sum, all_sum;
+    __shared__ uint64_t low_of[PART_WAVES], all_of[PART_WAVES];
     __shared__ uint32_t k_first, k_last, p_first, p_last, p_wide, few;
     __shared__ Listed list[PART_LISTED];
     const size_t row = blockIdx.x / a.parts;
@@ -420,27 +417,26 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
         if (lane == 0) mine.kept[wave] = kept;
         return;
     }
-    // Eight bins a thread: the parts' histograms, each as far below this row's as its base; what is below all bins is in the last.
+    // Four bins a thread: the parts' histograms, each as far below this row's as its base; what is below all bins is in the last.
     constexpr uint32_t EACH = BINS / PART_THREADS;
-    static_assert(EACH == 8, "two vectors of four");
+    static_assert(EACH == 4, "a vector");
     uint32_t n[EACH] = {};
     const uint32_t b0 = threadIdx.x * EACH;
 #pragma unroll 1
     for (uint32_t p = 0; p < a.parts; p += 4) {
-        u32x4 v[4], u[4];
+        u32x4 v[4];
         uint32_t shift[4];
 #pragma unroll
         for (uint32_t q = 0; q < 4; ++q) {                      // (loads that do not wait for one another)
             const uint32_t o = p + q < a.parts ? p + q : p;
             shift[q] = (uint32_t)top.grid.base - (uint32_t)of_lane(top.base, o);
-            const u32x4 *from = reinterpret_cast<const u32x4 *>(a.bins + (row * a.parts + o) * BINS + (shift[q] <= b0 ? b0 - shift[q] : 0));
-            v[q] = from[0], u[q] = from[1];
+            v[q] = *reinterpret_cast<const u32x4 *>(a.bins + (row * a.parts + o) * BINS + (shift[q] <= b0 ? b0 - shift[q] : 0));
             shift[q] = p + q < a.parts ? shift[q] : 0xFFFFFFFFu;
         }
 #pragma unroll
         for (uint32_t q = 0; q < 4; ++q)
 #pragma unroll
-            for (uint32_t j = 0; j < 4; ++j) n[j] += shift[q] <= b0 ? v[q][j] : 0, n[4 + j] += shift[q] <= b0 ? u[q][j] : 0;
+            for (uint32_t j = 0; j < 4; ++j) n[j] += shift[q] <= b0 ? v[q][j] : 0;
     }
     // Tokens and weights up to each bin, the latter by the bins' middles, and the variance of what one in eight was counted of (the last bin has no weight to speak of).
     const uint32_t exact = a.vocab > FULLY_COUNTED ? top.grid.bin(counted) : BINS;
@@ -457,7 +453,7 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
     }
     if (threadIdx.x == 0) {
         k_first = k_last = p_first = p_last = p_wide = BINS - 1, few = 0xFFFFFFFFu;
-        n_listed = 0, over_sum = 0, low_sum = all_sum = 0, k_mass = k_off = 0;
+        n_listed = 0, k_mass = k_off = 0;
     }
     const uint32_t n_before = block_before<PART_WAVES>(n_sum, waves, n_all);
     const float e_before = block_before<PART_WAVES>(e_sum, waves_f, e_all);
@@ -591,28 +587,18 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
     low -= weighed * magic, all_weights -= weighed * magic, kept -= weighed * magic;
     kept = wave_sum(some_kept ? kept : low);
     if (lane == 0) mine.kept[wave] = kept;
-    if (how.by_mass) {
-        low = wave_sum(low), all_weights = wave_sum(all_weights);
-        if (lane == 0) add(low_sum, low), add(all_sum, all_weights);
-    }
-    if (how.top_k) {
-        over = wave_sum(over);
-        if (lane == 0) atomicAdd(&over_sum, over);
-    }
+    low = wave_sum(low), all_weights = wave_sum(all_weights), over = wave_sum(over);
+    if (lane == 0) low_of[wave] = low, all_of[wave] = all_weights, over_of[wave] = over;
     __syncthreads();
     if (threadIdx.x == 0) {
-        mine.low = low_sum, mine.all = all_sum, mine.over = over_sum;
-        // (a part whose list is too short makes the row's too long)
-        reserved = n_listed ? atomicAdd(&a.rows[row].listed, n_listed <= PART_LISTED ? n_listed : LISTED + 1) : 0;
-        if (part == 0) {
-            Row &r = a.rows[row];
-            r.p_high = p_high, r.p_low = p_low, r.k_high = k_high, r.k_low = k_low;
-        }
+#pragma unroll
+        for (uint32_t i = 1; i < PART_WAVES; ++i) low += low_of[i], all_weights += all_of[i], over += over_of[i];
+        mine.low = low, mine.all = all_weights, mine.over = over, mine.listed = n_listed;
+        if (part == 0) a.rows[row] = Row{p_high, p_low, k_high, k_low};
     }
-    __syncthreads();
     const uint32_t many = n_listed < PART_LISTED ? n_listed : PART_LISTED;
-    for (uint32_t i = threadIdx.x; i < many; i += PART_THREADS)
-        if (reserved + i < LISTED) a.list[row * LISTED + reserved + i] = list[i];
+    Listed *to = a.list + (size_t)blockIdx.x * PART_LISTED;
+    for (uint32_t i = threadIdx.x; i < many; i += PART_THREADS) to[i] = list[i];
 }
 
 // ---- 3 ------------------------------------------------------------------------------
@@ -621,7 +607,7 @@ constexpr uint32_t FEW = 64;
 struct Shared {
     uint64_t mass[DIGITS];
     uint32_t count[DIGITS];
-    uint64_t wave_mass[16], wave_most[DRAW_WAVES], wave_least[DRAW_WAVES];
+    uint64_t wave_mass[16], wave_most[16], wave_least[16];
     uint32_t wave_count[16];
     uint64_t run_mass[MAX_PARTS * PART_WAVES];      // kept weights of each wave's run
     uint64_t few[FEW], few_weight[FEW];
@@ -684,16 +670,19 @@ template <int DT, bool MASS> __device__ __forceinline__ Cut select(const Rows &a
             }
         }
         __syncthreads();
-        // two digits a thread, in descending order
-        uint64_t m[2], total;
-        uint32_t digit[2];
-        for (uint32_t j = 0; j < 2; ++j) {
-            digit[j] = DIGITS - 1 - (2 * threadIdx.x + j);
-            m[j] = MASS ? s.mass[digit[j]] : s.count[digit[j]];
+        // some digits a thread, in descending order
+        constexpr uint32_t EACH = DIGITS / DRAW_THREADS;
+        uint64_t m[EACH], sum = 0, total;
+#pragma unroll
+        for (uint32_t j = 0; j < EACH; ++j) {
+            const uint32_t digit = DIGITS - 1 - (EACH * threadIdx.x + j);
+            sum += m[j] = MASS ? s.mass[digit] : s.count[digit];
         }
-        uint64_t before = block_before<DRAW_WAVES>(m[0] + m[1], s.wave_mass, total);
-        for (uint32_t j = 0; j < 2; ++j) {
-            if (before < target && target <= before + m[j]) s.found = digit[j], s.found_before = before, s.found_count = s.count[digit[j]];
+        uint64_t before = block_before<DRAW_WAVES>(sum, s.wave_mass, total);
+#pragma unroll
+        for (uint32_t j = 0; j < EACH; ++j) {
+            const uint32_t digit = DIGITS - 1 - (EACH * threadIdx.x + j);
+            if (before < target && target <= before + m[j]) s.found = digit, s.found_before = before, s.found_count = s.count[digit];
             before += m[j];
         }
         __syncthreads();
@@ -711,7 +700,7 @@ __device__ __forceinline__ uint64_t place_of(uint32_t key, uint32_t index) { ret
 
 // The same among the listed tokens, EACH_LISTED a thread, of which `target` is at most the sum of the weights (0: not to be cut): bins of the places between the first
 // and the last of them; those of the bin that the cut lies in again, until few are left, which are compared with one another.
-__device__ __forceinline__ Cut select_listed(const uint64_t (&place)[EACH_LISTED], uint64_t (&weight)[EACH_LISTED], uint64_t target, Shared &s)
+__device__ __forceinline__ Cut select_listed(const uint64_t (&place)[EACH_LISTED], uint64_t (&weight)[EACH_LISTED], uint32_t listed, uint64_t target, Shared &s)
 {
     const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
     constexpr uint64_t ALL = ~(uint64_t)0;
@@ -720,8 +709,9 @@ __device__ __forceinline__ Cut select_listed(const uint64_t (&place)[EACH_LISTED
         uint32_t n = 0;
 #pragma unroll
         for (uint32_t j = 0; j < EACH_LISTED; ++j) {
-            if (weight[j] == 0) continue;
-            most = place[j] > most ? place[j] : most, least = place[j] < least ? place[j] : least, ++n;
+            if (j * DRAW_THREADS >= listed) break;
+            const bool in = weight[j] != 0;
+            most = in && place[j] > most ? place[j] : most, least = in && place[j] < least ? place[j] : least, n += in;
         }
         most = wave_max(most, (uint64_t)0), least = wave_min(least, ALL), n = wave_sum(n);
         __syncthreads();
@@ -735,7 +725,7 @@ __device__ __forceinline__ Cut select_listed(const uint64_t (&place)[EACH_LISTED
         const int shift = spread < DRAW_THREADS ? 0 : 54 - __builtin_clzll(spread);         // spread >> shift is below 1024
 #pragma unroll
         for (uint32_t j = 0; j < EACH_LISTED; ++j)
-            if (weight[j]) add(s.mass[(most - place[j]) >> shift], weight[j]);
+            if (j * DRAW_THREADS < listed && weight[j]) add(s.mass[(most - place[j]) >> shift], weight[j]);
         __syncthreads();
         uint64_t total;
         const uint64_t m = s.mass[threadIdx.x], before = block_before<DRAW_WAVES>(m, s.wave_mass, total);
@@ -744,14 +734,15 @@ __device__ __forceinline__ Cut select_listed(const uint64_t (&place)[EACH_LISTED
         const uint32_t found = s.found;
         target -= s.found_before;
 #pragma unroll
-        for (uint32_t j = 0; j < EACH_LISTED; ++j) weight[j] = (most - place[j]) >> shift == found ? weight[j] : 0;
+        for (uint32_t j = 0; j < EACH_LISTED; ++j)
+            if (j * DRAW_THREADS < listed) weight[j] = (most - place[j]) >> shift == found ? weight[j] : 0;
     }
     __syncthreads();
     if (threadIdx.x == 0) s.n_few = 0;
     __syncthreads();
 #pragma unroll
     for (uint32_t j = 0; j < EACH_LISTED; ++j) {
-        if (weight[j] == 0) continue;
+        if (j * DRAW_THREADS >= listed || weight[j] == 0) continue;
         const uint32_t at = atomicAdd(&s.n_few, 1u);
         s.few[at] = place[j], s.few_weight[at] = weight[j];
     }
@@ -776,7 +767,7 @@ template <int DT> __global__ void __launch_bounds__(DRAW_THREADS) draw_kernel(Ro
     const Part &part = a.part[row * a.parts + ((threadIdx.x & 63) < a.parts ? threadIdx.x & 63 : 0)];
     const bool a_part = (threadIdx.x & 63) < a.parts;         // (lanes behind the parts add nothing)
     uint64_t low = a_part ? part.low : 0, weights = a_part ? part.all : 0;
-    uint32_t over = a_part ? part.over : 0;
+    uint32_t over = a_part ? part.over : 0, listed = a_part ? part.listed : 0;
     const Row r = a.rows[row];
     const How how(a, row);
     const bool good = how.good && top.good();
@@ -793,38 +784,57 @@ template <int DT> __global__ void __launch_bounds__(DRAW_THREADS) draw_kernel(Ro
     __syncthreads();
     Cut cut{0, a.vocab - 1};
     if (how.cuts()) {
-        bool done = r.listed <= LISTED;
+        // where each part's list begins among all
+        const bool whole = wave_max(listed, 0u) <= PART_LISTED;
+        const uint32_t lists = wave_up_to(listed), all_listed = of_lane(lists, 63);
+        bool done = whole && all_listed <= LISTED;
         if (done) {
             uint64_t place[EACH_LISTED], weight[EACH_LISTED], m[EACH_LISTED];
             uint32_t kept_too = 0;
             auto value_at = [&](uint32_t j) { return value_of((uint32_t)(place[j] >> 32)); };
-            auto mine = [&](uint32_t j) { return j * DRAW_THREADS + threadIdx.x < r.listed; };
+            auto mine = [&](uint32_t j) { return j * DRAW_THREADS + threadIdx.x < all_listed; };
 #pragma unroll
             for (uint32_t j = 0; j < EACH_LISTED; ++j) {
-                const uint32_t i = j * DRAW_THREADS + threadIdx.x;
-                const Listed l = i < r.listed ? a.list[row * LISTED + i] : Listed{LEAST_KEY, 0};
-                place[j] = place_of(l.key, l.index), m[j] = 0;
-                if (j * DRAW_THREADS < r.listed) {
-                    const double x = w.value(value_of(l.key));
-                    m[j] = mine(j) ? w.whole(x) : 0, kept_too |= mine(j) && least.keeps(x, l.index) ? 1u << j : 0;
+                place[j] = place_of(LEAST_KEY, 0), m[j] = weight[j] = 0;
+                if (j * DRAW_THREADS < all_listed) {
+                    const uint32_t i = j * DRAW_THREADS + threadIdx.x;
+                    uint32_t p = 0, begin = 0;
+                    for (uint32_t q = 0; q + 1 < a.parts; ++q) {
+                        const uint32_t end = of_lane(lists, q);
+                        p = i >= end ? q + 1 : p, begin = i >= end ? end : begin;
+                    }
+                    if (mine(j)) {
+                        const Listed l = a.list[(row * a.parts + p) * PART_LISTED + i - begin];
+                        place[j] = place_of(l.key, l.index);
+                    }
                 }
+            }
+#pragma unroll
+            for (uint32_t j = 0; j < EACH_LISTED; ++j) {
+                if (j * DRAW_THREADS >= all_listed) break;
+                const double x = w.value(value_at(j));
+                m[j] = mine(j) ? w.whole(x) : 0, kept_too |= mine(j) && least.keeps(x, 0xFFFFFFFFu - (uint32_t)place[j]) ? 1u << j : 0;
             }
             low = wave_sum(low), weights = wave_sum(weights), over = wave_sum(over);
             auto keeps = [&](uint32_t j) { return cut.keeps((uint32_t)(place[j] >> 32), 0xFFFFFFFFu - (uint32_t)place[j]); };
             if (how.top_k) {
                 uint32_t in = 0, all;
 #pragma unroll
-                for (uint32_t j = 0; j < EACH_LISTED; ++j) weight[j] = mine(j) && value_at(j) >= r.k_low && value_at(j) < r.k_high, in += (uint32_t)weight[j];
+                for (uint32_t j = 0; j < EACH_LISTED; ++j) {
+                    if (j * DRAW_THREADS >= all_listed) break;
+                    weight[j] = mine(j) && value_at(j) >= r.k_low && value_at(j) < r.k_high, in += (uint32_t)weight[j];
+                }
                 // (a plus infinity is no less than any border: it is over the list, and has been counted there)
                 block_before<DRAW_WAVES>(in, s.wave_count, all);
                 done = over < how.top_k && how.top_k - over <= all;
-                if (done) cut = select_listed(place, weight, how.top_k - over, s);
+                if (done) cut = select_listed(place, weight, all_listed, how.top_k - over, s);
             }
             if (how.by_mass && done) {
                 // (of all weights down to the end of top_k's list those are not kept that its cut leaves out)
                 uint64_t in = 0, out = 0, sum, left_out;
 #pragma unroll
                 for (uint32_t j = 0; j < EACH_LISTED; ++j) {
+                    if (j * DRAW_THREADS >= all_listed) break;
                     const bool here = value_at(j) >= r.p_low && value_at(j) < r.p_high, stays = keeps(j);
                     weight[j] = here && stays ? m[j] : 0;
                     in += weight[j], out += stays ? 0 : m[j];
@@ -834,12 +844,12 @@ template <int DT> __global__ void __launch_bounds__(DRAW_THREADS) draw_kernel(Ro
                 const double wanted = __builtin_ceil((double)how.top_p * (double)(weights - left_out));
                 const uint64_t target = wanted < 1.0 ? 1 : (uint64_t)wanted;
                 done = target > low && target <= low + sum;
-                if (done) cut = select_listed(place, weight, target - low, s);
+                if (done) cut = select_listed(place, weight, all_listed, target - low, s);
             }
             if (done) {
 #pragma unroll
                 for (uint32_t j = 0; j < EACH_LISTED; ++j)
-                    if (kept_too >> j & 1 && keeps(j)) add(s.run_mass[(0xFFFFFFFFu - (uint32_t)place[j]) / a.run], m[j]);
+                    if (j * DRAW_THREADS < all_listed && kept_too >> j & 1 && keeps(j)) add(s.run_mass[(0xFFFFFFFFu - (uint32_t)place[j]) / a.run], m[j]);
             }
         }
         if (__builtin_expect(!done, 0)) {
@@ -934,7 +944,7 @@ inline uint32_t part_of(size_t rows, size_t vocab)
     return (uint32_t)(pieces * PART_WAVES * PIECE);
 }
 inline size_t most_parts(size_t rows) { return rows * MAX_PARTS < rows + WORKGROUPS ? rows * MAX_PARTS : rows + WORKGROUPS; }
-constexpr size_t PART_BYTES = sizeof(Part) + BINS * 4, ROW_BYTES = sizeof(Row) + LISTED * sizeof(Listed);
+constexpr size_t PART_BYTES = sizeof(Part) + BINS * 4 + PART_LISTED * sizeof(Listed), ROW_BYTES = sizeof(Row);
 static_assert(sizeof(Part) % 16 == 0 && sizeof(Row) % 16 == 0, "what follows is aligned");
 
 }  // namespace

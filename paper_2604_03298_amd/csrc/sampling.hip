@@ -15,11 +15,11 @@ using namespace lowbit;
 //   3. draw: the cuts are picked from the list; then the token is drawn by the kept weights of each run of logits, and of one run's.
 // Where a cut turns out to lie outside the list, or the list is too short (many ties, scales without sense), the third launch finds the cut's key from its highest
 // bits down instead, which takes up to three passes over the row a cut and is always right.
-constexpr uint32_t PART_THREADS = 512, PART_WAVES = PART_THREADS / 64, DRAW_THREADS = 1024, DRAW_WAVES = DRAW_THREADS / 64;
+constexpr uint32_t PART_THREADS = 512, PART_WAVES = PART_THREADS / 64, DRAW_THREADS = 512, DRAW_WAVES = DRAW_THREADS / 64;
 constexpr uint32_t VEC = 8, PIECE = 64 * VEC, CHUNK = DRAW_THREADS * VEC;
 constexpr uint32_t MAX_VOCAB = 1u << 22, MAX_PARTS = 16, WORKGROUPS = 512;
 constexpr uint32_t FULLY_COUNTED = 16384;               // a vocabulary up to that
-constexpr uint32_t BINS = 2048, DIGITS = 2048, EACH_LISTED = 8, LISTED = EACH_LISTED * DRAW_THREADS, PART_LISTED = 4096, SAMPLE = 128;
+constexpr uint32_t BINS = 2048, DIGITS = 2048, LISTED = 6144, PART_LISTED = 4096, SAMPLE = 128;
 
 struct Part {
     uint32_t key, first;                // its largest logit's, and that logit's index
@@ -263,7 +263,9 @@ template <uint32_t WAVES, class T> __device__ __forceinline__ T block_before(T v
     __syncthreads();
     if (lane == 63) waves[wave] = up_to;
     __syncthreads();
-    const T sums = wave_up_to(lane < WAVES ? waves[lane & 15] : (T)0);
+    T sums = lane < WAVES ? waves[lane & 15] : (T)0;
+    sums += moved<0x111, 15>(sums, (T)0), sums += moved<0x112, 15>(sums, (T)0), sums += moved<0x114, 15>(sums, (T)0);
+    if constexpr (WAVES > 8) sums += moved<0x118, 15>(sums, (T)0);
     total = of_lane(sums, WAVES - 1);
     return (wave ? of_lane(sums, wave - 1) : (T)0) + (up_to - v);
 }
@@ -603,14 +605,16 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
 
 // ---- 3 ------------------------------------------------------------------------------
 
-constexpr uint32_t FEW = 64;
+constexpr uint32_t FEW = 64;                            // a wave's
+constexpr uint32_t TOGETHER = 4;                        // listed tokens that a thread asks for at once
 struct Shared {
     uint64_t mass[DIGITS];
     uint32_t count[DIGITS];
-    uint64_t wave_mass[16], wave_most[16], wave_least[16];
+    uint64_t wave_mass[16], wave_most[DRAW_WAVES], wave_least[DRAW_WAVES];
     uint32_t wave_count[16];
     uint64_t run_mass[MAX_PARTS * PART_WAVES];      // kept weights of each wave's run
     uint64_t few[FEW], few_weight[FEW];
+    uint64_t place[LISTED], weight[LISTED];         // the listed tokens'; in the weights' top bits whether min_p keeps them
     uint64_t found_before, found_place;
     uint32_t found, found_count, n_few;
 };
@@ -698,59 +702,59 @@ template <int DT, bool MASS> __device__ __forceinline__ Cut select(const Rows &a
 // A token's place in the order as one number, the first of the order having the largest.
 __device__ __forceinline__ uint64_t place_of(uint32_t key, uint32_t index) { return (uint64_t)key << 32 | (0xFFFFFFFFu - index); }
 
-// The same among the listed tokens, EACH_LISTED a thread, of which `target` is at most the sum of the weights (0: not to be cut): bins of the places between the first
-// and the last of them; those of the bin that the cut lies in again, until few are left, which are compared with one another.
-__device__ __forceinline__ Cut select_listed(const uint64_t (&place)[EACH_LISTED], uint64_t (&weight)[EACH_LISTED], uint32_t listed, uint64_t target, Shared &s)
+// The same among the listed tokens whose places are from `low` to `high`, of which `target` is at most the sum of the weights (each token's is one if not MASS): bins
+// between these places, then between those of the bin that the cut lies in, until few are left, which are compared with one another.  The loops are not unrolled, and
+// the list stands in shared memory for that: with one workgroup for a row, most of this kernel's time went into the fetching of its instructions.
+constexpr uint64_t KEPT = (uint64_t)1 << 63;
+__device__ __forceinline__ Cut select_listed(uint32_t listed, uint64_t low, uint64_t high, bool mass, uint64_t target, Shared &s)
 {
-    const uint32_t lane = threadIdx.x & 63, wave = threadIdx.x >> 6;
-    constexpr uint64_t ALL = ~(uint64_t)0;
-    for (;;) {
-        uint64_t most = 0, least = ALL;
-        uint32_t n = 0;
+    int shift;
+#pragma unroll 1
+    do {
+        const uint64_t spread = high - low;
+        shift = spread < DRAW_THREADS ? 0 : 64 - __builtin_ctz(DRAW_THREADS) - __builtin_clzll(spread);         // spread >> shift is below DRAW_THREADS
+        s.mass[threadIdx.x] = 0, s.count[threadIdx.x] = 0;
+        if (threadIdx.x == 0) s.n_few = 0;
+        __syncthreads();
+#pragma unroll 1
+        for (uint32_t j = threadIdx.x; j < listed; j += TOGETHER * DRAW_THREADS) {
+            uint64_t place[TOGETHER], m[TOGETHER];
 #pragma unroll
-        for (uint32_t j = 0; j < EACH_LISTED; ++j) {
-            if (j * DRAW_THREADS >= listed) break;
-            const bool in = weight[j] != 0;
-            most = in && place[j] > most ? place[j] : most, least = in && place[j] < least ? place[j] : least, n += in;
+            for (uint32_t i = 0; i < TOGETHER; ++i) {
+                const uint32_t at = j + i * DRAW_THREADS < listed ? j + i * DRAW_THREADS : j;
+                place[i] = s.place[at], m[i] = s.weight[at];
+            }
+#pragma unroll
+            for (uint32_t i = 0; i < TOGETHER; ++i) {
+                if (j + i * DRAW_THREADS >= listed || place[i] < low || place[i] > high) continue;
+                const uint32_t bin = (uint32_t)((high - place[i]) >> shift);
+                add(s.mass[bin], mass ? m[i] & ~KEPT : 1);
+                atomicAdd(&s.count[bin], 1u);
+            }
         }
-        most = wave_max(most, (uint64_t)0), least = wave_min(least, ALL), n = wave_sum(n);
-        __syncthreads();
-        s.mass[threadIdx.x] = 0;
-        if (lane == 0) s.wave_most[wave] = most, s.wave_least[wave] = least, s.wave_count[wave] = n;
-        __syncthreads();
-        const bool there = lane < DRAW_WAVES;
-        most = wave_max(there ? s.wave_most[lane & 15] : 0, (uint64_t)0), least = wave_min(there ? s.wave_least[lane & 15] : ALL, ALL);
-        if (wave_sum(there ? s.wave_count[lane & 15] : 0) <= FEW) break;
-        const uint64_t spread = most - least;
-        const int shift = spread < DRAW_THREADS ? 0 : 54 - __builtin_clzll(spread);         // spread >> shift is below 1024
-#pragma unroll
-        for (uint32_t j = 0; j < EACH_LISTED; ++j)
-            if (j * DRAW_THREADS < listed && weight[j]) add(s.mass[(most - place[j]) >> shift], weight[j]);
         __syncthreads();
         uint64_t total;
         const uint64_t m = s.mass[threadIdx.x], before = block_before<DRAW_WAVES>(m, s.wave_mass, total);
-        if (before < target && target <= before + m) s.found = threadIdx.x, s.found_before = before;
+        if (before < target && target <= before + m) s.found = threadIdx.x, s.found_before = before, s.found_count = s.count[threadIdx.x];
         __syncthreads();
-        const uint32_t found = s.found;
-        target -= s.found_before;
-#pragma unroll
-        for (uint32_t j = 0; j < EACH_LISTED; ++j)
-            if (j * DRAW_THREADS < listed) weight[j] = (most - place[j]) >> shift == found ? weight[j] : 0;
-    }
-    __syncthreads();
-    if (threadIdx.x == 0) s.n_few = 0;
-    __syncthreads();
-#pragma unroll
-    for (uint32_t j = 0; j < EACH_LISTED; ++j) {
-        if (j * DRAW_THREADS >= listed || weight[j] == 0) continue;
+        target -= s.found_before, high -= (uint64_t)s.found << shift;
+        const uint64_t rest = ((uint64_t)1 << shift) - 1;
+        low = high - low > rest ? high - rest : low;
+    } while (s.found_count > FEW);
+#pragma unroll 1
+    for (uint32_t i = threadIdx.x; i < listed; i += DRAW_THREADS) {
+        const uint64_t place = s.place[i];
+        if (place < low || place > high) continue;
         const uint32_t at = atomicAdd(&s.n_few, 1u);
-        s.few[at] = place[j], s.few_weight[at] = weight[j];
+        s.few[at] = place, s.few_weight[at] = mass ? s.weight[i] & ~KEPT : 1;
     }
     __syncthreads();
-    if (threadIdx.x < s.n_few) {
-        const uint64_t mine = s.few[threadIdx.x], own = s.few_weight[threadIdx.x];
+    if (threadIdx.x < 64) {                             // (a lane each)
+        const uint32_t n = __builtin_amdgcn_readfirstlane(s.n_few);
+        const uint64_t mine = threadIdx.x < n ? s.few[threadIdx.x] : 0, own = threadIdx.x < n ? s.few_weight[threadIdx.x] : 0;
         uint64_t sum = 0;
-        for (uint32_t i = 0; i < s.n_few; ++i) sum += s.few[i] > mine ? s.few_weight[i] : 0;
+#pragma unroll 1
+        for (uint32_t i = 0; i < n; ++i) sum += of_lane(mine, i) > mine ? of_lane(own, i) : 0;
         if (sum < target && target <= sum + own) s.found_place = mine;
     }
     __syncthreads();
@@ -789,67 +793,66 @@ template <int DT> __global__ void __launch_bounds__(DRAW_THREADS) draw_kernel(Ro
         const uint32_t lists = wave_up_to(listed), all_listed = of_lane(lists, 63);
         bool done = whole && all_listed <= LISTED;
         if (done) {
-            uint64_t place[EACH_LISTED], weight[EACH_LISTED], m[EACH_LISTED];
-            uint32_t kept_too = 0;
-            auto value_at = [&](uint32_t j) { return value_of((uint32_t)(place[j] >> 32)); };
-            auto mine = [&](uint32_t j) { return j * DRAW_THREADS + threadIdx.x < all_listed; };
+            // top_k's part of the list, from its border to below the upper one (a plus infinity is no less than any border: it is over the list, and was counted there)
+            uint64_t k_low = (uint64_t)key_of(r.k_low) << 32, k_high = ((uint64_t)key_of(r.k_high) << 32) - 1, most = 0, least_place = ~(uint64_t)0;
+            uint32_t in_k = 0, all_k;
+#pragma unroll 1
+            for (uint32_t j = threadIdx.x; j < all_listed; j += TOGETHER * DRAW_THREADS) {
+                Listed l[TOGETHER];
+                uint32_t p[TOGETHER] = {}, begin[TOGETHER] = {};
+#pragma unroll 1
+                for (uint32_t q = 0; q + 1 < a.parts; ++q) {
+                    const uint32_t end = of_lane(lists, q);
 #pragma unroll
-            for (uint32_t j = 0; j < EACH_LISTED; ++j) {
-                place[j] = place_of(LEAST_KEY, 0), m[j] = weight[j] = 0;
-                if (j * DRAW_THREADS < all_listed) {
-                    const uint32_t i = j * DRAW_THREADS + threadIdx.x;
-                    uint32_t p = 0, begin = 0;
-                    for (uint32_t q = 0; q + 1 < a.parts; ++q) {
-                        const uint32_t end = of_lane(lists, q);
-                        p = i >= end ? q + 1 : p, begin = i >= end ? end : begin;
-                    }
-                    if (mine(j)) {
-                        const Listed l = a.list[(row * a.parts + p) * PART_LISTED + i - begin];
-                        place[j] = place_of(l.key, l.index);
-                    }
+                    for (uint32_t i = 0; i < TOGETHER; ++i)
+                        if (j + i * DRAW_THREADS >= end) p[i] = q + 1, begin[i] = end;
+                }
+#pragma unroll
+                for (uint32_t i = 0; i < TOGETHER; ++i)                     // (loads that do not wait for one another)
+                    l[i] = j + i * DRAW_THREADS < all_listed ? a.list[(row * a.parts + p[i]) * PART_LISTED + (j + i * DRAW_THREADS - begin[i])] : Listed{};
+#pragma unroll
+                for (uint32_t i = 0; i < TOGETHER; ++i) {
+                    if (j + i * DRAW_THREADS >= all_listed) break;
+                    const uint64_t place = place_of(l[i].key, l[i].index);
+                    const double x = w.value(value_of(l[i].key));
+                    s.place[j + i * DRAW_THREADS] = place, s.weight[j + i * DRAW_THREADS] = w.whole(x) | (least.keeps(x, l[i].index) ? KEPT : 0);
+                    most = place > most ? place : most, least_place = place < least_place ? place : least_place;
+                    in_k += place >= k_low && place <= k_high;
                 }
             }
-#pragma unroll
-            for (uint32_t j = 0; j < EACH_LISTED; ++j) {
-                if (j * DRAW_THREADS >= all_listed) break;
-                const double x = w.value(value_at(j));
-                m[j] = mine(j) ? w.whole(x) : 0, kept_too |= mine(j) && least.keeps(x, 0xFFFFFFFFu - (uint32_t)place[j]) ? 1u << j : 0;
-            }
+            most = wave_max(most, (uint64_t)0), least_place = wave_min(least_place, ~(uint64_t)0);
             low = wave_sum(low), weights = wave_sum(weights), over = wave_sum(over);
-            auto keeps = [&](uint32_t j) { return cut.keeps((uint32_t)(place[j] >> 32), 0xFFFFFFFFu - (uint32_t)place[j]); };
+            if ((threadIdx.x & 63) == 0) s.wave_most[threadIdx.x >> 6] = most, s.wave_least[threadIdx.x >> 6] = least_place;
+            block_before<DRAW_WAVES>(in_k, s.wave_count, all_k);
+            most = wave_max(s.wave_most[threadIdx.x % DRAW_WAVES], (uint64_t)0), least_place = wave_min(s.wave_least[threadIdx.x % DRAW_WAVES], ~(uint64_t)0);
             if (how.top_k) {
-                uint32_t in = 0, all;
-#pragma unroll
-                for (uint32_t j = 0; j < EACH_LISTED; ++j) {
-                    if (j * DRAW_THREADS >= all_listed) break;
-                    weight[j] = mine(j) && value_at(j) >= r.k_low && value_at(j) < r.k_high, in += (uint32_t)weight[j];
-                }
-                // (a plus infinity is no less than any border: it is over the list, and has been counted there)
-                block_before<DRAW_WAVES>(in, s.wave_count, all);
-                done = over < how.top_k && how.top_k - over <= all;
-                if (done) cut = select_listed(place, weight, all_listed, how.top_k - over, s);
+                done = over < how.top_k && how.top_k - over <= all_k;
+                if (done) cut = select_listed(all_listed, k_low > least_place ? k_low : least_place, k_high < most ? k_high : most, false, how.top_k - over, s);
             }
+            const uint64_t cut_place = place_of(cut.key, cut.last);
             if (how.by_mass && done) {
                 // (of all weights down to the end of top_k's list those are not kept that its cut leaves out)
-                uint64_t in = 0, out = 0, sum, left_out;
-#pragma unroll
-                for (uint32_t j = 0; j < EACH_LISTED; ++j) {
-                    if (j * DRAW_THREADS >= all_listed) break;
-                    const bool here = value_at(j) >= r.p_low && value_at(j) < r.p_high, stays = keeps(j);
-                    weight[j] = here && stays ? m[j] : 0;
-                    in += weight[j], out += stays ? 0 : m[j];
+                uint64_t p_low = (uint64_t)key_of(r.p_low) << 32, p_high = ((uint64_t)key_of(r.p_high) << 32) - 1, in = 0, out = 0, sum, left_out;
+                p_low = p_low > cut_place ? p_low : cut_place, p_low = p_low > least_place ? p_low : least_place, p_high = p_high < most ? p_high : most;
+#pragma unroll 4
+                for (uint32_t i = threadIdx.x; i < all_listed; i += DRAW_THREADS) {
+                    const uint64_t place = s.place[i], m = s.weight[i] & ~KEPT;
+                    in += place >= p_low && place <= p_high ? m : 0, out += place >= cut_place ? 0 : m;
                 }
                 block_before<DRAW_WAVES>(in, s.wave_mass, sum);
                 block_before<DRAW_WAVES>(out, s.wave_mass, left_out);
                 const double wanted = __builtin_ceil((double)how.top_p * (double)(weights - left_out));
                 const uint64_t target = wanted < 1.0 ? 1 : (uint64_t)wanted;
                 done = target > low && target <= low + sum;
-                if (done) cut = select_listed(place, weight, all_listed, target - low, s);
+                if (done) cut = select_listed(all_listed, p_low, p_high, true, target - low, s);
             }
             if (done) {
-#pragma unroll
-                for (uint32_t j = 0; j < EACH_LISTED; ++j)
-                    if (j * DRAW_THREADS < all_listed && kept_too >> j & 1 && keeps(j)) add(s.run_mass[(0xFFFFFFFFu - (uint32_t)place[j]) / a.run], m[j]);
+                const uint64_t end = place_of(cut.key, cut.last);
+#pragma unroll 1
+                for (uint32_t i = threadIdx.x; i < all_listed; i += DRAW_THREADS) {
+                    const uint64_t place = s.place[i], m = s.weight[i];
+                    if (place >= end && m > KEPT) add(s.run_mass[(0xFFFFFFFFu - (uint32_t)place) / a.run], m & ~KEPT);
+                }
             }
         }
         if (__builtin_expect(!done, 0)) {
@@ -896,28 +899,30 @@ template <int DT> __global__ void __launch_bounds__(DRAW_THREADS) draw_kernel(Ro
 #pragma unroll 1
     for (uint32_t c = begin; c < end; c += CHUNK) {
         float v[VEC];
-        uint64_t m[VEC], sum = 0;
+        uint64_t sum = 0;
         const uint32_t first = c + threadIdx.x * VEC;
         const uint32_t there = load_chunk<DT>(a, row, first, end, v);
+        // of the chunk's j-th token, which then goes to the end of the eight
+        auto next = [&](uint32_t j) {
+            const float l = v[0];
+            const double x = w.value(l);
 #pragma unroll
-        for (uint32_t j = 0; j < VEC; ++j) {
-            const double x = w.value(v[j]);
-            m[j] = j < there && cut.keeps(key_of(v[j]), first + j) && least.keeps(x, first + j) ? w.whole(x) : 0;
-            sum += m[j];
-        }
+            for (uint32_t i = 0; i + 1 < VEC; ++i) v[i] = v[i + 1];
+            v[VEC - 1] = l;
+            return j < there && cut.keeps(key_of(l), first + j) && least.keeps(x, first + j) ? w.whole(x) : 0;
+        };
+#pragma unroll 4
+        for (uint32_t j = 0; j < VEC; ++j) sum += next(j);
         uint64_t before = block_before<DRAW_WAVES>(sum, s.wave_mass, all);
         if (all <= left) {
             left -= all;
             continue;
         }
+        if (left < before || left >= before + sum) return;
         uint64_t mine = 0;
         uint32_t token = 0;
-#pragma unroll
-        for (uint32_t j = 0; j < VEC; ++j) {
-            const bool here = before <= left && left < before + m[j];
-            mine = here ? m[j] : mine, token = here ? first + j : token;
-            before += m[j];
-        }
+#pragma unroll 1
+        for (uint32_t j = 0; j < VEC && left >= before; ++j) mine = next(j), token = first + j, before += mine;
         if (mine) {
             a.tokens[row] = (int32_t)token;
             if (a.log_probs) a.log_probs[row] = (float)-log1p((double)(total - mine) / (double)mine);

@@ -114,24 +114,23 @@ template <int K> __device__ __forceinline__ double series(double p, double r)
     else return series<K - 1>(__builtin_fma(p, r, TERM<K>), r);
 }
 struct Weights {
-    double top, scale, magic;           // the largest logit, 1 / (T ln 2)
-    bool infinite;                      // the largest is
+    double top, scale, least, magic;    // the largest logit, 1 / (T ln 2), and -60 of that (2^-60 is rounded to nothing)
+    // (infinities stand for 2^128, over all other floats, and are so far over them that these weigh nothing)
     __device__ __forceinline__ Weights(const Rows &a, const How &how, uint32_t most)
     {
-        infinite = most == INFINITY_KEY;
-        top = (double)value_of(infinite ? INFINITY_KEY - 1 : most), scale = 1.0 / LN2 / (double)how.temperature;
+        const bool infinite = most == INFINITY_KEY;
+        top = infinite ? 0x1p128 : (double)value_of(most), scale = infinite ? 1.0 : 1.0 / LN2 / (double)how.temperature;
+        least = infinite ? -60.0 : -60.0 * LN2 * (double)how.temperature;
         magic = __builtin_bit_cast(double, (uint64_t)(1023 + 52 - a.log_unit) << 52);
     }
     __device__ __forceinline__ double value(float v) const
     {
-        constexpr double WHOLE = 6755399441055744.0, NOTHING = -60.0;          // (2^-60 is rounded to nothing)
-        double t = __builtin_fmax(((double)v - top) * scale, NOTHING);
-        if (infinite) t = v == __builtin_inff() ? 0.0 : NOTHING;
-        const double shifted = t + WHOLE, r = t - (shifted - WHOLE);
-        const double p = series<10>(TERM<11>, r);
-        const uint64_t bits = __builtin_bit_cast(uint64_t, p);
-        const uint32_t n = (uint32_t)__builtin_bit_cast(uint64_t, shifted) << 20;
-        return __builtin_bit_cast(double, (uint64_t)((uint32_t)(bits >> 32) + n) << 32 | (uint32_t)bits);
+        constexpr double WHOLE = 6755399441055744.0;
+        const double d = __builtin_fmax(__builtin_fmin((double)v, top) - top, least);
+        const double shifted = __builtin_fma(d, scale, WHOLE), r = __builtin_fma(d, scale, WHOLE - shifted);
+        u32x2 p = __builtin_bit_cast(u32x2, series<10>(TERM<11>, r));
+        p[1] += __builtin_bit_cast(u32x2, shifted)[0] << 20;
+        return __builtin_bit_cast(double, p);
     }
     // as a whole number, and that on top of a constant, which sums take off in one go
     __device__ __forceinline__ uint64_t raised(double w) const { return __builtin_bit_cast(uint64_t, w + magic); }
@@ -540,42 +539,38 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
             for (uint32_t j = 0; j < VEC; ++j) any |= v[j] >= k_low;
             if (!__any(any)) return;                        // (a wave of tokens behind top_k's cut)
         }
-        uint32_t in = 0;
+        uint64_t in[VEC], some = 0;                         // lanes whose j-th logit is listed
         weighed += VEC;
         if (by_count || some_kept) {
 #pragma unroll
             for (uint32_t j = 0; j < VEC; ++j) {
-                in |= listed(v[j]) ? 1u << j : 0;
+                in[j] = __ballot(listed(v[j])), some |= in[j];
                 weigh(v[j], first + j);
             }
         } else {
 #pragma unroll
             for (uint32_t j = 0; j < VEC; ++j) {
-                in |= v[j] >= p_low && v[j] < p_high ? 1u << j : 0;
+                in[j] = __ballot(v[j] >= p_low && v[j] < p_high), some |= in[j];
                 const double x = w.value(v[j]);
-                all_weights += w.raised(x), low += w.raised(v[j] >= p_high ? x : 0.0);
+                u32x2 over = __builtin_bit_cast(u32x2, x);
+                over[1] = v[j] >= p_high ? over[1] : 0;     // (what is left of it is nothing)
+                all_weights += w.raised(x), low += w.raised(__builtin_bit_cast(double, over));
             }
         }
-        if (__any(in != 0)) {
-            // one addition a wave; the lanes' places by the bits of their counts
-            const uint32_t n = (uint32_t)__builtin_popcount(in);
-            uint32_t at = 0, sum = 0;
+        if (some) {
+            // one addition a wave, and a lane's place by the lanes before it
+            uint32_t sum = 0, at = 0;
 #pragma unroll
-            for (uint32_t k = 0; k < 4; ++k) {
-                const uint64_t set = __ballot(n >> k & 1);
-                at += (uint32_t)__builtin_amdgcn_mbcnt_hi((uint32_t)(set >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)set, 0)) << k;
-                sum += (uint32_t)__builtin_popcountll(set) << k;
-            }
+            for (uint32_t j = 0; j < VEC; ++j) sum += (uint32_t)__builtin_popcountll(in[j]);
             const uint32_t leader = (uint32_t)__builtin_ctzll(__ballot(1));
-            uint32_t base = 0;
-            if (lane == leader) base = atomicAdd(&n_listed, sum);
-            at += __builtin_amdgcn_readlane(base, leader);
+            if (lane == leader) at = atomicAdd(&n_listed, sum);
+            at = __builtin_amdgcn_readlane(at, leader);
 #pragma unroll
             for (uint32_t j = 0; j < VEC; ++j) {
-                if (in >> j & 1) {
-                    if (at < PART_LISTED) list[at] = Listed{key_of(v[j]), first + j};
-                    ++at;
-                }
+                if (in[j] == 0) continue;
+                const uint32_t to = at + __builtin_amdgcn_mbcnt_hi((uint32_t)(in[j] >> 32), __builtin_amdgcn_mbcnt_lo((uint32_t)in[j], 0));
+                if (in[j] >> lane & 1 && to < PART_LISTED) list[to] = Listed{key_of(v[j]), first + j};
+                at += (uint32_t)__builtin_popcountll(in[j]);
             }
         }
     });

@@ -1,8 +1,8 @@
 /*
  * libenec, second part -- what a decoding step reads, held in few bits, on AMD MI355X (gfx950): weights and activations in
  * microscaled 4-bit or blockwise 8-bit floating point with the products that read them, and a paged 8-bit cache of keys and values
- * with the rotation of positions on the way into it and the attention that reads it.  The codec of enec.h brings a layer's weights back bit for bit; this part is for the layers that are
- * kept in few bits instead, and for the cache, which has no exact form to return to.
+ * with the rotation of positions on the way into it and the attention that reads it.  The codec of enec.h brings a layer's weights back
+ * bit for bit; this part is for the layers that are kept in few bits instead, and for the cache, which has no exact form to return to.
  *
  * Conventions are those of enec.h: plain pointers and sizes, status codes of enec_status, all work enqueued on `stream`, no
  * device memory allocated by the library, a call returns as soon as its work is enqueued, and errors that the host can see return
@@ -166,7 +166,7 @@ int enec_cache_write(const enec_cache *cache, const enec_cache_batch *batch, con
  *   turns   DEVICE, fp32, positions x rotary / 2 pairs (cosine, sine), 8-byte aligned, without gaps
  *   rotary  a multiple of 16 from 16 to head_dim
  * A sequence whose length exceeds `positions` is left out, and told of like the others.
- * ENEC_E_ARG also if q_heads / kv_heads exceeds 65535, or (n_tokens div page_tokens + 2 batch) (2 kv_heads + q_heads) 2^30. */
+ * ENEC_E_ARG also if q_heads / kv_heads = g exceeds 65535, or (n_tokens div page_tokens + 2 batch) kv_heads (2 + (g + 3) div 4) reaches 2^31. */
 int enec_cache_write_rotated(const enec_cache *cache, const enec_cache_batch *batch, const void *k, size_t k_token_stride, size_t k_head_stride,
                              const void *v, size_t v_token_stride, size_t v_head_stride, const void *q, size_t q_token_stride, size_t q_head_stride,
                              void *q_out, size_t q_out_token_stride, size_t q_out_head_stride, uint32_t q_heads, int dtype, const void *turns,

@@ -934,7 +934,7 @@ using namespace enec::sampling;
 namespace {
 
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-inline bool sizes_ok(size_t rows, size_t vocab) { return vocab != 0 && vocab <= MAX_VOCAB && rows <= (1u << 24); }
+inline bool sizes_ok(size_t rows, size_t vocab) { return vocab != 0 && vocab <= MAX_VOCAB && rows <= (1u << 22); }      // (threads of a launch have 32 bits)
 // parts of a row, whole pieces for each wave: enough for the card, and no more than that many beyond one a row
 inline uint32_t part_of(size_t rows, size_t vocab)
 {

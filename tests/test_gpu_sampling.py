@@ -130,6 +130,29 @@ def test_rows_apart_and_at_odd_addresses(sampling):
         check(sampling, held[1:].as_strided((4, 2900), (2999, 1), 1), rng.random(4), top_k=[5, 50, 500, 0], top_p=[0.9, 0.5, 0.99, 0.7])
 
 
+def test_more_rows_than_parts_and_a_long_vocabulary(sampling):
+    """Rows that are not divided, weights of which some tokens are of a coarser unit, and rows of one value, whose cuts lie among more ties than any list holds."""
+    rng = np.random.default_rng(11)
+    for rows, vocab in ((600, 3001), (2, 300001)):
+        logits = rows_of(rng, rows, vocab, torch.float32)
+        logits[-1] = 1.5
+        check(sampling, logits, rng.random(rows), temperature=0.3 + rng.random(rows), top_k=rng.choice([0, 7, 1000, 2900], rows), top_p=rng.choice([0.5, 0.9, 1.0], rows),
+              min_p=rng.choice([0.0, 0.01], rows))
+
+
+def test_one_piece_of_memory_serves_fewer_rows(sampling):
+    rng = np.random.default_rng(13)
+    vocab = 20011
+    space = torch.empty(sampling.sample_workspace(300, vocab), dtype=torch.uint8, device="cuda")
+    for rows in (1, 33, 300):
+        space.fill_(0xFF)                                  # (whatever it held before)
+        logits, u, p = rows_of(rng, rows, vocab, torch.float32), torch.from_numpy(rng.random(rows).astype(np.float32)), torch.full((rows,), 0.9, device="cuda")
+        tokens = torch.empty(rows, dtype=torch.int32, device="cuda")
+        assert sampling.sample(logits, u.cuda(), tokens, top_p=p, workspace=space) == OK
+        l = logits.cpu().numpy().astype(np.float64)
+        assert tokens.tolist() == [draw(l[r], top_p=float(np.float32(0.9)), uniform=u[r].item())[0] for r in range(rows)]
+
+
 def test_draws_follow_the_probabilities(sampling):
     """4096 equally spaced numbers: each token is drawn as often as its share says, to within the one draw at either end."""
     rng = np.random.default_rng(7)

@@ -387,8 +387,9 @@ struct Top {
 
 template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(Rows a)
 {
-    __shared__ uint32_t waves[16], n_listed, over_of[PART_WAVES];
-    __shared__ float waves_f[16], k_mass, k_off;
+    __shared__ uint32_t n_listed, over_of[PART_WAVES];
+    __shared__ float k_mass, k_off, p_off;
+    __shared__ f32x4 sums_of[PART_WAVES];
     __shared__ uint64_t low_of[PART_WAVES], all_of[PART_WAVES];
     __shared__ uint32_t k_first, k_last, p_first, p_last, p_wide, few;
     __shared__ Listed list[PART_LISTED];
@@ -443,8 +444,8 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
     const uint32_t exact = a.vocab > FULLY_COUNTED ? top.grid.bin(counted) : BINS;
     const float cold = 1.0f / how.temperature, step = top.width * cold;
     const float middle_of_0 = (float)((((double)top.grid.base + 0.5) * (double)top.width - (double)value_of(top.key)) * (double)cold);
-    float e[EACH], e_sum = 0, e_all, v_sum = 0, v_before, v_all, c_sum = 0, c_all;
-    uint32_t n_sum = 0, n_all;
+    float e[EACH], e_sum = 0, v_sum = 0, c_sum = 0;
+    uint32_t n_sum = 0;
 #pragma unroll
     for (uint32_t j = 0; j < EACH; ++j) {
         const float d = middle_of_0 - (float)(b0 + j) * step, each = b0 + j == BINS - 1 ? 0.0f : d > 0.0f ? 1.0f : __expf(d);
@@ -454,13 +455,28 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
     }
     if (threadIdx.x == 0) {
         k_first = k_last = p_first = p_last = p_wide = BINS - 1, few = 0xFFFFFFFFu;
-        n_listed = 0, k_mass = k_off = 0;
+        n_listed = 0, k_mass = k_off = p_off = 0;
     }
-    const uint32_t n_before = block_before<PART_WAVES>(n_sum, waves, n_all);
-    const float e_before = block_before<PART_WAVES>(e_sum, waves_f, e_all);
+    // (the four sums over the threads before this one meet once)
+    const uint32_t n_to = wave_up_to(n_sum);
+    const float e_to = wave_up_to(e_sum), v_to = wave_up_to(v_sum), c_to = wave_up_to(c_sum);
+    if (lane == 63) sums_of[wave] = f32x4{f32_of_bits(n_to), e_to, v_to, c_to};
+    __syncthreads();
+    const f32x4 sums = lane < PART_WAVES ? sums_of[lane & (PART_WAVES - 1)] : f32x4{};
+    auto of_waves = [&](auto v, auto to, auto own, auto &all) {
+        using T = decltype(v);
+        v += moved<0x111, 15>(v, (T)0), v += moved<0x112, 15>(v, (T)0), v += moved<0x114, 15>(v, (T)0);
+        all = of_lane(v, PART_WAVES - 1);
+        return (wave ? of_lane(v, wave - 1) : (T)0) + (to - own);
+    };
+    static_assert(PART_WAVES <= 8, "three steps");
+    uint32_t n_all;
+    float e_all, v_all, c_all;
+    const uint32_t n_before = of_waves(bits_of(sums[0]), n_to, n_sum, n_all);
+    const float e_before = of_waves(sums[1], e_to, e_sum, e_all), v_before = of_waves(sums[2], v_to, v_sum, v_all), c_before = of_waves(sums[3], c_to, c_sum, c_all);
     if (how.top_k) {
         // the bins that the cut may lie in: four standard deviations around where it seems to
-        const float wanted = (float)how.top_k, c_before = block_before<PART_WAVES>(c_sum, waves_f, c_all);
+        const float wanted = (float)how.top_k;
         uint32_t before = n_before;
         float at = e_before, c = c_before;
 #pragma unroll
@@ -486,11 +502,10 @@ template <int DT> __global__ void __launch_bounds__(PART_THREADS) weigh_kernel(R
     if (how.by_mass) {
         // The same.  A share p of the sum of all is passed as early as what lies above is estimated too high and what lies below too low: p^2 and (1 - p)^2 of
         // their variances.  And half a bin's width for the estimate by middles, by far less where many tokens share in it.
-        v_before = block_before<PART_WAVES>(v_sum, waves_f, v_all);
         const float p = how.top_p > 1e-6f ? how.top_p : 1e-6f, target = p * e_all;
-        if (e_before < target && target <= e_before + e_sum) k_off = v_before + v_sum;
+        if (e_before < target && target <= e_before + e_sum) p_off = v_before + v_sum;
         __syncthreads();
-        const float off = 4.0f * __builtin_sqrtf((1.0f - p) * (1.0f - p) * k_off + p * p * (v_all - k_off > 0.0f ? v_all - k_off : 0.0f)), width = target * step;
+        const float off = 4.0f * __builtin_sqrtf((1.0f - p) * (1.0f - p) * p_off + p * p * (v_all - p_off > 0.0f ? v_all - p_off : 0.0f)), width = target * step;
         float at = e_before;
 #pragma unroll
         for (uint32_t j = 0; j < EACH; ++j) {

@@ -324,7 +324,7 @@ _BATCH = struct.Struct("=QQQIII4xQ")          # a BatchStruct: packed in one go,
 assert _BATCH.size == C.sizeof(BatchStruct)
 
 
-_int32 = None
+_int32 = _float32 = None
 
 
 def _batch(cache, x, y, table, starts, lengths, n_tokens, status, workspace=None):
@@ -372,26 +372,33 @@ def cache_write(cache, k, v, table, starts, lengths, status=None, stream=None) -
 def cache_write_rotated(cache, k, v, q, q_out, turns, table, starts, lengths, interleaved: bool = False, status=None, stream=None) -> int:
     """Enqueues enec_cache_write_rotated: cache_write with keys rotated by their positions, and q (tokens, q_heads, head_dim) into q_out.  q and
     q_out may be one tensor, or None: keys only.  turns: (positions, rotary / 2, 2) of fp32, cosines and sines."""
-    import torch
-    tokens, kt, kh, vt, vh = _tokens(k, v, cache.heads, cache.head_dim, "k and v")
-    if len(turns.shape) != 3 or turns.shape[2] != 2 or turns.dtype is not torch.float32 or not turns.is_contiguous():
+    global _float32
+    if _float32 is None:
+        import torch
+        _float32 = torch.float32
+    dim, device, shape = cache.head_dim, cache.device, turns.shape
+    tokens, kt, kh, vt, vh = _tokens(k, v, cache.heads, dim, "k and v")
+    if len(shape) != 3 or shape[2] != 2 or turns.dtype is not _float32 or not turns.is_contiguous():
         raise ValueError("turns: (positions, rotary / 2, 2) of fp32 without gaps are wanted")
-    if (q is None) != (q_out is None):
-        raise ValueError("q and q_out, or neither, are wanted")
-    heads, queries = 0, (None, 0, 0, None, 0, 0)
-    if q is not None:
-        if len(q.shape) != 3 or q.shape[0] != tokens or q.dtype != k.dtype:
+    if q is not None and q_out is not None:
+        q_shape = q.shape
+        heads = q_shape[1] if len(q_shape) == 3 else 0
+        q_tokens, qt, qh, ot, oh = _tokens(q, q_out, heads, dim, "q and q_out")
+        if q_tokens != tokens or q.dtype is not k.dtype:
             raise ValueError("q: as many tokens as k has, of its format, are wanted")
-        heads = q.shape[1]
-        _, qt, qh, ot, oh = _tokens(q, q_out, heads, cache.head_dim, "q and q_out")
-        queries = (q.data_ptr(), qt, qh, q_out.data_ptr(), ot, oh)
-        if not q.get_device() == q_out.get_device() == cache.device:
-            _on_gpu(cache.tensors[0], q, q_out)
-    if turns.get_device() != cache.device:
-        _on_gpu(cache.tensors[0], turns)
+        if not q.get_device() == q_out.get_device() == turns.get_device() == device:
+            _on_gpu(cache.tensors[0], q, q_out, turns)
+        q_at, out_at = q.data_ptr(), q_out.data_ptr()
+    elif q is None and q_out is None:
+        if turns.get_device() != device:
+            _on_gpu(cache.tensors[0], turns)
+        q_at = out_at = None
+        heads = qt = qh = ot = oh = 0
+    else:
+        raise ValueError("q and q_out, or neither, are wanted")
     b = _batch(cache, k, v, table, starts, lengths, tokens, status)
-    return lib().enec_cache_write_rotated(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, *queries, heads, _dtype(k), turns.data_ptr(),
-                                          turns.shape[0], 2 * turns.shape[1], int(interleaved), enec._stream_handle(stream))
+    return lib().enec_cache_write_rotated(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, q_at, qt, qh, out_at, ot, oh, heads, _dtype(k),
+                                          turns.data_ptr(), shape[0], 2 * shape[1], int(interleaved), enec._stream_handle(stream))
 
 
 def cache_read(cache, k, v, table, starts, lengths, status=None, stream=None) -> int:

@@ -273,6 +273,7 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_k
 // Chunk i lies at place i ^ turn(row): the sixteen lanes of a read's quarter are rows {0-3, 12-15} of one g and {4-11} of the next, and find sixteen places.
 // With X_INSIDE the workgroup brings the few tokens' 16-bit values into 8 bits itself, while its first weights are on their way.
 __device__ __forceinline__ uint32_t thin_turn(uint32_t r) { return (r >> 1 & 1) | (r >> 1 & 4); }
+constexpr uint32_t X_EACH = 4;                  // vectors of the tokens that a thread brings into 8 bits, at most
 template <bool EXACT, int X_INSIDE, int XT, int WAVES>
 __global__ void __launch_bounds__(64 * WAVES, 2) fp8_thin_kernel(Product8 a)
 {
@@ -311,8 +312,8 @@ __global__ void __launch_bounds__(64 * WAVES, 2) fp8_thin_kernel(Product8 a)
     uint32_t ws = scale_at(w_scales, wave), xs[XT], next_xs[XT];
 #pragma unroll
     for (uint32_t u = 0; u < XT; ++u) xs[u] = x_scale_at(u, wave);
-    // The tokens' values: sixteen threads a block, eight values each, the first ones asked for before any weights.
-    constexpr int DT = X_INSIDE ? X_INSIDE - 1 : 0, AHEAD = 4;
+    // The tokens' values: sixteen threads a block, eight values each, asked for before any weights.
+    constexpr int DT = X_INSIDE ? X_INSIDE - 1 : 0;
     const uint32_t per_row = a.groups * 16, all = X_INSIDE ? a.m * per_row : 0;
     auto load_x = [&](uint32_t i, float (&v)[8]) {
         const uint32_t r = i / per_row, col = (i - r * per_row) * 8;
@@ -336,21 +337,17 @@ __global__ void __launch_bounds__(64 * WAVES, 2) fp8_thin_kernel(Product8 a)
         *reinterpret_cast<u32x2 *>(x_codes + r * pitch + (col & ~127u) + ((col >> 4 & 7) ^ thin_turn(r)) * 16 + (col & 8)) = fp8_codes(v, byte);
         if ((i & 15) == 0) x_bytes[r * a.groups + (col >> 7)] = (uint8_t)byte;
     };
-    float first_x[AHEAD][8];
+    float x_values[X_EACH][8];
     if constexpr (X_INSIDE != 0) {
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) load_x(threadIdx.x + u * 64 * WAVES, first_x[u]);
+        for (uint32_t u = 0; u < X_EACH; ++u) load_x(threadIdx.x + u * 64 * WAVES, x_values[u]);
         __builtin_amdgcn_sched_barrier(0);
     }
 #pragma unroll
     for (uint32_t j = 0; j < 4; ++j) fetch(4 * wave + j, j);
     if constexpr (X_INSIDE != 0) {
 #pragma unroll
-        for (int u = 0; u < AHEAD; ++u) store_x(threadIdx.x + u * 64 * WAVES, first_x[u]);
-        for (uint32_t i = threadIdx.x + AHEAD * 64 * WAVES; i < all; i += 64 * WAVES) {
-            float v[8];
-            load_x(i, v), store_x(i, v);
-        }
+        for (uint32_t u = 0; u < X_EACH; ++u) store_x(threadIdx.x + u * 64 * WAVES, x_values[u]);
         asm volatile("s_waitcnt lgkmcnt(0)\n\ts_barrier" ::: "memory");
     }
     const uint32_t low = ((2 * g) ^ thin_turn(c)) * 16, high = ((2 * g + 1) ^ thin_turn(c)) * 16;
@@ -519,8 +516,15 @@ template <bool EXACT> bool launch_shape(const Product8 &a, const Plan &p, hipStr
     }
 }
 
-constexpr size_t X_INSIDE_BYTES = 32 * 1024;            // codes of the tokens that a workgroup makes itself
-inline bool x_inside(uint32_t m, uint32_t groups) { return m <= 16 && (size_t)m * groups * 128 <= X_INSIDE_BYTES; }
+// Waves of a workgroup for few tokens: with more of them more weights are on their way and fewer units follow one another in a wave, but more wait for one
+// another at the end.  With the tokens brought into 8 bits inside, which more threads do faster, 1 token x 4096 x 1024 / 2048 / 4096 / 8192 took 3.7 / 4.8 / 7.7 / 14.1 us with
+// two waves, 3.8 / 4.2 / 6.2 / 10.5 with four and 4.0 / 4.4 / 6.4 / 10.0 with eight; without, 8 tokens x 11008 x 4096 / 8192 14.8 / 22.3 with two, 16.4 / 24.8 with four, x 28672 x 8192
+// 51 and 49, x 4096 x 8192 13.7 and 12.9.
+// Bringing them into 8 bits inside saves a launch and costs every workgroup the work again: where four vectors a thread are enough, 1 token x 11008 x 4096 took 12.8 us
+// against 14.4, 4 tokens x 4096 x 2048 5.4 against 6.4, 2 tokens x 32003 x 4096, the worst found, 31.1 against 30.9; with eight a thread 2 tokens x 4096 x 4096 took 9.9
+// against 8.6, with thirty-two 16 tokens x 32003 x 2048 65 against 20.
+inline uint32_t waves_inside(uint32_t groups) { return groups <= 8 ? 2 : groups <= 32 ? 4 : 8; }
+inline bool x_inside(uint32_t m, uint32_t groups) { return m <= 16 && (uint64_t)m * groups * 16 <= X_EACH * 64 * waves_inside(groups); }
 
 template <bool EXACT, int X_INSIDE, int XT, int WAVES> bool launch_thin_of(const Product8 &a, hipStream_t s)
 {
@@ -528,17 +532,19 @@ template <bool EXACT, int X_INSIDE, int XT, int WAVES> bool launch_thin_of(const
     constexpr size_t RINGS = WAVES * 4 * (X_INSIDE ? 2048 : 2048 * (1 + XT));
     const size_t lds = RINGS + (X_INSIDE ? (size_t)a.m * a.groups * 129 : 0);
     const auto kernel = fp8_thin_kernel<EXACT, X_INSIDE, XT, WAVES>;
-    if (lds > 65536 && !allow_lds((const void *)kernel, RINGS + (X_INSIDE ? X_INSIDE_BYTES * 129 / 128 : 0), allowed)) return false;
+    if (lds > 65536 && !allow_lds((const void *)kernel, RINGS + (X_INSIDE ? X_EACH * 64 * WAVES * 8 * 129 / 128 : 0), allowed)) return false;
     kernel<<<up(a.n, 16), 64 * WAVES, lds, s>>>(a);
     return true;
 }
-template <bool EXACT, int X_INSIDE, int XT> bool launch_thin(const Product8 &a, hipStream_t s)
+template <int X_INSIDE> bool launch_thin_inside(const Product8 &a, hipStream_t s)
 {
-    const uint32_t units = up(a.groups, 4);
-    constexpr int MOST = XT > 2 ? 2 : XT > 1 ? 4 : 8;
-    if (units <= 8 || MOST == 2) return launch_thin_of<EXACT, X_INSIDE, XT, 2>(a, s);
-    if (units <= 16) return launch_thin_of<EXACT, X_INSIDE, XT, MOST < 4 ? MOST : 4>(a, s);
-    return launch_thin_of<EXACT, X_INSIDE, XT, MOST>(a, s);
+    const uint32_t waves = waves_inside(a.groups);
+    return waves == 2 ? launch_thin_of<false, X_INSIDE, 1, 2>(a, s) : waves == 4 ? launch_thin_of<false, X_INSIDE, 1, 4>(a, s) : launch_thin_of<false, X_INSIDE, 1, 8>(a, s);
+}
+template <bool EXACT, int XT> bool launch_thin(const Product8 &a, hipStream_t s)
+{
+    constexpr int MOST = XT > 2 ? 2 : 4;
+    return a.groups <= 32 ? launch_thin_of<EXACT, 0, XT, 2>(a, s) : launch_thin_of<EXACT, 0, XT, MOST>(a, s);
 }
 
 template <bool EXACT> int launch(Product8 a, void *parts, hipStream_t s)
@@ -551,7 +557,7 @@ template <bool EXACT> int launch(Product8 a, void *parts, hipStream_t s)
     bool ok = true;
     const Plan p = plan_of(a.m, a.n, a.groups, EXACT);
     if (p.shape < 0) {
-        ok = a.m <= 16 ? launch_thin<EXACT, 0, 1>(a, s) : a.m <= 32 ? launch_thin<EXACT, 0, 2>(a, s) : launch_thin<EXACT, 0, 4>(a, s);
+        ok = a.m <= 16 ? launch_thin<EXACT, 1>(a, s) : a.m <= 32 ? launch_thin<EXACT, 2>(a, s) : launch_thin<EXACT, 4>(a, s);
     } else {
         a.split_stages = p.split_stages;
         if (p.splits > 1) a.parts = static_cast<float *>(parts), a.part_row = part_row(a.n);
@@ -607,7 +613,7 @@ int enec_fp8_linear(const void *x, size_t m, size_t x_stride, int dtype, const v
                (uint32_t)k, (uint32_t)((k + 127) / 128), (uint32_t)fp8_scale_row(k), 0, 0, 0, dtype};
     if (k != 0 && x_inside(a.m, a.groups)) {
         a.x = static_cast<const uint8_t *>(x);
-        const bool ok = dtype == ENEC_BF16 ? launch_thin<false, BF16 + 1, 1>(a, s) : launch_thin<false, FP16 + 1, 1>(a, s);
+        const bool ok = dtype == ENEC_BF16 ? launch_thin_inside<BF16 + 1>(a, s) : launch_thin_inside<FP16 + 1>(a, s);
         return ok && hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
     }
     if (k != 0)

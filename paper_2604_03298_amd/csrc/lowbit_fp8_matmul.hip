@@ -47,6 +47,9 @@ __device__ __forceinline__ bf16x8 eight_values(const i32x8 &v, int q, int byte)
 // turn: a row's eight chunks of 16 bytes lie side by side, chunk i at place i ^ (row div 2 mod 8), so that the sixteen lanes of a read's quarter find
 // sixteen different places of 256 bytes.  A wave reads the next half stage into registers while it multiplies this one; the only barrier of a stage is between
 // its halves, when all waves have the second half in registers: the stage's buffer is free then, and the next stage has landed.
+// Bound by the matrix unit's power and the way of the tiles into LDS: 4096 x 28672 x 8192 (tokens, rows, columns) takes 724 us, 2660 TFLOP/s, with the unit busy for 65 to 70 % of the
+// cycles, at a clock that its power brings down to 1.5 to 1.8 GHz, and no read meeting another one's bank; the copies alone take 536 us of it (620 before lines were touched ahead, the
+// whole 735).  2048 x 11008 x 4096: 88 us, 2100 TFLOP/s, 344 tiles of 256 x 192 in two rounds.  EXACT: 96 x 4096 x 11008 22 us with its splits' join.
 template <bool EXACT, int RA, int RB, int WA, int WB, int BUFFERS>
 __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_kernel(Product8 a)
 {
@@ -58,7 +61,7 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_k
     uint8_t *scale_bytes = shared + BUFFERS * STAGE;        // of four stages, three in turn: four bytes of each row, then of each token
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, c = lane & 31;
     const uint32_t wa = wave % WA, wb = wave / WA;
-    // Workgroups are dealt out to the eight dies one by one: each die takes a run of tiles, in bands of tiles of tokens (see product_tile_kernel).
+    // Workgroups are dealt out to the eight dies one by one: each die takes a run of tiles, in bands of tiles of tokens (see product_tile_kernel; 4 and 8 took as long within 2 %).
     constexpr uint32_t BAND = 6;
     const uint32_t tiles = a.n_tiles * a.m_tiles, per_die = (tiles + 7) / 8, tile = blockIdx.x % 8 * per_die + blockIdx.x / 8;
     if (blockIdx.x / 8 >= per_die || tile >= tiles) return;
@@ -272,6 +275,7 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_k
 // multiplies sixteen rows and sixteen tokens over a whole block: a lane has row (or token) lane mod 16 and chunks 2 g and 2 g + 1 of its eight, g = lane div 16.
 // Chunk i lies at place i ^ turn(row): the sixteen lanes of a read's quarter are rows {0-3, 12-15} of one g and {4-11} of the next, and find sixteen places.
 // With X_INSIDE the workgroup brings the few tokens' 16-bit values into 8 bits itself, while its first weights are on their way.
+// 1 token x 28672 x 8192: 43 us, 5.5 TB/s; x 11008 x 4096 12.7, 3.6 TB/s, of which 4 to 5 us are a launch's start, the first weights' way and the join of the waves' sums.
 __device__ __forceinline__ uint32_t thin_turn(uint32_t r) { return (r >> 1 & 1) | (r >> 1 & 4); }
 constexpr uint32_t X_EACH = 4;                  // vectors of the tokens that a thread brings into 8 bits, at most
 template <bool EXACT, int X_INSIDE, int XT, int WAVES>
@@ -520,11 +524,17 @@ template <bool EXACT> bool launch_shape(const Product8 &a, const Plan &p, hipStr
 // another at the end.  With the tokens brought into 8 bits inside, which more threads do faster, 1 token x 4096 x 1024 / 2048 / 4096 / 8192 took 3.7 / 4.8 / 7.7 / 14.1 us with
 // two waves, 3.8 / 4.2 / 6.2 / 10.5 with four and 4.0 / 4.4 / 6.4 / 10.0 with eight; without, 8 tokens x 11008 x 4096 / 8192 14.8 / 22.3 with two, 16.4 / 24.8 with four, x 28672 x 8192
 // 51 and 49, x 4096 x 8192 13.7 and 12.9.
+// Where a compute unit has three workgroups, and some two, two waves are better: 1 token x 8192 / 11008 / 16384 / 32003 x 4096 took 10.1 / 12.8 / 16.1 / 27.2 us with four and
+// 10.5 / 12.6 / 17.3 / 29.8 with two (from the last-level cache 9.5 / 11.7 / 14.9 / 27.2 and 10.0 / 10.8 / 13.5 / 29.7), x 11008 / 32003 x 2048 7.1 / 14.8 and 6.7 / 13.5.
 // Bringing them into 8 bits inside saves a launch and costs every workgroup the work again: where four vectors a thread are enough, 1 token x 11008 x 4096 took 12.8 us
 // against 14.4, 4 tokens x 4096 x 2048 5.4 against 6.4, 2 tokens x 32003 x 4096, the worst found, 31.1 against 30.9; with eight a thread 2 tokens x 4096 x 4096 took 9.9
 // against 8.6, with thirty-two 16 tokens x 32003 x 2048 65 against 20.
-inline uint32_t waves_inside(uint32_t groups) { return groups <= 8 ? 2 : groups <= 32 ? 4 : 8; }
-inline bool x_inside(uint32_t m, uint32_t groups) { return m <= 16 && (uint64_t)m * groups * 16 <= X_EACH * 64 * waves_inside(groups); }
+inline uint32_t waves_inside(uint32_t n, uint32_t groups)
+{
+    const uint32_t per_unit = up(up(n, 16), UNITS);
+    return groups <= 8 ? 2 : groups <= 16 ? (per_unit <= 2 ? 4 : 2) : groups <= 32 ? (per_unit <= 2 || per_unit > 3 ? 4 : 2) : 8;
+}
+inline bool x_inside(uint32_t m, uint32_t n, uint32_t groups) { return m <= 16 && (uint64_t)m * groups * 16 <= X_EACH * 64 * waves_inside(n, groups); }
 
 template <bool EXACT, int X_INSIDE, int XT, int WAVES> bool launch_thin_of(const Product8 &a, hipStream_t s)
 {
@@ -538,7 +548,7 @@ template <bool EXACT, int X_INSIDE, int XT, int WAVES> bool launch_thin_of(const
 }
 template <int X_INSIDE> bool launch_thin_inside(const Product8 &a, hipStream_t s)
 {
-    const uint32_t waves = waves_inside(a.groups);
+    const uint32_t waves = waves_inside(a.n, a.groups);
     return waves == 2 ? launch_thin_of<false, X_INSIDE, 1, 2>(a, s) : waves == 4 ? launch_thin_of<false, X_INSIDE, 1, 4>(a, s) : launch_thin_of<false, X_INSIDE, 1, 8>(a, s);
 }
 template <bool EXACT, int XT> bool launch_thin(const Product8 &a, hipStream_t s)
@@ -611,7 +621,7 @@ int enec_fp8_linear(const void *x, size_t m, size_t x_stride, int dtype, const v
     uint8_t *x_codes = static_cast<uint8_t *>(workspace), *x_scales = x_codes + codes_space(m, k), *parts = x_scales + scales_space(m, k);
     Product8 a{x_codes, x_scales, static_cast<const uint8_t *>(codes), static_cast<const uint8_t *>(scales), y, x_stride, y_stride, 0, nullptr, (uint32_t)m, (uint32_t)n,
                (uint32_t)k, (uint32_t)((k + 127) / 128), (uint32_t)fp8_scale_row(k), 0, 0, 0, dtype};
-    if (k != 0 && x_inside(a.m, a.groups)) {
+    if (k != 0 && x_inside(a.m, a.n, a.groups)) {
         a.x = static_cast<const uint8_t *>(x);
         const bool ok = dtype == ENEC_BF16 ? launch_thin_inside<BF16 + 1>(a, s) : launch_thin_inside<FP16 + 1>(a, s);
         return ok && hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;

@@ -49,7 +49,7 @@ __device__ __forceinline__ bf16x8 eight_values(const i32x8 &v, int q, int byte)
 // its halves, when all waves have the second half in registers: the stage's buffer is free then, and the next stage has landed.
 // Bound by the matrix unit's power and the way of the tiles into LDS: 4096 x 28672 x 8192 (tokens, rows, columns) takes 724 us, 2660 TFLOP/s, with the unit busy for 65 to 70 % of the
 // cycles, at a clock that its power brings down to 1.5 to 1.8 GHz, and no read meeting another one's bank; the copies alone take 536 us of it (620 before lines were touched ahead, the
-// whole 735).  2048 x 11008 x 4096: 88 us, 2100 TFLOP/s, 344 tiles of 256 x 192 in two rounds.  EXACT: 96 x 4096 x 11008 22 us with its splits' join.
+// whole 735).  2048 x 11008 x 4096: 88 us, 2100 TFLOP/s, 473 tiles of 256 x 192 in two rounds.  EXACT: 96 x 4096 x 11008 22 us with its splits' join.
 template <bool EXACT, int RA, int RB, int WA, int WB, int BUFFERS>
 __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_kernel(Product8 a)
 {
@@ -61,8 +61,9 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_k
     uint8_t *scale_bytes = shared + BUFFERS * STAGE;        // of four stages, three in turn: four bytes of each row, then of each token
     const uint32_t lane = threadIdx.x & 63, wave = __builtin_amdgcn_readfirstlane(threadIdx.x >> 6), g = lane >> 5, c = lane & 31;
     const uint32_t wa = wave % WA, wb = wave / WA;
-    // Workgroups are dealt out to the eight dies one by one: each die takes a run of tiles, in bands of tiles of tokens (see product_tile_kernel; 4 and 8 took as long within 2 %).
-    constexpr uint32_t BAND = 6;
+    // Workgroups are dealt out to the eight dies one by one: each die takes a run of tiles, in bands of tiles of tokens (see product_tile_kernel).
+    // 4096 x 8192 x 28672 took 946 us with bands of one, 730 of four, 744 of six, 735 of eight, 745 of twelve.
+    constexpr uint32_t BAND = 4;
     const uint32_t tiles = a.n_tiles * a.m_tiles, per_die = (tiles + 7) / 8, tile = blockIdx.x % 8 * per_die + blockIdx.x / 8;
     if (blockIdx.x / 8 >= per_die || tile >= tiles) return;
     const uint32_t before = tile / (BAND * a.n_tiles) * BAND, band = a.m_tiles - before < BAND ? a.m_tiles - before : BAND;
@@ -275,7 +276,7 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_k
 // multiplies sixteen rows and sixteen tokens over a whole block: a lane has row (or token) lane mod 16 and chunks 2 g and 2 g + 1 of its eight, g = lane div 16.
 // Chunk i lies at place i ^ turn(row): the sixteen lanes of a read's quarter are rows {0-3, 12-15} of one g and {4-11} of the next, and find sixteen places.
 // With X_INSIDE the workgroup brings the few tokens' 16-bit values into 8 bits itself, while its first weights are on their way.
-// 1 token x 28672 x 8192: 43 us, 5.5 TB/s; x 11008 x 4096 12.7, 3.6 TB/s, of which 4 to 5 us are a launch's start, the first weights' way and the join of the waves' sums.
+// 1 token x 28672 x 8192: 43 us, 5.5 TB/s; x 11008 x 4096 12.7, 3.6 TB/s; 1024 x 1024, a launch's start, one way from memory and the join of the waves' sums, 3.4.
 __device__ __forceinline__ uint32_t thin_turn(uint32_t r) { return (r >> 1 & 1) | (r >> 1 & 4); }
 constexpr uint32_t X_EACH = 4;                  // vectors of the tokens that a thread brings into 8 bits, at most
 template <bool EXACT, int X_INSIDE, int XT, int WAVES>

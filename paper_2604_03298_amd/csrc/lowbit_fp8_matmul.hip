@@ -428,14 +428,16 @@ using namespace enec::lowbit;
 
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
-// The tiles there are; with one on every compute unit a stage takes `us`, for y in 16 and in 32 bits (fitted, as are plan_of's constants, to times of products of 1 to
-// 4096 tokens with matrices of 1024 x 4096 to 28672 x 8192, every tile and split forced).
+// The tiles there are.  With one on every compute unit a stage takes `us`, with two on each, where two fit, `us_two`; the same for y in 32 bits.  (These and plan_of's constants are
+// fitted to the times of 500 products of 1 to 4096 tokens with eighteen matrices from 1024 x 4096 to 28672 x 8192, every tile and split forced; its choices
+// are 0.6 % above the best ones in the mean and 26 % at worst, and of 252 other products 1.3 %, 16 of them more than 5 %, and 23 % at worst.)
 struct Shape {
     uint32_t rows, tokens;
-    double us, us_exact;
+    double us, us_two, us_exact, us_exact_two;
 };
 constexpr int SHAPES = 7, FIRST_EXACT = 3;
-constexpr Shape SHAPE[SHAPES] = {{256, 256, 1.52, 0}, {256, 192, 1.22, 0}, {256, 128, 0.88, 0}, {128, 128, 0.60, 1.08}, {128, 64, 0.36, 0.58}, {64, 64, 0.25, 0.37}, {64, 32, 0.225, 0.36}};
+constexpr Shape SHAPE[SHAPES] = {{256, 256, 1.30, 0, 0, 0},      {256, 192, 1.08, 0, 0, 0},        {256, 128, 0.79, 0, 0, 0},        {128, 128, 0.585, 0, 0.91, 0},
+                                 {128, 64, 0.40, 0.69, 0.53, 0.95}, {64, 64, 0.25, 0.40, 0.35, 0.555}, {64, 32, 0.215, 0.305, 0.34, 0.46}};
 constexpr uint32_t THIN = 64;                       // tokens at most of the kernel for few
 constexpr uint32_t UNITS = 256;                     // compute units
 constexpr uint32_t MOST_SPLITS = 16, UNIT = 4;      // a split is whole blocks of scales: so many stages, or a multiple
@@ -448,29 +450,38 @@ struct Plan {
 };
 inline bool too_large(const Shape &s, uint32_t m) { return s.tokens > 32 && s.tokens >= 2 * up(m, 16) * 16; }      // half of the tile or more would be empty
 
+inline uint32_t thin_tiles(uint32_t m) { return m <= 16 ? 1 : m <= 32 ? 2 : 4; }
+inline uint32_t thin_waves(uint32_t tiles, uint32_t groups) { return groups <= 32 || tiles > 2 ? 2 : 4; }
+
 Plan plan_of(uint32_t m, uint32_t n, uint32_t groups, bool exact)
 {
     Plan p{-1, 1, up(groups, UNIT) * UNIT};
-    const double matrix = (double)n * groups * 128, from_memory = matrix / 5.0e6 + 4;
+    const double matrix = (double)n * groups * 128, from_memory = matrix / 6.1e6 + 1.5;
+    // the weights' way from memory and the units' work overlap in part
+    const auto both = [&](double us) { return us > from_memory ? us + 0.38 * from_memory : from_memory + 0.38 * us; };
     double best = 1e300;
     if (m <= THIN) {
-        // every sixteen rows read all tokens again, at what the dies' caches give
-        const uint32_t tiles = m <= 16 ? 1 : m <= 32 ? 2 : 4;
-        const double cached = 3 + matrix * (1 + tiles) / 12.5e6;
-        best = cached > from_memory ? cached : from_memory;
+        // every sixteen rows read all tokens again; the unit with the most rows, or a wave's units one after the other, take the time
+        const uint32_t tiles = thin_tiles(m);
+        const double read = (double)up(up(n, 16), UNITS) * UNITS * 16 * groups * 128 * (1 + tiles) / (exact ? 13.8e6 : 19e6);
+        const double chain = up(up(groups, UNIT), thin_waves(tiles, groups)) * (exact ? 0.14 : 0.23) * (1 + tiles) / 2;
+        best = both(2 + (read > chain ? read : chain));
     }
     for (int i = exact ? FIRST_EXACT : 0; i < SHAPES; ++i) {
         const Shape &s = SHAPE[i];
         if (too_large(s, m)) continue;
         const uint64_t tiles = (uint64_t)up(n, s.rows) * up(m, s.tokens);
         const bool splittable = i >= FIRST_EXACT && (uint64_t)m * up(n, 4) < 1u << 31;
+        const double one = exact ? s.us_exact : s.us, two = exact ? s.us_exact_two : s.us_two, start = exact ? 3.1 : i >= FIRST_EXACT ? 2.3 : 6.8;
+        const uint32_t places = two > 0 ? 2 * UNITS : UNITS;
         for (uint32_t splits = 1; splits == 1 || (splittable && splits <= MOST_SPLITS && splits * UNIT <= groups && tiles * splits <= MOST_SPLIT_TILES); ++splits) {
             const uint32_t each = up(up(groups, splits), UNIT) * UNIT, count = up(groups, each);
-            const uint64_t all = tiles * count, rounds = (all + UNITS - 1) / UNITS;
-            // a workgroup's start and end are 3 us; units that have none leave the others more of the memory; joining is a launch, the sums' way out and back
-            const double stage = (exact ? s.us_exact : s.us) * (all <= 192 ? 0.87 : 1.0);
-            double us = (double)rounds * (each * stage + 3);
-            us = (us > from_memory ? us : from_memory) + (count > 1 ? 3 + (double)count * m * n * 8 / 4e6 : 0);
+            const uint64_t all = tiles * count, full = all / places, rest = all % places;
+            // whole rounds and what is left (units that have none leave the others more of the memory); joining is a launch, the sums' way out and back, one split after the other
+            double us = (double)full * (each * (two > 0 ? two : one) + start);
+            if (rest > UNITS) us += each * two + start;
+            else if (rest) us += each * one * (rest <= 192 ? 0.92 : 1) + start;
+            us = both(us) + (count > 1 ? 1.7 + 0.27 * count + (double)count * m * n * 8 / 5.4e6 : 0);
             if (us < best) best = us, p.shape = i, p.splits = count, p.split_stages = each;
         }
     }
@@ -555,7 +566,7 @@ template <int X_INSIDE> bool launch_thin_inside(const Product8 &a, hipStream_t s
 template <bool EXACT, int XT> bool launch_thin(const Product8 &a, hipStream_t s)
 {
     constexpr int MOST = XT > 2 ? 2 : 4;
-    return a.groups <= 32 ? launch_thin_of<EXACT, 0, XT, 2>(a, s) : launch_thin_of<EXACT, 0, XT, MOST>(a, s);
+    return thin_waves(XT, a.groups) == 2 ? launch_thin_of<EXACT, 0, XT, 2>(a, s) : launch_thin_of<EXACT, 0, XT, MOST>(a, s);
 }
 
 template <bool EXACT> int launch(Product8 a, void *parts, hipStream_t s)
@@ -568,7 +579,8 @@ template <bool EXACT> int launch(Product8 a, void *parts, hipStream_t s)
     bool ok = true;
     const Plan p = plan_of(a.m, a.n, a.groups, EXACT);
     if (p.shape < 0) {
-        ok = a.m <= 16 ? launch_thin<EXACT, 1>(a, s) : a.m <= 32 ? launch_thin<EXACT, 2>(a, s) : launch_thin<EXACT, 4>(a, s);
+        const uint32_t tiles = thin_tiles(a.m);
+        ok = tiles == 1 ? launch_thin<EXACT, 1>(a, s) : tiles == 2 ? launch_thin<EXACT, 2>(a, s) : launch_thin<EXACT, 4>(a, s);
     } else {
         a.split_stages = p.split_stages;
         if (p.splits > 1) a.parts = static_cast<float *>(parts), a.part_row = part_row(a.n);

@@ -152,11 +152,16 @@ def test_products_of_values(lowbit, m, n, k, dtype):
     assert (out[m] == 7).all()
 
 
-def test_long_sums_and_many_rows(lowbit):
-    """Splits of the columns, whole rounds of tiles and pieces of them; compared in 64 bits on the GPU."""
+@pytest.mark.parametrize("sizes", [((1, 5000, 16384), (16, 300, 30000), (40, 600, 16384), (96, 4096, 2560), (513, 2050, 1000), (1100, 2304, 640), (3, 70000, 257)),
+                                   ((409, 21914, 787), (263, 22171, 803), (131, 22829, 794)), ((65, 17501, 782), (65, 4239, 6236), (67, 4139, 4739)),
+                                   ((34, 16515, 798), (2062, 68, 4672), (2069, 65, 3561)), ((33, 8321, 813), (2118, 17, 3139), (66, 4194, 791), (1276, 17, 2435)),
+                                   ((68, 17, 784), (33, 17, 4718), (65, 17, 1540), (1, 17, 17567)), ((1, 17, 4100), (17, 17, 4595), (34, 17, 4400), (2, 8200, 2047))])
+def test_every_tile_and_split(lowbit, sizes):
+    """Long sums and many rows, and sizes at which each tile, alone and with splits of the columns, and each kernel for few tokens is the one that is chosen; compared in
+    64 bits on the GPU."""
     g = torch.Generator(device="cuda")
     g.manual_seed(1)
-    for m, n, k in ((1, 5000, 16384), (16, 300, 30000), (40, 600, 16384), (96, 4096, 2560), (513, 2050, 1000), (1100, 2304, 640), (3, 70000, 257)):
+    for m, n, k in sizes:
         x, w = (torch.randn(r, k, generator=g, device="cuda").to(torch.bfloat16) for r in (m, n))
         xc, xs = lowbit.fp8_empty(m, k)
         wc, ws = lowbit.fp8_empty(n, k)

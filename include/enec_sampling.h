@@ -40,7 +40,7 @@ typedef struct {
  * two); smaller ones than half of that are never drawn.
  * The token is -1, and log_probs NaN, of a row that has a NaN, nothing but minus infinities, or a temperature, top_p, min_p or uniform out of
  * range (T below zero or not finite, NaN, uniform outside [0, 1)).
- * ENEC_E_ARG also if vocab is 0 or exceeds 2^22, or rows exceed 2^22. */
+ * ENEC_E_ARG also if vocab is 0 or exceeds 2^22, or rows, or rows times the vocabulary's pieces of 65536 (at most 16), exceed 2^22. */
 size_t enec_sample_workspace(size_t rows, size_t vocab);
 int enec_sample(const void *logits, size_t rows, size_t vocab, size_t row_stride, int dtype, const enec_sampling *how, int32_t *tokens,
                 float *log_probs, void *workspace, size_t workspace_bytes, void *stream);

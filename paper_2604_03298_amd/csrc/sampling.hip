@@ -20,9 +20,9 @@ using namespace lowbit;
 // Threads of the third launch: with 1024 one row took 26.6 instead of 24.3 us with every filter, 64 rows with top_p, whose lists are long, 43.1 instead of 44.3.
 constexpr uint32_t PART_THREADS = 512, PART_WAVES = PART_THREADS / 64, DRAW_THREADS = 512, DRAW_WAVES = DRAW_THREADS / 64;
 constexpr uint32_t VEC = 8, PIECE = 64 * VEC, CHUNK = DRAW_THREADS * VEC;
-constexpr uint32_t MAX_VOCAB = 1u << 22, MAX_PARTS = 16, WORKGROUPS = 512;
+constexpr uint32_t MAX_VOCAB = 1u << 22, MAX_PARTS = 16, MOST_PART = 65536;
 constexpr uint32_t FULLY_COUNTED = 16384;               // a vocabulary up to that
-constexpr uint32_t BINS = 2048, DIGITS = 2048, LISTED = 6144, PART_LISTED = 4096, SAMPLE = 128;
+constexpr uint32_t BINS = 2048, DIGITS = 2048, LISTED = 6144, PART_LISTED = LISTED, SAMPLE = 128;
 
 struct Part {
     uint32_t key, first;                // its largest logit's, and that logit's index
@@ -952,16 +952,37 @@ using namespace enec::sampling;
 namespace {
 
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
-inline bool sizes_ok(size_t rows, size_t vocab) { return vocab != 0 && vocab <= MAX_VOCAB && rows <= (1u << 22); }      // (threads of a launch have 32 bits)
-// parts of a row, whole pieces for each wave: enough for the card, and no more than that many beyond one a row
+// Parts of a row, whole pieces for each wave: as long as there are fewer workgroups than compute units, of 4096 logits, and as long as there are fewer than four for each, of 16384; of no
+// more than 65536 (where 16 parts allow that).  64 rows of 32000 with top_p took 40 us in four parts and 44 in eight, 64 of 8000 38 in two and 50 in one; 256 of 131072 116 in four
+// and 121 in two, 128 of 50000 50 in four and 53 in seven; 512 of 131072 302 in two and 534 in one.
+constexpr size_t UNITS = 256;
+inline size_t least_parts(size_t vocab)
+{
+    const size_t parts = (vocab + MOST_PART - 1) / MOST_PART;
+    return parts < MAX_PARTS ? parts : MAX_PARTS;
+}
 inline uint32_t part_of(size_t rows, size_t vocab)
 {
-    size_t parts = rows ? WORKGROUPS / rows : 1;
-    parts = parts < 1 ? 1 : parts > MAX_PARTS ? MAX_PARTS : parts;
+    const auto up_to = [&](size_t each, size_t workgroups) {
+        const size_t by_length = (vocab + each - 1) / each, by_rows = workgroups / rows;
+        return by_length < by_rows ? by_length : by_rows;
+    };
+    const size_t few = up_to(4096, UNITS), many = up_to(16384, 4 * UNITS);
+    size_t parts = few > many ? few : many;
+    parts = parts < MAX_PARTS ? parts : MAX_PARTS, parts = parts > least_parts(vocab) ? parts : least_parts(vocab);
     const size_t pieces = (vocab + parts * PART_WAVES * PIECE - 1) / (parts * PART_WAVES * PIECE);
     return (uint32_t)(pieces * PART_WAVES * PIECE);
 }
-inline size_t most_parts(size_t rows) { return rows * MAX_PARTS < rows + WORKGROUPS ? rows * MAX_PARTS : rows + WORKGROUPS; }
+// of all rows together, however few they are
+inline size_t most_parts(size_t rows, size_t vocab)
+{
+    const size_t all = rows * MAX_PARTS < 4 * UNITS ? rows * MAX_PARTS : 4 * UNITS, long_ones = rows * least_parts(vocab);
+    return all > long_ones ? all : long_ones;
+}
+inline bool sizes_ok(size_t rows, size_t vocab)         // (threads of a launch have 32 bits)
+{
+    return vocab != 0 && vocab <= MAX_VOCAB && rows <= (1u << 22) && rows * least_parts(vocab) <= (1u << 22);
+}
 constexpr size_t PART_BYTES = sizeof(Part) + BINS * 4 + PART_LISTED * sizeof(Listed), ROW_BYTES = sizeof(Row);
 static_assert(sizeof(Part) % 16 == 0 && sizeof(Row) % 16 == 0, "what follows is aligned");
 
@@ -972,7 +993,7 @@ extern "C" {
 size_t enec_sample_workspace(size_t rows, size_t vocab)
 {
     if (!sizes_ok(rows, vocab) || rows == 0) return 0;
-    return most_parts(rows) * PART_BYTES + rows * ROW_BYTES;
+    return most_parts(rows, vocab) * PART_BYTES + rows * ROW_BYTES;
 }
 
 int enec_sample(const void *logits, size_t rows, size_t vocab, size_t row_stride, int dtype, const enec_sampling *how, int32_t *tokens, float *log_probs,

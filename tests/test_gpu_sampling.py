@@ -140,6 +140,14 @@ def test_more_rows_than_parts_and_a_long_vocabulary(sampling):
               min_p=rng.choice([0.0, 0.01], rows))
 
 
+def test_the_longest_vocabulary(sampling):
+    """2^22 tokens, also with a run of them that no filter cuts; the last ones are drawn, too."""
+    rng = np.random.default_rng(17)
+    logits = torch.from_numpy((3 * rng.standard_normal((3, 1 << 22))).astype(np.float32)).cuda()
+    logits[2, -1] = 40.0
+    check(sampling, logits, [0.3, 0.999, 0.5], temperature=[1.0, 0.7, 1.0], top_k=[1000, 0, 0], top_p=[0.9, 0.5, 1.0])
+
+
 def test_one_piece_of_memory_serves_fewer_rows(sampling):
     rng = np.random.default_rng(13)
     vocab = 20011

@@ -9,12 +9,12 @@ using namespace lowbit;
 
 // The order of a row is never made.  Three launches, the first two with a workgroup for each part of a row, the last with one for each row:
 //   1. survey: each part's largest logit, and a histogram of its logits in bins that ascend with them.  Logits well over the others are counted all, of the
-//      others one in eight, as atomics on LDS are what this launch would spend its time on (256 rows of 131072: all counted 123 us, one in four 52, one in eight 42;
-//      30 without cuts, 4.5 TB/s);
+//      others one in eight, as atomics on LDS are what this launch would spend its time on (256 rows of 131072 in two parts each: all counted 123 us, one in four 52, one in eight
+//      42, in four parts 37; without cuts 30, 4.5 TB/s);
 //   2. weigh: the histogram says about where a cut lies, and how far off that may be.  Weights of logits above are summed in 64 bits and their tokens counted, and
-//      the tokens in between, some tens to some thousands, are listed.  Bound by the vector unit, 21 instructions for a weight and some 10 around it: 59 us of those rows;
+//      the tokens in between, some tens to some thousands, are listed.  Bound by the vector unit, 21 instructions for a weight and some 10 around it: 64 us of those rows;
 //   3. draw: the cuts are picked from the list; then the token is drawn by the kept weights of each run of logits, and of one run's.  Bound by the latency of one workgroup:
-//      27 us of those rows, 11 of one row of 32003 with every filter, whose other launches take 4.5 and 10.
+//      26 us of those rows, 11 of one row of 32003 with every filter, whose other launches take 4.6 and 9.3.
 // Where a cut turns out to lie outside the list, or the list is too short (many ties, scales without sense), the third launch finds the cut's key from its highest
 // bits down instead, which takes up to three passes over the row a cut and is always right.
 // Threads of the third launch: with 1024 one row took 26.6 instead of 24.3 us with every filter, 64 rows with top_p, whose lists are long, 43.1 instead of 44.3.

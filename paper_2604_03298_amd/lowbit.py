@@ -91,6 +91,24 @@ def _on_gpu(*tensors):
             raise ValueError("tensors on one GPU are wanted")
 
 
+_current_device = _raw_stream = None
+
+
+def _stream_on(device, stream):
+    """The handle of the stream (None: the current one) that a call with tensors on this GPU is enqueued on.  The GPU has to be the current one, where kernels are launched, and the
+    stream its own."""
+    global _current_device, _raw_stream
+    if _current_device is None:
+        import torch
+        _current_device, _raw_stream = torch._C._cuda_getDevice, getattr(torch._C, "_cuda_getCurrentRawStream", None)
+    if device >= 0:
+        if device != _current_device() or (stream is not None and stream.device.index != device):
+            raise ValueError("the tensors' GPU is not the current one, or not the stream's")
+        if stream is None and _raw_stream is not None:
+            return _raw_stream(device)
+    return enec._stream_handle(stream)
+
+
 def _rows(t, what):
     """(rows, columns, row stride) of a matrix whose rows are runs."""
     shape = t.shape                                         # (an attribute of a tensor costs 0.1 us: each is asked for once)
@@ -234,10 +252,11 @@ def fp8_quantize(src, codes, scales, stream=None) -> int:
     _same_padding(padded, cols)
     if n != rows:
         raise ValueError("src and codes differ in their rows")
-    if not src.get_device() == codes.get_device() == scales.get_device() >= 0:
+    device = codes.get_device()
+    if not src.get_device() == device == scales.get_device() >= 0:
         _on_gpu(src, codes, scales)
     return lib().enec_fp8_quantize(src.data_ptr(), rows, cols, stride, _dtype(src), codes.data_ptr(), scales.data_ptr(),
-                                   enec._stream_handle(stream))
+                                   _stream_on(device, stream))
 
 
 def fp8_dequantize(codes, scales, out, stream=None) -> int:
@@ -247,10 +266,11 @@ def fp8_dequantize(codes, scales, out, stream=None) -> int:
     _same_padding(padded, cols)
     if n != rows:
         raise ValueError("out and codes differ in their rows")
-    if not codes.get_device() == scales.get_device() == out.get_device() >= 0:
+    device = codes.get_device()
+    if not device == scales.get_device() == out.get_device() >= 0:
         _on_gpu(codes, scales, out)
     return lib().enec_fp8_dequantize(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), stride, _dtype(out),
-                                     enec._stream_handle(stream))
+                                     _stream_on(device, stream))
 
 
 def fp8_linear_workspace(m: int, n: int, k: int) -> int:
@@ -269,7 +289,7 @@ def fp8_linear(x, codes, scales, out, workspace=None, stream=None) -> int:
         _on_gpu(x, codes, scales, out, workspace)
     ws, size = _space(workspace)
     return lib().enec_fp8_linear(x.data_ptr(), m, x_stride, _dtype(x), codes.data_ptr(), scales.data_ptr(), n, k, out.data_ptr(), y_stride,
-                                 ws, size, enec._stream_handle(stream))
+                                 ws, size, _stream_on(codes.get_device(), stream))
 
 
 def fp8_matmul_workspace(m: int, n: int, k: int) -> int:
@@ -288,7 +308,7 @@ def fp8_matmul(x_codes, x_scales, codes, scales, out, workspace=None, stream=Non
         _on_gpu(x_codes, x_scales, codes, scales, out, workspace)
     ws, size = _space(workspace)
     return lib().enec_fp8_matmul(x_codes.data_ptr(), x_scales.data_ptr(), m, codes.data_ptr(), scales.data_ptr(), n, padded, out.data_ptr(),
-                                 y_stride, _dtype(out), ws, size, enec._stream_handle(stream))
+                                 y_stride, _dtype(out), ws, size, _stream_on(codes.get_device(), stream))
 
 
 # ---- the cache ----------------------------------------------------------------------
@@ -398,7 +418,7 @@ def cache_write_rotated(cache, k, v, q, q_out, turns, table, starts, lengths, in
         raise ValueError("q and q_out, or neither, are wanted")
     b = _batch(cache, k, v, table, starts, lengths, tokens, status)
     return lib().enec_cache_write_rotated(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, q_at, qt, qh, out_at, ot, oh, heads, _dtype(k),
-                                          turns.data_ptr(), shape[0], 2 * shape[1], int(interleaved), enec._stream_handle(stream))
+                                          turns.data_ptr(), shape[0], 2 * shape[1], int(interleaved), _stream_on(device, stream))
 
 
 def cache_read(cache, k, v, table, starts, lengths, status=None, stream=None) -> int:

@@ -9,7 +9,7 @@ import ctypes as C
 
 from . import enec
 from .enec import E_ARG, E_CAPACITY, E_DTYPE, OK, strerror  # noqa: F401
-from .lowbit import _dtype, _on_gpu, _rows, _space
+from .lowbit import _dtype, _on_gpu, _rows, _space, _stream_on
 
 EXPORTS = ["enec_sample_workspace", "enec_sample"]
 
@@ -59,4 +59,4 @@ def sample(logits, uniform, tokens, temperature=None, top_k=None, top_p=None, mi
         _on_gpu(logits, workspace)
     ws, size = _space(workspace)
     return lib().enec_sample(logits.data_ptr(), rows, vocab, stride, _dtype(logits), C.byref(SamplingStruct(*at[:5])), at[5], at[6], ws, size,
-                             enec._stream_handle(stream))
+                             _stream_on(device, stream))

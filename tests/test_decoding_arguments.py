@@ -3,6 +3,7 @@ followed."""
 import ctypes as C
 import os
 import re
+import types
 
 import pytest
 
@@ -191,3 +192,22 @@ def test_tensors_that_the_binding_refuses(lowbit, sampling):
                 {"turns": f(9, 32)}, {"turns": f(9, 32, 3)}, {"turns": bf(9, 32, 2)}, {"turns": f(9, 32, 2, device=1)}):
         with pytest.raises(ValueError):
             write(**bad)
+
+
+def test_another_gpu_than_the_current_one(lowbit, sampling, monkeypatch):
+    """Kernels are launched on the current GPU: tensors on another one, or a stream of another one, are refused before that."""
+    import torch
+    z = lambda *shape, dtype=torch.uint8: FakeTensor(torch.zeros(*shape, dtype=dtype), 1)  # noqa: E731
+    bf, i = (lambda *shape: z(*shape, dtype=torch.bfloat16)), (lambda *shape: z(*shape, dtype=torch.int32))
+    f = lambda *shape: z(*shape, dtype=torch.float32)  # noqa: E731
+    cache = lowbit.Cache(z(3, 2, 16, 64), z(3, 2), z(3, 2, 64, 16), z(3, 2))
+    cache.device = 1
+    c, s, stream = z(4, 256), z(4, 4), types.SimpleNamespace(device=torch.device("cuda", 0), cuda_stream=0)
+    for current, how in ((0, {}), (1, {"stream": stream})):
+        monkeypatch.setattr(lowbit, "_current_device", lambda: current)
+        for call in (lambda: lowbit.fp8_quantize(bf(4, 200), c, s, **how), lambda: lowbit.fp8_dequantize(c, s, bf(4, 200), **how),
+                     lambda: lowbit.fp8_linear(bf(2, 200), c, s, bf(2, 4), **how), lambda: lowbit.fp8_matmul(z(2, 256), z(2, 4), c, s, f(2, 4), **how),
+                     lambda: sampling.sample(f(4, 9), f(4), i(4), **how),
+                     lambda: lowbit.cache_write_rotated(cache, bf(5, 2, 64), bf(5, 2, 64), None, None, f(9, 32, 2), i(1, 2), i(2), i(1), **how)):
+            with pytest.raises(ValueError, match="current one"):
+                call()

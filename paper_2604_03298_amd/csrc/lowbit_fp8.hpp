@@ -12,6 +12,11 @@ inline size_t fp8_scale_row(size_t cols) { return (fp8_padded(cols) / FP8_BLOCK 
 // as enec.h's tensors; vectors of eight are at most 2^31
 inline bool fp8_fits(size_t rows, size_t cols) { return cols <= (size_t)1 << 31 && (cols == 0 || rows <= ((size_t)1 << 34) / fp8_padded(cols)); }
 
+template <int CONTROL> __device__ __forceinline__ uint32_t larger_moved(uint32_t a)
+{
+    const uint32_t b = (uint32_t)__builtin_amdgcn_update_dpp(0, (int)a, CONTROL, 15, 15, true);
+    return a > b ? a : b;
+}
 // The scale's byte of a block of which this thread and the others of its sixteen have eight values each.
 __device__ __forceinline__ uint32_t block_byte(const float (&v)[8])
 {
@@ -21,11 +26,8 @@ __device__ __forceinline__ uint32_t block_byte(const float (&v)[8])
         const uint32_t b = bits_of(v[j]) & 0x7FFFFFFFu;
         a = a > b ? a : b;
     }
-#pragma unroll
-    for (int k = 1; k < 16; k *= 2) {
-        const uint32_t b = __shfl_xor(a, k);
-        a = a > b ? a : b;
-    }
+    // (by lane moves: from the neighbour, from the other pair, from the half row's other four, from the row's other eight)
+    a = larger_moved<0xB1>(a), a = larger_moved<0x4E>(a), a = larger_moved<0x141>(a), a = larger_moved<0x140>(a);
     return a >= 0x7F800000u ? 255 : scale_byte(a);
 }
 // eight values as E4M3 codes of v / 2^(byte - 127); zeros if the byte says that the block has no values

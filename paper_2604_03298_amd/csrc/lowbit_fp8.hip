@@ -9,32 +9,38 @@ namespace lowbit {
 // threads a block of 128; the largest magnitude of a block takes four moves between lanes (through LDS instead they cost 0.3 us of 4 x 4096).  It is found on the bits: magnitudes of
 // floats order as whole numbers do, and a NaN or an infinity has the exponent field 255.  The scale is a power of two, so the division is exact
 // wherever its result is not below all of E4M3's values, and nearest even is the instruction's rounding.
-// 28672 x 8192 bf16: 113 us, 6.3 TB/s, in a series of calls 118, with two vectors a thread as well; 4 x 4096 2.15 us, with two 2.33; 2048 x 4096 6.9 and 7.0.
-template <int DT>
+// 28672 x 8192 bf16: 113 us, 6.3 TB/s; 2048 x 4096 6.9; 4 x 4096 2.15.
+template <int DT, int U>
 __global__ void __launch_bounds__(256) fp8_quantize_kernel(const void *__restrict__ in, uint32_t cols, size_t stride, Divide per_row, uint32_t n_vec,
                                                            uint32_t scale_row, u32x2 *__restrict__ codes, uint8_t *__restrict__ scales)
 {
-    float v[8];
-    const uint32_t at = blockIdx.x * 256u + threadIdx.x;
-    const uint32_t row = quotient(at, per_row), vector = at - row * per_row.by, col = vector * 8u;
-    const size_t i = (size_t)row * stride + col;
-    if (at < n_vec && col + 8 <= cols) {
-        load8<DT>(in, i, v);
-    } else if (at < n_vec && col < cols) {                  // (loads that do not wait for one another)
-        for (int j = 0; j < 8; ++j) v[j] = load1<DT>(in, i + (col + j < cols ? j : cols - 1 - col));
-        for (int j = 0; j < 8; ++j) v[j] = col + j < cols ? v[j] : 0.0f;
-    } else {
-        for (int j = 0; j < 8; ++j) v[j] = 0.0f;
+    float v[U][8];
+    const uint32_t first = blockIdx.x * (256u * U) + threadIdx.x;
+    for (int u = 0; u < U; ++u) {
+        const uint32_t at = first + u * 256u;
+        const uint32_t row = quotient(at, per_row), col = (at - row * per_row.by) * 8u;
+        const size_t i = (size_t)row * stride + col;
+        if (at < n_vec && col + 8 <= cols) {
+            load8<DT>(in, i, v[u]);
+        } else if (at < n_vec && col < cols) {              // (loads that do not wait for one another)
+            for (int j = 0; j < 8; ++j) v[u][j] = load1<DT>(in, i + (col + j < cols ? j : cols - 1 - col));
+            for (int j = 0; j < 8; ++j) v[u][j] = col + j < cols ? v[u][j] : 0.0f;
+        } else {
+            for (int j = 0; j < 8; ++j) v[u][j] = 0.0f;
+        }
     }
-    if (at >= n_vec) return;                                // (blocks are whole: sixteen lanes go or stay)
-    const uint32_t byte = block_byte(v);
-    codes[at] = fp8_codes(v, byte);
-    if ((at & 15) == 0) {
-        const uint32_t group = vector >> 4, groups = per_row.by >> 4;
-        uint8_t *to = scales + (size_t)row * scale_row;
-        to[group] = (uint8_t)byte;
-        if (group + 1 == groups)
-            for (uint32_t g = groups; g < scale_row; ++g) to[g] = 0;
+    for (int u = 0; u < U; ++u) {
+        const uint32_t at = first + u * 256u;
+        if (at >= n_vec) return;                            // (blocks are whole: sixteen lanes go or stay)
+        const uint32_t byte = block_byte(v[u]);
+        codes[at] = fp8_codes(v[u], byte);
+        if ((at & 15) == 0) {
+            const uint32_t row = quotient(at, per_row), group = (at - row * per_row.by) >> 4, groups = per_row.by >> 4;
+            uint8_t *to = scales + (size_t)row * scale_row;
+            to[group] = (uint8_t)byte;
+            if (group + 1 == groups)
+                for (uint32_t g = groups; g < scale_row; ++g) to[g] = 0;
+        }
     }
 }
 
@@ -78,8 +84,13 @@ inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) =
 int quantize_to_fp8(const void *in, size_t rows, size_t cols, size_t row_stride, int dtype, void *codes, void *scales, hipStream_t s)
 {
     const uint32_t vectors = (uint32_t)(fp8_padded(cols) / 8), n_vec = (uint32_t)(rows * vectors);
-    auto kernel = dtype == ENEC_BF16 ? fp8_quantize_kernel<BF16> : dtype == ENEC_FP16 ? fp8_quantize_kernel<FP16> : fp8_quantize_kernel<FP32>;
-    kernel<<<dim3((n_vec - 1) / 256 + 1), 256, 0, s>>>(in, (uint32_t)cols, row_stride, divide_by(vectors), n_vec, (uint32_t)fp8_scale_row(cols),
+    // One vector a thread, and two for large matrices: 4 x 4096 took 2.15 and 2.35 us, 256 x 4096 2.6 and 2.95, 4096 x 4096 11.9 and 12.3, there and back 11008 x 4096 45.4 and 44.2,
+    // 28672 x 8192 230 and 228.
+    const uint32_t each = n_vec <= 1u << 22 ? 1 : 2;
+    auto kernel = dtype == ENEC_BF16   ? (each == 1 ? fp8_quantize_kernel<BF16, 1> : fp8_quantize_kernel<BF16, 2>)
+                  : dtype == ENEC_FP16 ? (each == 1 ? fp8_quantize_kernel<FP16, 1> : fp8_quantize_kernel<FP16, 2>)
+                                       : (each == 1 ? fp8_quantize_kernel<FP32, 1> : fp8_quantize_kernel<FP32, 2>);
+    kernel<<<dim3((n_vec - 1) / (256 * each) + 1), 256, 0, s>>>(in, (uint32_t)cols, row_stride, divide_by(vectors), n_vec, (uint32_t)fp8_scale_row(cols),
                                                                   static_cast<u32x2 *>(codes), static_cast<uint8_t *>(scales));
     return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
 }

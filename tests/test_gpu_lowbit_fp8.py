@@ -100,6 +100,21 @@ def test_rows_apart_and_at_odd_addresses(lowbit):
 
 
 @pytest.mark.parametrize("dtype", FORMATS)
+def test_a_large_matrix_as_its_parts(lowbit, dtype):
+    """A matrix of more than 2^25 values, whose threads have more of them, and its rows in two calls."""
+    rows, cols = 8201, 4203
+    x = torch.randn(rows, cols, generator=torch.Generator(device="cuda").manual_seed(3), device="cuda").to(dtype)
+    x[5, 7], x[8200, 4202], x[4100, :128] = float("nan"), float("-inf"), 0
+    whole, parts = lowbit.fp8_empty(rows, cols), lowbit.fp8_empty(rows, cols)
+    for t in whole + parts:
+        t.fill_(77)
+    assert lowbit.fp8_quantize(x, *whole) == OK
+    for part in (slice(0, 4000), slice(4000, rows)):
+        assert lowbit.fp8_quantize(x[part], *(t[part] for t in parts)) == OK
+    assert all(torch.equal(a, b) for a, b in zip(whole, parts))
+
+
+@pytest.mark.parametrize("dtype", FORMATS)
 def test_every_code_and_scale_back(lowbit, dtype):
     codes = np.tile(np.arange(256, dtype=np.uint8), (256, 1))
     scales = np.zeros((256, 4), dtype=np.uint8)

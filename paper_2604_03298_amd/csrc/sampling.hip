@@ -844,13 +844,14 @@ template <int DT> __global__ void __launch_bounds__(DRAW_THREADS) draw_kernel(Ro
             }
             const uint64_t cut_place = place_of(cut.key, cut.last);
             if (how.by_mass && done) {
-                // (of all weights down to the end of top_k's list those are not kept that its cut leaves out)
+                // (of all weights down to the end of top_k's list those are not kept that its cut leaves out; listed ones below that end, which top_p's borders reach, are not among them)
+                const uint64_t counted = how.top_k ? k_low : 0;
                 uint64_t p_low = (uint64_t)key_of(r.p_low) << 32, p_high = ((uint64_t)key_of(r.p_high) << 32) - 1, in = 0, out = 0, sum, left_out;
                 p_low = p_low > cut_place ? p_low : cut_place, p_low = p_low > least_place ? p_low : least_place, p_high = p_high < most ? p_high : most;
 #pragma unroll 4
                 for (uint32_t i = threadIdx.x; i < all_listed; i += DRAW_THREADS) {
                     const uint64_t place = s.place[i], m = s.weight[i] & ~KEPT;
-                    in += place >= p_low && place <= p_high ? m : 0, out += place >= cut_place ? 0 : m;
+                    in += place >= p_low && place <= p_high ? m : 0, out += place < cut_place && place >= counted ? m : 0;
                 }
                 block_before<DRAW_WAVES>(in, s.wave_mass, sum);
                 block_before<DRAW_WAVES>(out, s.wave_mass, left_out);

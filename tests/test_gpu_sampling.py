@@ -92,6 +92,14 @@ def test_ties(sampling, vocab, dtype):
         check(sampling, logits, u, min_p=[0.0, 1.0, 1.5, 0.3, 0.36, 0.14])
 
 
+def test_cuts_next_to_one_another(sampling):
+    """Half of a nearly flat row's tokens, and of those all but the last hundredth: both cuts lie in one stretch of the order, which is listed beyond top_k's end."""
+    rng = np.random.default_rng(19)
+    for vocab, rows in ((18584, 48), (45887, 16)):
+        logits = torch.from_numpy(-rng.exponential(3, (rows, vocab)).astype(np.float32)).cuda()
+        check(sampling, logits, rng.random(rows), temperature=[50.0] * rows, top_k=[vocab // 2] * rows, top_p=rng.choice([0.99, 0.995, 0.98], rows))
+
+
 def test_borders_that_are_exact(sampling):
     """Weights of 1, 1/2, 1/4 ... (T so that logits are powers of two): sums that a share meets exactly."""
     logits = torch.zeros(4, 8, device="cuda")

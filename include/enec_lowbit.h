@@ -97,9 +97,10 @@ int enec_fp8_dequantize(const void *codes, const void *scales, size_t rows, size
  *   y       DEVICE, m x n values (bf16, fp16 or fp32), y_stride (>= n); must not overlap the inputs
  *   workspace      DEVICE, 16-byte aligned, or NULL if workspace_bytes = enec_fp8_matmul_workspace(m, n, k) is 0.  What it says serves
  *                  every product of fewer rows with the same n and k as well.
- * Sums are held in 32 bits, and y is rounded once.  For y in 16 bits the matrix unit's 8-bit instructions multiply: they align the products of
- * eight columns (8 i ... 8 i + 7) to the largest of them and drop what lies below 2^-13 of the power of two in it, which for normal values is 1.5e-5 of
- * y's norm.  For y in 32 bits products are exact, at half the rate; there scale bytes below 3 lose what lies below 2^-133.
+ * Sums are held in 32 bits, and y is rounded once.  For y in fp16 and fp32 products are exact; there scale bytes below 3 lose what lies below 2^-133.
+ * For y in bf16 the matrix unit's 8-bit instructions multiply, at twice the rate and more: they align the products of eight columns (8 i ... 8 i + 7) to the
+ * largest of them and drop what lies below 2^-13 of the power of two in it.  That is 1.5e-5 of y's norm for normal values and 4e-5 where single channels
+ * stand out by an order of magnitude (bf16's rounding: 1.7e-3), and shows where large products cancel; y in fp32 avoids it.
  * ENEC_E_ARG also beyond m = 2^21, n = 2^26, k = 2^21, m k or n k = 2^34 or m n = 2^40. */
 size_t enec_fp8_matmul_workspace(size_t m, size_t n, size_t k);
 int enec_fp8_matmul(const void *x_codes, const void *x_scales, size_t m, const void *codes, const void *scales, size_t n, size_t k,

@@ -26,9 +26,9 @@ __device__ __forceinline__ i32x8 halves(const u32x4 &a, const u32x4 &b)
 }
 
 // The 8-bit matrix instructions align the products of eight columns (consecutive ones, as they are read here) to the largest of them and drop what
-// lies below 2^-13 of its power of two; beyond that they sum in 32 bits.  For y in 16 bits that is far below its own rounding: 1.5e-5 of the norm for normal
-// values, bf16's rounding 1.7e-3.  For y in 32 bits (EXACT) codes become bf16 values, which is exact from scale bytes of 3 on, and bf16 instructions,
-// which sum in 32 bits, multiply them at half the rate.
+// lies below 2^-13 of its power of two; beyond that they sum in 32 bits.  For y in bf16 that is far below its own rounding: 1.5e-5 of the norm for normal
+// values, 4e-5 where some channels stand out, bf16's rounding 1.7e-3.  An fp16 y is rounded to 2.1e-4, and would show it.  For y in fp16 and fp32 (EXACT) codes become
+// bf16 values, which is exact from scale bytes of 3 on, and bf16 instructions, which sum in 32 bits, multiply them at half the rate.
 template <bool HIGH> __device__ __forceinline__ uint32_t two_values(int codes, float scale)
 {
     return __builtin_bit_cast(uint32_t, __builtin_amdgcn_cvt_scalef32_pk_bf16_fp8((uint32_t)codes, scale, HIGH));
@@ -214,7 +214,7 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_k
     }
     if (s < end) step(s, 0);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (no copy may come after the workgroup, nor into what follows)
-    if (!EXACT && !a.parts) {
+    if ((!EXACT || a.y_dtype == FP16) && !a.parts) {
         // 16-bit values by way of LDS, a token's rows side by side there: a lane's four rows of a token would be stores of 8 bytes, 32 tokens apart
         constexpr uint32_t PITCH = ROWS * 2 + 16, CHUNKS = ROWS / 8;
         __syncthreads();
@@ -225,8 +225,8 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_k
 #pragma unroll
                 for (int e = 0; e < 4; ++e) {
                     const f32x16 &v = acc[t][u];
-                    const u32x2 w = a.y_dtype == BF16 ? u32x2{pack2<BF16>(v[4 * e], v[4 * e + 1]), pack2<BF16>(v[4 * e + 2], v[4 * e + 3])}
-                                                      : u32x2{pack2<FP16>(v[4 * e], v[4 * e + 1]), pack2<FP16>(v[4 * e + 2], v[4 * e + 3])};
+                    constexpr int Y = EXACT ? FP16 : BF16;
+                    const u32x2 w = {pack2<Y>(v[4 * e], v[4 * e + 1]), pack2<Y>(v[4 * e + 2], v[4 * e + 3])};
                     *reinterpret_cast<u32x2 *>(shared + (wb * (32 * RB) + 32 * u + c) * PITCH + (wa * (32 * RA) + 32 * t + 8 * e + 4 * g) * 2) = w;
                 }
         __syncthreads();
@@ -428,7 +428,7 @@ using namespace enec::lowbit;
 
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
-// The tiles there are.  With one on every compute unit a stage takes `us`, with two on each, where two fit, `us_two`; the same for y in 32 bits.  (These and plan_of's constants are
+// The tiles there are.  With one on every compute unit a stage takes `us`, with two on each, where two fit, `us_two`; the same for y in fp16 and fp32.  (These and plan_of's constants are
 // fitted to the times of 500 products of 1 to 4096 tokens with eighteen matrices from 1024 x 4096 to 28672 x 8192, every tile and split forced; its choices
 // are 0.6 % above the best ones in the mean and 26 % at worst, and of 252 other products 1.3 %, 16 of them more than 5 %, and 23 % at worst.)
 struct Shape {
@@ -558,10 +558,11 @@ template <bool EXACT, int X_INSIDE, int XT, int WAVES> bool launch_thin_of(const
     kernel<<<up(a.n, 16), 64 * WAVES, lds, s>>>(a);
     return true;
 }
-template <int X_INSIDE> bool launch_thin_inside(const Product8 &a, hipStream_t s)
+template <int DT> bool launch_thin_inside(const Product8 &a, hipStream_t s)
 {
+    constexpr bool EXACT = DT == FP16;
     const uint32_t waves = waves_inside(a.n, a.groups);
-    return waves == 2 ? launch_thin_of<false, X_INSIDE, 1, 2>(a, s) : waves == 4 ? launch_thin_of<false, X_INSIDE, 1, 4>(a, s) : launch_thin_of<false, X_INSIDE, 1, 8>(a, s);
+    return waves == 2 ? launch_thin_of<EXACT, DT + 1, 1, 2>(a, s) : waves == 4 ? launch_thin_of<EXACT, DT + 1, 1, 4>(a, s) : launch_thin_of<EXACT, DT + 1, 1, 8>(a, s);
 }
 template <bool EXACT, int XT> bool launch_thin(const Product8 &a, hipStream_t s)
 {
@@ -636,12 +637,12 @@ int enec_fp8_linear(const void *x, size_t m, size_t x_stride, int dtype, const v
                (uint32_t)k, (uint32_t)((k + 127) / 128), (uint32_t)fp8_scale_row(k), 0, 0, 0, dtype};
     if (k != 0 && x_inside(a.m, a.n, a.groups)) {
         a.x = static_cast<const uint8_t *>(x);
-        const bool ok = dtype == ENEC_BF16 ? launch_thin_inside<BF16 + 1>(a, s) : launch_thin_inside<FP16 + 1>(a, s);
+        const bool ok = dtype == ENEC_BF16 ? launch_thin_inside<BF16>(a, s) : launch_thin_inside<FP16>(a, s);
         return ok && hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
     }
     if (k != 0)
         if (const int rc = quantize_to_fp8(x, m, k, x_stride, dtype, x_codes, x_scales, s)) return rc;
-    return launch<false>(a, parts, s);
+    return dtype == ENEC_BF16 ? launch<false>(a, parts, s) : launch<true>(a, parts, s);
 }
 
 int enec_fp8_matmul(const void *x_codes, const void *x_scales, size_t m, const void *codes, const void *scales, size_t n, size_t k, void *y, size_t y_stride,
@@ -660,7 +661,7 @@ int enec_fp8_matmul(const void *x_codes, const void *x_scales, size_t m, const v
                      static_cast<const uint8_t *>(scales), y, 0, y_stride, 0, nullptr, (uint32_t)m, (uint32_t)n, (uint32_t)k, (uint32_t)((k + 127) / 128),
                      (uint32_t)fp8_scale_row(k), 0, 0, 0, dtype};
     const hipStream_t s = (hipStream_t)stream;
-    return dtype == ENEC_FP32 ? launch<true>(a, workspace, s) : launch<false>(a, workspace, s);
+    return dtype == ENEC_BF16 ? launch<false>(a, workspace, s) : launch<true>(a, workspace, s);
 }
 
 }  // extern "C"

@@ -72,12 +72,13 @@ def compression_calls(params, blocks, nblocks):
 
 
 def kernel_sources_sha256():
-    """Hash of the codec's sources with // comments, blank lines and indentation taken out (no string literal of these
-    files holds "//"), so that a reworded comment does not retire a measurement.  (The low-bit kernels are units of their own.)"""
+    """Hash of the codec's sources (enec*) with // comments, blank lines and indentation taken out (no string literal of these
+    files holds "//"), so that a reworded comment does not retire a measurement.  (All other kernels are units of their own, which the
+    codec's sources do not include.)"""
     csrc = os.path.join(ROOT, "paper_2604_03298_amd", "csrc")
     h = hashlib.sha256()
     for name in sorted(os.listdir(csrc)):
-        if name.endswith((".hip", ".hpp")) and not name.startswith("lowbit"):
+        if name.endswith((".hip", ".hpp")) and name.startswith("enec"):
             with open(os.path.join(csrc, name), "r", encoding="utf-8") as f:
                 lines = [ln.split("//", 1)[0].strip() for ln in f]
             h.update(name.encode() + b"\0" + "\n".join(ln for ln in lines if ln).encode())

@@ -347,12 +347,15 @@ __device__ __forceinline__ void turn_queries(const Pages &c, const Page &p, cons
 // 32 sequences, pages of 64: 7.8 us.
 struct Order {
     Divide per_page, per_head;
+    uint32_t blocks, per_row;       // all workgroups, and those of a row of the grid
 };
 template <int DT, int ROTATION>
 __global__ void __launch_bounds__(256) cache_write_rotated_kernel(Pages c, NewTokens n, Queries q, Turns turns, Order order)
 {
     __shared__ uint32_t shared[4];
-    const uint32_t item = quotient(blockIdx.x, order.per_page), within = blockIdx.x - item * order.per_page.by;
+    const uint32_t block = blockIdx.y * order.per_row + blockIdx.x;
+    if (block >= order.blocks) return;
+    const uint32_t item = quotient(block, order.per_page), within = block - item * order.per_page.by;
     const uint32_t head = quotient(within, order.per_head), part = within - head * order.per_head.by;
     const Page p = page_of_item(c, item, turns.positions);
     if (!p.good) return;
@@ -497,13 +500,16 @@ int enec_cache_write_rotated(const enec_cache *cache, const enec_cache_batch *ba
     const uint32_t parts = 2 + (group + QUERY_HEADS - 1) / QUERY_HEADS;
     const uint64_t blocks = ((uint64_t)(p.n_tokens >> p.log_page) + 2 * p.batch) * p.heads * parts;
     if (blocks >= (uint64_t)1 << 31) return ENEC_E_ARG;
+    // (a grid's axis holds fewer than 2^32 threads, 256 a workgroup: what is more goes into further rows)
+    constexpr uint32_t MOST_PER_ROW = (1u << 24) - 1;
+    const uint32_t rows = (uint32_t)((blocks + MOST_PER_ROW - 1) / MOST_PER_ROW), per_row = (uint32_t)((blocks + rows - 1) / rows);
     auto kernel = dtype == ENEC_BF16 ? (interleaved ? cache_write_rotated_kernel<BF16, NEIGHBOURS> : cache_write_rotated_kernel<BF16, HALVES>)
                                      : (interleaved ? cache_write_rotated_kernel<FP16, NEIGHBOURS> : cache_write_rotated_kernel<FP16, HALVES>);
-    kernel<<<dim3((unsigned)blocks), threads_of(p), 0, (hipStream_t)stream>>>(
+    kernel<<<dim3(per_row, rows), threads_of(p), 0, (hipStream_t)stream>>>(
         p, NewTokens{k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride},
         Queries{q, q_out, q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride, q_heads, group, divide_by(units)},
         Turns{static_cast<const float *>(turns), rotary / 2, positions < (uint32_t)MAX_SEQUENCE ? (int32_t)positions : MAX_SEQUENCE},
-        Order{divide_by(p.heads * parts), divide_by(parts)});
+        Order{divide_by(p.heads * parts), divide_by(parts), (uint32_t)blocks, per_row});
     return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;
 }
 

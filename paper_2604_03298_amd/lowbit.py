@@ -77,8 +77,8 @@ def _dtype(t) -> int:
 
 
 def _on_gpu(*tensors):
-    """All of them (None: none) lie on one GPU, or in pinned host memory, which its kernels reach too.  (The calls compare the numbers of their tensors' GPUs
-    themselves, 0.04 us each, and ask here where these differ.)"""
+    """The number of the GPU that all of them (None: none) lie on, or in pinned host memory, which its kernels reach too (-1: all are there).  (The calls compare the
+    numbers of their tensors' GPUs themselves, 0.04 us each, and ask here where these differ.)"""
     device = -1
     for t in tensors:
         at = -1 if t is None else t.get_device()
@@ -89,6 +89,7 @@ def _on_gpu(*tensors):
             device = at
         elif at != device:
             raise ValueError("tensors on one GPU are wanted")
+    return device
 
 
 _current_device = _raw_stream = None
@@ -161,10 +162,11 @@ def mx4_quantize(src, codes, scales, stream=None) -> int:
     _same_padding(padded, cols)
     if n != rows:
         raise ValueError("src and codes differ in their rows")
-    if not src.get_device() == codes.get_device() == scales.get_device() >= 0:
-        _on_gpu(src, codes, scales)
+    device = codes.get_device()
+    if not src.get_device() == device == scales.get_device() >= 0:
+        device = _on_gpu(src, codes, scales)
     return lib().enec_mx4_quantize(src.data_ptr(), rows, cols, stride, _dtype(src), codes.data_ptr(), scales.data_ptr(),
-                                   enec._stream_handle(stream))
+                                   _stream_on(device, stream))
 
 
 def mx4_dequantize(codes, scales, out, stream=None) -> int:
@@ -174,10 +176,11 @@ def mx4_dequantize(codes, scales, out, stream=None) -> int:
     _same_padding(padded, cols)
     if n != rows:
         raise ValueError("out and codes differ in their rows")
-    if not codes.get_device() == scales.get_device() == out.get_device() >= 0:
-        _on_gpu(codes, scales, out)
+    device = codes.get_device()
+    if not device == scales.get_device() == out.get_device() >= 0:
+        device = _on_gpu(codes, scales, out)
     return lib().enec_mx4_dequantize(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), stride, _dtype(out),
-                                     enec._stream_handle(stream))
+                                     _stream_on(device, stream))
 
 
 def mx4_linear_workspace(m: int, n: int, k: int) -> int:
@@ -192,11 +195,12 @@ def mx4_linear(x, codes, scales, out, workspace=None, stream=None) -> int:
     rows, cols, y_stride = _rows(out, "out")
     if (rows, cols) != (m, n) or out.dtype != x.dtype:
         raise ValueError(f"out: ({m}, {n}) of x's format is wanted")
-    if not x.get_device() == codes.get_device() == scales.get_device() == out.get_device() == (x if workspace is None else workspace).get_device() >= 0:
-        _on_gpu(x, codes, scales, out, workspace)
+    device = codes.get_device()
+    if not x.get_device() == device == scales.get_device() == out.get_device() == (x if workspace is None else workspace).get_device() >= 0:
+        device = _on_gpu(x, codes, scales, out, workspace)
     ws, size = _space(workspace)
     return lib().enec_mx4_linear(x.data_ptr(), m, x_stride, _dtype(x), codes.data_ptr(), scales.data_ptr(), n, k, out.data_ptr(), y_stride,
-                                 ws, size, enec._stream_handle(stream))
+                                 ws, size, _stream_on(device, stream))
 
 
 def mx4_matmul_workspace(m: int, n: int, k: int) -> int:
@@ -210,12 +214,13 @@ def mx4_matmul(x_codes, x_scales, codes, scales, out, workspace=None, stream=Non
     rows, cols, y_stride = _rows(out, "out")
     if padded != other or (rows, cols) != (m, n):
         raise ValueError(f"matrices of as many columns and out ({m}, {n}) are wanted")
-    if not x_codes.get_device() == x_scales.get_device() == codes.get_device() == scales.get_device() == out.get_device() \
+    device = codes.get_device()
+    if not x_codes.get_device() == x_scales.get_device() == device == scales.get_device() == out.get_device() \
             == (out if workspace is None else workspace).get_device() >= 0:
-        _on_gpu(x_codes, x_scales, codes, scales, out, workspace)
+        device = _on_gpu(x_codes, x_scales, codes, scales, out, workspace)
     ws, size = _space(workspace)
     return lib().enec_mx4_matmul(x_codes.data_ptr(), x_scales.data_ptr(), m, codes.data_ptr(), scales.data_ptr(), n, padded, out.data_ptr(),
-                                 y_stride, _dtype(out), ws, size, enec._stream_handle(stream))
+                                 y_stride, _dtype(out), ws, size, _stream_on(device, stream))
 
 
 # ---- matrices in 8 bits -------------------------------------------------------------
@@ -254,7 +259,7 @@ def fp8_quantize(src, codes, scales, stream=None) -> int:
         raise ValueError("src and codes differ in their rows")
     device = codes.get_device()
     if not src.get_device() == device == scales.get_device() >= 0:
-        _on_gpu(src, codes, scales)
+        device = _on_gpu(src, codes, scales)
     return lib().enec_fp8_quantize(src.data_ptr(), rows, cols, stride, _dtype(src), codes.data_ptr(), scales.data_ptr(),
                                    _stream_on(device, stream))
 
@@ -268,7 +273,7 @@ def fp8_dequantize(codes, scales, out, stream=None) -> int:
         raise ValueError("out and codes differ in their rows")
     device = codes.get_device()
     if not device == scales.get_device() == out.get_device() >= 0:
-        _on_gpu(codes, scales, out)
+        device = _on_gpu(codes, scales, out)
     return lib().enec_fp8_dequantize(codes.data_ptr(), scales.data_ptr(), rows, cols, out.data_ptr(), stride, _dtype(out),
                                      _stream_on(device, stream))
 
@@ -285,11 +290,12 @@ def fp8_linear(x, codes, scales, out, workspace=None, stream=None) -> int:
     rows, cols, y_stride = _rows(out, "out")
     if (rows, cols) != (m, n) or out.dtype != x.dtype:
         raise ValueError(f"out: ({m}, {n}) of x's format is wanted")
-    if not x.get_device() == codes.get_device() == scales.get_device() == out.get_device() == (x if workspace is None else workspace).get_device() >= 0:
-        _on_gpu(x, codes, scales, out, workspace)
+    device = codes.get_device()
+    if not x.get_device() == device == scales.get_device() == out.get_device() == (x if workspace is None else workspace).get_device() >= 0:
+        device = _on_gpu(x, codes, scales, out, workspace)
     ws, size = _space(workspace)
     return lib().enec_fp8_linear(x.data_ptr(), m, x_stride, _dtype(x), codes.data_ptr(), scales.data_ptr(), n, k, out.data_ptr(), y_stride,
-                                 ws, size, _stream_on(codes.get_device(), stream))
+                                 ws, size, _stream_on(device, stream))
 
 
 def fp8_matmul_workspace(m: int, n: int, k: int) -> int:
@@ -303,12 +309,13 @@ def fp8_matmul(x_codes, x_scales, codes, scales, out, workspace=None, stream=Non
     rows, cols, y_stride = _rows(out, "out")
     if padded != other or (rows, cols) != (m, n):
         raise ValueError(f"matrices of as many columns and out ({m}, {n}) are wanted")
-    if not x_codes.get_device() == x_scales.get_device() == codes.get_device() == scales.get_device() == out.get_device() \
+    device = codes.get_device()
+    if not x_codes.get_device() == x_scales.get_device() == device == scales.get_device() == out.get_device() \
             == (out if workspace is None else workspace).get_device() >= 0:
-        _on_gpu(x_codes, x_scales, codes, scales, out, workspace)
+        device = _on_gpu(x_codes, x_scales, codes, scales, out, workspace)
     ws, size = _space(workspace)
     return lib().enec_fp8_matmul(x_codes.data_ptr(), x_scales.data_ptr(), m, codes.data_ptr(), scales.data_ptr(), n, padded, out.data_ptr(),
-                                 y_stride, _dtype(out), ws, size, _stream_on(codes.get_device(), stream))
+                                 y_stride, _dtype(out), ws, size, _stream_on(device, stream))
 
 
 # ---- the cache ----------------------------------------------------------------------
@@ -348,6 +355,7 @@ _int32 = _float32 = None
 
 
 def _batch(cache, x, y, table, starts, lengths, n_tokens, status, workspace=None):
+    """A packed BatchStruct, and the number of the call's GPU."""
     global _int32
     if _int32 is None:
         import torch
@@ -361,11 +369,12 @@ def _batch(cache, x, y, table, starts, lengths, n_tokens, status, workspace=None
         raise ValueError("table, starts and lengths are int32 without gaps")
     if status is not None and (status.dtype is not _int32 or status.numel() == 0):
         raise ValueError("status: an int32 word, or None, is wanted")
+    device = cache.device
     if not x.get_device() == y.get_device() == table.get_device() == starts.get_device() == lengths.get_device() == (x if status is None else status).get_device() \
-            == (x if workspace is None else workspace).get_device() == cache.device >= 0:
-        _on_gpu(cache.tensors[0], x, y, table, starts, lengths, status, workspace)
+            == (x if workspace is None else workspace).get_device() == device >= 0:
+        device = _on_gpu(cache.tensors[0], x, y, table, starts, lengths, status, workspace)
     return _BATCH.pack(table.data_ptr(), starts.data_ptr(), lengths.data_ptr(), shape[1], batch, n_tokens,
-                       0 if status is None else status.data_ptr())
+                       0 if status is None else status.data_ptr()), device
 
 
 def _tokens(t, other, heads, dim, what):
@@ -385,8 +394,8 @@ def cache_write(cache, k, v, table, starts, lengths, status=None, stream=None) -
     """Enqueues enec_cache_write.  k, v: (tokens, heads, head_dim) of bf16 or fp16, the newest tokens of their sequences; table (batch,
     pages), starts (batch + 1) and lengths (batch, new tokens included): int32 on the device; status: None or an int32 word holding 0."""
     tokens, kt, kh, vt, vh = _tokens(k, v, cache.heads, cache.head_dim, "k and v")
-    b = _batch(cache, k, v, table, starts, lengths, tokens, status)
-    return lib().enec_cache_write(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, _dtype(k), enec._stream_handle(stream))
+    b, device = _batch(cache, k, v, table, starts, lengths, tokens, status)
+    return lib().enec_cache_write(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, _dtype(k), _stream_on(device, stream))
 
 
 def cache_write_rotated(cache, k, v, q, q_out, turns, table, starts, lengths, interleaved: bool = False, status=None, stream=None) -> int:
@@ -396,7 +405,7 @@ def cache_write_rotated(cache, k, v, q, q_out, turns, table, starts, lengths, in
     if _float32 is None:
         import torch
         _float32 = torch.float32
-    dim, device, shape = cache.head_dim, cache.device, turns.shape
+    dim, shape = cache.head_dim, turns.shape
     tokens, kt, kh, vt, vh = _tokens(k, v, cache.heads, dim, "k and v")
     if len(shape) != 3 or shape[2] != 2 or turns.dtype is not _float32 or not turns.is_contiguous():
         raise ValueError("turns: (positions, rotary / 2, 2) of fp32 without gaps are wanted")
@@ -406,17 +415,15 @@ def cache_write_rotated(cache, k, v, q, q_out, turns, table, starts, lengths, in
         q_tokens, qt, qh, ot, oh = _tokens(q, q_out, heads, dim, "q and q_out")
         if q_tokens != tokens or q.dtype is not k.dtype:
             raise ValueError("q: as many tokens as k has, of its format, are wanted")
-        if not q.get_device() == q_out.get_device() == turns.get_device() == device:
-            _on_gpu(cache.tensors[0], q, q_out, turns)
         q_at, out_at = q.data_ptr(), q_out.data_ptr()
     elif q is None and q_out is None:
-        if turns.get_device() != device:
-            _on_gpu(cache.tensors[0], turns)
         q_at = out_at = None
         heads = qt = qh = ot = oh = 0
     else:
         raise ValueError("q and q_out, or neither, are wanted")
-    b = _batch(cache, k, v, table, starts, lengths, tokens, status)
+    b, device = _batch(cache, k, v, table, starts, lengths, tokens, status)
+    if not turns.get_device() == (turns if q is None else q).get_device() == (turns if q is None else q_out).get_device() == device >= 0:
+        device = _on_gpu(cache.tensors[0], k, v, q, q_out, turns, table, starts, lengths, status)
     return lib().enec_cache_write_rotated(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, q_at, qt, qh, out_at, ot, oh, heads, _dtype(k),
                                           turns.data_ptr(), shape[0], 2 * shape[1], int(interleaved), _stream_on(device, stream))
 
@@ -424,8 +431,8 @@ def cache_write_rotated(cache, k, v, q, q_out, turns, table, starts, lengths, in
 def cache_read(cache, k, v, table, starts, lengths, status=None, stream=None) -> int:
     """Enqueues enec_cache_read: the newest tokens' keys and values into k, v (bf16, fp16 or fp32); starts of whole lengths read all."""
     tokens, kt, kh, vt, vh = _tokens(k, v, cache.heads, cache.head_dim, "k and v")
-    b = _batch(cache, k, v, table, starts, lengths, tokens, status)
-    return lib().enec_cache_read(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, _dtype(k), enec._stream_handle(stream))
+    b, device = _batch(cache, k, v, table, starts, lengths, tokens, status)
+    return lib().enec_cache_read(cache.ref, b, k.data_ptr(), kt, kh, v.data_ptr(), vt, vh, _dtype(k), _stream_on(device, stream))
 
 
 def cache_attention_workspace(cache, batch: int, n_tokens: int, q_heads: int, max_new: int, max_length: int) -> int:
@@ -437,7 +444,7 @@ def cache_attention(cache, q, out, table, starts, lengths, max_new: int, max_len
     """Enqueues enec_cache_attention.  q, out: (tokens, q_heads, head_dim) of bf16 or fp16; scale: head_dim ** -0.5 unless given."""
     heads, dim = q.shape[1], cache.head_dim
     tokens, qt, qh, ot, oh = _tokens(q, out, heads, dim, "q and out")
-    b = _batch(cache, q, out, table, starts, lengths, tokens, status, workspace)
+    b, device = _batch(cache, q, out, table, starts, lengths, tokens, status, workspace)
     ws, size = _space(workspace)
     return lib().enec_cache_attention(cache.ref, b, q.data_ptr(), qt, qh, out.data_ptr(), ot, oh, _dtype(q), heads, max_new, max_length,
-                                      dim ** -0.5 if scale is None else scale, ws, size, enec._stream_handle(stream))
+                                      dim ** -0.5 if scale is None else scale, ws, size, _stream_on(device, stream))

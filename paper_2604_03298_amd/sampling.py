@@ -43,7 +43,7 @@ def sample(logits, uniform, tokens, temperature=None, top_k=None, top_p=None, mi
     import torch
     rows, vocab, stride = _rows(logits, "logits")
     device = logits.get_device()
-    at = []
+    at, there, others = [], [logits, workspace], device < 0 or (workspace is not None and workspace.get_device() != device)
     for t, kind, name in ((temperature, torch.float32, "temperature"), (top_k, torch.int32, "top_k"), (top_p, torch.float32, "top_p"),
                           (min_p, torch.float32, "min_p"), (uniform, torch.float32, "uniform"), (tokens, torch.int32, "tokens"),
                           (log_probs, torch.float32, "log_probs")):
@@ -52,11 +52,12 @@ def sample(logits, uniform, tokens, temperature=None, top_k=None, top_p=None, mi
             continue
         if t.dtype is not kind or t.shape != (rows,) or not t.is_contiguous():
             raise ValueError(f"{name}: ({rows},) of {kind} without gaps is wanted")
-        if t.get_device() != device or device < 0:
-            _on_gpu(logits, t)
+        if t.get_device() != device:
+            others = True
+        there.append(t)
         at.append(t.data_ptr())
-    if device < 0 or (workspace is not None and workspace.get_device() != device):
-        _on_gpu(logits, workspace)
+    if others:
+        device = _on_gpu(*there)
     ws, size = _space(workspace)
     return lib().enec_sample(logits.data_ptr(), rows, vocab, stride, _dtype(logits), C.byref(SamplingStruct(*at[:5])), at[5], at[6], ws, size,
                              _stream_on(device, stream))

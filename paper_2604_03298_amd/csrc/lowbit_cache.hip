@@ -233,9 +233,10 @@ __device__ __forceinline__ void write_page(const Pages &c, const Page &p, uint32
     Tile<DT, V, ROTATION> t;
     uint32_t a = 0;
     const int32_t number = number_of(c, p);
+    if (ROTATION != STAY && p.position < 0) return;         // (there are no turns for negative positions, and nothing is stored)
     for (uint32_t i = threadIdx.x; i < tiles; i += blockDim.x) {
         t.at(i, log_dims);
-        if (ROTATION == STAY || p.position >= 0) t.load(in, token_stride, head * head_stride, p, turns);
+        t.load(in, token_stride, head * head_stride, p, turns);
         const uint32_t b = t.largest();
         a = a > b ? a : b;
     }
@@ -285,7 +286,7 @@ struct Queries {
     const void *in;
     void *out;
     size_t in_token, in_head, out_token, out_head;
-    uint32_t heads, per_group;              // all, and of those that share a key
+    uint32_t per_group;                     // heads that share a key
     Divide units;                           // of a head
 };
 constexpr uint32_t QUERY_HEADS = 4;         // of a workgroup
@@ -507,7 +508,7 @@ int enec_cache_write_rotated(const enec_cache *cache, const enec_cache_batch *ba
                                      : (interleaved ? cache_write_rotated_kernel<FP16, NEIGHBOURS> : cache_write_rotated_kernel<FP16, HALVES>);
     kernel<<<dim3(per_row, rows), threads_of(p), 0, (hipStream_t)stream>>>(
         p, NewTokens{k, v, k_token_stride, k_head_stride, v_token_stride, v_head_stride},
-        Queries{q, q_out, q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride, q_heads, group, divide_by(units)},
+        Queries{q, q_out, q_token_stride, q_head_stride, q_out_token_stride, q_out_head_stride, group, divide_by(units)},
         Turns{static_cast<const float *>(turns), rotary / 2, positions < (uint32_t)MAX_SEQUENCE ? (int32_t)positions : MAX_SEQUENCE},
         Order{divide_by(p.heads * parts), divide_by(parts), (uint32_t)blocks, per_row});
     return hipGetLastError() == hipSuccess ? ENEC_OK : ENEC_E_HIP;

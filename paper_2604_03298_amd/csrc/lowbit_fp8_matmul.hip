@@ -214,7 +214,8 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_k
     }
     if (s < end) step(s, 0);
     asm volatile("s_waitcnt vmcnt(0)" ::: "memory");        // (no copy may come after the workgroup, nor into what follows)
-    if ((!EXACT || a.y_dtype == FP16) && !a.parts) {
+    constexpr bool ONLY_16 = RA * RB >= 8;                  // tiles that are never split, of y in bf16
+    if (ONLY_16 || ((!EXACT || a.y_dtype == FP16) && !a.parts)) {
         // 16-bit values by way of LDS, a token's rows side by side there: a lane's four rows of a token would be stores of 8 bytes, 32 tokens apart
         constexpr uint32_t PITCH = ROWS * 2 + 16, CHUNKS = ROWS / 8;
         __syncthreads();
@@ -246,25 +247,27 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_k
         }
         return;
     }
-    // 32-bit values: four rows of a token are 16 bytes
-    float *to = a.parts ? a.parts + (size_t)blockIdx.y * a.m * a.part_row : static_cast<float *>(a.y);
-    const size_t stride = a.parts ? a.part_row : a.y_stride;
+    if constexpr (!ONLY_16) {
+        // 32-bit values: four rows of a token are 16 bytes
+        float *to = a.parts ? a.parts + (size_t)blockIdx.y * a.m * a.part_row : static_cast<float *>(a.y);
+        const size_t stride = a.parts ? a.part_row : a.y_stride;
 #pragma unroll
-    for (int u = 0; u < RB; ++u) {
-        const uint32_t token = m0 + wb * (32 * RB) + 32 * u + c;
-        if (token >= a.m) continue;
+        for (int u = 0; u < RB; ++u) {
+            const uint32_t token = m0 + wb * (32 * RB) + 32 * u + c;
+            if (token >= a.m) continue;
 #pragma unroll
-        for (int t = 0; t < RA; ++t) {
+            for (int t = 0; t < RA; ++t) {
 #pragma unroll
-            for (int e = 0; e < 4; ++e) {
-                const uint32_t r = n0 + wa * (32 * RA) + 32 * t + 8 * e + 4 * g;
-                const f32x4 v = {acc[t][u][4 * e], acc[t][u][4 * e + 1], acc[t][u][4 * e + 2], acc[t][u][4 * e + 3]};
-                if (r + 4 <= a.n) {
-                    *reinterpret_cast<f32x4_a4 *>(to + (size_t)token * stride + r) = v;
-                } else {
+                for (int e = 0; e < 4; ++e) {
+                    const uint32_t r = n0 + wa * (32 * RA) + 32 * t + 8 * e + 4 * g;
+                    const f32x4 v = {acc[t][u][4 * e], acc[t][u][4 * e + 1], acc[t][u][4 * e + 2], acc[t][u][4 * e + 3]};
+                    if (r + 4 <= a.n) {
+                        *reinterpret_cast<f32x4_a4 *>(to + (size_t)token * stride + r) = v;
+                    } else {
 #pragma unroll
-                    for (uint32_t j = 0; j < 3; ++j)
-                        if (r + j < a.n) to[(size_t)token * stride + r + j] = v[j];
+                        for (uint32_t j = 0; j < 3; ++j)
+                            if (r + j < a.n) to[(size_t)token * stride + r + j] = v[j];
+                    }
                 }
             }
         }

@@ -1,7 +1,8 @@
 """Builds libenec.so (HIP, gfx950) in-tree with hipcc.  `python -m paper_2604_03298_amd.build`.
 
 libenec_test.so is the same library with ENEC_TEST_HOOKS defined for the host code: there the environment
-variable ENEC_SPIN_LIMIT lowers the bound of the scan's waits, which the tests of that bound need.
+variable ENEC_SPIN_LIMIT lowers the bound of the scan's waits, which the tests of that bound need, and enec_test_fp8_plan
+says how a product in 8 bits is cut up, for the test that the tested sizes take every way.
 
 The host code (csrc/enec_api.hip, csrc/enec_pipeline.hip), the compression kernels for one tuple per data block
 (csrc/enec_per_block.hip, its fp32 kernels with deferred stores apart) and for tensors of one block (csrc/enec_single.hip), the
@@ -47,6 +48,7 @@ def _units():
              ("enec_pipeline.o", [SOURCES[3]]), ("enec_single.o", [SOURCES[5]]),
              ("enec_decompress.o", ["-DENEC_ONE=0", SOURCES[4]]), ("enec_decompress_one.o", ["-DENEC_ONE=1", SOURCES[4]])]
     units += [(os.path.basename(path)[:-4] + ".o", [path]) for path in LOWBIT + [SAMPLING]]
+    units += [("lowbit_fp8_matmul_test.o", ["-DENEC_TEST_HOOKS", os.path.join(CSRC, "lowbit_fp8_matmul.hip")])]
     for lpg in (2, 1, 4):           # lanes per group: group lengths 16, 8, 32
         for dt in (0, 2, 1):
             for logb in (14, 0):    # block size: the default one as a constant, any as an argument
@@ -72,9 +74,9 @@ def build(verbose: bool = False) -> str:
     workers = max(1, min(8, os.cpu_count() or 1))
     with ThreadPoolExecutor(workers) as pool:
         objects = list(pool.map(compile_one, _units()))
-    api, api_test = os.path.join(OBJ, "enec_api.o"), os.path.join(OBJ, "enec_api_test.o")
-    for lib, skip in ((LIB, api_test), (TEST_LIB, api)):
-        cmd = ["hipcc", "--offload-arch=gfx950", "-fPIC", "-shared", "-o", lib] + [o for o in objects if o != skip]
+    hooked = [o for o in objects if o.endswith("_test.o")]
+    for lib, skip in ((LIB, hooked), (TEST_LIB, [o[:-len("_test.o")] + ".o" for o in hooked])):
+        cmd = ["hipcc", "--offload-arch=gfx950", "-fPIC", "-shared", "-o", lib] + [o for o in objects if o not in skip]
         if verbose:
             print(" ".join(cmd), flush=True)
         res = subprocess.run(cmd, capture_output=True, text=True)

@@ -604,6 +604,8 @@ inline bool sizes_ok(size_t m, size_t n, size_t k)
            && (k != 0 || m * n < (size_t)1 << 33);
 }
 
+inline bool exact_of(int y_dtype) { return y_dtype != ENEC_BF16; }
+
 // a linear layer's activations in 8 bits, codes and scales
 inline size_t codes_space(size_t m, size_t k) { return m * fp8_padded(k); }
 inline size_t scales_space(size_t m, size_t k) { return (m * fp8_scale_row(k) + 15) / 16 * 16; }
@@ -645,7 +647,7 @@ int enec_fp8_linear(const void *x, size_t m, size_t x_stride, int dtype, const v
     }
     if (k != 0)
         if (const int rc = quantize_to_fp8(x, m, k, x_stride, dtype, x_codes, x_scales, s)) return rc;
-    return dtype == ENEC_BF16 ? launch<false>(a, parts, s) : launch<true>(a, parts, s);
+    return exact_of(dtype) ? launch<true>(a, parts, s) : launch<false>(a, parts, s);
 }
 
 int enec_fp8_matmul(const void *x_codes, const void *x_scales, size_t m, const void *codes, const void *scales, size_t n, size_t k, void *y, size_t y_stride,
@@ -664,7 +666,22 @@ int enec_fp8_matmul(const void *x_codes, const void *x_scales, size_t m, const v
                      static_cast<const uint8_t *>(scales), y, 0, y_stride, 0, nullptr, (uint32_t)m, (uint32_t)n, (uint32_t)k, (uint32_t)((k + 127) / 128),
                      (uint32_t)fp8_scale_row(k), 0, 0, 0, dtype};
     const hipStream_t s = (hipStream_t)stream;
-    return dtype == ENEC_BF16 ? launch<false>(a, workspace, s) : launch<true>(a, workspace, s);
+    return exact_of(dtype) ? launch<true>(a, workspace, s) : launch<false>(a, workspace, s);
 }
+
+#ifdef ENEC_TEST_HOOKS
+// What a call of these sizes launches: the tile's number, -1 for the kernel for few tokens, -2 for the one that brings them into 8 bits itself; splits; the latter two kernels' waves,
+// and their tiles of sixteen tokens.
+void enec_test_fp8_plan(size_t m, size_t n, size_t k, int y_dtype, int linear, int32_t *out)
+{
+    const uint32_t groups = (uint32_t)((k + 127) / 128), tiles = thin_tiles((uint32_t)m);
+    if (linear && x_inside((uint32_t)m, (uint32_t)n, groups)) {
+        out[0] = -2, out[1] = 1, out[2] = (int32_t)waves_inside((uint32_t)n, groups), out[3] = 1;
+        return;
+    }
+    const Plan p = plan_of((uint32_t)m, (uint32_t)n, groups, exact_of(y_dtype));
+    out[0] = p.shape, out[1] = (int32_t)p.splits, out[2] = p.shape < 0 ? (int32_t)thin_waves(tiles, groups) : 0, out[3] = p.shape < 0 ? (int32_t)tiles : 0;
+}
+#endif
 
 }  // extern "C"

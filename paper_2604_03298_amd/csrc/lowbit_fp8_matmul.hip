@@ -539,15 +539,17 @@ template <bool EXACT> bool launch_shape(const Product8 &a, const Plan &p, hipStr
 // another at the end.  With the tokens brought into 8 bits inside, which more threads do faster, 1 token x 4096 x 1024 / 2048 / 4096 / 8192 took 3.7 / 4.8 / 7.7 / 14.1 us with
 // two waves, 3.8 / 4.2 / 6.2 / 10.5 with four and 4.0 / 4.4 / 6.4 / 10.0 with eight; without, 8 tokens x 11008 x 4096 / 8192 14.8 / 22.3 with two, 16.4 / 24.8 with four, x 28672 x 8192
 // 51 and 49, x 4096 x 8192 13.7 and 12.9.
-// Where a compute unit has three workgroups, and some two, two waves are better: 1 token x 8192 / 11008 / 16384 / 32003 x 4096 took 10.1 / 12.8 / 16.1 / 27.2 us with four and
-// 10.5 / 12.6 / 17.3 / 29.8 with two (from the last-level cache 9.5 / 11.7 / 14.9 / 27.2 and 10.0 / 10.8 / 13.5 / 29.7), x 11008 / 32003 x 2048 7.1 / 14.8 and 6.7 / 13.5.
+// Up to 2048 columns two waves are better where there are many workgroups, up to 4096 four are: with weights from memory 1 token x 4096 / 9216 / 11008 / 16384 / 32003 x 2048 took
+// 4.0 / 7.1 / 7.2 / 8.7 / 14.9 us with four and 4.2 / 6.8 / 7.1 / 8.8 / 13.6 with two, x 11008 x 2560 8.3 and 8.1, x 11008 / 12288 x 3328 9.6 / 10.1 and 10.1 / 10.7,
+// x 8192 / 9216 / 11008 / 12288 / 16384 / 32003 x 4096 10.1 / 11.7 / 12.2 / 13.0 / 16.2 / 27.5 and 10.7 / 11.6 / 12.7 / 13.6 / 17.4 / 29.9.  (From the last-level cache, where a model's
+// weights do not lie, 11008 x 4096 took 11.7 and 10.8.)
 // Bringing them into 8 bits inside saves a launch and costs every workgroup the work again: where four vectors a thread are enough, 1 token x 11008 x 4096 took 12.8 us
 // against 14.4, 4 tokens x 4096 x 2048 5.4 against 6.4, 2 tokens x 32003 x 4096, the worst found, 31.1 against 30.9; with eight a thread 2 tokens x 4096 x 4096 took 9.9
 // against 8.6, with thirty-two 16 tokens x 32003 x 2048 65 against 20.
 inline uint32_t waves_inside(uint32_t n, uint32_t groups)
 {
     const uint32_t per_unit = up(up(n, 16), UNITS);
-    return groups <= 8 ? 2 : groups <= 16 ? (per_unit <= 2 ? 4 : 2) : groups <= 32 ? (per_unit <= 2 || per_unit > 3 ? 4 : 2) : 8;
+    return groups <= 8 ? 2 : groups <= 16 ? (per_unit <= 2 ? 4 : 2) : groups <= 32 ? 4 : 8;
 }
 inline bool x_inside(uint32_t m, uint32_t n, uint32_t groups) { return m <= 16 && (uint64_t)m * groups * 16 <= X_EACH * 64 * waves_inside(n, groups); }
 

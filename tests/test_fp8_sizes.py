@@ -36,3 +36,9 @@ def test_the_tested_sizes_take_every_way(way, dtype, linear, ways):
     taken = {way(m, n, k, dtype, linear) for m, n, k in SIZES}
     assert ways <= taken, sorted(ways - taken)
     assert taken <= ways | FEW_WAYS
+
+
+@pytest.mark.parametrize("k", [2049, 2560, 3328, 4096])
+def test_rows_of_weights_do_not_change_the_waves_of_long_rows(way, k):
+    """One rule for all of them: with weights from memory four waves are better, or as good, over the whole range."""
+    assert {way(1, n, k, BF16, 1) for n in (16, 300, 4096, 8192, 8193, 11008, 12288, 12289, 32003, 70000)} == {(INSIDE, False, 4, 1)}

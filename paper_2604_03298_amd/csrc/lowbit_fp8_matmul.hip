@@ -47,9 +47,10 @@ __device__ __forceinline__ bf16x8 eight_values(const i32x8 &v, int q, int byte)
 // turn: a row's eight chunks of 16 bytes lie side by side, chunk i at place i ^ (row div 2 mod 8), so that the sixteen lanes of a read's quarter find
 // sixteen different places of 256 bytes.  A wave reads the next half stage into registers while it multiplies this one; the only barrier of a stage is between
 // its halves, when all waves have the second half in registers: the stage's buffer is free then, and the next stage has landed.
-// Bound by the matrix unit's power and the way of the tiles into LDS: 4096 x 28672 x 8192 (tokens, rows, columns) takes 724 us, 2660 TFLOP/s, with the unit busy for 65 to 70 % of the
-// cycles, at a clock that its power brings down to 1.5 to 1.8 GHz, and no read meeting another one's bank; the copies alone take 536 us of it (620 before lines were touched ahead, the
-// whole 735).  2048 x 11008 x 4096: 88 us, 2100 TFLOP/s, 473 tiles of 256 x 192 in two rounds.  EXACT: 96 x 4096 x 11008 22 us with its splits' join.
+// Bound by the matrix unit's power and the way of the tiles into LDS: 4096 x 28672 x 8192 (tokens, rows, columns) takes 715 to 747 us by the card and its warmth, 2580 to 2690 TFLOP/s, with the unit
+// busy for 65 to 70 % of the cycles, at a clock that its power brings down to 1.5 to 1.8 GHz, and no read meeting another one's bank; the copies alone take 536 us of it (620 before lines
+// were touched ahead).  2048 x 11008 x 4096: 88 us, 2100 TFLOP/s, 473 tiles of 256 x 192 in two rounds.  EXACT: 96 x 4096 x 11008 22 us with its splits' join, 4096 x 28672 x 8192
+// 1740 to 1840, 1050 to 1110 TFLOP/s: each wave makes bf16 values of all codes that it uses.
 template <bool EXACT, int RA, int RB, int WA, int WB, int BUFFERS>
 __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_kernel(Product8 a)
 {
@@ -279,7 +280,7 @@ __global__ void __launch_bounds__(64 * WA * WB, RA * RB >= 8 ? 1 : 2) fp8_tile_k
 // multiplies sixteen rows and sixteen tokens over a whole block: a lane has row (or token) lane mod 16 and chunks 2 g and 2 g + 1 of its eight, g = lane div 16.
 // Chunk i lies at place i ^ turn(row): the sixteen lanes of a read's quarter are rows {0-3, 12-15} of one g and {4-11} of the next, and find sixteen places.
 // With X_INSIDE the workgroup brings the few tokens' 16-bit values into 8 bits itself, while its first weights are on their way.
-// 1 token x 28672 x 8192: 43 us, 5.5 TB/s; x 11008 x 4096 12.7, 3.6 TB/s; 1024 x 1024, a launch's start, one way from memory and the join of the waves' sums, 3.4.
+// 1 token x 28672 x 8192: 43 to 48 us, 5.5 to 4.9 TB/s; x 11008 x 4096 12.2 to 12.6, 3.7 TB/s; 1024 x 1024, a launch's start, one way from memory and the join of the waves' sums, 3.4.
 __device__ __forceinline__ uint32_t thin_turn(uint32_t r) { return (r >> 1 & 1) | (r >> 1 & 4); }
 constexpr uint32_t X_EACH = 4;                  // vectors of the tokens that a thread brings into 8 bits, at most
 template <bool EXACT, int X_INSIDE, int XT, int WAVES>
@@ -432,7 +433,7 @@ using namespace enec::lowbit;
 inline bool aligned(const void *p, size_t a) { return ((uintptr_t)p & (a - 1)) == 0; }
 
 // The tiles there are.  With one on every compute unit a stage takes `us`, with two on each, where two fit, `us_two`; the same for y in fp16 and fp32.  (These and plan_of's constants are
-// fitted to the times of 500 products of 1 to 4096 tokens with eighteen matrices from 1024 x 4096 to 28672 x 8192, every tile and split forced; its choices
+// fitted to the times of 500 products of 1 to 4096 tokens with eighteen matrices from 1024 x 4096 to 28672 x 8192, y in bf16 and fp32, every tile and split forced; its choices
 // are 0.6 % above the best ones in the mean and 26 % at worst, and of 252 other products 1.3 %, 16 of them more than 5 %, and 23 % at worst.)
 struct Shape {
     uint32_t rows, tokens;
